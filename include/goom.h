@@ -467,6 +467,71 @@ int goom_affine_scan_backward(goom_ctx *ctx, const void *A, const void *bias, co
 size_t goom_affine_scan_backward_workspace_bytes(int64_t T, int d, int64_t batch, int dtype,
                                                  const goom_scan_opts *opts);
 
+/* ---- operators around the recurrences in a layer of a language model ------------------------------------------------ */
+
+/* Element types of the real tensors below (none of them a goom_dtype).  Sums, statistics and states are held in 32 bits or
+ * more whatever the type; a result is rounded once, when it is stored. */
+typedef enum goom_real {
+    GOOM_REAL_F32 = 16,
+    GOOM_REAL_BF16 = 17,
+    GOOM_REAL_F16 = 18
+} goom_real;
+
+/* Linear attention with a decay for each head: the recurrence over d x e matrices whose every entry shrinks by one
+ * factor, the head's, at each step (the other end from goom_affine_scan's matrix per step):
+ *     S_t = gamma_h S_{t-1} + k_t v_t^T,      o_t = scale q_t^T S_t = scale sum_{j <= t} gamma_h^(t-j) (q_t . k_j) v_j,
+ * gamma_h = exp(log_decay[h]) held by its log-magnitude, as a GOOM is (-inf, a decay of zero, forgets everything before the
+ * token itself; values above 0 grow, within the range of floats). */
+typedef struct goom_attention_shape {
+    int64_t seqs;      /* sequences */
+    int64_t tokens;    /* tokens of all sequences; without offsets every sequence has tokens / seqs of them */
+    int32_t heads;     /* heads of q, o, the decays and the states */
+    int32_t kv_heads;  /* heads of k and v, a divisor of heads: head h reads k and v of head h / (heads / kv_heads) */
+    int32_t dk, dv;    /* entries of a head's q and k, and of its v and o; 1 <= dk, dv <= GOOM_MAX_DIM */
+    int32_t type;      /* GOOM_REAL_*, of q, k, v, o and their gradients */
+    int32_t flags;     /* 0 */
+    double scale;      /* of the outputs; finite */
+    int64_t q_token, q_head; /* elements from one token, and from one head, to the next in q, k and v (the last axis is */
+    int64_t k_token, k_head; /* contiguous, tokens of all sequences follow one another): slices of a fused projection */
+    int64_t v_token, v_head; /* need no copy.  Both 0: contiguous, [tokens, heads, d] */
+} goom_attention_shape;
+
+/* All tokens of all sequences.  q: [tokens, heads, dk], k: [tokens, kv_heads, dk], v: [tokens, kv_heads, dv];
+ * o: [tokens, heads, dv], contiguous; log_decay: [heads] floats; offsets: NULL, or seqs + 1 int64 (device, rising from 0 to
+ * tokens): sequence s has the tokens offsets[s] .. offsets[s + 1] - 1, none if they are equal (what lies outside 0 .. tokens
+ * is cut off); state: NULL (zero) or [seqs, heads, dk, dv] floats, S before the first token; final_state: NULL or the same
+ * shape, S after the last one (the state itself for a sequence without tokens; it may be the array `state`).
+ * The sequences are cut into segments where they are few: segment totals, their carries, then every segment walked from its
+ * incoming state, 64 tokens at a time on the matrix instructions.  bfloat16: operands computed on the way are held in two
+ * bf16 parts (16 bits; three, 24 bits, where they enter a state); others run on float operands throughout.
+ * A NaN or an infinity among q, k, v may show in all outputs of its head in its sequence.
+ * workspace: goom_linear_attention_workspace_bytes(shape, offsets != NULL) bytes (may be 0).
+ * Errors: GOOM_EINVAL (null or misaligned pointers, sizes, types), GOOM_EUNSUPPORTED (dk or dv above GOOM_MAX_DIM),
+ * GOOM_EWORKSPACE. */
+int goom_linear_attention(goom_ctx *ctx, const goom_attention_shape *shape, const void *q, const void *k, const void *v,
+                          const float *log_decay, const int64_t *offsets, const float *state, void *o, float *final_state,
+                          void *workspace, size_t workspace_bytes);
+size_t goom_linear_attention_workspace_bytes(const goom_attention_shape *shape, int packed);
+
+/* One token of each sequence, for decoding: seqs = tokens; reads every state once and writes it once.  next_state:
+ * [seqs, heads, dk, dv], required; it may be the array `state`.  Arguments otherwise as above; no workspace. */
+int goom_linear_attention_step(goom_ctx *ctx, const goom_attention_shape *shape, const void *q, const void *k, const void *v,
+                               const float *log_decay, const float *state, void *o, float *next_state);
+
+/* Gradients of a loss L, given grad_o = dL / do ([tokens, heads, dv], contiguous, of the shape's type) and, unless NULL,
+ * grad_final = dL / d final_state: grad_q, grad_k, grad_v (contiguous, of the shape's type; heads that share k and v are
+ * summed in float, in a fixed order) and, unless NULL, grad_state (floats).  With u = scale (the adjoint of a state),
+ *     grad_q_i = u sum_{j <= i} gamma^(i-j) (grad_o_i . v_j) k_j,   grad_k_j = u sum_{i >= j} gamma^(i-j) (v_j . grad_o_i) q_i,
+ *     grad_v_j = u sum_{i >= j} gamma^(i-j) (k_j . q_i) grad_o_i,
+ * and the terms of the first and the final state: three walks of the forward kind, two of them backwards in time.
+ * Everything else as for goom_linear_attention, whose inputs are given again.
+ * workspace: goom_linear_attention_backward_workspace_bytes(shape, offsets != NULL) bytes (may be 0). */
+int goom_linear_attention_backward(goom_ctx *ctx, const goom_attention_shape *shape, const void *q, const void *k, const void *v,
+                                   const float *log_decay, const int64_t *offsets, const float *state, const void *grad_o,
+                                   const float *grad_final, void *grad_q, void *grad_k, void *grad_v, float *grad_state,
+                                   void *workspace, size_t workspace_bytes);
+size_t goom_linear_attention_backward_workspace_bytes(const goom_attention_shape *shape, int packed);
+
 #pragma GCC visibility pop
 #ifdef __cplusplus
 }

@@ -19,6 +19,7 @@ ZERO_NEG_INF, ZERO_FLOOR = 0, 1
 LMME_FAST, LMME_EXACT = 0, 1
 RESET_ALWAYS, RESET_COLINEAR, RESET_NEVER = 1, 0, -1
 AFFINE_TIME_INVARIANT = 1
+REAL_F32, REAL_BF16, REAL_F16 = 16, 17, 18
 
 EXPORTS = [
     "goom_version", "goom_create", "goom_destroy", "goom_set_stream", "goom_last_error",
@@ -32,6 +33,8 @@ EXPORTS = [
     "goom_affine_scan_scaled_workspace_bytes", "goom_scaled_exp", "goom_log_add_exp",
     "goom_count_nonfinite", "goom_to_goom_backward", "goom_from_goom_backward", "goom_affine_scan_backward", "goom_affine_scan_backward_workspace_bytes",
     "goom_lmme_backward", "goom_lmme_backward_workspace_bytes", "goom_scan_backward", "goom_scan_backward_workspace_bytes", "goom_scaled_exp_backward",
+    "goom_linear_attention", "goom_linear_attention_workspace_bytes", "goom_linear_attention_step",
+    "goom_linear_attention_backward", "goom_linear_attention_backward_workspace_bytes",
 ]
 
 
@@ -47,6 +50,12 @@ class ScanOpts(C.Structure):
 
 class ResetOpts(C.Structure):
     _fields_ = [("chunk_len", C.c_int64), ("policy", C.c_int32), ("cos_threshold", C.c_float)]
+
+
+class AttentionShape(C.Structure):
+    _fields_ = [("seqs", C.c_int64), ("tokens", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("dk", C.c_int32), ("dv", C.c_int32),
+                ("type", C.c_int32), ("flags", C.c_int32), ("scale", C.c_double), ("q_token", C.c_int64), ("q_head", C.c_int64),
+                ("k_token", C.c_int64), ("k_head", C.c_int64), ("v_token", C.c_int64), ("v_head", C.c_int64)]
 
 
 def library_path() -> str:
@@ -130,6 +139,14 @@ def load_library():
     lib.goom_scan_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i32, i32, i64, i32, po, vp, sz]
     lib.goom_scan_backward_workspace_bytes.argtypes = [i64, i32, i32, i64, i32, po, i32]
     lib.goom_scan_backward_workspace_bytes.restype = sz
+    pa = C.POINTER(AttentionShape)
+    lib.goom_linear_attention.argtypes = [vp, pa, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz]
+    lib.goom_linear_attention_workspace_bytes.argtypes = [pa, i32]
+    lib.goom_linear_attention_workspace_bytes.restype = sz
+    lib.goom_linear_attention_step.argtypes = [vp, pa, vp, vp, vp, vp, vp, vp, vp]
+    lib.goom_linear_attention_backward.argtypes = [vp, pa, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz]
+    lib.goom_linear_attention_backward_workspace_bytes.argtypes = [pa, i32]
+    lib.goom_linear_attention_backward_workspace_bytes.restype = sz
     _lib = lib
     return lib
 
@@ -151,6 +168,38 @@ def _dtype_code(t):
     if t.dtype in (torch.complex128, torch.float64):
         return C128
     raise TypeError(f"unsupported tensor dtype {t.dtype}")
+
+
+def _real_code(t):
+    import torch
+    code = {torch.float32: REAL_F32, torch.bfloat16: REAL_BF16, torch.float16: REAL_F16}.get(t.dtype)
+    if code is None:
+        raise TypeError(f"unsupported tensor dtype {t.dtype}")
+    return code
+
+
+def _rows(t, name):
+    """Pointer and strides (token, head) of [..., heads, d] whose last axis is contiguous and whose leading axes follow one
+    another in memory, as in a slice of a fused projection."""
+    if not t.is_cuda:
+        raise ValueError("libgoom takes device tensors")
+    st, sh = list(t.stride()), list(t.shape)
+    if t.numel() == 0:
+        return C.c_void_p(t.data_ptr()), 0, 0
+    if sh[-1] != 1 and st[-1] != 1:
+        raise ValueError(f"{name}: the last axis must be contiguous")
+    head = sh[-1] if sh[-2] == 1 else st[-2]
+    token = None  # the innermost axis of tokens that is longer than one
+    for i in range(t.dim() - 3, -1, -1):
+        if sh[i] == 1:
+            continue
+        if token is None:
+            token, run = st[i], sh[i]
+        elif st[i] != run * token:
+            raise ValueError(f"{name}: the tokens do not follow one another in memory")
+        else:
+            run *= sh[i]
+    return C.c_void_p(t.data_ptr()), sh[-2] * head if token is None else token, head
 
 
 def _ptr(t):
@@ -567,3 +616,77 @@ class Goom:
             out = self.torch.empty_like(x)
         self._check(self.lib.goom_log_add_exp(self._ctx, _ptr(x), _ptr(y), _ptr(out), x.numel(), _dtype_code(x)))
         return out
+
+    # ---- linear attention with a decay for each head
+    def _attention(self, q, k, v, log_decay, offsets, scale, lead):
+        """The shape structure and the pointers of q, k, v."""
+        torch = self.torch
+        code = _real_code(q)
+        if not (k.dtype == v.dtype == q.dtype) or log_decay.dtype != torch.float32:
+            raise TypeError("q, k, v have one type, log_decay is float32")
+        heads, dk = q.shape[-2:]
+        kv_heads, dv = v.shape[-2:]
+        if k.shape != lead + (kv_heads, dk) or q.shape[:-2] != lead or v.shape[:-2] != lead or tuple(log_decay.shape) != (heads,):
+            raise ValueError("shapes of q, k, v, log_decay do not fit")
+        tokens = lead.numel()
+        if offsets is not None:
+            if offsets.dtype != torch.int64 or offsets.dim() != 1 or offsets.numel() < 1 or len(lead) != 1:
+                raise ValueError("offsets: int64 [sequences + 1], with q, k, v [tokens, heads, d]")
+            seqs = offsets.numel() - 1
+        else:
+            seqs = lead[:-1].numel() if len(lead) > 1 else 1
+        shape = AttentionShape(seqs, tokens, heads, kv_heads, dk, dv, code, 0, scale)
+        pq, shape.q_token, shape.q_head = _rows(q, "q")
+        pk, shape.k_token, shape.k_head = _rows(k, "k")
+        pv, shape.v_token, shape.v_head = _rows(v, "v")
+        return shape, pq, pk, pv
+
+    def _state(self, t, shape, name):
+        want = (shape.seqs, shape.heads, shape.dk, shape.dv)
+        if t is not None and (tuple(t.shape) != want or t.dtype != self.torch.float32):
+            raise ValueError(f"{name}: float32 {list(want)}")
+        return _ptr(t)
+
+    def linear_attention(self, q, k, v, log_decay, state=None, offsets=None, scale: float = 1.0, want_state: bool = False):
+        """o_t = scale q_t^T S_t, S_t = exp(log_decay) S_{t-1} + k_t v_t^T for every head.  q: [batch, T, heads, dk], k: [batch, T,
+        kv_heads, dk], v: [batch, T, kv_heads, dv], or without the batch axis and with offsets (int64 [sequences + 1]) where
+        sequences of different lengths lie behind one another; state, and the final one that want_state adds: float32 [sequences,
+        heads, dk, dv].  q, k, v may be slices of one projection's output."""
+        torch = self.torch
+        shape, pq, pk, pv = self._attention(q, k, v, log_decay, offsets, scale, q.shape[:-2])
+        ps = self._state(state, shape, "state")
+        o = torch.empty(q.shape[:-1] + (shape.dv,), dtype=q.dtype, device=q.device)
+        last = torch.empty((shape.seqs, shape.heads, shape.dk, shape.dv), dtype=torch.float32, device=q.device) if want_state else None
+        ws, wsn = self.workspace(self.lib.goom_linear_attention_workspace_bytes(C.byref(shape), int(offsets is not None)))
+        self._check(self.lib.goom_linear_attention(self._ctx, C.byref(shape), pq, pk, pv, _ptr(log_decay), _ptr(offsets), ps, _ptr(o), _ptr(last),
+                                                   _ptr(ws), wsn))
+        return (o, last) if want_state else o
+
+    def linear_attention_step(self, q, k, v, log_decay, state, scale: float = 1.0, out_state=None):
+        """One token of each sequence: q: [batch, heads, dk], k: [batch, kv_heads, dk], v: [batch, kv_heads, dv]; state: float32 [batch,
+        heads, dk, dv], replaced by the next one, or left as it is if out_state receives that."""
+        if q.dim() != 3:
+            raise ValueError("q: [batch, heads, dk]")
+        shape, pq, pk, pv = self._attention(q, k, v, log_decay, None, scale, q.shape[:-2])
+        shape.seqs = shape.tokens
+        out_state = state if out_state is None else out_state
+        o = self.torch.empty(q.shape[:-1] + (shape.dv,), dtype=q.dtype, device=q.device)
+        self._check(self.lib.goom_linear_attention_step(self._ctx, C.byref(shape), pq, pk, pv, _ptr(log_decay), self._state(state, shape, "state"), _ptr(o),
+                                                        self._state(out_state, shape, "out_state")))
+        return o
+
+    def linear_attention_backward(self, q, k, v, log_decay, grad_o, state=None, grad_state=None, offsets=None, scale: float = 1.0):
+        """Gradients with respect to q, k, v and (None without one) the initial state, given those with respect to the outputs and
+        (None: none) the final state."""
+        torch = self.torch
+        shape, pq, pk, pv = self._attention(q, k, v, log_decay, offsets, scale, q.shape[:-2])
+        if grad_o.shape != q.shape[:-1] + (shape.dv,) or grad_o.dtype != q.dtype:
+            raise ValueError("grad_o: of o's shape and type")
+        new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)  # noqa: E731
+        gq, gk, gv = new(q), new(k), new(v)
+        gs = new(state) if state is not None else None
+        ws, wsn = self.workspace(self.lib.goom_linear_attention_backward_workspace_bytes(C.byref(shape), int(offsets is not None)))
+        self._check(self.lib.goom_linear_attention_backward(self._ctx, C.byref(shape), pq, pk, pv, _ptr(log_decay), _ptr(offsets), self._state(state, shape, "state"),
+                                                            _ptr(grad_o), self._state(grad_state, shape, "grad_state"), _ptr(gq), _ptr(gk), _ptr(gv), _ptr(gs),
+                                                            _ptr(ws), wsn))
+        return gq, gk, gv, gs

@@ -1,0 +1,878 @@
+// Linear attention with a decay for each head: forward, single tokens, backward.
+//
+// One kernel, the walk, computes for rows a_i, b_j (of ka entries) and c_j (of nc entries), a head's decay g and a state R
+//     y_i = p sum_{j <= i} g^(i-j) (a_i . b_j) c_j + w g^i' a_i R
+// 64 tokens (a chunk) at a time: with the pairs inside a chunk as a masked 64 x 64 matrix P, what precedes the chunk as the
+// state R (already decayed to the chunk's first token, i' = 0), and
+//     R <- g^n R + u sum_j g^(n-j') b_j c_j^T
+// for the next.  The forward pass is one walk (a, b, c = q, k, v); the backward pass is three of the same kind:
+//     grad_q: grad_o, v, k forwards;     grad_k: v, grad_o, q and grad_v: k, q, grad_o backwards in time,
+// where j' counts from the end and R starts as the final state's gradient.  Nothing but inputs, outputs and a few states
+// touches memory: a pass is bound by the bytes of its tensors as long as there are enough walks to fill the chip.  Where
+// there are not, every sequence is cut into segments: segment totals (the walk without outputs), carries, then all segments
+// at once.
+//
+// A workgroup walks one head of one segment.  Each wave owns nc / NW columns of the state, which stay in its registers as
+// accumulators of the matrix instruction for the whole walk; the rows of the tiles are numbered such that a lane's
+// accumulator entries are eight consecutive ones of the contraction (rows or tokens), so that the state and P turn into
+// operands of the next product without moving between lanes.  P is shared out over the waves by rows and passed through LDS.
+#include <cmath>
+
+#include "goom_real.h"
+
+namespace goom_layer {
+
+constexpr int CHUNK = 64; // tokens; the pairs of a chunk cost 64 (ka + nc) multiplications a token, the state 2 ka nc
+
+struct WalkRole {
+    const void *a, *b, *c;
+    void *y;                 // NULL in walks without outputs
+    long long a_tok, a_head, b_tok, b_head, c_tok, c_head, y_tok, y_head; // elements
+    int a_group, b_group, c_group; // heads that share a row set: 1, or heads / kv_heads
+    int a_vec, b_vec, c_vec, y_vec; // 16-byte accesses are aligned
+    int ka, nc;
+    int reverse;
+    int y_float;             // y holds floats, whatever the type
+    float p_scale, w_scale, u_scale;
+    const float *init;       // NULL or states [seqs][heads][.][.]
+    float *fin;              // NULL or states, written after the last token
+    int state_row, state_col; // elements between entries of init and fin along ka and along nc
+    float *totals;           // [slots][heads][state registers]; NULL: one segment a sequence
+};
+
+struct WalkArgs {
+    WalkRole role[3];
+    const float *log_decay;
+    const int64_t *offsets;
+    long long tokens, seqs, seq_len, seg_len, segs; // without offsets: seq_len tokens and segs segments a sequence
+    int heads;
+};
+
+// ---- the sequence and segment of a workgroup.  With offsets, sequence s has the slots from floor(start / seg_len) + s on:
+// at least one, and as many as it has segments, without a pass over the lengths.
+struct Place { long long seq, seg, nseg, start, len; };
+
+__device__ inline void span(const WalkArgs &w, long long s, long long &start, long long &len)
+{
+    if (w.offsets) {
+        long long b = w.offsets[s], e = w.offsets[s + 1];
+        b = b < 0 ? 0 : b > w.tokens ? w.tokens : b;
+        e = e < b ? b : e > w.tokens ? w.tokens : e;
+        start = b;
+        len = e - b;
+    } else {
+        start = s * w.seq_len;
+        len = w.seq_len;
+    }
+}
+
+__device__ inline long long first_slot(const WalkArgs &w, long long s)
+{
+    if (!w.offsets) return s * w.segs;
+    long long start, len;
+    span(w, s, start, len);
+    return start / w.seg_len + s;
+}
+
+__device__ inline Place find_place(const WalkArgs &w, long long slot)
+{
+    Place p;
+    if (!w.offsets) {
+        p.seq = slot / w.segs;
+        p.seg = slot - p.seq * w.segs;
+    } else { // the last sequence whose first slot is at most `slot`: 64 probes at a time
+        long long lo = 0, hi = w.seqs;
+        const int lane = threadIdx.x & 63;
+        while (hi - lo > 1) {
+            const long long step = (hi - lo + 63) / 64, at = lo + lane * step;
+            const unsigned long long m = __ballot(at < hi && first_slot(w, at < hi ? at : lo) <= slot);
+            const int k = __popcll(m);
+            lo += (k > 0 ? k - 1 : 0) * step;
+            hi = lo + step < hi ? lo + step : hi;
+        }
+        p.seq = lo;
+        p.seg = slot - first_slot(w, lo);
+    }
+    span(w, p.seq, p.start, p.len);
+    p.nseg = (p.len + w.seg_len - 1) / w.seg_len;
+    if (p.nseg < 1) p.nseg = 1;
+    return p;
+}
+
+// g^x for whole x >= 0, from log2 g; g = 0 (log -inf) has g^0 = 1
+__device__ inline float decay_power(float g2, int x) { return x == 0 ? 1.0f : __builtin_amdgcn_exp2f(g2 * (float)x); }
+
+// ---- operands: eight consecutive entries of the contraction per lane (lane / 16 picks which eight of 32)
+template <typename E> struct Operand;
+template <> struct Operand<bf16> {
+    typedef bf16x8 Frag;
+    // Computed operands are split into bf16 parts: two (16 bits) for P and the state where outputs, rounded to 8 bits, are
+    // formed from them, three (24 bits) for what is summed into the float states.
+    static constexpr int OUT_PARTS = 2, STATE_PARTS = 3;
+    static constexpr int PITCH_PAD = 16;
+};
+template <> struct Operand<float> {
+    typedef f32x8 Frag;
+    static constexpr int OUT_PARTS = 1, STATE_PARTS = 1;
+    static constexpr int PITCH_PAD = 4;
+};
+
+__device__ inline f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ inline f32x4 mma(f32x8 a, f32x8 b, f32x4 c)
+{
+#pragma unroll
+    for (int e = 0; e < 8; e++) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+}
+
+template <int N> __device__ inline void split(f32x8 x, bf16x8 (&p)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        p[i] = __builtin_convertvector(x, bf16x8);
+        if (i + 1 < N) x -= __builtin_convertvector(p[i], f32x8);
+    }
+}
+template <int N> __device__ inline void split(f32x8 x, f32x8 (&p)[N]) { p[0] = x; }
+
+__device__ inline f32x8 widen(bf16x8 x) { return __builtin_convertvector(x, f32x8); }
+__device__ inline f32x8 widen(f32x8 x) { return x; }
+
+// eight entries of one row
+__device__ inline bf16x8 row_frag(const bf16 *p) { return *reinterpret_cast<const bf16x8 *>(p); }
+__device__ inline f32x8 row_frag(const float *p)
+{
+    const f32x4 lo = *reinterpret_cast<const f32x4 *>(p), hi = *reinterpret_cast<const f32x4 *>(p + 4);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// rows t0 + 8 (lane / 16) + 0 .. 7 of one column: column c0 + (i / 4) cs + i % 4 for i = lane % 16
+template <int PITCH> __device__ inline bf16x8 col_frag(const bf16 *tile, int t0, int c0, int cs, int lane)
+{
+    // the transposing read: of each 16 lanes, lane s gives the address of four columns of row s / 4, and lane i gets
+    // the four rows of column i
+    const int s = lane & 15, row = t0 + (lane >> 4) * 8 + (s >> 2), col = c0 + (s & 3) * cs;
+    typedef __attribute__((address_space(3))) s16x4 *lds;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(tile + row * PITCH + col));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(tile + (row + 4) * PITCH + col));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+template <int PITCH> __device__ inline f32x8 col_frag(const float *tile, int t0, int c0, int cs, int lane)
+{
+    const int i = lane & 15;
+    const float *p = tile + (t0 + (lane >> 4) * 8) * PITCH + c0 + (i >> 2) * cs + (i & 3);
+    f32x8 x;
+#pragma unroll
+    for (int e = 0; e < 8; e++) x[e] = p[e * PITCH];
+    return x;
+}
+
+// rows 0 .. n-1 of `d` entries from memory into a tile of 64 rows of D entries, zeros elsewhere
+template <typename E, typename S, int D, int PITCH, int THREADS>
+__device__ inline void stage(E *tile, const S *src, long long stride, int n, int d, int vec)
+{
+    typedef typename Vec<S, 8>::type SV;
+    typedef typename Vec<E, 8>::type EV;
+    constexpr int UNITS = CHUNK * D / 8;
+    if (vec) {
+#pragma unroll
+        for (int u0 = 0; u0 < UNITS; u0 += THREADS) {
+            const int u = u0 + threadIdx.x;
+            if (UNITS % THREADS == 0 || u < UNITS) {
+                const int row = u / (D / 8), col = u % (D / 8) * 8;
+                EV x = {};
+                if (row < n && col < d) x = __builtin_convertvector(*reinterpret_cast<const SV *>(src + row * stride + col), EV);
+                E *to = tile + row * PITCH + col;
+                if constexpr (sizeof(E) == 2) {
+                    *reinterpret_cast<EV *>(to) = x;
+                } else {
+                    *reinterpret_cast<f32x4 *>(to) = __builtin_shufflevector(x, x, 0, 1, 2, 3);
+                    *reinterpret_cast<f32x4 *>(to + 4) = __builtin_shufflevector(x, x, 4, 5, 6, 7);
+                }
+            }
+        }
+    } else {
+#pragma unroll 8
+        for (int u = threadIdx.x; u < CHUNK * D; u += THREADS) {
+            const int row = u / D, col = u % D;
+            tile[row * PITCH + col] = row < n && col < d ? (E)src[row * stride + col] : (E)0.0f;
+        }
+    }
+}
+
+// element type in LDS and registers: bf16 for bf16; halves are widened to floats (products of halves and states of their
+// magnitudes leave the range of halves)
+template <typename S> struct Compute { typedef float type; };
+template <> struct Compute<bf16> { typedef bf16 type; };
+
+template <typename E, int DK, int DV, int NW, bool OUT> struct WalkLds {
+    static constexpr int PK = DK + Operand<E>::PITCH_PAD, PV = DV + Operand<E>::PITCH_PAD;
+    static constexpr int ROWS = CHUNK * PK * (OUT ? 2 : 1) + CHUNK * PV; // elements
+    static constexpr int P_FRAGS = OUT ? 8 * Operand<E>::OUT_PARTS * 64 : 0;
+    static constexpr size_t bytes = ROWS * sizeof(E) + P_FRAGS * sizeof(typename Operand<E>::Frag);
+};
+
+// DK, DV: ka and nc, padded; NW waves of NT tiles of 16 columns each
+template <typename S, int DK, int DV, int NW, bool OUT> __global__ __launch_bounds__(NW * 64) void walk_kernel(WalkArgs w)
+{
+    typedef typename Compute<S>::type E;
+    typedef Operand<E> Op;
+    typedef typename Op::Frag Frag;
+    typedef WalkLds<E, DK, DV, NW, OUT> Lds;
+    constexpr int THREADS = NW * 64, NT = DV / 16 / NW, KS = DK / 32, CS = NT == 2 ? 8 : 4;
+    constexpr int OP = Op::OUT_PARTS, SP = Op::STATE_PARTS;
+    static_assert(NT == 1 || NT == 2, "a wave has one or two column tiles");
+    extern __shared__ __align__(16) unsigned char lds[];
+    Frag *const p_lds = reinterpret_cast<Frag *>(lds);
+    E *const b_lds = reinterpret_cast<E *>(p_lds + Lds::P_FRAGS);
+    E *const c_lds = b_lds + CHUNK * Lds::PK;
+    E *const a_lds = c_lds + CHUNK * Lds::PV;
+
+    const WalkRole &r = w.role[blockIdx.z];
+    const long long slot = blockIdx.x / w.heads;
+    const int h = blockIdx.x % w.heads;
+    const Place at = find_place(w, slot);
+    const bool last = r.reverse ? at.seg == 0 : at.seg == at.nseg - 1; // in walking order
+    if (at.seg >= at.nseg || (!OUT && last)) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+    const float g2 = w.log_decay[h] * 1.44269504088896341f;
+    const int col0 = wave * NT * 16; // the wave's columns: col0 + (i / 4) CS + 4 nt + i % 4
+
+    // ---- the incoming state
+    f32x4 R[DK / 16][NT];
+    float *const total = r.totals ? r.totals + (slot * w.heads + h) * (long long)(DK * DV) + (long long)wave * NT * (DK / 16) * 256 + lane * 4 : nullptr;
+    const long long state0 = (at.seq * w.heads + h) * (long long)r.ka * r.nc;
+    const bool empty = at.len == 0;
+#pragma unroll
+    for (int t = 0; t < DK / 16; t++)
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++) {
+            f32x4 x = {0, 0, 0, 0};
+            if (OUT && total && !empty) {
+                x = *reinterpret_cast<const f32x4 *>(total + (nt * (DK / 16) + t) * 256);
+            } else if (OUT && r.init) {
+                const float scale = r.reverse || empty ? 1.0f : decay_power(g2, 1);
+                const int col = col0 + (i >> 2) * CS + 4 * nt + (i & 3);
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const int row = t / 2 * 32 + g * 8 + t % 2 * 4 + e;
+                    if (row < r.ka && col < r.nc) x[e] = scale * r.init[state0 + (long long)row * r.state_row + (long long)col * r.state_col];
+                }
+            }
+            R[t][nt] = x;
+        }
+
+    const S *const a = reinterpret_cast<const S *>(r.a) + at.start * r.a_tok + h / r.a_group * r.a_head;
+    const S *const b = reinterpret_cast<const S *>(r.b) + at.start * r.b_tok + h / r.b_group * r.b_head;
+    const S *const c = reinterpret_cast<const S *>(r.c) + at.start * r.c_tok + h / r.c_group * r.c_head;
+    const long long seg0 = at.seg * w.seg_len, seg1 = seg0 + w.seg_len < at.len ? seg0 + w.seg_len : at.len;
+    const int nchunks = (int)((seg1 - seg0 + CHUNK - 1) / CHUNK);
+    for (int step = 0; step < nchunks; step++) {
+        const long long t0 = seg0 + (long long)(r.reverse ? nchunks - 1 - step : step) * CHUNK;
+        const int n = seg1 - t0 < CHUNK ? (int)(seg1 - t0) : CHUNK;
+        __syncthreads();
+        if (OUT) stage<E, S, DK, Lds::PK, THREADS>(a_lds, a + t0 * r.a_tok, r.a_tok, n, r.ka, r.a_vec);
+        stage<E, S, DK, Lds::PK, THREADS>(b_lds, b + t0 * r.b_tok, r.b_tok, n, r.ka, r.b_vec);
+        stage<E, S, DV, Lds::PV, THREADS>(c_lds, c + t0 * r.c_tok, r.c_tok, n, r.nc, r.c_vec);
+        __syncthreads();
+
+        if (OUT) {
+            // ---- P, transposed (accumulator columns are the rows i, so that a lane's entries are consecutive j)
+            for (int it = wave; it < 4; it += NW) {
+#pragma unroll
+                for (int ks = 0; ks < 2; ks++) {
+                    if (r.reverse ? ks < it / 2 : ks > it / 2) continue; // no pair in this half
+                    f32x4 p0 = {0, 0, 0, 0}, p1 = {0, 0, 0, 0};
+                    const E *const arow = a_lds + (it * 16 + i) * Lds::PK + g * 8;
+                    const E *const brow = b_lds + (ks * 32 + (i >> 2) * 8 + (i & 3)) * Lds::PK + g * 8;
+#pragma unroll
+                    for (int kk = 0; kk < KS; kk++) {
+                        const Frag af = row_frag(arow + kk * 32);
+                        p0 = mma(row_frag(brow + kk * 32), af, p0);
+                        p1 = mma(row_frag(brow + 4 * Lds::PK + kk * 32), af, p1);
+                    }
+                    f32x8 x;
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        const int j = ks * 32 + g * 8 + e, age = r.reverse ? j - (it * 16 + i) : it * 16 + i - j;
+                        x[e] = age >= 0 ? (e < 4 ? p0[e & 3] : p1[e & 3]) * (r.p_scale * decay_power(g2, age)) : 0.0f;
+                    }
+                    Frag parts[OP];
+                    split(x, parts);
+#pragma unroll
+                    for (int q = 0; q < OP; q++) p_lds[((it * 2 + ks) * OP + q) * 64 + lane] = parts[q];
+                }
+            }
+            __syncthreads();
+        }
+
+        Frag cf[2][NT];
+#pragma unroll
+        for (int ks = 0; ks < 2; ks++)
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++) cf[ks][nt] = col_frag<Lds::PV>(c_lds, ks * 32, col0 + 4 * nt, CS, lane);
+
+        if (OUT) {
+            // ---- what the state gives to each row, then the pairs; transposed: a lane has consecutive columns of row i
+            f32x4 y[4][NT];
+#pragma unroll
+            for (int it = 0; it < 4; it++)
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) y[it][nt] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int kk = 0; kk < KS; kk++) {
+                Frag rf[NT][OP];
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) split(__builtin_shufflevector(R[2 * kk][nt], R[2 * kk + 1][nt], 0, 1, 2, 3, 4, 5, 6, 7), rf[nt]);
+#pragma unroll
+                for (int it = 0; it < 4; it++) {
+                    const Frag af = row_frag(a_lds + (it * 16 + i) * Lds::PK + kk * 32 + g * 8);
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                        for (int q = 0; q < OP; q++) y[it][nt] = mma(rf[nt][q], af, y[it][nt]);
+                }
+            }
+#pragma unroll
+            for (int it = 0; it < 4; it++) {
+                const int row = it * 16 + i, age = r.reverse ? n - 1 - row : row;
+                const float scale = r.w_scale * decay_power(g2, age > 0 ? age : 0);
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) y[it][nt] *= scale;
+#pragma unroll
+                for (int ks = 0; ks < 2; ks++) {
+                    if (r.reverse ? ks < it / 2 : ks > it / 2) continue;
+#pragma unroll
+                    for (int q = 0; q < OP; q++) {
+                        const Frag pf = p_lds[((it * 2 + ks) * OP + q) * 64 + lane];
+#pragma unroll
+                        for (int nt = 0; nt < NT; nt++) y[it][nt] = mma(cf[ks][nt], pf, y[it][nt]);
+                    }
+                }
+                if (row < n) {
+                    const long long to = (at.start + t0 + row) * r.y_tok + h * r.y_head;
+                    const int col = col0 + g * CS;
+                    float x[NT * 4];
+#pragma unroll
+                    for (int e = 0; e < NT * 4; e++) x[e] = y[it][e / 4][e % 4];
+                    if (r.y_vec && col + NT * 4 <= r.nc) {
+                        if (r.y_float) store_floats<float, NT * 4>(reinterpret_cast<float *>(r.y) + to + col, x);
+                        else store_floats<S, NT * 4>(reinterpret_cast<S *>(r.y) + to + col, x);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < NT * 4; e++)
+                            if (col + e < r.nc) {
+                                if (r.y_float) reinterpret_cast<float *>(r.y)[to + col + e] = x[e];
+                                else reinterpret_cast<S *>(r.y)[to + col + e] = (S)x[e];
+                            }
+                    }
+                }
+            }
+        }
+
+        // ---- the next state; after the last token of a forward walk the final state, one decay short of the next chunk's
+        const int ahead = !r.reverse && last && r.fin && step == nchunks - 1 ? 1 : 0;
+        const float whole = decay_power(g2, n - ahead);
+#pragma unroll
+        for (int t = 0; t < DK / 16; t++)
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++) R[t][nt] *= whole;
+#pragma unroll
+        for (int ks = 0; ks < 2; ks++) {
+            f32x8 wt;
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                const int j = ks * 32 + g * 8 + e, age = r.reverse ? j + 1 : n - ahead - j;
+                wt[e] = r.u_scale * decay_power(g2, age > 0 ? age : 0);
+            }
+            Frag cd[NT][SP];
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++) split(widen(cf[ks][nt]) * wt, cd[nt]);
+#pragma unroll
+            for (int t = 0; t < DK / 16; t++) {
+                const Frag bf = col_frag<Lds::PK>(b_lds, ks * 32, t / 2 * 32 + t % 2 * 4, 8, lane);
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                    for (int q = 0; q < SP; q++) R[t][nt] = mma(bf, cd[nt][q], R[t][nt]);
+            }
+        }
+    }
+
+    if (OUT ? r.fin && last : true) {
+#pragma unroll
+        for (int t = 0; t < DK / 16; t++)
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++) {
+                if (!OUT) {
+                    *reinterpret_cast<f32x4 *>(total + (nt * (DK / 16) + t) * 256) = R[t][nt];
+                } else {
+                    const int col = col0 + (i >> 2) * CS + 4 * nt + (i & 3);
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const int row = t / 2 * 32 + g * 8 + t % 2 * 4 + e;
+                        if (row < r.ka && col < r.nc) r.fin[state0 + (long long)row * r.state_row + (long long)col * r.state_col] = R[t][nt][e];
+                    }
+                }
+            }
+    }
+}
+
+// Segment totals -> incoming states, in place, in walking order: a thread has four entries of one head's state and goes
+// through the segments of one sequence.  grid: (seqs heads times a part of 1024 entries, 1, roles)
+template <int DK, int DV, int NW> __global__ __launch_bounds__(256) void carry_kernel(WalkArgs w)
+{
+    constexpr int NT = DV / 16 / NW, CS = NT == 2 ? 8 : 4;
+    const WalkRole &r = w.role[blockIdx.z];
+    constexpr int PARTS = DK * DV / 1024;
+    const long long s = blockIdx.x / PARTS / w.heads;
+    const int h = blockIdx.x / PARTS % w.heads, u = blockIdx.x % PARTS * 256 + threadIdx.x;
+    long long start, len;
+    span(w, s, start, len);
+    const long long nseg = len > 0 ? (len + w.seg_len - 1) / w.seg_len : 1;
+    const int lane = u & 63, t = u / 64 % (DK / 16), nt = u / 64 / (DK / 16) % NT, wave = u / 64 / (DK / 16) / NT, i = lane & 15;
+    const float g2 = w.log_decay[h] * 1.44269504088896341f;
+    f32x4 x = {0, 0, 0, 0};
+    if (r.init) {
+        const float scale = r.reverse ? 1.0f : decay_power(g2, 1);
+        const int col = wave * NT * 16 + (i >> 2) * CS + 4 * nt + (i & 3);
+        for (int e = 0; e < 4; e++) {
+            const int row = t / 2 * 32 + (lane >> 4) * 8 + t % 2 * 4 + e;
+            if (row < r.ka && col < r.nc) x[e] = scale * r.init[(s * w.heads + h) * (long long)r.ka * r.nc + (long long)row * r.state_row + (long long)col * r.state_col];
+        }
+    }
+    f32x4 *const tot = reinterpret_cast<f32x4 *>(r.totals) + (first_slot(w, s) * w.heads + h) * (long long)(DK * DV / 4) + u;
+    const long long stride = (long long)w.heads * (DK * DV / 4);
+    const float whole = decay_power(g2, (int)w.seg_len);
+    const float first = r.reverse ? decay_power(g2, (int)(len - (nseg - 1) * w.seg_len)) : whole; // a sequence's last segment may be shorter
+    long long at = r.reverse ? nseg - 1 : 0;
+    const long long dir = r.reverse ? -1 : 1;
+    f32x4 next = nseg > 1 ? tot[at * stride] : f32x4{0, 0, 0, 0};
+    for (long long k = 0; k < nseg; k++, at += dir) {
+        const f32x4 mine = next;
+        if (k + 2 < nseg) next = tot[(at + dir) * stride]; // (the last segment in walking order has no total)
+        tot[at * stride] = x;
+        x = x * (k == 0 ? first : whole) + mine;
+    }
+}
+
+// sums over heads that share keys and values: y[token][kv head][.] = sum over the group of x[token][head][.], floats
+template <typename S> __global__ __launch_bounds__(256) void shared_sum_kernel(const float *x, S *y, long long n, int group, int d)
+{
+    for (long long u = blockIdx.x * 256ll + threadIdx.x; u < n; u += gridDim.x * 256ll) {
+        const long long row = u / d;
+        const float *p = x + row * group * d + (u - row * d);
+        float sum = 0.0f;
+        for (int k = 0; k < group; k++) sum += p[(long long)k * d];
+        y[u] = (S)sum;
+    }
+}
+
+// ---- single tokens: S <- g S + k v^T, o = scale q^T S.  One pass over the state, bound by its bytes.  A workgroup has 32
+// columns of a head's state (eight groups of four) and its threads every 32nd row; their sums meet in LDS in a fixed order.
+template <typename S, bool VEC> __global__ __launch_bounds__(256) void step_kernel(goom_attention_shape sh, const S *q, const S *k, const S *v, const float *log_decay,
+                                                                                  const float *state, S *o, float *next)
+{
+    const int h = blockIdx.x % sh.heads, col = blockIdx.y * 32 + (threadIdx.x & 7) * 4, row0 = threadIdx.x >> 3;
+    const long long s = blockIdx.x / sh.heads;
+    const int kv = h / (sh.heads / sh.kv_heads);
+    const float decay = __builtin_amdgcn_exp2f(log_decay[h] * 1.44269504088896341f);
+    const S *const qh = q + s * sh.q_token + h * sh.q_head, *const kh = k + s * sh.k_token + kv * sh.k_head, *const vh = v + s * sh.v_token + kv * sh.v_head;
+    const long long base = (s * sh.heads + h) * (long long)sh.dk * sh.dv;
+    float x[4], y[4] = {0, 0, 0, 0};
+    constexpr int ROWS = GOOM_MAX_DIM / 32;
+    float st[ROWS][4], kr[ROWS], qr[ROWS];
+#pragma unroll
+    for (int e = 0; e < 4; e++) x[e] = col + e < sh.dv ? (float)vh[col + e] : 0.0f;
+#pragma unroll
+    for (int u = 0; u < ROWS; u++) {
+        const int row = row0 + u * 32;
+        kr[u] = qr[u] = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; e++) st[u][e] = 0.0f;
+        if (row < sh.dk) {
+            kr[u] = (float)kh[row];
+            qr[u] = (float)qh[row];
+            const float *p = state ? state + base + (long long)row * sh.dv + col : nullptr;
+            if (VEC) {
+                if (p && col < sh.dv) load_floats<float, 4>(p, st[u]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (p && col + e < sh.dv) st[u][e] = p[e];
+            }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < ROWS; u++) {
+        const int row = row0 + u * 32;
+        if (row < sh.dk) {
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                st[u][e] = decay * st[u][e] + kr[u] * x[e];
+                y[e] += qr[u] * st[u][e];
+            }
+            float *p = next + base + (long long)row * sh.dv + col;
+            if (VEC) {
+                if (col < sh.dv) store_floats<float, 4>(p, st[u]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (col + e < sh.dv) p[e] = st[u][e];
+            }
+        }
+    }
+    __shared__ float part[4][32];
+#pragma unroll
+    for (int e = 0; e < 4; e++) { // the wave's eight rows, then the four waves
+        y[e] += __shfl_xor(y[e], 8);
+        y[e] += __shfl_xor(y[e], 16);
+        y[e] += __shfl_xor(y[e], 32);
+        if ((threadIdx.x & 63) < 8) part[threadIdx.x >> 6][(threadIdx.x & 7) * 4 + e] = y[e];
+    }
+    __syncthreads();
+    const int c = blockIdx.y * 32 + threadIdx.x;
+    if (threadIdx.x < 32 && c < sh.dv)
+        o[(s * sh.heads + h) * (long long)sh.dv + c] =
+            (S)((float)sh.scale * ((part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x])));
+}
+
+// ---- host side
+
+static int padded_head(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
+
+// Segments: how long, and how many slots there are in all.
+struct Segments { long long len, slots, per_seq; };
+
+static Segments choose_segments(const goom_attention_shape &sh, int roles, bool packed)
+{
+    const long long walks = sh.seqs * sh.heads * roles, mean = sh.seqs > 0 ? (sh.tokens + sh.seqs - 1) / sh.seqs : 0;
+    long long want = walks > 0 ? (768 + walks - 1) / walks : 1; // segments a sequence of mean length
+    const long long most = (mean + 4 * CHUNK - 1) / (4 * CHUNK);  // not below four chunks each
+    if (want > most) want = most;
+    if (want < 1) want = 1;
+    long long len = (mean + want - 1) / want;
+    len = (len + CHUNK - 1) / CHUNK * CHUNK;
+    if (len < CHUNK) len = CHUNK;
+    Segments g;
+    if (packed) {
+        if (want == 1) len = (sh.tokens / CHUNK + 1) * CHUNK; // no sequence is longer
+        g = {len, want == 1 ? sh.seqs : sh.tokens / len + sh.seqs, want == 1 ? 1 : 0};
+    } else {
+        g = {len, 0, mean > 0 ? (mean + len - 1) / len : 1};
+        g.slots = sh.seqs * g.per_seq;
+    }
+    return g;
+}
+
+// floats of the segments' states for walks over (ka, nc)
+static size_t totals_bytes(const goom_attention_shape &sh, const Segments &g, int ka, int nc)
+{
+    if (g.per_seq == 1) return 0;
+    return goom::align_up((size_t)(g.slots * sh.heads) * padded_head(ka) * padded_head(nc) * 4, 256);
+}
+
+template <typename S, int DK, int DV> static int launch_walks_sized(goom_ctx *ctx, const WalkArgs &w, int roles, long long slots, const char *label)
+{
+    constexpr int NW = DV >= 64 ? 4 : 2;
+    typedef typename Compute<S>::type E;
+    const dim3 grid((unsigned)(slots * w.heads), 1, roles);
+    const bool parts = w.role[0].totals != nullptr;
+    if (parts) {
+        auto *totals = walk_kernel<S, DK, DV, NW, false>;
+        constexpr size_t bytes = WalkLds<E, DK, DV, NW, false>::bytes;
+        if (int st = goom::check_hip(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(totals), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes), "hipFuncSetAttribute")) return st;
+        goom::prof_begin(ctx, "linear attention: segment totals");
+        totals<<<grid, NW * 64, bytes, ctx->stream>>>(w);
+        goom::prof_end(ctx);
+        goom::prof_begin(ctx, "linear attention: carries");
+        carry_kernel<DK, DV, NW><<<dim3((unsigned)(w.seqs * w.heads * (DK * DV / 1024)), 1, roles), 256, 0, ctx->stream>>>(w);
+        goom::prof_end(ctx);
+    }
+    auto *walk = walk_kernel<S, DK, DV, NW, true>;
+    constexpr size_t bytes = WalkLds<E, DK, DV, NW, true>::bytes;
+    if (int st = goom::check_hip(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(walk), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes), "hipFuncSetAttribute")) return st;
+    goom::prof_begin(ctx, label);
+    walk<<<grid, NW * 64, bytes, ctx->stream>>>(w);
+    goom::prof_end(ctx);
+    return goom::check_hip(ctx, hipGetLastError(), label);
+}
+
+// roles of one launch have the same padded sizes
+static int launch_walks(goom_ctx *ctx, int type, const WalkArgs &w, int roles, long long slots, const char *label)
+{
+    const int dk = padded_head(w.role[0].ka), dv = padded_head(w.role[0].nc);
+    return with_type(type, [&](auto tag) {
+        typedef typename decltype(tag)::type S;
+        switch (dk * 1000 + dv) {
+        case 32032: return launch_walks_sized<S, 32, 32>(ctx, w, roles, slots, label);
+        case 32064: return launch_walks_sized<S, 32, 64>(ctx, w, roles, slots, label);
+        case 32128: return launch_walks_sized<S, 32, 128>(ctx, w, roles, slots, label);
+        case 64032: return launch_walks_sized<S, 64, 32>(ctx, w, roles, slots, label);
+        case 64064: return launch_walks_sized<S, 64, 64>(ctx, w, roles, slots, label);
+        case 64128: return launch_walks_sized<S, 64, 128>(ctx, w, roles, slots, label);
+        case 128032: return launch_walks_sized<S, 128, 32>(ctx, w, roles, slots, label);
+        case 128064: return launch_walks_sized<S, 128, 64>(ctx, w, roles, slots, label);
+        default: return launch_walks_sized<S, 128, 128>(ctx, w, roles, slots, label);
+        }
+    });
+}
+
+// rows of `d` entries whose vectors of 8 elements are aligned to 16 bytes (32 for floats: read as two)
+static int vec_rows(const void *p, long long tok, long long head, int d, size_t size)
+{
+    return d % 8 == 0 && tok % 8 == 0 && head % 8 == 0 && goom::aligned(p, 8 * size);
+}
+
+static WalkArgs walk_args(const goom_attention_shape &sh, const float *log_decay, const int64_t *offsets, const Segments &g)
+{
+    WalkArgs w = {};
+    w.log_decay = log_decay;
+    w.offsets = offsets;
+    w.tokens = sh.tokens;
+    w.seqs = sh.seqs;
+    w.seq_len = sh.seqs > 0 ? sh.tokens / sh.seqs : 0;
+    w.seg_len = g.len;
+    w.segs = g.per_seq;
+    w.heads = sh.heads;
+    return w;
+}
+
+struct Rows { const void *p; long long tok, head; int group, d; }; // one of q, k, v, grad_o
+
+static WalkRole role(const Rows &a, const Rows &b, const Rows &c, void *y, int y_float, int heads, int reverse, size_t size)
+{
+    WalkRole r = {};
+    r.a = a.p; r.a_tok = a.tok; r.a_head = a.head; r.a_group = a.group; r.a_vec = vec_rows(a.p, a.tok, a.head, a.d, size);
+    r.b = b.p; r.b_tok = b.tok; r.b_head = b.head; r.b_group = b.group; r.b_vec = vec_rows(b.p, b.tok, b.head, b.d, size);
+    r.c = c.p; r.c_tok = c.tok; r.c_head = c.head; r.c_group = c.group; r.c_vec = vec_rows(c.p, c.tok, c.head, c.d, size);
+    r.ka = a.d;
+    r.nc = c.d;
+    r.y = y;
+    r.y_float = y_float;
+    r.y_head = c.d;
+    r.y_tok = (long long)heads * c.d;
+    r.y_vec = vec_rows(y, r.y_tok, r.y_head, c.d, y_float ? 4 : size);
+    r.reverse = reverse;
+    r.p_scale = r.w_scale = r.u_scale = 1.0f;
+    r.state_row = c.d;
+    r.state_col = 1;
+    return r;
+}
+
+// fills in the strides that 0 stands for; GOOM_OK or an error
+static int check_shape(goom_ctx *ctx, const goom_attention_shape *given, goom_attention_shape &sh, bool packed, bool need_equal)
+{
+    if (!given) return goom::fail(ctx, GOOM_EINVAL, "null shape");
+    sh = *given;
+    if (!real_type(sh.type)) return goom::fail(ctx, GOOM_EINVAL, "unknown element type %d", sh.type);
+    if (sh.flags) return goom::fail(ctx, GOOM_EINVAL, "unknown flags 0x%x", (unsigned)sh.flags);
+    if (sh.seqs < 0 || sh.tokens < 0) return goom::fail(ctx, GOOM_EINVAL, "negative number of sequences or tokens");
+    if (sh.heads <= 0 || sh.kv_heads <= 0 || sh.heads % sh.kv_heads) return goom::fail(ctx, GOOM_EINVAL, "kv_heads must be positive and divide heads");
+    if (sh.dk <= 0 || sh.dv <= 0) return goom::fail(ctx, GOOM_EINVAL, "dk and dv must be positive");
+    if (sh.dk > GOOM_MAX_DIM || sh.dv > GOOM_MAX_DIM) return goom::fail(ctx, GOOM_EUNSUPPORTED, "dk and dv go up to %d", GOOM_MAX_DIM);
+    if (!std::isfinite(sh.scale)) return goom::fail(ctx, GOOM_EINVAL, "scale must be finite");
+    if (sh.seqs == 0 && sh.tokens > 0) return goom::fail(ctx, GOOM_EINVAL, "tokens without a sequence");
+    if (!packed && sh.seqs > 0 && sh.tokens % sh.seqs) return goom::fail(ctx, GOOM_EINVAL, "without offsets the sequences have tokens / seqs tokens each");
+    if (need_equal && sh.seqs != sh.tokens) return goom::fail(ctx, GOOM_EINVAL, "one token a sequence");
+    if (sh.seqs > (1 << 26) / sh.heads || sh.tokens > (1ll << 40) || sh.tokens / CHUNK > (1 << 26) / sh.heads) return goom::fail(ctx, GOOM_EUNSUPPORTED, "too many sequences, heads or tokens");
+    const int64_t rows[3][3] = {{sh.q_token, sh.q_head, sh.dk}, {sh.k_token, sh.k_head, sh.dk}, {sh.v_token, sh.v_head, sh.dv}};
+    for (auto &x : rows)
+        if (x[0] < 0 || x[1] < 0 || ((x[0] || x[1]) && (x[0] < x[2] || x[1] < x[2])) || x[0] > (1ll << 32) || x[1] > (1ll << 32))
+            return goom::fail(ctx, GOOM_EINVAL, "strides of tokens and heads must be 0 (both: contiguous) or at least a head's entries");
+    if (!sh.q_token) { sh.q_token = (int64_t)sh.heads * sh.dk; sh.q_head = sh.dk; }
+    if (!sh.k_token) { sh.k_token = (int64_t)sh.kv_heads * sh.dk; sh.k_head = sh.dk; }
+    if (!sh.v_token) { sh.v_token = (int64_t)sh.kv_heads * sh.dv; sh.v_head = sh.dv; }
+    return GOOM_OK;
+}
+
+static int enter(goom_ctx *ctx)
+{
+    if (!ctx) return goom::fail(nullptr, GOOM_EINVAL, "null context");
+    if (!ctx->prof_keep) goom::prof_reset(ctx);
+    return goom::check_hip(ctx, hipSetDevice(ctx->device), "hipSetDevice");
+}
+
+static int check_workspace(goom_ctx *ctx, const void *ws, size_t given, size_t need)
+{
+    if (!need) return GOOM_OK;
+    if (!ws || given < need) return goom::fail(ctx, GOOM_EWORKSPACE, "workspace of %zu bytes needed, %zu given", need, ws ? given : (size_t)0);
+    if (!goom::aligned(ws, 256)) return goom::fail(ctx, GOOM_EINVAL, "workspace must be 256-byte aligned");
+    return GOOM_OK;
+}
+
+// bytes of the backward pass's workspace by parts: states of the three walks, floats of shared heads' gradients
+struct BackwardPlan {
+    Segments seg;
+    size_t totals_q, totals_k, totals_v, sum_k, sum_v, bytes;
+};
+
+static BackwardPlan backward_plan(const goom_attention_shape &sh, bool packed)
+{
+    BackwardPlan p;
+    p.seg = choose_segments(sh, 3, packed);
+    p.totals_q = totals_bytes(sh, p.seg, sh.dv, sh.dk);
+    p.totals_k = totals_bytes(sh, p.seg, sh.dv, sh.dk);
+    p.totals_v = totals_bytes(sh, p.seg, sh.dk, sh.dv);
+    const bool shared = sh.heads != sh.kv_heads;
+    p.sum_k = shared ? goom::align_up((size_t)sh.tokens * sh.heads * sh.dk * 4, 256) : 0;
+    p.sum_v = shared ? goom::align_up((size_t)sh.tokens * sh.heads * sh.dv * 4, 256) : 0;
+    p.bytes = p.totals_q + p.totals_k + p.totals_v + p.sum_k + p.sum_v;
+    return p;
+}
+
+template <typename S> static void launch_shared_sum(goom_ctx *ctx, const float *x, void *y, long long rows, int group, int d)
+{
+    const long long n = rows * d, blocks = (n + 255) / 256;
+    goom::prof_begin(ctx, "linear attention: shared heads");
+    shared_sum_kernel<S><<<(unsigned)(blocks < 16384 ? blocks : 16384), 256, 0, ctx->stream>>>(x, reinterpret_cast<S *>(y), n, group, d);
+    goom::prof_end(ctx);
+}
+
+} // namespace goom_layer
+
+using namespace goom_layer;
+using goom::aligned;
+using goom::fail;
+
+extern "C" {
+
+size_t goom_linear_attention_workspace_bytes(const goom_attention_shape *shape, int packed)
+{
+    goom_attention_shape sh;
+    if (check_shape(nullptr, shape, sh, packed != 0, false)) return 0;
+    return totals_bytes(sh, choose_segments(sh, 1, packed != 0), sh.dk, sh.dv);
+}
+
+int goom_linear_attention(goom_ctx *ctx, const goom_attention_shape *shape, const void *q, const void *k, const void *v, const float *log_decay,
+                          const int64_t *offsets, const float *state, void *o, float *final_state, void *workspace, size_t workspace_bytes)
+{
+    goom_attention_shape sh;
+    if (int s = check_shape(ctx, shape, sh, offsets != nullptr, false)) return s;
+    if (sh.seqs == 0) return ctx ? GOOM_OK : fail(nullptr, GOOM_EINVAL, "null context");
+    const size_t size = real_bytes(sh.type);
+    if (!log_decay || (sh.tokens > 0 && (!q || !k || !v || !o))) return fail(ctx, GOOM_EINVAL, "null data pointer");
+    if (!aligned(q, size) || !aligned(k, size) || !aligned(v, size) || !aligned(o, size) || !aligned(log_decay, 4) || !aligned(state, 4) || !aligned(final_state, 4) ||
+        !aligned(offsets, 8))
+        return fail(ctx, GOOM_EINVAL, "misaligned data pointer");
+    const Segments g = choose_segments(sh, 1, offsets != nullptr);
+    const size_t need = totals_bytes(sh, g, sh.dk, sh.dv);
+    if (int s = check_workspace(ctx, workspace, workspace_bytes, need)) return s;
+    if (int s = enter(ctx)) return s;
+    WalkArgs w = walk_args(sh, log_decay, offsets, g);
+    const int group = sh.heads / sh.kv_heads;
+    const Rows rq = {q, sh.q_token, sh.q_head, 1, sh.dk}, rk = {k, sh.k_token, sh.k_head, group, sh.dk}, rv = {v, sh.v_token, sh.v_head, group, sh.dv};
+    WalkRole &r = w.role[0];
+    r = role(rq, rk, rv, o, 0, sh.heads, 0, size);
+    r.p_scale = r.w_scale = (float)sh.scale;
+    r.init = state;
+    r.fin = final_state;
+    r.totals = need ? reinterpret_cast<float *>(workspace) : nullptr;
+    return launch_walks(ctx, sh.type, w, 1, g.slots, "linear attention");
+}
+
+int goom_linear_attention_step(goom_ctx *ctx, const goom_attention_shape *shape, const void *q, const void *k, const void *v, const float *log_decay, const float *state,
+                               void *o, float *next_state)
+{
+    goom_attention_shape sh;
+    if (int s = check_shape(ctx, shape, sh, false, true)) return s;
+    if (sh.seqs == 0) return ctx ? GOOM_OK : fail(nullptr, GOOM_EINVAL, "null context");
+    const size_t size = real_bytes(sh.type);
+    if (!q || !k || !v || !log_decay || !o || !next_state) return fail(ctx, GOOM_EINVAL, "null data pointer");
+    if (!aligned(q, size) || !aligned(k, size) || !aligned(v, size) || !aligned(o, size) || !aligned(log_decay, 4) || !aligned(state, 4) || !aligned(next_state, 4))
+        return fail(ctx, GOOM_EINVAL, "misaligned data pointer");
+    if (int s = enter(ctx)) return s;
+    const dim3 grid((unsigned)(sh.seqs * sh.heads), (sh.dv + 31) / 32);
+    const bool vec = sh.dv % 4 == 0 && aligned(state, 16) && aligned(next_state, 16);
+    goom::prof_begin(ctx, "linear attention: one token");
+    const int rc = with_type(sh.type, [&](auto tag) {
+        typedef typename decltype(tag)::type S;
+        auto *kernel = vec ? step_kernel<S, true> : step_kernel<S, false>;
+        kernel<<<grid, 256, 0, ctx->stream>>>(sh, reinterpret_cast<const S *>(q), reinterpret_cast<const S *>(k), reinterpret_cast<const S *>(v), log_decay, state,
+                                              reinterpret_cast<S *>(o), next_state);
+        return goom::check_hip(ctx, hipGetLastError(), "linear attention step");
+    });
+    goom::prof_end(ctx);
+    return rc;
+}
+
+size_t goom_linear_attention_backward_workspace_bytes(const goom_attention_shape *shape, int packed)
+{
+    goom_attention_shape sh;
+    if (check_shape(nullptr, shape, sh, packed != 0, false)) return 0;
+    return backward_plan(sh, packed != 0).bytes;
+}
+
+int goom_linear_attention_backward(goom_ctx *ctx, const goom_attention_shape *shape, const void *q, const void *k, const void *v, const float *log_decay,
+                                   const int64_t *offsets, const float *state, const void *grad_o, const float *grad_final, void *grad_q, void *grad_k, void *grad_v,
+                                   float *grad_state, void *workspace, size_t workspace_bytes)
+{
+    goom_attention_shape sh;
+    if (int s = check_shape(ctx, shape, sh, offsets != nullptr, false)) return s;
+    if (sh.seqs == 0) return ctx ? GOOM_OK : fail(nullptr, GOOM_EINVAL, "null context");
+    const size_t size = real_bytes(sh.type);
+    if (!log_decay || (sh.tokens > 0 && (!q || !k || !v || !grad_o || !grad_q || !grad_k || !grad_v))) return fail(ctx, GOOM_EINVAL, "null data pointer");
+    const void *const typed[] = {q, k, v, grad_o, grad_q, grad_k, grad_v}, *const floats[] = {log_decay, state, grad_final, grad_state};
+    for (const void *p : typed)
+        if (!aligned(p, size)) return fail(ctx, GOOM_EINVAL, "misaligned data pointer");
+    for (const void *p : floats)
+        if (!aligned(p, 4)) return fail(ctx, GOOM_EINVAL, "misaligned data pointer");
+    if (!aligned(offsets, 8)) return fail(ctx, GOOM_EINVAL, "misaligned data pointer");
+    const BackwardPlan plan = backward_plan(sh, offsets != nullptr);
+    if (int s = check_workspace(ctx, workspace, workspace_bytes, plan.bytes)) return s;
+    if (int s = enter(ctx)) return s;
+
+    unsigned char *ws = reinterpret_cast<unsigned char *>(workspace);
+    auto take = [&](size_t bytes) {
+        void *p = bytes ? ws : nullptr;
+        ws += bytes;
+        return reinterpret_cast<float *>(p);
+    };
+    float *const totals_q = take(plan.totals_q), *const totals_k = take(plan.totals_k), *const totals_v = take(plan.totals_v);
+    float *const sum_k = take(plan.sum_k), *const sum_v = take(plan.sum_v);
+    const int group = sh.heads / sh.kv_heads, shared = group > 1;
+    const Rows rq = {q, sh.q_token, sh.q_head, 1, sh.dk}, rk = {k, sh.k_token, sh.k_head, group, sh.dk}, rv = {v, sh.v_token, sh.v_head, group, sh.dv},
+               rg = {grad_o, (long long)sh.heads * sh.dv, sh.dv, 1, sh.dv};
+    const float scale = (float)sh.scale;
+    WalkRole gq = role(rg, rv, rk, grad_q, 0, sh.heads, 0, size);
+    gq.p_scale = gq.w_scale = scale;
+    gq.init = state;
+    gq.state_row = 1;
+    gq.state_col = sh.dv;
+    gq.totals = totals_q;
+    WalkRole gk = role(rv, rg, rq, shared ? (void *)sum_k : grad_k, shared, sh.heads, 1, size);
+    gk.p_scale = gk.u_scale = scale;
+    gk.init = grad_final;
+    gk.state_row = 1;
+    gk.state_col = sh.dv;
+    gk.totals = totals_k;
+    WalkRole gv = role(rk, rq, rg, shared ? (void *)sum_v : grad_v, shared, sh.heads, 1, size);
+    gv.p_scale = gv.u_scale = scale;
+    gv.init = grad_final;
+    gv.fin = grad_state;
+    gv.totals = totals_v;
+
+    WalkArgs w = walk_args(sh, log_decay, offsets, plan.seg);
+    w.role[0] = gq;
+    w.role[1] = gk;
+    w.role[2] = gv;
+    if (padded_head(sh.dk) == padded_head(sh.dv)) {
+        if (int s = launch_walks(ctx, sh.type, w, 3, plan.seg.slots, "linear attention: gradients")) return s;
+    } else {
+        if (int s = launch_walks(ctx, sh.type, w, 2, plan.seg.slots, "linear attention: gradients of q and k")) return s;
+        w.role[0] = gv;
+        if (int s = launch_walks(ctx, sh.type, w, 1, plan.seg.slots, "linear attention: gradient of v")) return s;
+    }
+    if (shared && sh.tokens > 0) {
+        const long long rows = sh.tokens * sh.kv_heads;
+        return with_type(sh.type, [&](auto tag) {
+            typedef typename decltype(tag)::type S;
+            launch_shared_sum<S>(ctx, sum_k, grad_k, rows, group, sh.dk);
+            launch_shared_sum<S>(ctx, sum_v, grad_v, rows, group, sh.dv);
+            return goom::check_hip(ctx, hipGetLastError(), "linear attention: shared heads");
+        });
+    }
+    return GOOM_OK;
+}
+
+} // extern "C"
