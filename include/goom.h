@@ -532,6 +532,51 @@ int goom_linear_attention_backward(goom_ctx *ctx, const goom_attention_shape *sh
                                    void *workspace, size_t workspace_bytes);
 size_t goom_linear_attention_backward_workspace_bytes(const goom_attention_shape *shape, int packed);
 
+/* Group norm with an activation, channels last.  x: [items, length, channels]; a group is channels / groups neighbouring
+ * channels over the whole length of an item (length 1: over one position, as after the heads of a recurrence):
+ *     y = act((x - mean) rstd weight + bias),    rstd = 1 / sqrt(variance + eps). */
+#define GOOM_ACT_NONE 0
+#define GOOM_ACT_SILU 1 /* z / (1 + e^-z) */
+#define GOOM_ACT_GELU 2 /* z (1 + erf(z / sqrt 2)) / 2 */
+typedef struct goom_norm_shape {
+    int64_t items, length;
+    int32_t channels, groups; /* groups divides channels */
+    int32_t type;             /* GOOM_REAL_* of x, y and their gradients */
+    int32_t param_type;       /* GOOM_REAL_* of weight, bias and their gradients */
+    int32_t activation;       /* GOOM_ACT_* */
+    int32_t flags;            /* 0 */
+    double eps;               /* >= 0 */
+} goom_norm_shape;
+
+/* weight, bias: NULL (1 and 0) or [channels]; y: of x's shape; mean, rstd: NULL or [items, groups] floats, what the backward
+ * pass takes.  Groups of up to 2048 elements are held in registers and read once; longer ones (length above 1) are read a
+ * second time for the output.  workspace: goom_group_norm_workspace_bytes(shape) bytes (may be 0). */
+int goom_group_norm(goom_ctx *ctx, const goom_norm_shape *shape, const void *x, const void *weight, const void *bias, void *y,
+                    float *mean, float *rstd, void *workspace, size_t workspace_bytes);
+size_t goom_group_norm_workspace_bytes(const goom_norm_shape *shape);
+
+/* Gradients, given grad_y and the forward call's mean and rstd: with z = xhat weight + bias, dz = grad_y act'(z),
+ *     grad_x = rstd (dz weight - mean(dz weight) - xhat mean(dz weight xhat)),   grad_weight = sum dz xhat,   grad_bias = sum dz,
+ * means over the group, sums over items and length in a fixed order.  grad_weight, grad_bias: NULL or [channels] of param_type.
+ * workspace: goom_group_norm_backward_workspace_bytes(shape) bytes, required. */
+int goom_group_norm_backward(goom_ctx *ctx, const goom_norm_shape *shape, const void *x, const void *grad_y, const float *mean,
+                             const float *rstd, const void *weight, const void *bias, void *grad_x, void *grad_weight,
+                             void *grad_bias, void *workspace, size_t workspace_bytes);
+size_t goom_group_norm_backward_workspace_bytes(const goom_norm_shape *shape);
+
+/* Token embeddings: rows[i] = scale table[tokens[i]].  table: [vocab, width], rows: [n, width] of one type; tokens: [n] int64
+ * (device); a token outside 0 .. vocab - 1 (padding) gives a row of zeros and takes no gradient. */
+int goom_embedding(goom_ctx *ctx, const void *table, const int64_t *tokens, void *rows, int64_t n, int64_t vocab, int width,
+                   int type, double scale);
+
+/* Its gradient: grad_table[t] = scale (sum of grad[i] over the i with tokens[i] = t), every row of [vocab, width] written, rows
+ * without a token as zeros.  The positions are sorted by token (stably), each token's gradients are summed in float in the order
+ * of their positions, in groups of 64 sorted positions, so that results do not vary from run to run.  type: of grad; table_type:
+ * of grad_table.  workspace: goom_embedding_backward_workspace_bytes(n, vocab, width) bytes. */
+int goom_embedding_backward(goom_ctx *ctx, const int64_t *tokens, const void *grad, void *grad_table, int64_t n, int64_t vocab,
+                            int width, int type, int table_type, double scale, void *workspace, size_t workspace_bytes);
+size_t goom_embedding_backward_workspace_bytes(int64_t n, int64_t vocab, int width);
+
 #pragma GCC visibility pop
 #ifdef __cplusplus
 }

@@ -20,6 +20,7 @@ LMME_FAST, LMME_EXACT = 0, 1
 RESET_ALWAYS, RESET_COLINEAR, RESET_NEVER = 1, 0, -1
 AFFINE_TIME_INVARIANT = 1
 REAL_F32, REAL_BF16, REAL_F16 = 16, 17, 18
+ACTIVATIONS = {"none": 0, "silu": 1, "gelu": 2}
 
 EXPORTS = [
     "goom_version", "goom_create", "goom_destroy", "goom_set_stream", "goom_last_error",
@@ -35,6 +36,8 @@ EXPORTS = [
     "goom_lmme_backward", "goom_lmme_backward_workspace_bytes", "goom_scan_backward", "goom_scan_backward_workspace_bytes", "goom_scaled_exp_backward",
     "goom_linear_attention", "goom_linear_attention_workspace_bytes", "goom_linear_attention_step",
     "goom_linear_attention_backward", "goom_linear_attention_backward_workspace_bytes",
+    "goom_group_norm", "goom_group_norm_workspace_bytes", "goom_group_norm_backward", "goom_group_norm_backward_workspace_bytes",
+    "goom_embedding", "goom_embedding_backward", "goom_embedding_backward_workspace_bytes",
 ]
 
 
@@ -56,6 +59,11 @@ class AttentionShape(C.Structure):
     _fields_ = [("seqs", C.c_int64), ("tokens", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("dk", C.c_int32), ("dv", C.c_int32),
                 ("type", C.c_int32), ("flags", C.c_int32), ("scale", C.c_double), ("q_token", C.c_int64), ("q_head", C.c_int64),
                 ("k_token", C.c_int64), ("k_head", C.c_int64), ("v_token", C.c_int64), ("v_head", C.c_int64)]
+
+
+class NormShape(C.Structure):
+    _fields_ = [("items", C.c_int64), ("length", C.c_int64), ("channels", C.c_int32), ("groups", C.c_int32), ("type", C.c_int32),
+                ("param_type", C.c_int32), ("activation", C.c_int32), ("flags", C.c_int32), ("eps", C.c_double)]
 
 
 def library_path() -> str:
@@ -147,6 +155,15 @@ def load_library():
     lib.goom_linear_attention_backward.argtypes = [vp, pa, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz]
     lib.goom_linear_attention_backward_workspace_bytes.argtypes = [pa, i32]
     lib.goom_linear_attention_backward_workspace_bytes.restype = sz
+    pn = C.POINTER(NormShape)
+    lib.goom_group_norm.argtypes = [vp, pn, vp, vp, vp, vp, vp, vp, vp, sz]
+    lib.goom_group_norm_backward.argtypes = [vp, pn, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz]
+    for f in (lib.goom_group_norm_workspace_bytes, lib.goom_group_norm_backward_workspace_bytes):
+        f.argtypes, f.restype = [pn], sz
+    lib.goom_embedding.argtypes = [vp, vp, vp, vp, i64, i64, i32, i32, C.c_double]
+    lib.goom_embedding_backward.argtypes = [vp, vp, vp, vp, i64, i64, i32, i32, i32, C.c_double, vp, sz]
+    lib.goom_embedding_backward_workspace_bytes.argtypes = [i64, i64, i32]
+    lib.goom_embedding_backward_workspace_bytes.restype = sz
     _lib = lib
     return lib
 
@@ -690,3 +707,65 @@ class Goom:
                                                             _ptr(grad_o), self._state(grad_state, shape, "grad_state"), _ptr(gq), _ptr(gk), _ptr(gv), _ptr(gs),
                                                             _ptr(ws), wsn))
         return gq, gk, gv, gs
+
+    # ---- group norm with an activation, channels last
+    def _norm(self, x, groups, weight, bias, eps, activation):
+        if x.dim() < 2 or activation not in ACTIVATIONS:
+            raise ValueError("x: [items, ..., channels]; activation: one of " + ", ".join(ACTIVATIONS))
+        params = [p for p in (weight, bias) if p is not None]
+        if any(p.dtype != params[0].dtype or tuple(p.shape) != (x.shape[-1],) for p in params):
+            raise ValueError("weight and bias: [channels], of one type")
+        items, channels = x.shape[0], x.shape[-1]
+        code = _real_code(params[0]) if params else REAL_F32
+        return NormShape(items, x.shape[1:-1].numel(), channels, groups, _real_code(x), code, ACTIVATIONS[activation], 0, eps)
+
+    def group_norm(self, x, groups: int, weight=None, bias=None, eps: float = 1e-5, activation: str = "none", want_stats: bool = False):
+        """act(normalised x * weight + bias); x: [items, ..., channels], statistics over the axes between and channels / groups
+        neighbouring channels ([tokens, channels]: every token by itself).  want_stats: also mean and rstd, float32 [items, groups]."""
+        torch = self.torch
+        shape = self._norm(x, groups, weight, bias, eps, activation)
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        mean, rstd = (torch.empty((shape.items, groups), dtype=torch.float32, device=x.device) if want_stats else None for _ in range(2))
+        ws, wsn = self.workspace(self.lib.goom_group_norm_workspace_bytes(C.byref(shape)))
+        self._check(self.lib.goom_group_norm(self._ctx, C.byref(shape), _ptr(x), _ptr(weight), _ptr(bias), _ptr(y), _ptr(mean), _ptr(rstd), _ptr(ws), wsn))
+        return (y, mean, rstd) if want_stats else y
+
+    def group_norm_backward(self, x, grad_y, mean, rstd, groups: int, weight=None, bias=None, activation: str = "none"):
+        """Gradients with respect to x, weight and bias (of their type; float32 where there is none)."""
+        torch = self.torch
+        shape = self._norm(x, groups, weight, bias, 0.0, activation)
+        if grad_y.shape != x.shape or grad_y.dtype != x.dtype or tuple(mean.shape) != (shape.items, groups) or mean.shape != rstd.shape \
+                or mean.dtype != torch.float32 or rstd.dtype != torch.float32:
+            raise ValueError("grad_y: of x's shape and type; mean, rstd: float32 [items, groups]")
+        ptype = weight.dtype if weight is not None else bias.dtype if bias is not None else torch.float32
+        gx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        gw, gb = (torch.empty(x.shape[-1], dtype=ptype, device=x.device) for _ in range(2))
+        ws, wsn = self.workspace(self.lib.goom_group_norm_backward_workspace_bytes(C.byref(shape)))
+        self._check(self.lib.goom_group_norm_backward(self._ctx, C.byref(shape), _ptr(x), _ptr(grad_y), _ptr(mean), _ptr(rstd), _ptr(weight), _ptr(bias), _ptr(gx),
+                                                      _ptr(gw), _ptr(gb), _ptr(ws), wsn))
+        return gx, gw, gb
+
+    # ---- token embeddings
+    def embedding(self, table, tokens, scale: float = 1.0, out=None):
+        """scale * table[tokens], zeros for tokens outside the table (padding); table: [vocab, width], tokens: int64."""
+        torch = self.torch
+        if table.dim() != 2 or tokens.dtype != torch.int64:
+            raise ValueError("table: [vocab, width]; tokens: int64")
+        if out is None:
+            out = torch.empty(tuple(tokens.shape) + (table.shape[1],), dtype=table.dtype, device=table.device)
+        elif tuple(out.shape) != tuple(tokens.shape) + (table.shape[1],) or out.dtype != table.dtype:
+            raise ValueError("out: the tokens' shape with the table's width, of its type")
+        self._check(self.lib.goom_embedding(self._ctx, _ptr(table), _ptr(tokens), _ptr(out), tokens.numel(), table.shape[0], table.shape[1], _real_code(table), scale))
+        return out
+
+    def embedding_backward(self, tokens, grad, vocab: int, scale: float = 1.0, dtype=None):
+        """Gradient with respect to the table, [vocab, width], of type `dtype` (grad's if None), given grad: the tokens' shape with
+        the width."""
+        torch = self.torch
+        if tokens.dtype != torch.int64 or grad.shape[:-1] != tokens.shape:
+            raise ValueError("tokens: int64; grad: the tokens' shape with the width")
+        out = torch.empty((vocab, grad.shape[-1]), dtype=dtype or grad.dtype, device=grad.device)
+        ws, wsn = self.workspace(self.lib.goom_embedding_backward_workspace_bytes(tokens.numel(), vocab, grad.shape[-1]))
+        self._check(self.lib.goom_embedding_backward(self._ctx, _ptr(tokens), _ptr(grad), _ptr(out), tokens.numel(), vocab, grad.shape[-1], _real_code(grad),
+                                                     _real_code(out), scale, _ptr(ws), wsn))
+        return out

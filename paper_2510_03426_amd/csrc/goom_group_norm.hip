@@ -1,0 +1,687 @@
+// Group norm with an activation, channels last, and its gradient.
+//
+// Bound by the bytes of its tensors.  Two ways:
+//   short groups (up to 32 elements a lane of a wave): a team of 2^k lanes holds one group in registers, so that every tensor
+//     is read once; statistics are taken about the mean itself.  A team keeps its group number from item to item, so weights are
+//     loaded once and their gradients are summed in registers.
+//   long groups (over many positions): a workgroup takes a slab of whole groups and a chunk of positions; sums first, then
+//     the output in a second launch, whose reads mostly hit the last-level cache.  Sums for the mean and the variance are
+//     double and taken about the group's first element: no cancellation, whatever the mean.
+// Weight gradients: one partial sum per workgroup and channel, added up in a fixed order by a last launch.
+#include <cmath>
+
+#include "goom_real.h"
+
+namespace goom_layer {
+
+constexpr int TEAM_ELEMENTS = 32;    // of a group, per lane
+constexpr int CHUNK_ROWS = 128;      // positions a thread of the long kernels sums at most, in floats
+
+struct NormArgs {
+    const void *x, *gy;
+    const void *weight, *bias;
+    void *y;                 // or grad_x
+    float *mean, *rstd;      // forward: outputs (may be NULL); backward: inputs
+    long long items, length;
+    int channels, groups, cg; // cg: channels of a group
+    int type_w, act;
+    float eps;
+    // short
+    int team, gpw, ipw;      // lanes of a team; groups and items that a workgroup has at once
+    float *partial;          // [workgroups along x][2][channels]: sums of dz xhat, of dz
+    // long
+    double *stats;           // [items][chunks][groups][2]
+    float *sums;             // [items][chunks][2][channels]
+    float *means;            // [items][groups][2]
+    int gps, rows_at_once, threads;  // groups of a slab, positions at once
+    long long chunks, chunk_len;
+};
+
+__device__ inline float param(const void *p, int type, int i, float otherwise)
+{
+    if (!p) return otherwise;
+    return type == GOOM_REAL_F32 ? reinterpret_cast<const float *>(p)[i] : type == GOOM_REAL_BF16 ? (float)reinterpret_cast<const bf16 *>(p)[i] : (float)reinterpret_cast<const f16 *>(p)[i];
+}
+
+__device__ inline float activate(float z, int act)
+{
+    if (act == GOOM_ACT_SILU) return z / (1.0f + expf(-z));
+    if (act == GOOM_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    return z;
+}
+
+__device__ inline float activate_slope(float z, int act)
+{
+    if (act == GOOM_ACT_SILU) {
+        const float p = 1.0f / (1.0f + expf(-z));
+        return p * (1.0f + z * (1.0f - p));
+    }
+    if (act == GOOM_ACT_GELU) return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * expf(-0.5f * z * z);
+    return 1.0f;
+}
+
+__device__ inline float team_sum(float v, int team)
+{
+    for (int s = 1; s < team; s *= 2) v += __shfl_xor(v, s);
+    return v;
+}
+
+// ---- short groups.  Unit u of a group (u < length cg / V): position u / (cg / V), channels V (u % (cg / V)) on; lane l of the
+// team has the units l, l + team, ...  grid: (workgroups over items, parts of the groups)
+template <typename S, int V, int J, bool BACK> __global__ __launch_bounds__(256) void norm_team_kernel(NormArgs a)
+{
+    const int lane = threadIdx.x % a.team, team = threadIdx.x / a.team, ti = team / a.gpw, group = blockIdx.y * a.gpw + team % a.gpw;
+    const bool live = ti < a.ipw && group < a.groups;
+    const int cu = a.cg / V, units = cu * (int)a.length;
+    const float count = (float)a.cg * (float)a.length;
+    int off[J], chan[J];     // of this lane's units: element offsets within the item, channels
+    float w[J][V], b[J][V], sw[J][V], sb[J][V];
+#pragma unroll
+    for (int j = 0; j < J; j++) {
+        const int u = lane + j * a.team;
+        chan[j] = live && u < units ? group * a.cg + u % cu * V : -1;
+        off[j] = chan[j] >= 0 ? u / cu * a.channels + chan[j] : 0;
+#pragma unroll
+        for (int e = 0; e < V; e++) {
+            w[j][e] = chan[j] >= 0 ? param(a.weight, a.type_w, chan[j] + e, 1.0f) : 0.0f;
+            b[j][e] = chan[j] >= 0 ? param(a.bias, a.type_w, chan[j] + e, 0.0f) : 0.0f;
+            sw[j][e] = sb[j][e] = 0.0f;
+        }
+    }
+    const long long size = a.length * a.channels;
+    const S *const xs = reinterpret_cast<const S *>(a.x);
+    const S *const gs = reinterpret_cast<const S *>(a.gy);
+    S *const ys = reinterpret_cast<S *>(a.y);
+    for (long long item0 = (long long)blockIdx.x * a.ipw; item0 < a.items; item0 += (long long)gridDim.x * a.ipw) {
+        const long long item = item0 + ti;
+        const bool here = live && item < a.items; // (the same for a whole team; other lanes go along for the shuffles)
+        float x[J][V], dz[J][V];
+#pragma unroll
+        for (int j = 0; j < J; j++) {
+            if (here && chan[j] >= 0) {
+                load_floats<S, V>(xs + item * size + off[j], x[j]);
+                if (BACK) load_floats<S, V>(gs + item * size + off[j], dz[j]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; e++) x[j][e] = dz[j][e] = 0.0f;
+            }
+        }
+        if (!BACK) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < J; j++)
+#pragma unroll
+                for (int e = 0; e < V; e++) sum += x[j][e];
+            const float mean = team_sum(sum, a.team) / count;
+            float square = 0.0f;
+#pragma unroll
+            for (int j = 0; j < J; j++)
+                if (chan[j] >= 0) {
+#pragma unroll
+                    for (int e = 0; e < V; e++) {
+                        x[j][e] -= mean;
+                        square += x[j][e] * x[j][e];
+                    }
+                }
+            const float rstd = 1.0f / sqrtf(team_sum(square, a.team) / count + a.eps);
+            if (here && lane == 0) {
+                if (a.mean) a.mean[item * a.groups + group] = mean;
+                if (a.rstd) a.rstd[item * a.groups + group] = rstd;
+            }
+#pragma unroll
+            for (int j = 0; j < J; j++)
+                if (here && chan[j] >= 0) {
+#pragma unroll
+                    for (int e = 0; e < V; e++) x[j][e] = activate(x[j][e] * rstd * w[j][e] + b[j][e], a.act);
+                    store_floats<S, V>(ys + item * size + off[j], x[j]);
+                }
+        } else {
+            const float mean = here ? a.mean[item * a.groups + group] : 0.0f, rstd = here ? a.rstd[item * a.groups + group] : 0.0f;
+            float m1 = 0.0f, m2 = 0.0f;
+#pragma unroll
+            for (int j = 0; j < J; j++)
+                if (here && chan[j] >= 0) {
+#pragma unroll
+                    for (int e = 0; e < V; e++) {
+                        x[j][e] = (x[j][e] - mean) * rstd;
+                        dz[j][e] *= activate_slope(x[j][e] * w[j][e] + b[j][e], a.act);
+                        sw[j][e] += dz[j][e] * x[j][e];
+                        sb[j][e] += dz[j][e];
+                        dz[j][e] *= w[j][e];
+                        m1 += dz[j][e];
+                        m2 += dz[j][e] * x[j][e];
+                    }
+                }
+            m1 = team_sum(m1, a.team) / count;
+            m2 = team_sum(m2, a.team) / count;
+#pragma unroll
+            for (int j = 0; j < J; j++)
+                if (here && chan[j] >= 0) {
+#pragma unroll
+                    for (int e = 0; e < V; e++) x[j][e] = rstd * (dz[j][e] - m1 - x[j][e] * m2);
+                    store_floats<S, V>(ys + item * size + off[j], x[j]);
+                }
+        }
+    }
+    if (BACK) { // the workgroup's channels: sums over its teams of a group and over positions, in order
+        __shared__ float meet[256 * J * V];
+        const int span = a.gpw * a.cg; // channels of this workgroup
+        for (int which = 0; which < 2; which++) {
+#pragma unroll
+            for (int j = 0; j < J; j++)
+#pragma unroll
+                for (int e = 0; e < V; e++) meet[(j * V + e) * 256 + threadIdx.x] = which ? sb[j][e] : sw[j][e];
+            __syncthreads();
+            for (int c = threadIdx.x; c < span; c += 256) {
+                const int tg = c / a.cg, cc = c % a.cg;
+                if (blockIdx.y * a.gpw + tg >= a.groups) continue;
+                float sum = 0.0f;
+                for (int t = 0; t < a.ipw; t++)
+                    for (int u = cc / V; u < units; u += cu) sum += meet[(u / a.team * V + cc % V) * 256 + (t * a.gpw + tg) * a.team + u % a.team];
+                a.partial[((long long)blockIdx.x * 2 + which) * a.channels + (blockIdx.y * a.gpw) * a.cg + c] = sum;
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// gw[c] = sum of partial[k][0][c], gb[c] = sum of partial[k][1][c] over k < n; 32 channels a workgroup, eight runs of k each
+__global__ __launch_bounds__(256) void norm_weight_kernel(const float *partial, long long n, int channels, void *gw, void *gb, int type_w)
+{
+    __shared__ double meet[8][32];
+    const int c = blockIdx.x * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
+    const long long len = (n + 7) / 8, begin = part * len, end = begin + len < n ? begin + len : n;
+    double sum = 0.0;
+    if (c < channels)
+        for (long long k = begin; k < end; k++) sum += (double)partial[(k * 2 + blockIdx.y) * channels + c];
+    meet[part][threadIdx.x & 31] = sum;
+    __syncthreads();
+    void *out = blockIdx.y ? gb : gw;
+    if (part == 0 && c < channels && out) {
+        for (int k = 1; k < 8; k++) sum += meet[k][threadIdx.x];
+        if (type_w == GOOM_REAL_F32) reinterpret_cast<float *>(out)[c] = (float)sum;
+        else if (type_w == GOOM_REAL_BF16) reinterpret_cast<bf16 *>(out)[c] = (bf16)(float)sum;
+        else reinterpret_cast<f16 *>(out)[c] = (f16)(float)sum;
+    }
+}
+
+// ---- long groups.  Thread (tx, ty): units tx, tx + columns, ... of the slab's V-element units, positions ty, ty + rows_at_once,
+// ... of the chunk.  A slab of several groups has at most as many units as a workgroup has columns.  grid: (items chunks, slabs)
+struct Slab { int group0, ngroups, units, columns, tx, ty; long long item, chunk, row0, row1; bool live; };
+
+template <int V> __device__ inline Slab slab_of(const NormArgs &a)
+{
+    Slab s;
+    s.group0 = blockIdx.y * a.gps;
+    s.ngroups = a.groups - s.group0 < a.gps ? a.groups - s.group0 : a.gps;
+    s.units = s.ngroups * (a.cg / V);
+    s.columns = a.threads / a.rows_at_once;
+    s.tx = threadIdx.x % s.columns;
+    s.ty = threadIdx.x / s.columns;
+    s.live = s.ty < a.rows_at_once;
+    s.item = blockIdx.x / a.chunks;
+    s.chunk = blockIdx.x % a.chunks;
+    s.row0 = s.chunk * a.chunk_len;
+    s.row1 = s.row0 + a.chunk_len < a.length ? s.row0 + a.chunk_len : a.length;
+    return s;
+}
+
+template <typename S, int V> __global__ __launch_bounds__(512) void norm_stats_kernel(NormArgs a)
+{
+    __shared__ double meet[2][512];
+    const Slab s = slab_of<V>(a);
+    const S *const x = reinterpret_cast<const S *>(a.x) + s.item * a.length * a.channels + s.group0 * a.cg;
+    const int cu = a.cg / V;
+    double sum = 0.0, square = 0.0;
+    for (int u = s.tx; s.live && u < s.units; u += s.columns) {
+        const double pivot = (double)(float)x[u / cu * a.cg]; // first element of the group
+        for (long long row = s.row0 + s.ty; row < s.row1; row += a.rows_at_once) {
+            float v[V];
+            load_floats<S, V>(x + row * a.channels + u * V, v);
+#pragma unroll
+            for (int e = 0; e < V; e++) {
+                const double d = (double)v[e] - pivot;
+                sum += d;
+                square += d * d;
+            }
+        }
+    }
+    meet[0][threadIdx.x] = sum;
+    meet[1][threadIdx.x] = square;
+    __syncthreads();
+    // a wave a group: its threads are the columns [g cu, (g + 1) cu) in every row, or (one group) all
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = (blockDim.x + 63) / 64;
+    for (int g = wave; g < s.ngroups; g += waves) {
+        const int width = s.ngroups == 1 ? s.columns : cu, total = width * a.rows_at_once;
+        double p = 0.0, q = 0.0;
+        for (int k = lane; k < total; k += 64) {
+            const int t = k / width * s.columns + (s.ngroups == 1 ? 0 : g * cu) + k % width;
+            p += meet[0][t];
+            q += meet[1][t];
+        }
+        for (int m = 1; m < 64; m *= 2) {
+            p += __shfl_xor(p, m);
+            q += __shfl_xor(q, m);
+        }
+        if (lane == 0) {
+            double *to = a.stats + ((s.item * a.chunks + s.chunk) * a.groups + s.group0 + g) * 2;
+            to[0] = p;
+            to[1] = q;
+        }
+    }
+}
+
+template <typename S, int V> __global__ __launch_bounds__(512) void norm_apply_kernel(NormArgs a)
+{
+    __shared__ float stat[512][2];
+    const Slab s = slab_of<V>(a);
+    const long long base = s.item * a.length * a.channels + s.group0 * a.cg;
+    const S *const x = reinterpret_cast<const S *>(a.x) + base;
+    S *const y = reinterpret_cast<S *>(a.y) + base;
+    const int cu = a.cg / V;
+    for (int g = threadIdx.x; g < s.ngroups; g += blockDim.x) {
+        double p = 0.0, q = 0.0;
+        for (long long k = 0; k < a.chunks; k++) {
+            const double *from = a.stats + ((s.item * a.chunks + k) * a.groups + s.group0 + g) * 2;
+            p += from[0];
+            q += from[1];
+        }
+        const double n = (double)a.length * a.cg, d = p / n;
+        const double var = q / n - d * d;
+        stat[g][0] = (float)((double)(float)x[g * a.cg] + d);
+        stat[g][1] = (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + (double)a.eps));
+        if (s.chunk == 0) {
+            if (a.mean) a.mean[s.item * a.groups + s.group0 + g] = stat[g][0];
+            if (a.rstd) a.rstd[s.item * a.groups + s.group0 + g] = stat[g][1];
+        }
+    }
+    __syncthreads();
+    for (int u = s.tx; s.live && u < s.units; u += s.columns) {
+        const float mean = stat[u / cu][0], rstd = stat[u / cu][1];
+        float w[V], b[V];
+#pragma unroll
+        for (int e = 0; e < V; e++) {
+            w[e] = param(a.weight, a.type_w, s.group0 * a.cg + u * V + e, 1.0f);
+            b[e] = param(a.bias, a.type_w, s.group0 * a.cg + u * V + e, 0.0f);
+        }
+        for (long long row = s.row0 + s.ty; row < s.row1; row += a.rows_at_once) {
+            float v[V];
+            load_floats<S, V>(x + row * a.channels + u * V, v);
+#pragma unroll
+            for (int e = 0; e < V; e++) v[e] = activate((v[e] - mean) * rstd * w[e] + b[e], a.act);
+            store_floats<S, V>(y + row * a.channels + u * V, v);
+        }
+    }
+}
+
+// per channel: sums over the chunk's positions of dz xhat and of dz
+template <typename S, int V> __global__ __launch_bounds__(512) void norm_sums_kernel(NormArgs a)
+{
+    __shared__ float meet[2 * V][512];
+    const Slab s = slab_of<V>(a);
+    const long long base = s.item * a.length * a.channels + s.group0 * a.cg;
+    const S *const x = reinterpret_cast<const S *>(a.x) + base;
+    const S *const gy = reinterpret_cast<const S *>(a.gy) + base;
+    const int cu = a.cg / V;
+    for (int u0 = 0; u0 < s.units; u0 += s.columns) {
+        const int u = u0 + s.tx;
+        float sw[V] = {}, sb[V] = {};
+        if (s.live && u < s.units) {
+            const float mean = a.mean[s.item * a.groups + s.group0 + u / cu], rstd = a.rstd[s.item * a.groups + s.group0 + u / cu];
+            float w[V], b[V];
+#pragma unroll
+            for (int e = 0; e < V; e++) {
+                w[e] = param(a.weight, a.type_w, s.group0 * a.cg + u * V + e, 1.0f);
+                b[e] = param(a.bias, a.type_w, s.group0 * a.cg + u * V + e, 0.0f);
+            }
+            for (long long row = s.row0 + s.ty; row < s.row1; row += a.rows_at_once) {
+                float v[V], g[V];
+                load_floats<S, V>(x + row * a.channels + u * V, v);
+                load_floats<S, V>(gy + row * a.channels + u * V, g);
+#pragma unroll
+                for (int e = 0; e < V; e++) {
+                    const float xhat = (v[e] - mean) * rstd, dz = g[e] * activate_slope(xhat * w[e] + b[e], a.act);
+                    sw[e] += dz * xhat;
+                    sb[e] += dz;
+                }
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < V; e++) {
+            meet[e][threadIdx.x] = sw[e];
+            meet[V + e][threadIdx.x] = sb[e];
+        }
+        __syncthreads();
+        if (s.ty == 0 && u < s.units) {
+            float *const to = a.sums + (s.item * a.chunks + s.chunk) * 2 * a.channels + s.group0 * a.cg + u * V;
+#pragma unroll
+            for (int e = 0; e < 2 * V; e++) {
+                float sum = 0.0f;
+                for (int r = 0; r < a.rows_at_once; r++) sum += meet[e][r * s.columns + s.tx];
+                to[(e / V) * a.channels + e % V] = sum;
+            }
+        }
+    }
+}
+
+// means over a group of dz w and of dz w xhat; one wave a group.  grid: items groups
+__global__ __launch_bounds__(64) void norm_means_kernel(NormArgs a)
+{
+    const long long item = blockIdx.x / a.groups;
+    const int group = blockIdx.x % a.groups;
+    double m1 = 0.0, m2 = 0.0;
+    for (int c = threadIdx.x; c < a.cg; c += 64) {
+        const int ch = group * a.cg + c;
+        double p = 0.0, q = 0.0;
+        for (long long k = 0; k < a.chunks; k++) {
+            const float *from = a.sums + (item * a.chunks + k) * 2 * a.channels + ch;
+            q += (double)from[0];
+            p += (double)from[a.channels];
+        }
+        const double w = (double)param(a.weight, a.type_w, ch, 1.0f);
+        m1 += w * p;
+        m2 += w * q;
+    }
+    for (int m = 1; m < 64; m *= 2) {
+        m1 += __shfl_xor(m1, m);
+        m2 += __shfl_xor(m2, m);
+    }
+    if (threadIdx.x == 0) {
+        const double n = (double)a.length * a.cg;
+        a.means[blockIdx.x * 2ll] = (float)(m1 / n);
+        a.means[blockIdx.x * 2ll + 1] = (float)(m2 / n);
+    }
+}
+
+template <typename S, int V> __global__ __launch_bounds__(512) void norm_grad_kernel(NormArgs a)
+{
+    const Slab s = slab_of<V>(a);
+    const long long base = s.item * a.length * a.channels + s.group0 * a.cg;
+    const S *const x = reinterpret_cast<const S *>(a.x) + base;
+    const S *const gy = reinterpret_cast<const S *>(a.gy) + base;
+    S *const gx = reinterpret_cast<S *>(a.y) + base;
+    const int cu = a.cg / V;
+    for (int u = s.tx; s.live && u < s.units; u += s.columns) {
+        const long long at = s.item * a.groups + s.group0 + u / cu;
+        const float mean = a.mean[at], rstd = a.rstd[at], m1 = a.means[at * 2], m2 = a.means[at * 2 + 1];
+        float w[V], b[V];
+#pragma unroll
+        for (int e = 0; e < V; e++) {
+            w[e] = param(a.weight, a.type_w, s.group0 * a.cg + u * V + e, 1.0f);
+            b[e] = param(a.bias, a.type_w, s.group0 * a.cg + u * V + e, 0.0f);
+        }
+        for (long long row = s.row0 + s.ty; row < s.row1; row += a.rows_at_once) {
+            float v[V], g[V];
+            load_floats<S, V>(x + row * a.channels + u * V, v);
+            load_floats<S, V>(gy + row * a.channels + u * V, g);
+#pragma unroll
+            for (int e = 0; e < V; e++) {
+                const float xhat = (v[e] - mean) * rstd, dz = g[e] * activate_slope(xhat * w[e] + b[e], a.act);
+                v[e] = rstd * (dz * w[e] - m1 - xhat * m2);
+            }
+            store_floats<S, V>(gx + row * a.channels + u * V, v);
+        }
+    }
+}
+
+// ---- host side
+
+struct NormPlan {
+    bool team;
+    int v, j;
+    long long blocks, parts;             // grid: along items (and chunks), along groups
+    NormArgs a;                          // the plan's own fields
+    size_t stats, sums, means, partial;  // bytes in the workspace
+};
+
+// v: elements of an access.  Short if a group's units fit a wave with TEAM_ELEMENTS elements a lane.
+static NormPlan norm_plan(const goom_norm_shape &sh, int v, bool back)
+{
+    NormPlan p = {};
+    NormArgs &a = p.a;
+    a.items = sh.items;
+    a.length = sh.length;
+    a.channels = sh.channels;
+    a.groups = sh.groups;
+    a.cg = sh.channels / sh.groups;
+    a.type_w = sh.param_type;
+    a.act = sh.activation;
+    a.eps = (float)sh.eps;
+    p.v = v;
+    const long long units = (long long)sh.length * (a.cg / v);
+    const int most = TEAM_ELEMENTS / v < 8 ? TEAM_ELEMENTS / v : 8;
+    p.team = units <= 64ll * most;
+    if (p.team) {
+        // as many lanes as hold the group with up to four units each: wide enough to have loads in flight
+        p.j = 1;
+        while (p.j < most && (p.j < 2 ? units > 16 : units > 64ll * p.j)) p.j *= 2;
+        a.team = 1;
+        while ((long long)a.team * p.j < units) a.team *= 2;
+        const int teams = 256 / a.team;
+        a.gpw = sh.groups < teams ? sh.groups : teams;
+        a.ipw = teams / a.gpw;
+        p.parts = (sh.groups + a.gpw - 1) / a.gpw;
+        p.blocks = (sh.items + a.ipw - 1) / a.ipw;
+        // Workgroups go over several items: where the weights' gradients are summed, no more partial sums than needed to fill
+        // the chip
+        const long long cap = (back ? 1024 : 8192) / p.parts > 0 ? (back ? 1024 : 8192) / p.parts : 1;
+        if (p.blocks > cap) p.blocks = cap;
+        p.partial = back ? goom::align_up((size_t)p.blocks * 2 * sh.channels * 4, 256) : 0;
+        return p;
+    }
+    const int cu = a.cg / v;
+    a.gps = cu >= 256 ? 1 : 256 / cu;
+    if (a.gps > sh.groups) a.gps = sh.groups;
+    const int columns = a.gps * cu < 256 ? a.gps * cu : 256;
+    a.rows_at_once = 512 / columns > 0 ? 512 / columns : 1;
+    if (columns * a.rows_at_once > 320 && a.rows_at_once > 1) { // 256 to 320 threads where that wastes fewer lanes
+        const int half = a.rows_at_once / 2;
+        if (columns * half >= 192) a.rows_at_once = half;
+    }
+    a.threads = columns * a.rows_at_once;
+    p.parts = (sh.groups + a.gps - 1) / a.gps;
+    // chunks: at most CHUNK_ROWS positions a thread, and enough workgroups to fill the chip
+    long long chunks = (sh.length + (long long)CHUNK_ROWS * a.rows_at_once - 1) / ((long long)CHUNK_ROWS * a.rows_at_once);
+    const long long want = 2048 / (sh.items * p.parts) + 1, most_chunks = (sh.length + 8ll * a.rows_at_once - 1) / (8ll * a.rows_at_once);
+    if (chunks < want) chunks = want < most_chunks ? want : most_chunks > chunks ? most_chunks : chunks;
+    a.chunk_len = (sh.length + chunks - 1) / chunks;
+    a.chunks = (sh.length + a.chunk_len - 1) / a.chunk_len;
+    p.blocks = sh.items * a.chunks;
+    p.stats = back ? 0 : goom::align_up((size_t)(sh.items * a.chunks * sh.groups) * 16, 256);
+    p.sums = back ? goom::align_up((size_t)(sh.items * a.chunks) * 2 * sh.channels * 4, 256) : 0;
+    p.means = back ? goom::align_up((size_t)(sh.items * sh.groups) * 8, 256) : 0;
+    return p;
+}
+
+// bytes that hold for every access width (the workspace is asked for before the addresses are known)
+static size_t norm_bytes(const goom_norm_shape &sh, bool back)
+{
+    size_t most = 0;
+    for (int v = 1; v <= 8; v *= 2)
+        if ((sh.channels / sh.groups) % v == 0 && v * real_bytes(sh.type) <= 16) {
+            const NormPlan p = norm_plan(sh, v, back);
+            const size_t need = p.stats + p.sums + p.means + p.partial;
+            if (need > most) most = need;
+        }
+    return most;
+}
+
+static int norm_width(const goom_norm_shape &sh, const void *a, const void *b, const void *c)
+{
+    const size_t size = real_bytes(sh.type);
+    const int cg = sh.channels / sh.groups;
+    int v = 8;
+    while (v > 1 && (v * size > 16 || cg % v || !goom::aligned(a, v * size) || !goom::aligned(b, v * size) || !goom::aligned(c, v * size))) v /= 2;
+    return v;
+}
+
+static int check_norm(goom_ctx *ctx, const goom_norm_shape *sh)
+{
+    if (!sh) return goom::fail(ctx, GOOM_EINVAL, "null shape");
+    if (!real_type(sh->type) || !real_type(sh->param_type)) return goom::fail(ctx, GOOM_EINVAL, "unknown element type %d", real_type(sh->type) ? sh->param_type : sh->type);
+    if (sh->flags) return goom::fail(ctx, GOOM_EINVAL, "unknown flags 0x%x", (unsigned)sh->flags);
+    if (sh->items < 0 || sh->length <= 0 || sh->channels <= 0) return goom::fail(ctx, GOOM_EINVAL, "items must not be negative, length and channels positive");
+    if (sh->groups <= 0 || sh->channels % sh->groups) return goom::fail(ctx, GOOM_EINVAL, "groups must be positive and divide channels");
+    if (sh->activation < GOOM_ACT_NONE || sh->activation > GOOM_ACT_GELU) return goom::fail(ctx, GOOM_EINVAL, "unknown activation %d", sh->activation);
+    if (!(sh->eps >= 0.0) || !std::isfinite(sh->eps)) return goom::fail(ctx, GOOM_EINVAL, "eps must be finite and not negative");
+    if (sh->items > (1ll << 31) || sh->length > (1ll << 31) || sh->channels > (1 << 20) || (double)sh->items * sh->length * sh->channels > 1e15 || (double)sh->items * sh->groups > 2e9)
+        return goom::fail(ctx, GOOM_EUNSUPPORTED, "too many items, positions or channels");
+    return GOOM_OK;
+}
+
+// f(vector width, units a lane)
+template <typename S, typename F> static int with_team(int v, int j, F f)
+{
+    auto units = [&](auto vec) {
+        constexpr int V = decltype(vec)::value;
+        if constexpr (V * sizeof(S) <= 16) {
+            if constexpr (V <= 4)
+                if (j == 8) return f(vec, std::integral_constant<int, 8>());
+            if (j == 4) return f(vec, std::integral_constant<int, 4>());
+            if (j == 2) return f(vec, std::integral_constant<int, 2>());
+            return f(vec, std::integral_constant<int, 1>());
+        }
+        return 0;
+    };
+    return v == 8 ? units(std::integral_constant<int, 8>()) : v == 4 ? units(std::integral_constant<int, 4>()) : v == 2 ? units(std::integral_constant<int, 2>()) : units(std::integral_constant<int, 1>());
+}
+
+template <typename S, typename F> static int with_width(int v, F f)
+{
+    if constexpr (sizeof(S) == 2)
+        if (v == 8) return f(std::integral_constant<int, 8>());
+    return v == 4 ? f(std::integral_constant<int, 4>()) : v == 2 ? f(std::integral_constant<int, 2>()) : f(std::integral_constant<int, 1>());
+}
+
+} // namespace goom_layer
+
+using namespace goom_layer;
+using goom::aligned;
+using goom::fail;
+
+extern "C" {
+
+size_t goom_group_norm_workspace_bytes(const goom_norm_shape *shape) { return check_norm(nullptr, shape) || shape->items == 0 ? 0 : norm_bytes(*shape, false); }
+
+size_t goom_group_norm_backward_workspace_bytes(const goom_norm_shape *shape) { return check_norm(nullptr, shape) || shape->items == 0 ? 0 : norm_bytes(*shape, true); }
+
+int goom_group_norm(goom_ctx *ctx, const goom_norm_shape *shape, const void *x, const void *weight, const void *bias, void *y, float *mean, float *rstd, void *workspace,
+                    size_t workspace_bytes)
+{
+    if (int s = check_norm(ctx, shape)) return s;
+    if (shape->items == 0) return ctx ? GOOM_OK : fail(nullptr, GOOM_EINVAL, "null context");
+    if (!x || !y) return fail(ctx, GOOM_EINVAL, "null data pointer");
+    const size_t size = real_bytes(shape->type), wsize = real_bytes(shape->param_type);
+    if (!aligned(x, size) || !aligned(y, size) || !aligned(weight, wsize) || !aligned(bias, wsize) || !aligned(mean, 4) || !aligned(rstd, 4))
+        return fail(ctx, GOOM_EINVAL, "misaligned data pointer");
+    if (int s = check_workspace(ctx, workspace, workspace_bytes, norm_bytes(*shape, false))) return s;
+    if (int s = enter(ctx)) return s;
+    NormPlan p = norm_plan(*shape, norm_width(*shape, x, y, nullptr), false);
+    NormArgs &a = p.a;
+    a.x = x;
+    a.weight = weight;
+    a.bias = bias;
+    a.y = y;
+    a.mean = mean;
+    a.rstd = rstd;
+    a.stats = reinterpret_cast<double *>(workspace);
+    return with_type(shape->type, [&](auto tag) {
+        typedef typename decltype(tag)::type S;
+        const dim3 grid((unsigned)p.blocks, (unsigned)p.parts);
+        if (p.team) {
+            goom::prof_begin(ctx, "group norm");
+            with_team<S>(p.v, p.j, [&](auto vec, auto units) {
+                norm_team_kernel<S, decltype(vec)::value, decltype(units)::value, false><<<grid, 256, 0, ctx->stream>>>(a);
+                return 0;
+            });
+            goom::prof_end(ctx);
+        } else {
+            const int threads = (a.threads + 63) / 64 * 64;
+            goom::prof_begin(ctx, "group norm: sums");
+            with_width<S>(p.v, [&](auto vec) {
+                norm_stats_kernel<S, decltype(vec)::value><<<grid, threads, 0, ctx->stream>>>(a);
+                return 0;
+            });
+            goom::prof_end(ctx);
+            goom::prof_begin(ctx, "group norm: output");
+            with_width<S>(p.v, [&](auto vec) {
+                norm_apply_kernel<S, decltype(vec)::value><<<grid, threads, 0, ctx->stream>>>(a);
+                return 0;
+            });
+            goom::prof_end(ctx);
+        }
+        return goom::check_hip(ctx, hipGetLastError(), "group norm");
+    });
+}
+
+int goom_group_norm_backward(goom_ctx *ctx, const goom_norm_shape *shape, const void *x, const void *grad_y, const float *mean, const float *rstd, const void *weight, const void *bias,
+                             void *grad_x, void *grad_weight, void *grad_bias, void *workspace, size_t workspace_bytes)
+{
+    if (int s = check_norm(ctx, shape)) return s;
+    const size_t size = real_bytes(shape->type), wsize = real_bytes(shape->param_type);
+    if (shape->items > 0 && (!x || !grad_y || !mean || !rstd || !grad_x)) return fail(ctx, GOOM_EINVAL, "null data pointer");
+    const void *const typed[] = {x, grad_y, grad_x}, *const params[] = {weight, bias, grad_weight, grad_bias};
+    for (const void *q : typed)
+        if (!aligned(q, size)) return fail(ctx, GOOM_EINVAL, "misaligned data pointer");
+    for (const void *q : params)
+        if (!aligned(q, wsize)) return fail(ctx, GOOM_EINVAL, "misaligned data pointer");
+    if (!aligned(mean, 4) || !aligned(rstd, 4)) return fail(ctx, GOOM_EINVAL, "misaligned data pointer");
+    if (int s = check_workspace(ctx, workspace, workspace_bytes, shape->items ? norm_bytes(*shape, true) : 0)) return s;
+    if (int s = enter(ctx)) return s;
+    NormPlan p = {};
+    const float *partial = nullptr;
+    long long partials = 0;
+    if (shape->items > 0) {
+        p = norm_plan(*shape, norm_width(*shape, x, grad_y, grad_x), true);
+        NormArgs &a = p.a;
+        a.x = x;
+        a.gy = grad_y;
+        a.weight = weight;
+        a.bias = bias;
+        a.y = grad_x;
+        a.mean = const_cast<float *>(mean);
+        a.rstd = const_cast<float *>(rstd);
+        a.partial = a.sums = reinterpret_cast<float *>(workspace);
+        a.means = reinterpret_cast<float *>(reinterpret_cast<unsigned char *>(workspace) + p.sums);
+        partial = a.partial;
+        partials = p.blocks; // workgroups along the items, or items chunks: [partials][2][channels] either way
+        const int rc = with_type(shape->type, [&](auto tag) {
+            typedef typename decltype(tag)::type S;
+            const dim3 grid((unsigned)p.blocks, (unsigned)p.parts);
+            if (p.team) {
+                goom::prof_begin(ctx, "group norm gradient");
+                with_team<S>(p.v, p.j, [&](auto vec, auto units) {
+                    norm_team_kernel<S, decltype(vec)::value, decltype(units)::value, true><<<grid, 256, 0, ctx->stream>>>(a);
+                    return 0;
+                });
+                goom::prof_end(ctx);
+            } else {
+                const int threads = (a.threads + 63) / 64 * 64;
+                goom::prof_begin(ctx, "group norm gradient: sums");
+                with_width<S>(p.v, [&](auto vec) {
+                    norm_sums_kernel<S, decltype(vec)::value><<<grid, threads, 0, ctx->stream>>>(a);
+                    return 0;
+                });
+                norm_means_kernel<<<(unsigned)(a.items * a.groups), 64, 0, ctx->stream>>>(a);
+                goom::prof_end(ctx);
+                goom::prof_begin(ctx, "group norm gradient");
+                with_width<S>(p.v, [&](auto vec) {
+                    norm_grad_kernel<S, decltype(vec)::value><<<grid, threads, 0, ctx->stream>>>(a);
+                    return 0;
+                });
+                goom::prof_end(ctx);
+            }
+            return goom::check_hip(ctx, hipGetLastError(), "group norm gradient");
+        });
+        if (rc) return rc;
+    }
+    if (grad_weight || grad_bias) {
+        goom::prof_begin(ctx, "group norm gradient: weights");
+        norm_weight_kernel<<<dim3((shape->channels + 31) / 32, 2), 256, 0, ctx->stream>>>(partial, partials, shape->channels, grad_weight, grad_bias, shape->param_type);
+        goom::prof_end(ctx);
+    }
+    return goom::check_hip(ctx, hipGetLastError(), "group norm gradient: weights");
+}
+
+} // extern "C"

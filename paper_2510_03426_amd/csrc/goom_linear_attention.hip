@@ -686,14 +686,14 @@ static int check_shape(goom_ctx *ctx, const goom_attention_shape *given, goom_at
     return GOOM_OK;
 }
 
-static int enter(goom_ctx *ctx)
+int enter(goom_ctx *ctx)
 {
     if (!ctx) return goom::fail(nullptr, GOOM_EINVAL, "null context");
     if (!ctx->prof_keep) goom::prof_reset(ctx);
     return goom::check_hip(ctx, hipSetDevice(ctx->device), "hipSetDevice");
 }
 
-static int check_workspace(goom_ctx *ctx, const void *ws, size_t given, size_t need)
+int check_workspace(goom_ctx *ctx, const void *ws, size_t given, size_t need)
 {
     if (!need) return GOOM_OK;
     if (!ws || given < need) return goom::fail(ctx, GOOM_EWORKSPACE, "workspace of %zu bytes needed, %zu given", need, ws ? given : (size_t)0);

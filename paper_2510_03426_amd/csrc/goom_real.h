@@ -50,4 +50,8 @@ template <typename F> int with_type(int type, F f)
     }
 }
 
+// entry checks that the layer operators share (goom_linear_attention.hip)
+int enter(goom_ctx *ctx);
+int check_workspace(goom_ctx *ctx, const void *ws, size_t given, size_t need);
+
 } // namespace goom_layer
