@@ -571,7 +571,7 @@ int goom_embedding(goom_ctx *ctx, const void *table, const int64_t *tokens, void
 
 /* Its gradient: grad_table[t] = scale (sum of grad[i] over the i with tokens[i] = t), every row of [vocab, width] written, rows
  * without a token as zeros.  The positions are sorted by token (stably), each token's gradients are summed in float in the order
- * of their positions, in groups of 64 sorted positions, so that results do not vary from run to run.  type: of grad; table_type:
+ * of their positions, in groups of 32 sorted positions, so that results do not vary from run to run.  type: of grad; table_type:
  * of grad_table.  workspace: goom_embedding_backward_workspace_bytes(n, vocab, width) bytes. */
 int goom_embedding_backward(goom_ctx *ctx, const int64_t *tokens, const void *grad, void *grad_table, int64_t n, int64_t vocab,
                             int width, int type, int table_type, double scale, void *workspace, size_t workspace_bytes);

@@ -2,17 +2,17 @@
 //
 // Forward: one pass, bound by the rows read and written.
 // Gradient: a sum over the positions of each token, in a fixed order.  The positions are sorted by token (a stable radix
-// sort, up to 9 bits a pass), so that a token's gradients are a run of sorted positions; one wave a table row adds its run up
-// and writes the row, zeros where the run is empty, so that the table is written once and never read.  Tokens of text are far
-// from equally frequent: blocks of 64 sorted positions that lie inside one run are summed beforehand, side by side, and the
-// row's wave takes their sums.
+// sort, up to 9 bits a pass), so that a token's gradients are a run of sorted positions; the waves of a table row, each with its
+// columns, add the run up and write the row, zeros where the run is empty, so that the table is written once and never read.  Tokens of text are far
+// from equally frequent: blocks of 32 sorted positions that lie inside one run are summed beforehand, side by side, and the
+// row's waves take their sums.
 #include <cmath>
 
 #include "goom_real.h"
 
 namespace goom_layer {
 
-constexpr int RUN = 64;       // sorted positions of a block that is summed beforehand
+constexpr int RUN = 32;       // sorted positions of a block that is summed beforehand
 constexpr int MAX_BINS = 512; // digits of a sorting pass
 
 template <typename S, int V> __global__ __launch_bounds__(256) void embedding_kernel(const S *table, const int64_t *tokens, S *rows, long long n, long long vocab, int width, float scale)
@@ -80,10 +80,15 @@ __global__ __launch_bounds__(256) void sort_scatter_kernel(SortPass p)
     for (int k = 0; k < 2; k++) {
         const int d = threadIdx.x * 2 + k;
         if (d < bins)
-            for (unsigned t = 0; t < gridDim.x; t++) {
-                const unsigned c = p.counts[t * (unsigned)bins + d];
-                total[k] += c;
-                before[k] += t < blockIdx.x ? c : 0;
+            for (unsigned t0 = 0; t0 < gridDim.x; t0 += 16) {
+                unsigned c[16];
+#pragma unroll
+                for (int t = 0; t < 16; t++) c[t] = t0 + t < gridDim.x ? p.counts[(t0 + t) * (unsigned)bins + d] : 0;
+#pragma unroll
+                for (int t = 0; t < 16; t++) {
+                    total[k] += c[t];
+                    before[k] += t0 + t < blockIdx.x ? c[t] : 0;
+                }
             }
     }
     sums[threadIdx.x] = total[0] + total[1];
@@ -159,12 +164,12 @@ __global__ __launch_bounds__(256) void run_start_kernel(const unsigned *keys, un
 // x += rows of grad at sorted positions [i, end), in order
 template <typename S, int V> __device__ inline void add_rows(float (&x)[V], const S *grad, const unsigned *values, unsigned i, unsigned end, int width, int col)
 {
-    for (; i + 4 <= end; i += 4) { // four rows in flight
-        float y[4][V];
+    for (; i + 8 <= end; i += 8) { // eight rows in flight
+        float y[8][V];
 #pragma unroll
-        for (int k = 0; k < 4; k++) load_floats<S, V>(grad + (long long)values[i + k] * width + col, y[k]);
+        for (int k = 0; k < 8; k++) load_floats<S, V>(grad + (long long)values[i + k] * width + col, y[k]);
 #pragma unroll
-        for (int k = 0; k < 4; k++)
+        for (int k = 0; k < 8; k++)
 #pragma unroll
             for (int e = 0; e < V; e++) x[e] += y[k][e];
     }
@@ -189,32 +194,41 @@ template <typename S, int V> __global__ __launch_bounds__(64) void run_block_ker
     store_floats<float, V>(sums + (long long)blockIdx.x * width + col, x);
 }
 
-// one row of the table a wave: the run's head, its whole blocks, its tail
-template <typename S, typename W, int V> __global__ __launch_bounds__(256) void table_row_kernel(const S *grad, const unsigned *values, const unsigned *start, const float *sums, W *table, long long vocab, int width, float scale)
+// 64 V columns of a table row a wave: the run's head, its whole blocks, its tail.  grid: vocab parts / 4
+template <typename S, typename W, int V> __global__ __launch_bounds__(256) void table_row_kernel(const S *grad, const unsigned *values, const unsigned *start, const float *sums, W *table, long long vocab, int width, int parts, float scale)
 {
-    const long long row = blockIdx.x * 4ll + (threadIdx.x >> 6);
+    const long long task = blockIdx.x * 4ll + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = task / parts;
+    const int col = ((int)(task - row * parts) * 64 + (threadIdx.x & 63)) * V;
     if (row >= vocab) return;
     const unsigned begin = start[row], end = start[row + 1];
     const unsigned first = (begin + RUN - 1) / RUN, last = end / RUN; // whole blocks: first .. last - 1
-    for (int col = (threadIdx.x & 63) * V; col < width; col += 64 * V) {
-        float x[V] = {};
-        if (first < last) {
-            add_rows<S, V>(x, grad, values, begin, first * RUN, width, col);
-            unsigned b = first;
-            for (; b < last; b++) {
-                float y[V];
-                load_floats<float, V>(sums + (long long)b * width + col, y);
+    if (col >= width) return;
+    float x[V] = {};
+    if (first < last) {
+        add_rows<S, V>(x, grad, values, begin, first * RUN, width, col);
+        unsigned b = first;
+        for (; b + 8 <= last; b += 8) {
+            float y[8][V];
 #pragma unroll
-                for (int e = 0; e < V; e++) x[e] += y[e];
-            }
-            add_rows<S, V>(x, grad, values, last * RUN, end, width, col);
-        } else {
-            add_rows<S, V>(x, grad, values, begin, end, width, col);
+            for (int k = 0; k < 8; k++) load_floats<float, V>(sums + (long long)(b + k) * width + col, y[k]);
+#pragma unroll
+            for (int k = 0; k < 8; k++)
+#pragma unroll
+                for (int e = 0; e < V; e++) x[e] += y[k][e];
         }
+        for (; b < last; b++) {
+            float y[V];
+            load_floats<float, V>(sums + (long long)b * width + col, y);
 #pragma unroll
-        for (int e = 0; e < V; e++) x[e] *= scale;
-        store_floats<W, V>(table + row * width + col, x);
+            for (int e = 0; e < V; e++) x[e] += y[e];
+        }
+        add_rows<S, V>(x, grad, values, last * RUN, end, width, col);
+    } else {
+        add_rows<S, V>(x, grad, values, begin, end, width, col);
     }
+#pragma unroll
+    for (int e = 0; e < V; e++) x[e] *= scale;
+    store_floats<W, V>(table + row * width + col, x);
 }
 
 struct EmbeddingPlan {
@@ -245,7 +259,7 @@ static EmbeddingPlan embedding_plan(long long n, long long vocab, int width)
 static int check_embedding(goom_ctx *ctx, long long n, long long vocab, int width)
 {
     if (n < 0 || vocab <= 0 || width <= 0) return goom::fail(ctx, GOOM_EINVAL, "n must not be negative, vocab and width positive");
-    if (n >= (1ll << 31) || vocab >= (1ll << 31)) return goom::fail(ctx, GOOM_EUNSUPPORTED, "up to 2^31 - 1 tokens and table rows");
+    if (n >= (1ll << 31) || vocab >= (1ll << 31) || (double)vocab * width > 1e12) return goom::fail(ctx, GOOM_EUNSUPPORTED, "up to 2^31 - 1 tokens and table rows, and 10^12 entries");
     return GOOM_OK;
 }
 
@@ -360,7 +374,8 @@ int goom_embedding_backward(goom_ctx *ctx, const int64_t *tokens, const void *gr
                 goom::prof_begin(ctx, "embedding gradient: rows");
                 with_type(table_type, [&](auto wtag) {
                     typedef typename decltype(wtag)::type W;
-                    table_row_kernel<S, W, V><<<(unsigned)((vocab + 3) / 4), 256, 0, ctx->stream>>>(gr, values, start, sums, reinterpret_cast<W *>(grad_table), vocab, width, (float)scale);
+                    const int parts = (width + 64 * V - 1) / (64 * V);
+                    table_row_kernel<S, W, V><<<(unsigned)((vocab * parts + 3) / 4), 256, 0, ctx->stream>>>(gr, values, start, sums, reinterpret_cast<W *>(grad_table), vocab, width, parts, (float)scale);
                     return 0;
                 });
                 goom::prof_end(ctx);

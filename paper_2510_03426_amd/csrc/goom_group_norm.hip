@@ -43,9 +43,31 @@ __device__ inline float param(const void *p, int type, int i, float otherwise)
     return type == GOOM_REAL_F32 ? reinterpret_cast<const float *>(p)[i] : type == GOOM_REAL_BF16 ? (float)reinterpret_cast<const bf16 *>(p)[i] : (float)reinterpret_cast<const f16 *>(p)[i];
 }
 
+// V parameters of neighbouring channels from a multiple of V on
+template <int V> __device__ inline void params(const void *p, int type, int i, float otherwise, float (&x)[V])
+{
+    if (p && type == GOOM_REAL_F32 && V > 1 && (reinterpret_cast<uintptr_t>(p) & (V > 4 ? 15 : 4 * V - 1)) == 0) {
+        constexpr int N = V > 4 ? 4 : V;
+#pragma unroll
+        for (int e = 0; e < V; e += N) {
+            float y[N];
+            load_floats<float, N>(reinterpret_cast<const float *>(p) + i + e, y);
+#pragma unroll
+            for (int k = 0; k < N; k++) x[e + k] = y[k];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; e++) x[e] = param(p, type, i + e, otherwise);
+    }
+}
+
+// 1 / (1 + e^-z) by the hardware's exponential and reciprocal (1 ulp each; the exponent's rounding adds |z| u where the value
+// is near e^z): library exp and division were 25 of the 40 instructions an element and took longer than its bytes
+__device__ inline float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504088896341f)); }
+
 __device__ inline float activate(float z, int act)
 {
-    if (act == GOOM_ACT_SILU) return z / (1.0f + expf(-z));
+    if (act == GOOM_ACT_SILU) return z * logistic(z);
     if (act == GOOM_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
     return z;
 }
@@ -53,7 +75,7 @@ __device__ inline float activate(float z, int act)
 __device__ inline float activate_slope(float z, int act)
 {
     if (act == GOOM_ACT_SILU) {
-        const float p = 1.0f / (1.0f + expf(-z));
+        const float p = logistic(z);
         return p * (1.0f + z * (1.0f - p));
     }
     if (act == GOOM_ACT_GELU) return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * expf(-0.5f * z * z);
@@ -81,31 +103,39 @@ template <typename S, int V, int J, bool BACK> __global__ __launch_bounds__(256)
         const int u = lane + j * a.team;
         chan[j] = live && u < units ? group * a.cg + u % cu * V : -1;
         off[j] = chan[j] >= 0 ? u / cu * a.channels + chan[j] : 0;
+        params<V>(a.weight, a.type_w, chan[j] >= 0 ? chan[j] : 0, 1.0f, w[j]);
+        params<V>(a.bias, a.type_w, chan[j] >= 0 ? chan[j] : 0, 0.0f, b[j]);
 #pragma unroll
-        for (int e = 0; e < V; e++) {
-            w[j][e] = chan[j] >= 0 ? param(a.weight, a.type_w, chan[j] + e, 1.0f) : 0.0f;
-            b[j][e] = chan[j] >= 0 ? param(a.bias, a.type_w, chan[j] + e, 0.0f) : 0.0f;
-            sw[j][e] = sb[j][e] = 0.0f;
-        }
+        for (int e = 0; e < V; e++) sw[j][e] = sb[j][e] = 0.0f;
     }
     const long long size = a.length * a.channels;
     const S *const xs = reinterpret_cast<const S *>(a.x);
     const S *const gs = reinterpret_cast<const S *>(a.gy);
     S *const ys = reinterpret_cast<S *>(a.y);
+    typedef typename Vec<S, V>::type SV;
+    SV next_x[J], next_g[J]; // the next item's elements are on their way while one is worked on
+    auto fetch = [&](long long item) {
+        const long long from = item < a.items ? item : 0;
+#pragma unroll
+        for (int j = 0; j < J; j++) {
+            next_x[j] = *reinterpret_cast<const SV *>(xs + from * size + off[j]);
+            if (BACK) next_g[j] = *reinterpret_cast<const SV *>(gs + from * size + off[j]);
+        }
+    };
+    fetch((long long)blockIdx.x * a.ipw + ti);
     for (long long item0 = (long long)blockIdx.x * a.ipw; item0 < a.items; item0 += (long long)gridDim.x * a.ipw) {
         const long long item = item0 + ti;
         const bool here = live && item < a.items; // (the same for a whole team; other lanes go along for the shuffles)
         float x[J][V], dz[J][V];
 #pragma unroll
-        for (int j = 0; j < J; j++) {
-            if (here && chan[j] >= 0) {
-                load_floats<S, V>(xs + item * size + off[j], x[j]);
-                if (BACK) load_floats<S, V>(gs + item * size + off[j], dz[j]);
-            } else {
+        for (int j = 0; j < J; j++)
 #pragma unroll
-                for (int e = 0; e < V; e++) x[j][e] = dz[j][e] = 0.0f;
+            for (int e = 0; e < V; e++) {
+                const bool there = here && chan[j] >= 0;
+                x[j][e] = there ? (float)next_x[j][e] : 0.0f;
+                dz[j][e] = BACK && there ? (float)next_g[j][e] : 0.0f;
             }
-        }
+        if (item0 + (long long)gridDim.x * a.ipw < a.items) fetch(item + (long long)gridDim.x * a.ipw);
         if (!BACK) {
             float sum = 0.0f;
 #pragma unroll
@@ -185,20 +215,27 @@ template <typename S, int V, int J, bool BACK> __global__ __launch_bounds__(256)
     }
 }
 
-// gw[c] = sum of partial[k][0][c], gb[c] = sum of partial[k][1][c] over k < n; 32 channels a workgroup, eight runs of k each
-__global__ __launch_bounds__(256) void norm_weight_kernel(const float *partial, long long n, int channels, void *gw, void *gb, int type_w)
+// gw[c] = sum of partial[k][0][c], gb[c] = sum of partial[k][1][c] over k < n; 32 channels a workgroup, 32 runs of k each
+__global__ __launch_bounds__(1024) void norm_weight_kernel(const float *partial, long long n, int channels, void *gw, void *gb, int type_w)
 {
-    __shared__ double meet[8][32];
+    __shared__ double meet[32][32];
     const int c = blockIdx.x * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
-    const long long len = (n + 7) / 8, begin = part * len, end = begin + len < n ? begin + len : n;
+    const long long len = (n + 31) / 32, begin = part * len, end = begin + len < n ? begin + len : n;
     double sum = 0.0;
     if (c < channels)
-        for (long long k = begin; k < end; k++) sum += (double)partial[(k * 2 + blockIdx.y) * channels + c];
+        for (long long k0 = begin; k0 < end; k0 += 32) {
+            float x[32];
+#pragma unroll
+            for (int k = 0; k < 32; k++) x[k] = partial[((k0 + k < end ? k0 + k : begin) * 2 + blockIdx.y) * channels + c];
+#pragma unroll
+            for (int k = 0; k < 32; k++) sum += k0 + k < end ? (double)x[k] : 0.0;
+        }
     meet[part][threadIdx.x & 31] = sum;
     __syncthreads();
     void *out = blockIdx.y ? gb : gw;
     if (part == 0 && c < channels && out) {
-        for (int k = 1; k < 8; k++) sum += meet[k][threadIdx.x];
+#pragma unroll
+        for (int k = 1; k < 32; k++) sum += meet[k][threadIdx.x];
         if (type_w == GOOM_REAL_F32) reinterpret_cast<float *>(out)[c] = (float)sum;
         else if (type_w == GOOM_REAL_BF16) reinterpret_cast<bf16 *>(out)[c] = (bf16)(float)sum;
         else reinterpret_cast<f16 *>(out)[c] = (f16)(float)sum;
@@ -279,13 +316,23 @@ template <typename S, int V> __global__ __launch_bounds__(512) void norm_apply_k
     const S *const x = reinterpret_cast<const S *>(a.x) + base;
     S *const y = reinterpret_cast<S *>(a.y) + base;
     const int cu = a.cg / V;
-    for (int g = threadIdx.x; g < s.ngroups; g += blockDim.x) {
+    int lanes = 64; // of a group, for its chunks' sums
+    while (lanes > 1 && lanes * s.ngroups > (int)blockDim.x) lanes /= 2;
+    const int per = blockDim.x / lanes;
+    for (int g0 = 0; g0 < s.ngroups; g0 += per) {
+        const int g = g0 + threadIdx.x / lanes;
         double p = 0.0, q = 0.0;
-        for (long long k = 0; k < a.chunks; k++) {
-            const double *from = a.stats + ((s.item * a.chunks + k) * a.groups + s.group0 + g) * 2;
-            p += from[0];
-            q += from[1];
+        if (g < s.ngroups)
+            for (long long k = threadIdx.x % lanes; k < a.chunks; k += lanes) {
+                const double *from = a.stats + ((s.item * a.chunks + k) * a.groups + s.group0 + g) * 2;
+                p += from[0];
+                q += from[1];
+            }
+        for (int m = 1; m < lanes; m *= 2) {
+            p += __shfl_xor(p, m);
+            q += __shfl_xor(q, m);
         }
+        if (g >= s.ngroups || threadIdx.x % lanes) continue;
         const double n = (double)a.length * a.cg, d = p / n;
         const double var = q / n - d * d;
         stat[g][0] = (float)((double)(float)x[g * a.cg] + d);
@@ -299,11 +346,8 @@ template <typename S, int V> __global__ __launch_bounds__(512) void norm_apply_k
     for (int u = s.tx; s.live && u < s.units; u += s.columns) {
         const float mean = stat[u / cu][0], rstd = stat[u / cu][1];
         float w[V], b[V];
-#pragma unroll
-        for (int e = 0; e < V; e++) {
-            w[e] = param(a.weight, a.type_w, s.group0 * a.cg + u * V + e, 1.0f);
-            b[e] = param(a.bias, a.type_w, s.group0 * a.cg + u * V + e, 0.0f);
-        }
+        params<V>(a.weight, a.type_w, s.group0 * a.cg + u * V, 1.0f, w);
+        params<V>(a.bias, a.type_w, s.group0 * a.cg + u * V, 0.0f, b);
         for (long long row = s.row0 + s.ty; row < s.row1; row += a.rows_at_once) {
             float v[V];
             load_floats<S, V>(x + row * a.channels + u * V, v);
@@ -329,11 +373,8 @@ template <typename S, int V> __global__ __launch_bounds__(512) void norm_sums_ke
         if (s.live && u < s.units) {
             const float mean = a.mean[s.item * a.groups + s.group0 + u / cu], rstd = a.rstd[s.item * a.groups + s.group0 + u / cu];
             float w[V], b[V];
-#pragma unroll
-            for (int e = 0; e < V; e++) {
-                w[e] = param(a.weight, a.type_w, s.group0 * a.cg + u * V + e, 1.0f);
-                b[e] = param(a.bias, a.type_w, s.group0 * a.cg + u * V + e, 0.0f);
-            }
+            params<V>(a.weight, a.type_w, s.group0 * a.cg + u * V, 1.0f, w);
+            params<V>(a.bias, a.type_w, s.group0 * a.cg + u * V, 0.0f, b);
             for (long long row = s.row0 + s.ty; row < s.row1; row += a.rows_at_once) {
                 float v[V], g[V];
                 load_floats<S, V>(x + row * a.channels + u * V, v);
@@ -365,32 +406,33 @@ template <typename S, int V> __global__ __launch_bounds__(512) void norm_sums_ke
     }
 }
 
-// means over a group of dz w and of dz w xhat; one wave a group.  grid: items groups
-__global__ __launch_bounds__(64) void norm_means_kernel(NormArgs a)
+// means over a group of dz w and of dz w xhat; a workgroup a group.  grid: items groups
+__global__ __launch_bounds__(256) void norm_means_kernel(NormArgs a)
 {
+    __shared__ double meet[2][4];
     const long long item = blockIdx.x / a.groups;
     const int group = blockIdx.x % a.groups;
     double m1 = 0.0, m2 = 0.0;
-    for (int c = threadIdx.x; c < a.cg; c += 64) {
-        const int ch = group * a.cg + c;
-        double p = 0.0, q = 0.0;
-        for (long long k = 0; k < a.chunks; k++) {
-            const float *from = a.sums + (item * a.chunks + k) * 2 * a.channels + ch;
-            q += (double)from[0];
-            p += (double)from[a.channels];
-        }
+    for (long long u = threadIdx.x; u < a.chunks * a.cg; u += 256) {
+        const long long k = u / a.cg;
+        const int ch = group * a.cg + (int)(u - k * a.cg);
+        const float *from = a.sums + (item * a.chunks + k) * 2 * a.channels + ch;
         const double w = (double)param(a.weight, a.type_w, ch, 1.0f);
-        m1 += w * p;
-        m2 += w * q;
+        m2 += w * (double)from[0];
+        m1 += w * (double)from[a.channels];
     }
     for (int m = 1; m < 64; m *= 2) {
         m1 += __shfl_xor(m1, m);
         m2 += __shfl_xor(m2, m);
     }
-    if (threadIdx.x == 0) {
+    if ((threadIdx.x & 63) == 0) {
+        meet[0][threadIdx.x >> 6] = m1;
+        meet[1][threadIdx.x >> 6] = m2;
+    }
+    __syncthreads();
+    if (threadIdx.x < 2) {
         const double n = (double)a.length * a.cg;
-        a.means[blockIdx.x * 2ll] = (float)(m1 / n);
-        a.means[blockIdx.x * 2ll + 1] = (float)(m2 / n);
+        a.means[blockIdx.x * 2ll + threadIdx.x] = (float)(((meet[threadIdx.x][0] + meet[threadIdx.x][1]) + (meet[threadIdx.x][2] + meet[threadIdx.x][3])) / n);
     }
 }
 
@@ -406,11 +448,8 @@ template <typename S, int V> __global__ __launch_bounds__(512) void norm_grad_ke
         const long long at = s.item * a.groups + s.group0 + u / cu;
         const float mean = a.mean[at], rstd = a.rstd[at], m1 = a.means[at * 2], m2 = a.means[at * 2 + 1];
         float w[V], b[V];
-#pragma unroll
-        for (int e = 0; e < V; e++) {
-            w[e] = param(a.weight, a.type_w, s.group0 * a.cg + u * V + e, 1.0f);
-            b[e] = param(a.bias, a.type_w, s.group0 * a.cg + u * V + e, 0.0f);
-        }
+        params<V>(a.weight, a.type_w, s.group0 * a.cg + u * V, 1.0f, w);
+        params<V>(a.bias, a.type_w, s.group0 * a.cg + u * V, 0.0f, b);
         for (long long row = s.row0 + s.ty; row < s.row1; row += a.rows_at_once) {
             float v[V], g[V];
             load_floats<S, V>(x + row * a.channels + u * V, v);
@@ -465,7 +504,7 @@ static NormPlan norm_plan(const goom_norm_shape &sh, int v, bool back)
         p.blocks = (sh.items + a.ipw - 1) / a.ipw;
         // Workgroups go over several items: where the weights' gradients are summed, no more partial sums than needed to fill
         // the chip
-        const long long cap = (back ? 1024 : 8192) / p.parts > 0 ? (back ? 1024 : 8192) / p.parts : 1;
+        const long long groups_at_once = back ? 1024 : 4096, cap = groups_at_once / p.parts > 0 ? groups_at_once / p.parts : 1;
         if (p.blocks > cap) p.blocks = cap;
         p.partial = back ? goom::align_up((size_t)p.blocks * 2 * sh.channels * 4, 256) : 0;
         return p;
@@ -483,7 +522,7 @@ static NormPlan norm_plan(const goom_norm_shape &sh, int v, bool back)
     p.parts = (sh.groups + a.gps - 1) / a.gps;
     // chunks: at most CHUNK_ROWS positions a thread, and enough workgroups to fill the chip
     long long chunks = (sh.length + (long long)CHUNK_ROWS * a.rows_at_once - 1) / ((long long)CHUNK_ROWS * a.rows_at_once);
-    const long long want = 2048 / (sh.items * p.parts) + 1, most_chunks = (sh.length + 8ll * a.rows_at_once - 1) / (8ll * a.rows_at_once);
+    const long long want = 1024 / (sh.items * p.parts) + 1, most_chunks = (sh.length + 8ll * a.rows_at_once - 1) / (8ll * a.rows_at_once);
     if (chunks < want) chunks = want < most_chunks ? want : most_chunks > chunks ? most_chunks : chunks;
     a.chunk_len = (sh.length + chunks - 1) / chunks;
     a.chunks = (sh.length + a.chunk_len - 1) / a.chunk_len;
@@ -663,7 +702,7 @@ int goom_group_norm_backward(goom_ctx *ctx, const goom_norm_shape *shape, const 
                     norm_sums_kernel<S, decltype(vec)::value><<<grid, threads, 0, ctx->stream>>>(a);
                     return 0;
                 });
-                norm_means_kernel<<<(unsigned)(a.items * a.groups), 64, 0, ctx->stream>>>(a);
+                norm_means_kernel<<<(unsigned)(a.items * a.groups), 256, 0, ctx->stream>>>(a);
                 goom::prof_end(ctx);
                 goom::prof_begin(ctx, "group norm gradient");
                 with_width<S>(p.v, [&](auto vec) {
@@ -678,7 +717,7 @@ int goom_group_norm_backward(goom_ctx *ctx, const goom_norm_shape *shape, const 
     }
     if (grad_weight || grad_bias) {
         goom::prof_begin(ctx, "group norm gradient: weights");
-        norm_weight_kernel<<<dim3((shape->channels + 31) / 32, 2), 256, 0, ctx->stream>>>(partial, partials, shape->channels, grad_weight, grad_bias, shape->param_type);
+        norm_weight_kernel<<<dim3((shape->channels + 31) / 32, 2), 1024, 0, ctx->stream>>>(partial, partials, shape->channels, grad_weight, grad_bias, shape->param_type);
         goom::prof_end(ctx);
     }
     return goom::check_hip(ctx, hipGetLastError(), "group norm gradient: weights");

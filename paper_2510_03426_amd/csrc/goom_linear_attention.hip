@@ -22,6 +22,21 @@
 
 namespace goom_layer {
 
+#ifndef LA_RES
+#define LA_RES (sh.dk > 64 || sh.dv > 64 ? 2 : 3)
+#endif
+#ifndef LA_NW32
+#define LA_NW32 4
+#endif
+#ifndef LA_EARLY
+#define LA_EARLY (!OUT)
+#endif
+#ifndef LA_OCC
+#define LA_OCC 1
+#endif
+#ifndef LA_NW
+#define LA_NW 4
+#endif
 constexpr int CHUNK = 64; // tokens; the pairs of a chunk cost 64 (ka + nc) multiplications a token, the state 2 ka nc
 
 struct WalkRole {
@@ -45,7 +60,8 @@ struct WalkArgs {
     const float *log_decay;
     const int64_t *offsets;
     long long tokens, seqs, seq_len, seg_len, segs; // without offsets: seq_len tokens and segs segments a sequence
-    int heads;
+    int heads, roles;
+    unsigned slots;
 };
 
 // ---- the sequence and segment of a workgroup.  With offsets, sequence s has the slots from floor(start / seg_len) + s on:
@@ -99,8 +115,14 @@ __device__ inline Place find_place(const WalkArgs &w, long long slot)
     return p;
 }
 
-// g^x for whole x >= 0, from log2 g; g = 0 (log -inf) has g^0 = 1
-__device__ inline float decay_power(float g2, int x) { return x == 0 ? 1.0f : __builtin_amdgcn_exp2f(g2 * (float)x); }
+// log2 of a decay.  2^-200 is zero as a float already: finite, so that g^0 = 1 for a decay of zero too (a NaN stays one)
+__device__ inline float log2_decay(float log_decay)
+{
+    const float g2 = log_decay * 1.44269504088896341f;
+    return g2 < -200.0f ? -200.0f : g2;
+}
+// g^x for whole x >= 0
+__device__ inline float decay_power(float g2, int x) { return __builtin_amdgcn_exp2f(g2 * (float)x); }
 
 // ---- operands: eight consecutive entries of the contraction per lane (lane / 16 picks which eight of 32)
 template <typename E> struct Operand;
@@ -125,17 +147,36 @@ __device__ inline f32x4 mma(f32x8 a, f32x8 b, f32x4 c)
     return c;
 }
 
+// Pairs share a word: the hardware converts two floats at once, and each half widens in one instruction.
+__device__ inline unsigned pack2(float a, float b) { return __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2){a, b}, bf16x2)); }
+__device__ inline float low_half(unsigned u) { return __builtin_bit_cast(float, u << 16); }
+__device__ inline float high_half(unsigned u) { return __builtin_bit_cast(float, u & 0xffff0000u); }
+
 template <int N> __device__ inline void split(f32x8 x, bf16x8 (&p)[N])
 {
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int i = 0; i < N; i++) {
-        p[i] = __builtin_convertvector(x, bf16x8);
-        if (i + 1 < N) x -= __builtin_convertvector(p[i], f32x8);
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            w[e] = pack2(x[2 * e], x[2 * e + 1]);
+            if (i + 1 < N) {
+                x[2 * e] -= low_half(w[e]);
+                x[2 * e + 1] -= high_half(w[e]);
+            }
+        }
+        p[i] = __builtin_bit_cast(bf16x8, w);
     }
 }
 template <int N> __device__ inline void split(f32x8 x, f32x8 (&p)[N]) { p[0] = x; }
 
-__device__ inline f32x8 widen(bf16x8 x) { return __builtin_convertvector(x, f32x8); }
+__device__ inline f32x8 widen(bf16x8 x)
+{
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+    const u32x4 w = __builtin_bit_cast(u32x4, x);
+    return f32x8{low_half(w[0]), high_half(w[0]), low_half(w[1]), high_half(w[1]), low_half(w[2]), high_half(w[2]), low_half(w[3]), high_half(w[3])};
+}
 __device__ inline f32x8 widen(f32x8 x) { return x; }
 
 // eight entries of one row
@@ -167,35 +208,75 @@ template <int PITCH> __device__ inline f32x8 col_frag(const float *tile, int t0,
     return x;
 }
 
-// rows 0 .. n-1 of `d` entries from memory into a tile of 64 rows of D entries, zeros elsewhere
-template <typename E, typename S, int D, int PITCH, int THREADS>
-__device__ inline void stage(E *tile, const S *src, long long stride, int n, int d, int vec)
-{
+// Rows 0 .. n-1 of `d` entries, on their way from memory into a tile of 64 rows of D entries with zeros elsewhere: fetched into
+// registers, all loads in flight at once (rows and columns that are not there are read from ones that are), and put into LDS
+// where the walk gets to them.
+template <typename S, int D, int THREADS> struct Rows64 {
     typedef typename Vec<S, 8>::type SV;
-    typedef typename Vec<E, 8>::type EV;
-    constexpr int UNITS = CHUNK * D / 8;
-    if (vec) {
+    static constexpr int UNITS = CHUNK * D / 8, N = (UNITS + THREADS - 1) / THREADS;
+    SV x[N];
+
+    // a thread's units lie in one column, STEP rows apart
+    static constexpr int STEP = THREADS / (D / 8);
+    static_assert(THREADS % (D / 8) == 0, "units of a thread in one column");
+    __device__ static inline int row0() { return threadIdx.x / (D / 8); }
+    __device__ static inline int col0() { return threadIdx.x % (D / 8) * 8; }
+
+    __device__ inline void fetch(const S *src, long long stride, int n, int d)
+    {
+        // byte offsets within the chunk, 32 bits (the host has longer strides taken element by element)
+        const unsigned col = (col0() < d ? col0() : 0) * sizeof(S), bytes = (unsigned)stride * sizeof(S);
+        const char *const p = reinterpret_cast<const char *>(src);
+        if (n == CHUNK) {
+            const unsigned at = row0() * bytes + col, step = STEP * bytes;
 #pragma unroll
-        for (int u0 = 0; u0 < UNITS; u0 += THREADS) {
-            const int u = u0 + threadIdx.x;
-            if (UNITS % THREADS == 0 || u < UNITS) {
-                const int row = u / (D / 8), col = u % (D / 8) * 8;
-                EV x = {};
-                if (row < n && col < d) x = __builtin_convertvector(*reinterpret_cast<const SV *>(src + row * stride + col), EV);
-                E *to = tile + row * PITCH + col;
+            for (int k = 0; k < N; k++)
+                if (UNITS % THREADS == 0 || row0() + k * STEP < CHUNK) x[k] = *reinterpret_cast<const SV *>(p + (at + k * step));
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; k++) {
+                const int row = row0() + k * STEP;
+                x[k] = *reinterpret_cast<const SV *>(p + ((row < n ? row : n - 1) * bytes + col));
+            }
+        }
+    }
+    template <typename E, int PITCH> __device__ inline void put(E *tile, int n, int d) const
+    {
+        typedef typename Vec<E, 8>::type EV;
+        const bool there = col0() < d;
+        E *const to0 = tile + row0() * PITCH + col0();
+#pragma unroll
+        for (int k = 0; k < N; k++) {
+            EV v = __builtin_convertvector(x[k], EV);
+            if (!there || (n != CHUNK && row0() + k * STEP >= n)) v = EV{};
+            if (UNITS % THREADS == 0 || row0() + k * STEP < CHUNK) {
+                E *const to = to0 + k * STEP * PITCH;
                 if constexpr (sizeof(E) == 2) {
-                    *reinterpret_cast<EV *>(to) = x;
+                    *reinterpret_cast<EV *>(to) = v;
                 } else {
-                    *reinterpret_cast<f32x4 *>(to) = __builtin_shufflevector(x, x, 0, 1, 2, 3);
-                    *reinterpret_cast<f32x4 *>(to + 4) = __builtin_shufflevector(x, x, 4, 5, 6, 7);
+                    *reinterpret_cast<f32x4 *>(to) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+                    *reinterpret_cast<f32x4 *>(to + 4) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
                 }
             }
         }
-    } else {
-#pragma unroll 8
-        for (int u = threadIdx.x; u < CHUNK * D; u += THREADS) {
-            const int row = u / D, col = u % D;
-            tile[row * PITCH + col] = row < n && col < d ? (E)src[row * stride + col] : (E)0.0f;
+    }
+};
+
+// the same for rows whose vectors are not aligned: straight into LDS, element by element
+template <typename E, typename S, int D, int PITCH, int THREADS> __device__ inline void stage_elements(E *tile, const S *src, long long stride, int n, int d)
+{
+#pragma unroll 1
+    for (int u0 = threadIdx.x; u0 < CHUNK * D; u0 += 16 * THREADS) {
+        S x[16];
+#pragma unroll
+        for (int k = 0; k < 16; k++) {
+            const int u = u0 + k * THREADS, row = u / D, col = u % D;
+            x[k] = src[(row < n ? row : n - 1) * stride + (col < d ? col : 0)];
+        }
+#pragma unroll
+        for (int k = 0; k < 16; k++) {
+            const int u = u0 + k * THREADS, row = u / D, col = u % D;
+            if (u < CHUNK * D) tile[row * PITCH + col] = row < n && col < d ? (E)x[k] : (E)0.0f;
         }
     }
 }
@@ -210,10 +291,15 @@ template <typename E, int DK, int DV, int NW, bool OUT> struct WalkLds {
     static constexpr int ROWS = CHUNK * PK * (OUT ? 2 : 1) + CHUNK * PV; // elements
     static constexpr int P_FRAGS = OUT ? 8 * Operand<E>::OUT_PARTS * 64 : 0;
     static constexpr size_t bytes = ROWS * sizeof(E) + P_FRAGS * sizeof(typename Operand<E>::Frag);
+    // workgroups of a CU: as many as its LDS holds, and no more than leave their waves the registers for the state (DK DV / 64 NW
+    // a lane), the outputs and the rows on their way
+    static constexpr int fit = (int)((160 << 10) / bytes), most = DK * DV / (64 * NW) * (int)sizeof(E) / 2 > 32 ? 2 : 3;
+    static constexpr int resident = fit < 1 ? 1 : fit > most ? most : fit;
 };
 
 // DK, DV: ka and nc, padded; NW waves of NT tiles of 16 columns each
-template <typename S, int DK, int DV, int NW, bool OUT> __global__ __launch_bounds__(NW * 64) void walk_kernel(WalkArgs w)
+template <typename S, int DK, int DV, int NW, bool OUT, bool REV>
+__device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &at, long long slot, int h, unsigned char *lds)
 {
     typedef typename Compute<S>::type E;
     typedef Operand<E> Op;
@@ -222,20 +308,15 @@ template <typename S, int DK, int DV, int NW, bool OUT> __global__ __launch_boun
     constexpr int THREADS = NW * 64, NT = DV / 16 / NW, KS = DK / 32, CS = NT == 2 ? 8 : 4;
     constexpr int OP = Op::OUT_PARTS, SP = Op::STATE_PARTS;
     static_assert(NT == 1 || NT == 2, "a wave has one or two column tiles");
-    extern __shared__ __align__(16) unsigned char lds[];
     Frag *const p_lds = reinterpret_cast<Frag *>(lds);
     E *const b_lds = reinterpret_cast<E *>(p_lds + Lds::P_FRAGS);
     E *const c_lds = b_lds + CHUNK * Lds::PK;
     E *const a_lds = c_lds + CHUNK * Lds::PV;
 
-    const WalkRole &r = w.role[blockIdx.z];
-    const long long slot = blockIdx.x / w.heads;
-    const int h = blockIdx.x % w.heads;
-    const Place at = find_place(w, slot);
-    const bool last = r.reverse ? at.seg == 0 : at.seg == at.nseg - 1; // in walking order
-    if (at.seg >= at.nseg || (!OUT && last)) return;
+    const bool last = REV ? at.seg == 0 : at.seg == at.nseg - 1; // in walking order
+    if (!OUT && last) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-    const float g2 = w.log_decay[h] * 1.44269504088896341f;
+    const float log2_g = log2_decay(w.log_decay[h]);
     const int col0 = wave * NT * 16; // the wave's columns: col0 + (i / 4) CS + 4 nt + i % 4
 
     // ---- the incoming state
@@ -251,7 +332,7 @@ template <typename S, int DK, int DV, int NW, bool OUT> __global__ __launch_boun
             if (OUT && total && !empty) {
                 x = *reinterpret_cast<const f32x4 *>(total + (nt * (DK / 16) + t) * 256);
             } else if (OUT && r.init) {
-                const float scale = r.reverse || empty ? 1.0f : decay_power(g2, 1);
+                const float scale = REV || empty ? 1.0f : decay_power(log2_g, 1);
                 const int col = col0 + (i >> 2) * CS + 4 * nt + (i & 3);
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
@@ -267,21 +348,44 @@ template <typename S, int DK, int DV, int NW, bool OUT> __global__ __launch_boun
     const S *const c = reinterpret_cast<const S *>(r.c) + at.start * r.c_tok + h / r.c_group * r.c_head;
     const long long seg0 = at.seg * w.seg_len, seg1 = seg0 + w.seg_len < at.len ? seg0 + w.seg_len : at.len;
     const int nchunks = (int)((seg1 - seg0 + CHUNK - 1) / CHUNK);
+    const bool a_vec = r.a_vec, b_vec = r.b_vec, c_vec = r.c_vec;
+    Rows64<S, DK, THREADS> ax, bx;
+    Rows64<S, DV, THREADS> cx;
+    auto chunk_at = [&](int step) { return seg0 + (long long)(REV ? nchunks - 1 - step : step) * CHUNK; };
+    auto chunk_rows = [&](long long t0) { return seg1 - t0 < CHUNK ? (int)(seg1 - t0) : CHUNK; };
+    auto fetch = [&](int step) {
+        const long long t0 = chunk_at(step);
+        const int n = chunk_rows(t0);
+        if (OUT && a_vec) ax.fetch(a + t0 * r.a_tok, r.a_tok, n, r.ka);
+        if (b_vec) bx.fetch(b + t0 * r.b_tok, r.b_tok, n, r.ka);
+        if (c_vec) cx.fetch(c + t0 * r.c_tok, r.c_tok, n, r.nc);
+    };
+    constexpr bool EARLY = LA_EARLY;
+    if (EARLY && nchunks > 0) fetch(0);
     for (int step = 0; step < nchunks; step++) {
-        const long long t0 = seg0 + (long long)(r.reverse ? nchunks - 1 - step : step) * CHUNK;
-        const int n = seg1 - t0 < CHUNK ? (int)(seg1 - t0) : CHUNK;
+        const long long t0 = chunk_at(step);
+        const int n = chunk_rows(t0);
+        float g2 = log2_g;
+        asm volatile("" : "+v"(g2)); // the chunk's weights are formed anew for each: kept, they would take some 50 registers
         __syncthreads();
-        if (OUT) stage<E, S, DK, Lds::PK, THREADS>(a_lds, a + t0 * r.a_tok, r.a_tok, n, r.ka, r.a_vec);
-        stage<E, S, DK, Lds::PK, THREADS>(b_lds, b + t0 * r.b_tok, r.b_tok, n, r.ka, r.b_vec);
-        stage<E, S, DV, Lds::PV, THREADS>(c_lds, c + t0 * r.c_tok, r.c_tok, n, r.nc, r.c_vec);
+        if (!EARLY) fetch(step);
+        if (OUT) {
+            if (a_vec) ax.template put<E, Lds::PK>(a_lds, n, r.ka);
+            else stage_elements<E, S, DK, Lds::PK, THREADS>(a_lds, a + t0 * r.a_tok, r.a_tok, n, r.ka);
+        }
+        if (b_vec) bx.template put<E, Lds::PK>(b_lds, n, r.ka);
+        else stage_elements<E, S, DK, Lds::PK, THREADS>(b_lds, b + t0 * r.b_tok, r.b_tok, n, r.ka);
+        if (c_vec) cx.template put<E, Lds::PV>(c_lds, n, r.nc);
+        else stage_elements<E, S, DV, Lds::PV, THREADS>(c_lds, c + t0 * r.c_tok, r.c_tok, n, r.nc);
         __syncthreads();
+        if (EARLY && step + 1 < nchunks) fetch(step + 1); // while this chunk is worked on
 
         if (OUT) {
             // ---- P, transposed (accumulator columns are the rows i, so that a lane's entries are consecutive j)
             for (int it = wave; it < 4; it += NW) {
 #pragma unroll
                 for (int ks = 0; ks < 2; ks++) {
-                    if (r.reverse ? ks < it / 2 : ks > it / 2) continue; // no pair in this half
+                    if (REV ? ks < it / 2 : ks > it / 2) continue; // no pair in this half
                     f32x4 p0 = {0, 0, 0, 0}, p1 = {0, 0, 0, 0};
                     const E *const arow = a_lds + (it * 16 + i) * Lds::PK + g * 8;
                     const E *const brow = b_lds + (ks * 32 + (i >> 2) * 8 + (i & 3)) * Lds::PK + g * 8;
@@ -292,10 +396,13 @@ template <typename S, int DK, int DV, int NW, bool OUT> __global__ __launch_boun
                         p1 = mma(row_frag(brow + 4 * Lds::PK + kk * 32), af, p1);
                     }
                     f32x8 x;
+                    int first = it * 16 + i - ks * 32 - g * 8; // i - j of the lane's first j
+                    asm volatile("" : "+v"(first));            // (and so are the masks)
+                    const float at = g2 * (float)(REV ? -first : first), by = REV ? g2 : -g2;
 #pragma unroll
                     for (int e = 0; e < 8; e++) {
-                        const int j = ks * 32 + g * 8 + e, age = r.reverse ? j - (it * 16 + i) : it * 16 + i - j;
-                        x[e] = age >= 0 ? (e < 4 ? p0[e & 3] : p1[e & 3]) * (r.p_scale * decay_power(g2, age)) : 0.0f;
+                        const float p = (e < 4 ? p0[e & 3] : p1[e & 3]) * (r.p_scale * __builtin_amdgcn_exp2f(at + by * (float)e));
+                        x[e] = (REV ? e >= first : e <= first) ? p : 0.0f;
                     }
                     Frag parts[OP];
                     split(x, parts);
@@ -307,11 +414,13 @@ template <typename S, int DK, int DV, int NW, bool OUT> __global__ __launch_boun
         }
 
         Frag cf[2][NT];
+        auto load_columns = [&] {
 #pragma unroll
-        for (int ks = 0; ks < 2; ks++)
+            for (int ks = 0; ks < 2; ks++)
 #pragma unroll
-            for (int nt = 0; nt < NT; nt++) cf[ks][nt] = col_frag<Lds::PV>(c_lds, ks * 32, col0 + 4 * nt, CS, lane);
-
+                for (int nt = 0; nt < NT; nt++) cf[ks][nt] = col_frag<Lds::PV>(c_lds, ks * 32, col0 + 4 * nt, CS, lane);
+        };
+        if (!OUT) load_columns();
         if (OUT) {
             // ---- what the state gives to each row, then the pairs; transposed: a lane has consecutive columns of row i
             f32x4 y[4][NT];
@@ -319,29 +428,38 @@ template <typename S, int DK, int DV, int NW, bool OUT> __global__ __launch_boun
             for (int it = 0; it < 4; it++)
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++) y[it][nt] = f32x4{0, 0, 0, 0};
+            // operands are read one step ahead of their products, and no further: registers are what the walk is short of
+            Frag af[2][4];
+            const E *const a0 = a_lds + i * Lds::PK + g * 8;
+#pragma unroll
+            for (int it = 0; it < 4; it++) af[0][it] = row_frag(a0 + it * 16 * Lds::PK);
 #pragma unroll
             for (int kk = 0; kk < KS; kk++) {
+                if (kk + 1 < KS) {
+#pragma unroll
+                    for (int it = 0; it < 4; it++) af[(kk + 1) & 1][it] = row_frag(a0 + it * 16 * Lds::PK + (kk + 1) * 32);
+                }
                 Frag rf[NT][OP];
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++) split(__builtin_shufflevector(R[2 * kk][nt], R[2 * kk + 1][nt], 0, 1, 2, 3, 4, 5, 6, 7), rf[nt]);
 #pragma unroll
-                for (int it = 0; it < 4; it++) {
-                    const Frag af = row_frag(a_lds + (it * 16 + i) * Lds::PK + kk * 32 + g * 8);
+                for (int it = 0; it < 4; it++)
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-                        for (int q = 0; q < OP; q++) y[it][nt] = mma(rf[nt][q], af, y[it][nt]);
-                }
+                        for (int q = 0; q < OP; q++) y[it][nt] = mma(rf[nt][q], af[kk & 1][it], y[it][nt]);
+                __builtin_amdgcn_sched_barrier(0);
             }
+            load_columns();
 #pragma unroll
             for (int it = 0; it < 4; it++) {
-                const int row = it * 16 + i, age = r.reverse ? n - 1 - row : row;
+                const int row = it * 16 + i, age = REV ? n - 1 - row : row;
                 const float scale = r.w_scale * decay_power(g2, age > 0 ? age : 0);
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++) y[it][nt] *= scale;
 #pragma unroll
                 for (int ks = 0; ks < 2; ks++) {
-                    if (r.reverse ? ks < it / 2 : ks > it / 2) continue;
+                    if (REV ? ks < it / 2 : ks > it / 2) continue;
 #pragma unroll
                     for (int q = 0; q < OP; q++) {
                         const Frag pf = p_lds[((it * 2 + ks) * OP + q) * 64 + lane];
@@ -349,6 +467,7 @@ template <typename S, int DK, int DV, int NW, bool OUT> __global__ __launch_boun
                         for (int nt = 0; nt < NT; nt++) y[it][nt] = mma(cf[ks][nt], pf, y[it][nt]);
                     }
                 }
+                __builtin_amdgcn_sched_barrier(0);
                 if (row < n) {
                     const long long to = (at.start + t0 + row) * r.y_tok + h * r.y_head;
                     const int col = col0 + g * CS;
@@ -371,7 +490,7 @@ template <typename S, int DK, int DV, int NW, bool OUT> __global__ __launch_boun
         }
 
         // ---- the next state; after the last token of a forward walk the final state, one decay short of the next chunk's
-        const int ahead = !r.reverse && last && r.fin && step == nchunks - 1 ? 1 : 0;
+        const int ahead = !REV && last && r.fin && step == nchunks - 1 ? 1 : 0;
         const float whole = decay_power(g2, n - ahead);
 #pragma unroll
         for (int t = 0; t < DK / 16; t++)
@@ -379,22 +498,29 @@ template <typename S, int DK, int DV, int NW, bool OUT> __global__ __launch_boun
             for (int nt = 0; nt < NT; nt++) R[t][nt] *= whole;
 #pragma unroll
         for (int ks = 0; ks < 2; ks++) {
-            f32x8 wt;
+            f32x8 wt; // u g^(n - j'); rows past the end, where it would grow, are zeros
+            const int first = REV ? ks * 32 + g * 8 + 1 : n - ahead - ks * 32 - g * 8;
+            const float at = g2 * (float)first, by = REV ? g2 : -g2;
+            if (n == CHUNK) {
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                const int j = ks * 32 + g * 8 + e, age = r.reverse ? j + 1 : n - ahead - j;
-                wt[e] = r.u_scale * decay_power(g2, age > 0 ? age : 0);
+                for (int e = 0; e < 8; e++) wt[e] = r.u_scale * __builtin_amdgcn_exp2f(at + by * (float)e);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; e++) wt[e] = !REV && first - e < 0 ? 0.0f : r.u_scale * __builtin_amdgcn_exp2f(at + by * (float)e);
             }
             Frag cd[NT][SP];
 #pragma unroll
             for (int nt = 0; nt < NT; nt++) split(widen(cf[ks][nt]) * wt, cd[nt]);
+            Frag bf[2];
+            bf[0] = col_frag<Lds::PK>(b_lds, ks * 32, 0, 8, lane);
 #pragma unroll
             for (int t = 0; t < DK / 16; t++) {
-                const Frag bf = col_frag<Lds::PK>(b_lds, ks * 32, t / 2 * 32 + t % 2 * 4, 8, lane);
+                if (t + 1 < DK / 16) bf[(t + 1) & 1] = col_frag<Lds::PK>(b_lds, ks * 32, (t + 1) / 2 * 32 + (t + 1) % 2 * 4, 8, lane);
 #pragma unroll
-                for (int nt = 0; nt < NT; nt++)
+                for (int q = 0; q < SP; q++)
 #pragma unroll
-                    for (int q = 0; q < SP; q++) R[t][nt] = mma(bf, cd[nt][q], R[t][nt]);
+                    for (int nt = 0; nt < NT; nt++) R[t][nt] = mma(bf[t & 1], cd[nt][q], R[t][nt]);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
     }
@@ -418,6 +544,23 @@ template <typename S, int DK, int DV, int NW, bool OUT> __global__ __launch_boun
     }
 }
 
+// grid: slots heads roles; the roles of a head and segment run on one XCD (of 8, dealt round robin), whose L2 has the rows they share
+template <typename S, int DK, int DV, int NW, bool OUT>
+__global__ __launch_bounds__(NW * 64, (WalkLds<typename Compute<S>::type, DK, DV, NW, OUT>::resident * NW / 4)) void walk_kernel(WalkArgs w)
+{
+    extern __shared__ __align__(16) unsigned char lds[];
+    const unsigned group = blockIdx.x / (8 * w.roles), in = blockIdx.x % (8 * w.roles);
+    const unsigned item = group * 8 + in % 8;
+    if (item >= w.slots * w.heads) return;
+    const WalkRole &r = w.role[in / 8];
+    const long long slot = item / w.heads;
+    const int h = item % w.heads;
+    const Place at = find_place(w, slot);
+    if (at.seg >= at.nseg) return;
+    if (r.reverse) walk<S, DK, DV, NW, OUT, true>(w, r, at, slot, h, lds);
+    else walk<S, DK, DV, NW, OUT, false>(w, r, at, slot, h, lds);
+}
+
 // Segment totals -> incoming states, in place, in walking order: a thread has four entries of one head's state and goes
 // through the segments of one sequence.  grid: (seqs heads times a part of 1024 entries, 1, roles)
 template <int DK, int DV, int NW> __global__ __launch_bounds__(256) void carry_kernel(WalkArgs w)
@@ -431,7 +574,7 @@ template <int DK, int DV, int NW> __global__ __launch_bounds__(256) void carry_k
     span(w, s, start, len);
     const long long nseg = len > 0 ? (len + w.seg_len - 1) / w.seg_len : 1;
     const int lane = u & 63, t = u / 64 % (DK / 16), nt = u / 64 / (DK / 16) % NT, wave = u / 64 / (DK / 16) / NT, i = lane & 15;
-    const float g2 = w.log_decay[h] * 1.44269504088896341f;
+    const float g2 = log2_decay(w.log_decay[h]);
     f32x4 x = {0, 0, 0, 0};
     if (r.init) {
         const float scale = r.reverse ? 1.0f : decay_power(g2, 1);
@@ -445,14 +588,18 @@ template <int DK, int DV, int NW> __global__ __launch_bounds__(256) void carry_k
     const long long stride = (long long)w.heads * (DK * DV / 4);
     const float whole = decay_power(g2, (int)w.seg_len);
     const float first = r.reverse ? decay_power(g2, (int)(len - (nseg - 1) * w.seg_len)) : whole; // a sequence's last segment may be shorter
-    long long at = r.reverse ? nseg - 1 : 0;
-    const long long dir = r.reverse ? -1 : 1;
-    f32x4 next = nseg > 1 ? tot[at * stride] : f32x4{0, 0, 0, 0};
-    for (long long k = 0; k < nseg; k++, at += dir) {
-        const f32x4 mine = next;
-        if (k + 2 < nseg) next = tot[(at + dir) * stride]; // (the last segment in walking order has no total)
-        tot[at * stride] = x;
-        x = x * (k == 0 ? first : whole) + mine;
+    const long long dir = r.reverse ? -1 : 1, at = r.reverse ? nseg - 1 : 0;
+    constexpr int AHEAD = 8; // totals in flight (the last segment in walking order has none)
+    for (long long k0 = 0; k0 < nseg; k0 += AHEAD) {
+        f32x4 mine[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; k++) mine[k] = k0 + k + 1 < nseg ? tot[(at + dir * (k0 + k)) * stride] : f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < AHEAD; k++)
+            if (k0 + k < nseg) {
+                tot[(at + dir * (k0 + k)) * stride] = x;
+                x = x * (k0 + k == 0 ? first : whole) + mine[k];
+            }
     }
 }
 
@@ -476,7 +623,7 @@ template <typename S, bool VEC> __global__ __launch_bounds__(256) void step_kern
     const int h = blockIdx.x % sh.heads, col = blockIdx.y * 32 + (threadIdx.x & 7) * 4, row0 = threadIdx.x >> 3;
     const long long s = blockIdx.x / sh.heads;
     const int kv = h / (sh.heads / sh.kv_heads);
-    const float decay = __builtin_amdgcn_exp2f(log_decay[h] * 1.44269504088896341f);
+    const float decay = decay_power(log2_decay(log_decay[h]), 1);
     const S *const qh = q + s * sh.q_token + h * sh.q_head, *const kh = k + s * sh.k_token + kv * sh.k_head, *const vh = v + s * sh.v_token + kv * sh.v_head;
     const long long base = (s * sh.heads + h) * (long long)sh.dk * sh.dv;
     float x[4], y[4] = {0, 0, 0, 0};
@@ -546,8 +693,8 @@ struct Segments { long long len, slots, per_seq; };
 
 static Segments choose_segments(const goom_attention_shape &sh, int roles, bool packed)
 {
-    const long long walks = sh.seqs * sh.heads * roles, mean = sh.seqs > 0 ? (sh.tokens + sh.seqs - 1) / sh.seqs : 0;
-    long long want = walks > 0 ? (768 + walks - 1) / walks : 1; // segments a sequence of mean length
+    const long long walks = sh.seqs * sh.heads * roles, round = 256 * LA_RES, mean = sh.seqs > 0 ? (sh.tokens + sh.seqs - 1) / sh.seqs : 0;
+    long long want = walks > 0 ? round / walks : 1; // segments a sequence of mean length
     const long long most = (mean + 4 * CHUNK - 1) / (4 * CHUNK);  // not below four chunks each
     if (want > most) want = most;
     if (want < 1) want = 1;
@@ -572,11 +719,13 @@ static size_t totals_bytes(const goom_attention_shape &sh, const Segments &g, in
     return goom::align_up((size_t)(g.slots * sh.heads) * padded_head(ka) * padded_head(nc) * 4, 256);
 }
 
-template <typename S, int DK, int DV> static int launch_walks_sized(goom_ctx *ctx, const WalkArgs &w, int roles, long long slots, const char *label)
+template <typename S, int DK, int DV> static int launch_walks_sized(goom_ctx *ctx, WalkArgs w, int roles, long long slots, const char *label)
 {
-    constexpr int NW = DV >= 64 ? 4 : 2;
     typedef typename Compute<S>::type E;
-    const dim3 grid((unsigned)(slots * w.heads), 1, roles);
+    constexpr int NW = DV == 128 ? (sizeof(E) == 4 ? LA_NW32 : LA_NW) : DV == 64 ? 4 : 2;
+    w.roles = roles;
+    w.slots = (unsigned)slots;
+    const unsigned grid = (unsigned)((slots * w.heads + 7) / 8 * 8 * roles);
     const bool parts = w.role[0].totals != nullptr;
     if (parts) {
         auto *totals = walk_kernel<S, DK, DV, NW, false>;
@@ -618,10 +767,11 @@ static int launch_walks(goom_ctx *ctx, int type, const WalkArgs &w, int roles, l
     });
 }
 
-// rows of `d` entries whose vectors of 8 elements are aligned to 16 bytes (32 for floats: read as two)
+// rows of `d` entries whose vectors of 8 elements are aligned to 16 bytes (32 for floats: read as two); a chunk's offsets
+// within 32 bits
 static int vec_rows(const void *p, long long tok, long long head, int d, size_t size)
 {
-    return d % 8 == 0 && tok % 8 == 0 && head % 8 == 0 && goom::aligned(p, 8 * size);
+    return d % 8 == 0 && tok % 8 == 0 && head % 8 == 0 && goom::aligned(p, 8 * size) && tok < (1ll << 24);
 }
 
 static WalkArgs walk_args(const goom_attention_shape &sh, const float *log_decay, const int64_t *offsets, const Segments &g)
