@@ -8,6 +8,7 @@ imag = 0 or pi).
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -187,22 +188,37 @@ def _dtype_code(t):
     raise TypeError(f"unsupported tensor dtype {t.dtype}")
 
 
+_real_codes = {}  # torch dtype -> GOOM_REAL_*
+
+
 def _real_code(t):
-    import torch
-    code = {torch.float32: REAL_F32, torch.bfloat16: REAL_BF16, torch.float16: REAL_F16}.get(t.dtype)
+    code = _real_codes.get(t.dtype)
     if code is None:
-        raise TypeError(f"unsupported tensor dtype {t.dtype}")
+        import torch
+        _real_codes.update({torch.float32: REAL_F32, torch.bfloat16: REAL_BF16, torch.float16: REAL_F16})
+        code = _real_codes.get(t.dtype)
+        if code is None:
+            raise TypeError(f"unsupported tensor dtype {t.dtype}")
     return code
 
 
+def _at(t):
+    """Address of a contiguous device tensor, None for None."""
+    if t is None:
+        return None
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("libgoom takes contiguous device tensors")
+    return t.data_ptr()
+
+
 def _rows(t, name):
-    """Pointer and strides (token, head) of [..., heads, d] whose last axis is contiguous and whose leading axes follow one
-    another in memory, as in a slice of a fused projection."""
+    """Address and strides (token, head; 0, 0: contiguous) of [..., heads, d] whose last axis is contiguous and whose leading axes
+    follow one another in memory, as in a slice of a fused projection."""
     if not t.is_cuda:
         raise ValueError("libgoom takes device tensors")
-    st, sh = list(t.stride()), list(t.shape)
-    if t.numel() == 0:
-        return C.c_void_p(t.data_ptr()), 0, 0
+    if t.is_contiguous():
+        return t.data_ptr(), 0, 0
+    st, sh = t.stride(), t.shape
     if sh[-1] != 1 and st[-1] != 1:
         raise ValueError(f"{name}: the last axis must be contiguous")
     head = sh[-1] if sh[-2] == 1 else st[-2]
@@ -216,7 +232,7 @@ def _rows(t, name):
             raise ValueError(f"{name}: the tokens do not follow one another in memory")
         else:
             run *= sh[i]
-    return C.c_void_p(t.data_ptr()), sh[-2] * head if token is None else token, head
+    return t.data_ptr(), sh[-2] * head if token is None else token, head
 
 
 def _ptr(t):
@@ -635,34 +651,35 @@ class Goom:
         return out
 
     # ---- linear attention with a decay for each head
-    def _attention(self, q, k, v, log_decay, offsets, scale, lead):
-        """The shape structure and the pointers of q, k, v."""
-        torch = self.torch
+    def _attention(self, q, k, v, log_decay, offsets, scale, step=False):
+        """The shape structure and the addresses of q, k, v."""
         code = _real_code(q)
-        if not (k.dtype == v.dtype == q.dtype) or log_decay.dtype != torch.float32:
+        if k.dtype != q.dtype or v.dtype != q.dtype or log_decay.dtype != self.torch.float32:
             raise TypeError("q, k, v have one type, log_decay is float32")
-        heads, dk = q.shape[-2:]
-        kv_heads, dv = v.shape[-2:]
-        if k.shape != lead + (kv_heads, dk) or q.shape[:-2] != lead or v.shape[:-2] != lead or tuple(log_decay.shape) != (heads,):
+        sq, sk, sv = tuple(q.shape), tuple(k.shape), tuple(v.shape)
+        lead, (heads, dk), (kv_heads, dv) = sq[:-2], sq[-2:], sv[-2:]
+        if len(sq) < 3 or sk != lead + (kv_heads, dk) or sv[:-2] != lead or tuple(log_decay.shape) != (heads,):
             raise ValueError("shapes of q, k, v, log_decay do not fit")
-        tokens = lead.numel()
+        tokens = math.prod(lead)
         if offsets is not None:
-            if offsets.dtype != torch.int64 or offsets.dim() != 1 or offsets.numel() < 1 or len(lead) != 1:
+            if offsets.dtype != self.torch.int64 or offsets.dim() != 1 or offsets.numel() < 1 or len(lead) != 1:
                 raise ValueError("offsets: int64 [sequences + 1], with q, k, v [tokens, heads, d]")
             seqs = offsets.numel() - 1
+        elif step:
+            seqs = tokens
         else:
-            seqs = lead[:-1].numel() if len(lead) > 1 else 1
-        shape = AttentionShape(seqs, tokens, heads, kv_heads, dk, dv, code, 0, scale)
-        pq, shape.q_token, shape.q_head = _rows(q, "q")
-        pk, shape.k_token, shape.k_head = _rows(k, "k")
-        pv, shape.v_token, shape.v_head = _rows(v, "v")
-        return shape, pq, pk, pv
+            seqs = math.prod(lead[:-1])
+        pq, q_token, q_head = _rows(q, "q")
+        pk, k_token, k_head = _rows(k, "k")
+        pv, v_token, v_head = _rows(v, "v")
+        return AttentionShape(seqs, tokens, heads, kv_heads, dk, dv, code, 0, scale, q_token, q_head, k_token, k_head, v_token, v_head), pq, pk, pv
 
     def _state(self, t, shape, name):
-        want = (shape.seqs, shape.heads, shape.dk, shape.dv)
-        if t is not None and (tuple(t.shape) != want or t.dtype != self.torch.float32):
-            raise ValueError(f"{name}: float32 {list(want)}")
-        return _ptr(t)
+        if t is None:
+            return None
+        if tuple(t.shape) != (shape.seqs, shape.heads, shape.dk, shape.dv) or t.dtype != self.torch.float32:
+            raise ValueError(f"{name}: float32 {[shape.seqs, shape.heads, shape.dk, shape.dv]}")
+        return _at(t)
 
     def linear_attention(self, q, k, v, log_decay, state=None, offsets=None, scale: float = 1.0, want_state: bool = False):
         """o_t = scale q_t^T S_t, S_t = exp(log_decay) S_{t-1} + k_t v_t^T for every head.  q: [batch, T, heads, dk], k: [batch, T,
@@ -670,13 +687,13 @@ class Goom:
         sequences of different lengths lie behind one another; state, and the final one that want_state adds: float32 [sequences,
         heads, dk, dv].  q, k, v may be slices of one projection's output."""
         torch = self.torch
-        shape, pq, pk, pv = self._attention(q, k, v, log_decay, offsets, scale, q.shape[:-2])
+        shape, pq, pk, pv = self._attention(q, k, v, log_decay, offsets, scale)
         ps = self._state(state, shape, "state")
         o = torch.empty(q.shape[:-1] + (shape.dv,), dtype=q.dtype, device=q.device)
         last = torch.empty((shape.seqs, shape.heads, shape.dk, shape.dv), dtype=torch.float32, device=q.device) if want_state else None
         ws, wsn = self.workspace(self.lib.goom_linear_attention_workspace_bytes(C.byref(shape), int(offsets is not None)))
-        self._check(self.lib.goom_linear_attention(self._ctx, C.byref(shape), pq, pk, pv, _ptr(log_decay), _ptr(offsets), ps, _ptr(o), _ptr(last),
-                                                   _ptr(ws), wsn))
+        self._check(self.lib.goom_linear_attention(self._ctx, C.byref(shape), pq, pk, pv, _at(log_decay), _at(offsets), ps, o.data_ptr(), _at(last),
+                                                   _at(ws), wsn))
         return (o, last) if want_state else o
 
     def linear_attention_step(self, q, k, v, log_decay, state, scale: float = 1.0, out_state=None):
@@ -684,50 +701,60 @@ class Goom:
         heads, dk, dv], replaced by the next one, or left as it is if out_state receives that."""
         if q.dim() != 3:
             raise ValueError("q: [batch, heads, dk]")
-        shape, pq, pk, pv = self._attention(q, k, v, log_decay, None, scale, q.shape[:-2])
-        shape.seqs = shape.tokens
-        out_state = state if out_state is None else out_state
-        o = self.torch.empty(q.shape[:-1] + (shape.dv,), dtype=q.dtype, device=q.device)
-        self._check(self.lib.goom_linear_attention_step(self._ctx, C.byref(shape), pq, pk, pv, _ptr(log_decay), self._state(state, shape, "state"), _ptr(o),
-                                                        self._state(out_state, shape, "out_state")))
+        shape, pq, pk, pv = self._attention(q, k, v, log_decay, None, scale, step=True)
+        ps = self._state(state, shape, "state")
+        pn = ps if out_state is None else self._state(out_state, shape, "out_state")
+        o = self.torch.empty((shape.seqs, shape.heads, shape.dv), dtype=q.dtype, device=q.device)
+        self._check(self.lib.goom_linear_attention_step(self._ctx, C.byref(shape), pq, pk, pv, _at(log_decay), ps, o.data_ptr(), pn))
         return o
 
     def linear_attention_backward(self, q, k, v, log_decay, grad_o, state=None, grad_state=None, offsets=None, scale: float = 1.0):
         """Gradients with respect to q, k, v and (None without one) the initial state, given those with respect to the outputs and
         (None: none) the final state."""
-        torch = self.torch
-        shape, pq, pk, pv = self._attention(q, k, v, log_decay, offsets, scale, q.shape[:-2])
+        empty = self.torch.empty
+        shape, pq, pk, pv = self._attention(q, k, v, log_decay, offsets, scale)
         if grad_o.shape != q.shape[:-1] + (shape.dv,) or grad_o.dtype != q.dtype:
             raise ValueError("grad_o: of o's shape and type")
-        new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)  # noqa: E731
-        gq, gk, gv = new(q), new(k), new(v)
-        gs = new(state) if state is not None else None
+        gq, gk, gv = (empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+        ps, pg = self._state(state, shape, "state"), self._state(grad_state, shape, "grad_state")
+        gs = empty(state.shape, dtype=state.dtype, device=state.device) if state is not None else None
         ws, wsn = self.workspace(self.lib.goom_linear_attention_backward_workspace_bytes(C.byref(shape), int(offsets is not None)))
-        self._check(self.lib.goom_linear_attention_backward(self._ctx, C.byref(shape), pq, pk, pv, _ptr(log_decay), _ptr(offsets), self._state(state, shape, "state"),
-                                                            _ptr(grad_o), self._state(grad_state, shape, "grad_state"), _ptr(gq), _ptr(gk), _ptr(gv), _ptr(gs),
-                                                            _ptr(ws), wsn))
+        self._check(self.lib.goom_linear_attention_backward(self._ctx, C.byref(shape), pq, pk, pv, _at(log_decay), _at(offsets), ps, _at(grad_o), pg,
+                                                            gq.data_ptr(), gk.data_ptr(), gv.data_ptr(), _at(gs), _at(ws), wsn))
         return gq, gk, gv, gs
 
     # ---- group norm with an activation, channels last
     def _norm(self, x, groups, weight, bias, eps, activation):
-        if x.dim() < 2 or activation not in ACTIVATIONS:
+        sh = tuple(x.shape)
+        act = ACTIVATIONS.get(activation)
+        if len(sh) < 2 or act is None:
             raise ValueError("x: [items, ..., channels]; activation: one of " + ", ".join(ACTIVATIONS))
-        params = [p for p in (weight, bias) if p is not None]
-        if any(p.dtype != params[0].dtype or tuple(p.shape) != (x.shape[-1],) for p in params):
-            raise ValueError("weight and bias: [channels], of one type")
-        items, channels = x.shape[0], x.shape[-1]
-        code = _real_code(params[0]) if params else REAL_F32
-        return NormShape(items, x.shape[1:-1].numel(), channels, groups, _real_code(x), code, ACTIVATIONS[activation], 0, eps)
+        code = REAL_F32
+        for p in (weight, bias):
+            if p is not None and tuple(p.shape) != sh[-1:]:
+                raise ValueError("weight and bias: [channels]")
+        if weight is not None:
+            code = _real_code(weight)
+            if bias is not None and bias.dtype != weight.dtype:
+                raise TypeError("weight and bias have one type")
+        elif bias is not None:
+            code = _real_code(bias)
+        return NormShape(sh[0], math.prod(sh[1:-1]), sh[-1], groups, _real_code(x), code, act, 0, eps)
 
     def group_norm(self, x, groups: int, weight=None, bias=None, eps: float = 1e-5, activation: str = "none", want_stats: bool = False):
         """act(normalised x * weight + bias); x: [items, ..., channels], statistics over the axes between and channels / groups
         neighbouring channels ([tokens, channels]: every token by itself).  want_stats: also mean and rstd, float32 [items, groups]."""
         torch = self.torch
         shape = self._norm(x, groups, weight, bias, eps, activation)
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        mean, rstd = (torch.empty((shape.items, groups), dtype=torch.float32, device=x.device) if want_stats else None for _ in range(2))
+        px = _at(x)
+        y = torch.empty_like(x)
+        mean = rstd = pm = pr = None
+        if want_stats:
+            mean = torch.empty((shape.items, groups), dtype=torch.float32, device=x.device)
+            rstd = torch.empty_like(mean)
+            pm, pr = mean.data_ptr(), rstd.data_ptr()
         ws, wsn = self.workspace(self.lib.goom_group_norm_workspace_bytes(C.byref(shape)))
-        self._check(self.lib.goom_group_norm(self._ctx, C.byref(shape), _ptr(x), _ptr(weight), _ptr(bias), _ptr(y), _ptr(mean), _ptr(rstd), _ptr(ws), wsn))
+        self._check(self.lib.goom_group_norm(self._ctx, C.byref(shape), px, _at(weight), _at(bias), y.data_ptr(), pm, pr, _at(ws), wsn))
         return (y, mean, rstd) if want_stats else y
 
     def group_norm_backward(self, x, grad_y, mean, rstd, groups: int, weight=None, bias=None, activation: str = "none"):
@@ -737,12 +764,13 @@ class Goom:
         if grad_y.shape != x.shape or grad_y.dtype != x.dtype or tuple(mean.shape) != (shape.items, groups) or mean.shape != rstd.shape \
                 or mean.dtype != torch.float32 or rstd.dtype != torch.float32:
             raise ValueError("grad_y: of x's shape and type; mean, rstd: float32 [items, groups]")
-        ptype = weight.dtype if weight is not None else bias.dtype if bias is not None else torch.float32
-        gx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        gw, gb = (torch.empty(x.shape[-1], dtype=ptype, device=x.device) for _ in range(2))
+        px = _at(x)
+        gx = torch.empty_like(x)
+        gw = torch.empty(shape.channels, dtype=weight.dtype if weight is not None else bias.dtype if bias is not None else torch.float32, device=x.device)
+        gb = torch.empty_like(gw)
         ws, wsn = self.workspace(self.lib.goom_group_norm_backward_workspace_bytes(C.byref(shape)))
-        self._check(self.lib.goom_group_norm_backward(self._ctx, C.byref(shape), _ptr(x), _ptr(grad_y), _ptr(mean), _ptr(rstd), _ptr(weight), _ptr(bias), _ptr(gx),
-                                                      _ptr(gw), _ptr(gb), _ptr(ws), wsn))
+        self._check(self.lib.goom_group_norm_backward(self._ctx, C.byref(shape), px, _at(grad_y), _at(mean), _at(rstd), _at(weight), _at(bias), gx.data_ptr(),
+                                                      gw.data_ptr(), gb.data_ptr(), _at(ws), wsn))
         return gx, gw, gb
 
     # ---- token embeddings
@@ -751,11 +779,12 @@ class Goom:
         torch = self.torch
         if table.dim() != 2 or tokens.dtype != torch.int64:
             raise ValueError("table: [vocab, width]; tokens: int64")
+        vocab, width = table.shape
         if out is None:
-            out = torch.empty(tuple(tokens.shape) + (table.shape[1],), dtype=table.dtype, device=table.device)
-        elif tuple(out.shape) != tuple(tokens.shape) + (table.shape[1],) or out.dtype != table.dtype:
+            out = torch.empty(tokens.shape + (width,), dtype=table.dtype, device=table.device)
+        elif out.shape != tokens.shape + (width,) or out.dtype != table.dtype:
             raise ValueError("out: the tokens' shape with the table's width, of its type")
-        self._check(self.lib.goom_embedding(self._ctx, _ptr(table), _ptr(tokens), _ptr(out), tokens.numel(), table.shape[0], table.shape[1], _real_code(table), scale))
+        self._check(self.lib.goom_embedding(self._ctx, _at(table), _at(tokens), _at(out), tokens.numel(), vocab, width, _real_code(table), scale))
         return out
 
     def embedding_backward(self, tokens, grad, vocab: int, scale: float = 1.0, dtype=None):
@@ -764,8 +793,9 @@ class Goom:
         torch = self.torch
         if tokens.dtype != torch.int64 or grad.shape[:-1] != tokens.shape:
             raise ValueError("tokens: int64; grad: the tokens' shape with the width")
-        out = torch.empty((vocab, grad.shape[-1]), dtype=dtype or grad.dtype, device=grad.device)
-        ws, wsn = self.workspace(self.lib.goom_embedding_backward_workspace_bytes(tokens.numel(), vocab, grad.shape[-1]))
-        self._check(self.lib.goom_embedding_backward(self._ctx, _ptr(tokens), _ptr(grad), _ptr(out), tokens.numel(), vocab, grad.shape[-1], _real_code(grad),
-                                                     _real_code(out), scale, _ptr(ws), wsn))
+        n, width = tokens.numel(), grad.shape[-1]
+        out = torch.empty((vocab, width), dtype=dtype or grad.dtype, device=grad.device)
+        ws, wsn = self.workspace(self.lib.goom_embedding_backward_workspace_bytes(n, vocab, width))
+        self._check(self.lib.goom_embedding_backward(self._ctx, _at(tokens), _at(grad), out.data_ptr(), n, vocab, width, _real_code(grad), _real_code(out), scale,
+                                                     _at(ws), wsn))
         return out

@@ -16,6 +16,7 @@
 // accumulators of the matrix instruction for the whole walk; the rows of the tiles are numbered such that a lane's
 // accumulator entries are eight consecutive ones of the contraction (rows or tokens), so that the state and P turn into
 // operands of the next product without moving between lanes.  P is shared out over the waves by rows and passed through LDS.
+#include <atomic>
 #include <cmath>
 
 #include "goom_real.h"
@@ -131,7 +132,7 @@ template <> struct Operand<bf16> {
     // Computed operands are split into bf16 parts: two (16 bits) for P and the state where outputs, rounded to 8 bits, are
     // formed from them, three (24 bits) for what is summed into the float states.
     static constexpr int OUT_PARTS = 2, STATE_PARTS = 3;
-    static constexpr int PITCH_PAD = 16;
+    static constexpr int PITCH_PAD = 8;
 };
 template <> struct Operand<float> {
     typedef f32x8 Frag;
@@ -719,6 +720,16 @@ static size_t totals_bytes(const goom_attention_shape &sh, const Segments &g, in
     return goom::align_up((size_t)(g.slots * sh.heads) * padded_head(ka) * padded_head(nc) * 4, 256);
 }
 
+// lets a kernel have `bytes` of dynamic LDS, once a device (`done`: one flag for each kernel)
+static int allow_lds(goom_ctx *ctx, const void *kernel, size_t bytes, std::atomic<unsigned long long> &done)
+{
+    const unsigned long long bit = 1ull << (ctx->device & 63);
+    if (ctx->device < 64 && (done.load(std::memory_order_relaxed) & bit)) return GOOM_OK;
+    if (int st = goom::check_hip(ctx, hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes), "hipFuncSetAttribute")) return st;
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return GOOM_OK;
+}
+
 template <typename S, int DK, int DV> static int launch_walks_sized(goom_ctx *ctx, WalkArgs w, int roles, long long slots, const char *label)
 {
     typedef typename Compute<S>::type E;
@@ -730,7 +741,8 @@ template <typename S, int DK, int DV> static int launch_walks_sized(goom_ctx *ct
     if (parts) {
         auto *totals = walk_kernel<S, DK, DV, NW, false>;
         constexpr size_t bytes = WalkLds<E, DK, DV, NW, false>::bytes;
-        if (int st = goom::check_hip(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(totals), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes), "hipFuncSetAttribute")) return st;
+        static std::atomic<unsigned long long> done{0};
+        if (int st = allow_lds(ctx, reinterpret_cast<const void *>(totals), bytes, done)) return st;
         goom::prof_begin(ctx, "linear attention: segment totals");
         totals<<<grid, NW * 64, bytes, ctx->stream>>>(w);
         goom::prof_end(ctx);
@@ -740,7 +752,8 @@ template <typename S, int DK, int DV> static int launch_walks_sized(goom_ctx *ct
     }
     auto *walk = walk_kernel<S, DK, DV, NW, true>;
     constexpr size_t bytes = WalkLds<E, DK, DV, NW, true>::bytes;
-    if (int st = goom::check_hip(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(walk), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes), "hipFuncSetAttribute")) return st;
+    static std::atomic<unsigned long long> done{0};
+    if (int st = allow_lds(ctx, reinterpret_cast<const void *>(walk), bytes, done)) return st;
     goom::prof_begin(ctx, label);
     walk<<<grid, NW * 64, bytes, ctx->stream>>>(w);
     goom::prof_end(ctx);

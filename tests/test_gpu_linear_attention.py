@@ -197,7 +197,7 @@ def test_final_state_may_replace_the_first(g):
     import ctypes as C
     q, k, v, _, ld, s0, _ = (x.cuda() for x in _inputs("bf16", 1500, 2, 2, 64, 64, 1, 9))
     o, last = g.linear_attention(q[None], k[None], v[None], ld, state=s0, want_state=True)
-    shape, pq, pk, pv = g._attention(q, k, v, ld, None, 1.0, q.shape[:-2])
+    shape, pq, pk, pv = g._attention(q[None], k[None], v[None], ld, None, 1.0)
     need = g.lib.goom_linear_attention_workspace_bytes(C.byref(shape), 0)
     assert need > 0  # one sequence of two heads is cut into segments
     ws = torch.empty(need, dtype=torch.uint8, device="cuda")
