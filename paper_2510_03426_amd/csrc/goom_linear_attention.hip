@@ -23,20 +23,11 @@
 
 namespace goom_layer {
 
-#ifndef LA_RES
-#define LA_RES (sh.dk > 64 || sh.dv > 64 ? 2 : 3)
-#endif
-#ifndef LA_NW32
-#define LA_NW32 4
+#ifndef LA_PK
+#define LA_PK 2
 #endif
 #ifndef LA_EARLY
 #define LA_EARLY (!OUT)
-#endif
-#ifndef LA_OCC
-#define LA_OCC 1
-#endif
-#ifndef LA_NW
-#define LA_NW 4
 #endif
 constexpr int CHUNK = 64; // tokens; the pairs of a chunk cost 64 (ka + nc) multiplications a token, the state 2 ka nc
 
@@ -61,7 +52,7 @@ struct WalkArgs {
     const float *log_decay;
     const int64_t *offsets;
     long long tokens, seqs, seq_len, seg_len, segs; // without offsets: seq_len tokens and segs segments a sequence
-    int heads, roles;
+    int heads, roles, parts; // parts: column parts of DV columns
     unsigned slots;
 };
 
@@ -125,26 +116,26 @@ __device__ inline float log2_decay(float log_decay)
 // g^x for whole x >= 0
 __device__ inline float decay_power(float g2, int x) { return __builtin_amdgcn_exp2f(g2 * (float)x); }
 
-// ---- operands: eight consecutive entries of the contraction per lane (lane / 16 picks which eight of 32)
-template <typename E> struct Operand;
-template <> struct Operand<bf16> {
-    typedef bf16x8 Frag;
-    // Computed operands are split into bf16 parts: two (16 bits) for P and the state where outputs, rounded to 8 bits, are
-    // formed from them, three (24 bits) for what is summed into the float states.
-    static constexpr int OUT_PARTS = 2, STATE_PARTS = 3;
-    static constexpr int PITCH_PAD = 8;
-};
-template <> struct Operand<float> {
-    typedef f32x8 Frag;
-    static constexpr int OUT_PARTS = 1, STATE_PARTS = 1;
-    static constexpr int PITCH_PAD = 4;
-};
+// ---- operands: eight consecutive entries of the contraction per lane (lane / 16 picks which eight of 32), as sums of bf16
+// parts, each 8 bits further down.  Inputs are held exactly: one part for bfloat16, two for halves (11 bits, and products and
+// states of halves may leave their range), three for floats.  Computed operands are split into as many as their result
+// needs: OUT for P and the state where outputs are formed from them, three where they enter a float state.  Of a product of
+// parts i and j those with i + j up to the number of parts matter.  (On floats' own matrix instruction a product takes eight
+// instructions of 32 cycles; six of 16 cycles here.)
+typedef bf16x8 Frag;
+template <typename S> struct Parts;
+template <> struct Parts<bf16> { static constexpr int IN = 1, OUT = 2, STATE = 3; };
+template <> struct Parts<f16> { static constexpr int IN = 2, OUT = 2, STATE = 3; };
+template <> struct Parts<float> { static constexpr int IN = 3, OUT = 3, STATE = 3; };
+constexpr int PITCH_PAD = 8;
 
-__device__ inline f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-__device__ inline f32x4 mma(f32x8 a, f32x8 b, f32x4 c)
+template <int LIMIT, int NA, int NB> __device__ inline f32x4 product(const Frag (&a)[NA], const Frag (&b)[NB], f32x4 c)
 {
 #pragma unroll
-    for (int e = 0; e < 8; e++) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+    for (int i = 0; i < NA; i++)
+#pragma unroll
+        for (int j = 0; j < NB; j++)
+            if (i + j < LIMIT) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], c, 0, 0, 0);
     return c;
 }
 
@@ -170,7 +161,6 @@ template <int N> __device__ inline void split(f32x8 x, bf16x8 (&p)[N])
         p[i] = __builtin_bit_cast(bf16x8, w);
     }
 }
-template <int N> __device__ inline void split(f32x8 x, f32x8 (&p)[N]) { p[0] = x; }
 
 __device__ inline f32x8 widen(bf16x8 x)
 {
@@ -178,36 +168,40 @@ __device__ inline f32x8 widen(bf16x8 x)
     const u32x4 w = __builtin_bit_cast(u32x4, x);
     return f32x8{low_half(w[0]), high_half(w[0]), low_half(w[1]), high_half(w[1]), low_half(w[2]), high_half(w[2]), low_half(w[3]), high_half(w[3])};
 }
-__device__ inline f32x8 widen(f32x8 x) { return x; }
-
-// eight entries of one row
-__device__ inline bf16x8 row_frag(const bf16 *p) { return *reinterpret_cast<const bf16x8 *>(p); }
-__device__ inline f32x8 row_frag(const float *p)
+template <int N> __device__ inline f32x8 widen(const Frag (&p)[N])
 {
-    const f32x4 lo = *reinterpret_cast<const f32x4 *>(p), hi = *reinterpret_cast<const f32x4 *>(p + 4);
-    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    f32x8 x = widen(p[N - 1]);
+#pragma unroll
+    for (int i = N - 2; i >= 0; i--) x += widen(p[i]);
+    return x;
+}
+
+// eight entries of one row; `plane` elements between the parts
+template <int N> __device__ inline void row_frag(Frag (&x)[N], const bf16 *p, int plane)
+{
+#pragma unroll
+    for (int k = 0; k < N; k++) x[k] = *reinterpret_cast<const Frag *>(p + k * plane);
 }
 
 // rows t0 + 8 (lane / 16) + 0 .. 7 of one column: column c0 + (i / 4) cs + i % 4 for i = lane % 16
-template <int PITCH> __device__ inline bf16x8 col_frag(const bf16 *tile, int t0, int c0, int cs, int lane)
+template <int PITCH, int N> __device__ inline void col_frag(Frag (&x)[N], const bf16 *tile, int t0, int c0, int cs, int lane)
 {
     // the transposing read: of each 16 lanes, lane s gives the address of four columns of row s / 4, and lane i gets
     // the four rows of column i
     const int s = lane & 15, row = t0 + (lane >> 4) * 8 + (s >> 2), col = c0 + (s & 3) * cs;
     typedef __attribute__((address_space(3))) s16x4 *lds;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(tile + row * PITCH + col));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(tile + (row + 4) * PITCH + col));
-    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-}
-template <int PITCH> __device__ inline f32x8 col_frag(const float *tile, int t0, int c0, int cs, int lane)
-{
-    const int i = lane & 15;
-    const float *p = tile + (t0 + (lane >> 4) * 8) * PITCH + c0 + (i >> 2) * cs + (i & 3);
-    f32x8 x;
 #pragma unroll
-    for (int e = 0; e < 8; e++) x[e] = p[e * PITCH];
-    return x;
+    for (int k = 0; k < N; k++) {
+        const bf16 *const p = tile + k * CHUNK * PITCH + row * PITCH + col;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(p + 4 * PITCH));
+        x[k] = __builtin_bit_cast(Frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
 }
+
+// eight elements of a type into parts
+__device__ inline void split_in(bf16x8 v, Frag (&p)[1]) { p[0] = v; }
+__device__ inline void split_in(f16x8 v, Frag (&p)[2]) { split(__builtin_convertvector(v, f32x8), p); }
+__device__ inline void split_in(f32x8 v, Frag (&p)[3]) { split(v, p); }
 
 // Rows 0 .. n-1 of `d` entries, on their way from memory into a tile of 64 rows of D entries with zeros elsewhere: fetched into
 // registers, all loads in flight at once (rows and columns that are not there are read from ones that are), and put into LDS
@@ -241,30 +235,25 @@ template <typename S, int D, int THREADS> struct Rows64 {
             }
         }
     }
-    template <typename E, int PITCH> __device__ inline void put(E *tile, int n, int d) const
+    template <int PITCH> __device__ inline void put(bf16 *tile, int n, int d) const
     {
-        typedef typename Vec<E, 8>::type EV;
         const bool there = col0() < d;
-        E *const to0 = tile + row0() * PITCH + col0();
+        bf16 *const to0 = tile + row0() * PITCH + col0();
 #pragma unroll
         for (int k = 0; k < N; k++) {
-            EV v = __builtin_convertvector(x[k], EV);
-            if (!there || (n != CHUNK && row0() + k * STEP >= n)) v = EV{};
-            if (UNITS % THREADS == 0 || row0() + k * STEP < CHUNK) {
-                E *const to = to0 + k * STEP * PITCH;
-                if constexpr (sizeof(E) == 2) {
-                    *reinterpret_cast<EV *>(to) = v;
-                } else {
-                    *reinterpret_cast<f32x4 *>(to) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
-                    *reinterpret_cast<f32x4 *>(to + 4) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
-                }
-            }
+            SV v = x[k];
+            if (!there || (n != CHUNK && row0() + k * STEP >= n)) v = SV{};
+            Frag p[Parts<S>::IN];
+            split_in(v, p);
+#pragma unroll
+            for (int q = 0; q < Parts<S>::IN; q++)
+                if (UNITS % THREADS == 0 || row0() + k * STEP < CHUNK) *reinterpret_cast<Frag *>(to0 + (q * CHUNK + k * STEP) * PITCH) = p[q];
         }
     }
 };
 
 // the same for rows whose vectors are not aligned: straight into LDS, element by element
-template <typename E, typename S, int D, int PITCH, int THREADS> __device__ inline void stage_elements(E *tile, const S *src, long long stride, int n, int d)
+template <typename S, int D, int PITCH, int THREADS> __device__ inline void stage_elements(bf16 *tile, const S *src, long long stride, int n, int d)
 {
 #pragma unroll 1
     for (int u0 = threadIdx.x; u0 < CHUNK * D; u0 += 16 * THREADS) {
@@ -277,42 +266,46 @@ template <typename E, typename S, int D, int PITCH, int THREADS> __device__ inli
 #pragma unroll
         for (int k = 0; k < 16; k++) {
             const int u = u0 + k * THREADS, row = u / D, col = u % D;
-            if (u < CHUNK * D) tile[row * PITCH + col] = row < n && col < d ? (E)x[k] : (E)0.0f;
+            float v = row < n && col < d ? (float)x[k] : 0.0f;
+#pragma unroll
+            for (int q = 0; q < Parts<S>::IN; q++) {
+                const bf16 part = (bf16)v;
+                v -= (float)part;
+                if (u < CHUNK * D) tile[(q * CHUNK + row) * PITCH + col] = part;
+            }
         }
     }
 }
 
-// element type in LDS and registers: bf16 for bf16; halves are widened to floats (products of halves and states of their
-// magnitudes leave the range of halves)
-template <typename S> struct Compute { typedef float type; };
-template <> struct Compute<bf16> { typedef bf16 type; };
-
-template <typename E, int DK, int DV, int NW, bool OUT> struct WalkLds {
-    static constexpr int PK = DK + Operand<E>::PITCH_PAD, PV = DV + Operand<E>::PITCH_PAD;
-    static constexpr int ROWS = CHUNK * PK * (OUT ? 2 : 1) + CHUNK * PV; // elements
-    static constexpr int P_FRAGS = OUT ? 8 * Operand<E>::OUT_PARTS * 64 : 0;
-    static constexpr size_t bytes = ROWS * sizeof(E) + P_FRAGS * sizeof(typename Operand<E>::Frag);
+template <typename S, int DK, int DV, int NW, bool OUT> struct WalkLds {
+    static constexpr int PK = DK + PITCH_PAD, PV = DV + PITCH_PAD;
+    static constexpr int K_TILE = CHUNK * PK * Parts<S>::IN, V_TILE = CHUNK * PV * Parts<S>::IN; // elements
+    static constexpr int P_FRAGS = OUT ? 6 * Parts<S>::OUT * 64 : 0; // the six 16 x 32 blocks of P with pairs in them
+    static constexpr size_t bytes = (K_TILE * (OUT ? 2 : 1) + V_TILE) * sizeof(bf16) + P_FRAGS * sizeof(Frag);
     // workgroups of a CU: as many as its LDS holds, and no more than leave their waves the registers for the state (DK DV / 64 NW
-    // a lane), the outputs and the rows on their way
-    static constexpr int fit = (int)((160 << 10) / bytes), most = DK * DV / (64 * NW) * (int)sizeof(E) / 2 > 32 ? 2 : 3;
+    // a lane), the outputs and the rows on their way: three waves a SIMD with 168 each, or two with 256
+    static constexpr int waves = DK * DV / (64 * NW) > 16 ? 2 : 3;
+    static constexpr int fit = (int)((160 << 10) / bytes), most = waves * 4 / NW;
     static constexpr int resident = fit < 1 ? 1 : fit > most ? most : fit;
+    static constexpr int per_simd = resident * NW / 4 > 0 ? resident * NW / 4 : 1;
 };
 
-// DK, DV: ka and nc, padded; NW waves of NT tiles of 16 columns each
+// which of the six blocks of P: rows 16 it on, columns 32 ks on
+template <bool REV> __device__ constexpr int p_block(int it, int ks) { return REV ? (it < 2 ? it * 2 + ks : it + 2) : (it < 2 ? it : it * 2 - 2 + ks); }
+
+// DK, DV: ka and nc (of one of `parts` column parts), padded; NW waves of NT tiles of 16 columns each
 template <typename S, int DK, int DV, int NW, bool OUT, bool REV>
-__device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &at, long long slot, int h, unsigned char *lds)
+__device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &at, long long slot, int h, int part, unsigned char *lds)
 {
-    typedef typename Compute<S>::type E;
-    typedef Operand<E> Op;
-    typedef typename Op::Frag Frag;
-    typedef WalkLds<E, DK, DV, NW, OUT> Lds;
+    typedef WalkLds<S, DK, DV, NW, OUT> Lds;
     constexpr int THREADS = NW * 64, NT = DV / 16 / NW, KS = DK / 32, CS = NT == 2 ? 8 : 4;
-    constexpr int OP = Op::OUT_PARTS, SP = Op::STATE_PARTS;
+    constexpr int IP = Parts<S>::IN, OP = Parts<S>::OUT, SP = Parts<S>::STATE;
+    constexpr int KP = CHUNK * Lds::PK; // elements from part to part
     static_assert(NT == 1 || NT == 2, "a wave has one or two column tiles");
     Frag *const p_lds = reinterpret_cast<Frag *>(lds);
-    E *const b_lds = reinterpret_cast<E *>(p_lds + Lds::P_FRAGS);
-    E *const c_lds = b_lds + CHUNK * Lds::PK;
-    E *const a_lds = c_lds + CHUNK * Lds::PV;
+    bf16 *const b_lds = reinterpret_cast<bf16 *>(p_lds + Lds::P_FRAGS);
+    bf16 *const c_lds = b_lds + Lds::K_TILE;
+    bf16 *const a_lds = c_lds + Lds::V_TILE;
 
     const bool last = REV ? at.seg == 0 : at.seg == at.nseg - 1; // in walking order
     if (!OUT && last) return;
@@ -322,8 +315,9 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
 
     // ---- the incoming state
     f32x4 R[DK / 16][NT];
-    float *const total = r.totals ? r.totals + (slot * w.heads + h) * (long long)(DK * DV) + (long long)wave * NT * (DK / 16) * 256 + lane * 4 : nullptr;
-    const long long state0 = (at.seq * w.heads + h) * (long long)r.ka * r.nc;
+    float *const total = r.totals ? r.totals + ((slot * w.heads + h) * w.parts + part) * (long long)(DK * DV) + (long long)wave * NT * (DK / 16) * 256 + lane * 4 : nullptr;
+    const int nc = r.nc - part * DV < DV ? r.nc - part * DV : DV;
+    const long long state0 = (at.seq * w.heads + h) * (long long)r.ka * r.nc + (long long)part * DV * r.state_col;
     const bool empty = at.len == 0;
 #pragma unroll
     for (int t = 0; t < DK / 16; t++)
@@ -338,7 +332,7 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
                     const int row = t / 2 * 32 + g * 8 + t % 2 * 4 + e;
-                    if (row < r.ka && col < r.nc) x[e] = scale * r.init[state0 + (long long)row * r.state_row + (long long)col * r.state_col];
+                    if (row < r.ka && col < nc) x[e] = scale * r.init[state0 + (long long)row * r.state_row + (long long)col * r.state_col];
                 }
             }
             R[t][nt] = x;
@@ -346,7 +340,7 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
 
     const S *const a = reinterpret_cast<const S *>(r.a) + at.start * r.a_tok + h / r.a_group * r.a_head;
     const S *const b = reinterpret_cast<const S *>(r.b) + at.start * r.b_tok + h / r.b_group * r.b_head;
-    const S *const c = reinterpret_cast<const S *>(r.c) + at.start * r.c_tok + h / r.c_group * r.c_head;
+    const S *const c = reinterpret_cast<const S *>(r.c) + at.start * r.c_tok + h / r.c_group * r.c_head + part * DV;
     const long long seg0 = at.seg * w.seg_len, seg1 = seg0 + w.seg_len < at.len ? seg0 + w.seg_len : at.len;
     const int nchunks = (int)((seg1 - seg0 + CHUNK - 1) / CHUNK);
     const bool a_vec = r.a_vec, b_vec = r.b_vec, c_vec = r.c_vec;
@@ -359,7 +353,7 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
         const int n = chunk_rows(t0);
         if (OUT && a_vec) ax.fetch(a + t0 * r.a_tok, r.a_tok, n, r.ka);
         if (b_vec) bx.fetch(b + t0 * r.b_tok, r.b_tok, n, r.ka);
-        if (c_vec) cx.fetch(c + t0 * r.c_tok, r.c_tok, n, r.nc);
+        if (c_vec) cx.fetch(c + t0 * r.c_tok, r.c_tok, n, nc);
     };
     constexpr bool EARLY = LA_EARLY;
     if (EARLY && nchunks > 0) fetch(0);
@@ -371,13 +365,13 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
         __syncthreads();
         if (!EARLY) fetch(step);
         if (OUT) {
-            if (a_vec) ax.template put<E, Lds::PK>(a_lds, n, r.ka);
-            else stage_elements<E, S, DK, Lds::PK, THREADS>(a_lds, a + t0 * r.a_tok, r.a_tok, n, r.ka);
+            if (a_vec) ax.template put<Lds::PK>(a_lds, n, r.ka);
+            else stage_elements<S, DK, Lds::PK, THREADS>(a_lds, a + t0 * r.a_tok, r.a_tok, n, r.ka);
         }
-        if (b_vec) bx.template put<E, Lds::PK>(b_lds, n, r.ka);
-        else stage_elements<E, S, DK, Lds::PK, THREADS>(b_lds, b + t0 * r.b_tok, r.b_tok, n, r.ka);
-        if (c_vec) cx.template put<E, Lds::PV>(c_lds, n, r.nc);
-        else stage_elements<E, S, DV, Lds::PV, THREADS>(c_lds, c + t0 * r.c_tok, r.c_tok, n, r.nc);
+        if (b_vec) bx.template put<Lds::PK>(b_lds, n, r.ka);
+        else stage_elements<S, DK, Lds::PK, THREADS>(b_lds, b + t0 * r.b_tok, r.b_tok, n, r.ka);
+        if (c_vec) cx.template put<Lds::PV>(c_lds, n, nc);
+        else stage_elements<S, DV, Lds::PV, THREADS>(c_lds, c + t0 * r.c_tok, r.c_tok, n, nc);
         __syncthreads();
         if (EARLY && step + 1 < nchunks) fetch(step + 1); // while this chunk is worked on
 
@@ -388,13 +382,16 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
                 for (int ks = 0; ks < 2; ks++) {
                     if (REV ? ks < it / 2 : ks > it / 2) continue; // no pair in this half
                     f32x4 p0 = {0, 0, 0, 0}, p1 = {0, 0, 0, 0};
-                    const E *const arow = a_lds + (it * 16 + i) * Lds::PK + g * 8;
-                    const E *const brow = b_lds + (ks * 32 + (i >> 2) * 8 + (i & 3)) * Lds::PK + g * 8;
+                    const bf16 *const arow = a_lds + (it * 16 + i) * Lds::PK + g * 8;
+                    const bf16 *const brow = b_lds + (ks * 32 + (i >> 2) * 8 + (i & 3)) * Lds::PK + g * 8;
 #pragma unroll
                     for (int kk = 0; kk < KS; kk++) {
-                        const Frag af = row_frag(arow + kk * 32);
-                        p0 = mma(row_frag(brow + kk * 32), af, p0);
-                        p1 = mma(row_frag(brow + 4 * Lds::PK + kk * 32), af, p1);
+                        Frag af[IP], b0[IP], b1[IP];
+                        row_frag(af, arow + kk * 32, KP);
+                        row_frag(b0, brow + kk * 32, KP);
+                        row_frag(b1, brow + 4 * Lds::PK + kk * 32, KP);
+                        p0 = product<3>(b0, af, p0);
+                        p1 = product<3>(b1, af, p1);
                     }
                     f32x8 x;
                     int first = it * 16 + i - ks * 32 - g * 8; // i - j of the lane's first j
@@ -408,18 +405,18 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
                     Frag parts[OP];
                     split(x, parts);
 #pragma unroll
-                    for (int q = 0; q < OP; q++) p_lds[((it * 2 + ks) * OP + q) * 64 + lane] = parts[q];
+                    for (int q = 0; q < OP; q++) p_lds[(p_block<REV>(it, ks) * OP + q) * 64 + lane] = parts[q];
                 }
             }
             __syncthreads();
         }
 
-        Frag cf[2][NT];
+        Frag cf[2][NT][IP];
         auto load_columns = [&] {
 #pragma unroll
             for (int ks = 0; ks < 2; ks++)
 #pragma unroll
-                for (int nt = 0; nt < NT; nt++) cf[ks][nt] = col_frag<Lds::PV>(c_lds, ks * 32, col0 + 4 * nt, CS, lane);
+                for (int nt = 0; nt < NT; nt++) col_frag<Lds::PV>(cf[ks][nt], c_lds, ks * 32, col0 + 4 * nt, CS, lane);
         };
         if (!OUT) load_columns();
         if (OUT) {
@@ -429,27 +426,29 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
             for (int it = 0; it < 4; it++)
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++) y[it][nt] = f32x4{0, 0, 0, 0};
-            // operands are read one step ahead of their products, and no further: registers are what the walk is short of
-            Frag af[2][4];
-            const E *const a0 = a_lds + i * Lds::PK + g * 8;
+            if (step > 0 || total || r.init) {
+                // operands are read one step ahead of their products, and no further: registers are what the walk is short of
+                constexpr int AHEAD = IP == 1 ? 2 : 1;
+                Frag af[AHEAD][4][IP];
+                const bf16 *const a0 = a_lds + i * Lds::PK + g * 8;
+                auto load_rows = [&](int kk) {
 #pragma unroll
-            for (int it = 0; it < 4; it++) af[0][it] = row_frag(a0 + it * 16 * Lds::PK);
+                    for (int it = 0; it < 4; it++) row_frag(af[kk % AHEAD][it], a0 + it * 16 * Lds::PK + kk * 32, KP);
+                };
+                if (AHEAD > 1) load_rows(0);
 #pragma unroll
-            for (int kk = 0; kk < KS; kk++) {
-                if (kk + 1 < KS) {
+                for (int kk = 0; kk < KS; kk++) {
+                    if (AHEAD == 1) load_rows(kk);
+                    else if (kk + 1 < KS) load_rows(kk + 1);
+                    Frag rf[NT][OP];
 #pragma unroll
-                    for (int it = 0; it < 4; it++) af[(kk + 1) & 1][it] = row_frag(a0 + it * 16 * Lds::PK + (kk + 1) * 32);
+                    for (int nt = 0; nt < NT; nt++) split(__builtin_shufflevector(R[2 * kk][nt], R[2 * kk + 1][nt], 0, 1, 2, 3, 4, 5, 6, 7), rf[nt]);
+#pragma unroll
+                    for (int it = 0; it < 4; it++)
+#pragma unroll
+                        for (int nt = 0; nt < NT; nt++) y[it][nt] = product<OP>(rf[nt], af[kk % AHEAD][it], y[it][nt]);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                Frag rf[NT][OP];
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++) split(__builtin_shufflevector(R[2 * kk][nt], R[2 * kk + 1][nt], 0, 1, 2, 3, 4, 5, 6, 7), rf[nt]);
-#pragma unroll
-                for (int it = 0; it < 4; it++)
-#pragma unroll
-                    for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                        for (int q = 0; q < OP; q++) y[it][nt] = mma(rf[nt][q], af[kk & 1][it], y[it][nt]);
-                __builtin_amdgcn_sched_barrier(0);
             }
             load_columns();
 #pragma unroll
@@ -461,27 +460,26 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
 #pragma unroll
                 for (int ks = 0; ks < 2; ks++) {
                     if (REV ? ks < it / 2 : ks > it / 2) continue;
+                    Frag pf[OP];
 #pragma unroll
-                    for (int q = 0; q < OP; q++) {
-                        const Frag pf = p_lds[((it * 2 + ks) * OP + q) * 64 + lane];
+                    for (int q = 0; q < OP; q++) pf[q] = p_lds[(p_block<REV>(it, ks) * OP + q) * 64 + lane];
 #pragma unroll
-                        for (int nt = 0; nt < NT; nt++) y[it][nt] = mma(cf[ks][nt], pf, y[it][nt]);
-                    }
+                    for (int nt = 0; nt < NT; nt++) y[it][nt] = product<OP>(cf[ks][nt], pf, y[it][nt]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 if (row < n) {
-                    const long long to = (at.start + t0 + row) * r.y_tok + h * r.y_head;
+                    const long long to = (at.start + t0 + row) * r.y_tok + h * r.y_head + part * DV;
                     const int col = col0 + g * CS;
                     float x[NT * 4];
 #pragma unroll
                     for (int e = 0; e < NT * 4; e++) x[e] = y[it][e / 4][e % 4];
-                    if (r.y_vec && col + NT * 4 <= r.nc) {
+                    if (r.y_vec && col + NT * 4 <= nc) {
                         if (r.y_float) store_floats<float, NT * 4>(reinterpret_cast<float *>(r.y) + to + col, x);
                         else store_floats<S, NT * 4>(reinterpret_cast<S *>(r.y) + to + col, x);
                     } else {
 #pragma unroll
                         for (int e = 0; e < NT * 4; e++)
-                            if (col + e < r.nc) {
+                            if (col + e < nc) {
                                 if (r.y_float) reinterpret_cast<float *>(r.y)[to + col + e] = x[e];
                                 else reinterpret_cast<S *>(r.y)[to + col + e] = (S)x[e];
                             }
@@ -490,6 +488,7 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
             }
         }
 
+        if (OUT && step == nchunks - 1 && !(last && r.fin)) break; // nobody needs the next state
         // ---- the next state; after the last token of a forward walk the final state, one decay short of the next chunk's
         const int ahead = !REV && last && r.fin && step == nchunks - 1 ? 1 : 0;
         const float whole = decay_power(g2, n - ahead);
@@ -512,15 +511,16 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
             Frag cd[NT][SP];
 #pragma unroll
             for (int nt = 0; nt < NT; nt++) split(widen(cf[ks][nt]) * wt, cd[nt]);
-            Frag bf[2];
-            bf[0] = col_frag<Lds::PK>(b_lds, ks * 32, 0, 8, lane);
+            constexpr int AHEAD = IP == 1 ? 2 : 1;
+            Frag bf[AHEAD][IP];
+            auto load_rows = [&](int t) { col_frag<Lds::PK>(bf[t % AHEAD], b_lds, ks * 32, t / 2 * 32 + t % 2 * 4, 8, lane); };
+            if (AHEAD > 1) load_rows(0);
 #pragma unroll
             for (int t = 0; t < DK / 16; t++) {
-                if (t + 1 < DK / 16) bf[(t + 1) & 1] = col_frag<Lds::PK>(b_lds, ks * 32, (t + 1) / 2 * 32 + (t + 1) % 2 * 4, 8, lane);
+                if (AHEAD == 1) load_rows(t);
+                else if (t + 1 < DK / 16) load_rows(t + 1);
 #pragma unroll
-                for (int q = 0; q < SP; q++)
-#pragma unroll
-                    for (int nt = 0; nt < NT; nt++) R[t][nt] = mma(bf[t & 1], cd[nt][q], R[t][nt]);
+                for (int nt = 0; nt < NT; nt++) R[t][nt] = product<SP>(bf[t % AHEAD], cd[nt], R[t][nt]);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -538,39 +538,41 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
 #pragma unroll
                     for (int e = 0; e < 4; e++) {
                         const int row = t / 2 * 32 + g * 8 + t % 2 * 4 + e;
-                        if (row < r.ka && col < r.nc) r.fin[state0 + (long long)row * r.state_row + (long long)col * r.state_col] = R[t][nt][e];
+                        if (row < r.ka && col < nc) r.fin[state0 + (long long)row * r.state_row + (long long)col * r.state_col] = R[t][nt][e];
                     }
                 }
             }
     }
 }
 
-// grid: slots heads roles; the roles of a head and segment run on one XCD (of 8, dealt round robin), whose L2 has the rows they share
+// grid: slots heads parts roles; the roles of a head and segment run on one XCD (of 8, dealt round robin), whose L2 has the rows
+// they share
 template <typename S, int DK, int DV, int NW, bool OUT>
-__global__ __launch_bounds__(NW * 64, (WalkLds<typename Compute<S>::type, DK, DV, NW, OUT>::resident * NW / 4)) void walk_kernel(WalkArgs w)
+__global__ __launch_bounds__(NW * 64, (WalkLds<S, DK, DV, NW, OUT>::per_simd)) void walk_kernel(WalkArgs w)
 {
     extern __shared__ __align__(16) unsigned char lds[];
     const unsigned group = blockIdx.x / (8 * w.roles), in = blockIdx.x % (8 * w.roles);
     const unsigned item = group * 8 + in % 8;
-    if (item >= w.slots * w.heads) return;
+    if (item >= w.slots * w.heads * w.parts) return;
     const WalkRole &r = w.role[in / 8];
-    const long long slot = item / w.heads;
-    const int h = item % w.heads;
+    const int part = item % w.parts, h = item / w.parts % w.heads;
+    const long long slot = item / w.parts / w.heads;
     const Place at = find_place(w, slot);
     if (at.seg >= at.nseg) return;
-    if (r.reverse) walk<S, DK, DV, NW, OUT, true>(w, r, at, slot, h, lds);
-    else walk<S, DK, DV, NW, OUT, false>(w, r, at, slot, h, lds);
+    if (r.reverse) walk<S, DK, DV, NW, OUT, true>(w, r, at, slot, h, part, lds);
+    else walk<S, DK, DV, NW, OUT, false>(w, r, at, slot, h, part, lds);
 }
 
 // Segment totals -> incoming states, in place, in walking order: a thread has four entries of one head's state and goes
-// through the segments of one sequence.  grid: (seqs heads times a part of 1024 entries, 1, roles)
+// through the segments of one sequence.  grid: (seqs heads parts times a group of 1024 entries, 1, roles)
 template <int DK, int DV, int NW> __global__ __launch_bounds__(256) void carry_kernel(WalkArgs w)
 {
     constexpr int NT = DV / 16 / NW, CS = NT == 2 ? 8 : 4;
     const WalkRole &r = w.role[blockIdx.z];
-    constexpr int PARTS = DK * DV / 1024;
-    const long long s = blockIdx.x / PARTS / w.heads;
-    const int h = blockIdx.x / PARTS % w.heads, u = blockIdx.x % PARTS * 256 + threadIdx.x;
+    constexpr int GROUPS = DK * DV / 1024;
+    const unsigned item = blockIdx.x / GROUPS;
+    const long long s = item / w.parts / w.heads;
+    const int part = item % w.parts, h = item / w.parts % w.heads, u = blockIdx.x % GROUPS * 256 + threadIdx.x;
     long long start, len;
     span(w, s, start, len);
     const long long nseg = len > 0 ? (len + w.seg_len - 1) / w.seg_len : 1;
@@ -579,14 +581,14 @@ template <int DK, int DV, int NW> __global__ __launch_bounds__(256) void carry_k
     f32x4 x = {0, 0, 0, 0};
     if (r.init) {
         const float scale = r.reverse ? 1.0f : decay_power(g2, 1);
-        const int col = wave * NT * 16 + (i >> 2) * CS + 4 * nt + (i & 3);
+        const int col = part * DV + wave * NT * 16 + (i >> 2) * CS + 4 * nt + (i & 3);
         for (int e = 0; e < 4; e++) {
             const int row = t / 2 * 32 + (lane >> 4) * 8 + t % 2 * 4 + e;
             if (row < r.ka && col < r.nc) x[e] = scale * r.init[(s * w.heads + h) * (long long)r.ka * r.nc + (long long)row * r.state_row + (long long)col * r.state_col];
         }
     }
-    f32x4 *const tot = reinterpret_cast<f32x4 *>(r.totals) + (first_slot(w, s) * w.heads + h) * (long long)(DK * DV / 4) + u;
-    const long long stride = (long long)w.heads * (DK * DV / 4);
+    f32x4 *const tot = reinterpret_cast<f32x4 *>(r.totals) + ((first_slot(w, s) * w.heads + h) * w.parts + part) * (long long)(DK * DV / 4) + u;
+    const long long stride = (long long)w.heads * w.parts * (DK * DV / 4);
     const float whole = decay_power(g2, (int)w.seg_len);
     const float first = r.reverse ? decay_power(g2, (int)(len - (nseg - 1) * w.seg_len)) : whole; // a sequence's last segment may be shorter
     const long long dir = r.reverse ? -1 : 1, at = r.reverse ? nseg - 1 : 0;
@@ -689,12 +691,35 @@ template <typename S, bool VEC> __global__ __launch_bounds__(256) void step_kern
 
 static int padded_head(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
 
+// f(element type, DK, DV, NW): the walk's kernel for rows of ka and columns of nc entries
+template <typename F> static auto with_walk(int type, int ka, int nc, F f)
+{
+    return with_type(type, [&](auto tag) {
+        typedef typename decltype(tag)::type S;
+        constexpr int IN = Parts<S>::IN;
+        auto columns = [&](auto rows) {
+            constexpr int DK = decltype(rows)::value;
+            if (nc <= 32) return f(tag, rows, std::integral_constant<int, 32>(), std::integral_constant<int, 2>());
+            // floats' three parts of 128 x 128 do not fit LDS: two halves of the columns
+            if constexpr (DK == 128 && IN == 3) return f(tag, rows, std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
+            else if (nc <= 64) return f(tag, rows, std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
+            // waves: each with two column tiles where two workgroups share a CU, with one (more waves) where LDS holds but one
+            else return f(tag, rows, std::integral_constant<int, 128>(), std::integral_constant<int, IN == 1 ? 4 : 8>());
+        };
+        return ka <= 32 ? columns(std::integral_constant<int, 32>()) : ka <= 64 ? columns(std::integral_constant<int, 64>()) : columns(std::integral_constant<int, 128>());
+    });
+}
+
 // Segments: how long, and how many slots there are in all.
 struct Segments { long long len, slots, per_seq; };
 
 static Segments choose_segments(const goom_attention_shape &sh, int roles, bool packed)
 {
-    const long long walks = sh.seqs * sh.heads * roles, round = 256 * LA_RES, mean = sh.seqs > 0 ? (sh.tokens + sh.seqs - 1) / sh.seqs : 0;
+    // As many walks as the chip holds at once: more would start a second round, fewer leave CUs idle
+    const long long resident = with_walk(sh.type, sh.dk, sh.dv, [&](auto tag, auto rows, auto cols, auto waves) {
+        return WalkLds<typename decltype(tag)::type, decltype(rows)::value, decltype(cols)::value, decltype(waves)::value, true>::resident;
+    });
+    const long long walks = sh.seqs * sh.heads * roles, round = 256 * resident * (packed ? LA_PK : 1), mean = sh.seqs > 0 ? (sh.tokens + sh.seqs - 1) / sh.seqs : 0;
     long long want = walks > 0 ? round / walks : 1; // segments a sequence of mean length
     const long long most = (mean + 4 * CHUNK - 1) / (4 * CHUNK);  // not below four chunks each
     if (want > most) want = most;
@@ -730,28 +755,27 @@ static int allow_lds(goom_ctx *ctx, const void *kernel, size_t bytes, std::atomi
     return GOOM_OK;
 }
 
-template <typename S, int DK, int DV> static int launch_walks_sized(goom_ctx *ctx, WalkArgs w, int roles, long long slots, const char *label)
+template <typename S, int DK, int DV, int NW> static int launch_walks_sized(goom_ctx *ctx, WalkArgs w, int roles, long long slots, const char *label)
 {
-    typedef typename Compute<S>::type E;
-    constexpr int NW = DV == 128 ? (sizeof(E) == 4 ? LA_NW32 : LA_NW) : DV == 64 ? 4 : 2;
     w.roles = roles;
     w.slots = (unsigned)slots;
-    const unsigned grid = (unsigned)((slots * w.heads + 7) / 8 * 8 * roles);
+    w.parts = (w.role[0].nc + DV - 1) / DV;
+    const unsigned grid = (unsigned)((slots * w.heads * w.parts + 7) / 8 * 8 * roles);
     const bool parts = w.role[0].totals != nullptr;
     if (parts) {
         auto *totals = walk_kernel<S, DK, DV, NW, false>;
-        constexpr size_t bytes = WalkLds<E, DK, DV, NW, false>::bytes;
+        constexpr size_t bytes = WalkLds<S, DK, DV, NW, false>::bytes;
         static std::atomic<unsigned long long> done{0};
         if (int st = allow_lds(ctx, reinterpret_cast<const void *>(totals), bytes, done)) return st;
         goom::prof_begin(ctx, "linear attention: segment totals");
         totals<<<grid, NW * 64, bytes, ctx->stream>>>(w);
         goom::prof_end(ctx);
         goom::prof_begin(ctx, "linear attention: carries");
-        carry_kernel<DK, DV, NW><<<dim3((unsigned)(w.seqs * w.heads * (DK * DV / 1024)), 1, roles), 256, 0, ctx->stream>>>(w);
+        carry_kernel<DK, DV, NW><<<dim3((unsigned)(w.seqs * w.heads * w.parts * (DK * DV / 1024)), 1, roles), 256, 0, ctx->stream>>>(w);
         goom::prof_end(ctx);
     }
     auto *walk = walk_kernel<S, DK, DV, NW, true>;
-    constexpr size_t bytes = WalkLds<E, DK, DV, NW, true>::bytes;
+    constexpr size_t bytes = WalkLds<S, DK, DV, NW, true>::bytes;
     static std::atomic<unsigned long long> done{0};
     if (int st = allow_lds(ctx, reinterpret_cast<const void *>(walk), bytes, done)) return st;
     goom::prof_begin(ctx, label);
@@ -760,23 +784,11 @@ template <typename S, int DK, int DV> static int launch_walks_sized(goom_ctx *ct
     return goom::check_hip(ctx, hipGetLastError(), label);
 }
 
-// roles of one launch have the same padded sizes
+// roles of one launch have the same kernel
 static int launch_walks(goom_ctx *ctx, int type, const WalkArgs &w, int roles, long long slots, const char *label)
 {
-    const int dk = padded_head(w.role[0].ka), dv = padded_head(w.role[0].nc);
-    return with_type(type, [&](auto tag) {
-        typedef typename decltype(tag)::type S;
-        switch (dk * 1000 + dv) {
-        case 32032: return launch_walks_sized<S, 32, 32>(ctx, w, roles, slots, label);
-        case 32064: return launch_walks_sized<S, 32, 64>(ctx, w, roles, slots, label);
-        case 32128: return launch_walks_sized<S, 32, 128>(ctx, w, roles, slots, label);
-        case 64032: return launch_walks_sized<S, 64, 32>(ctx, w, roles, slots, label);
-        case 64064: return launch_walks_sized<S, 64, 64>(ctx, w, roles, slots, label);
-        case 64128: return launch_walks_sized<S, 64, 128>(ctx, w, roles, slots, label);
-        case 128032: return launch_walks_sized<S, 128, 32>(ctx, w, roles, slots, label);
-        case 128064: return launch_walks_sized<S, 128, 64>(ctx, w, roles, slots, label);
-        default: return launch_walks_sized<S, 128, 128>(ctx, w, roles, slots, label);
-        }
+    return with_walk(type, w.role[0].ka, w.role[0].nc, [&](auto tag, auto rows, auto cols, auto waves) {
+        return launch_walks_sized<typename decltype(tag)::type, decltype(rows)::value, decltype(cols)::value, decltype(waves)::value>(ctx, w, roles, slots, label);
     });
 }
 
