@@ -27,7 +27,7 @@ namespace goom_layer {
 #define LA_PK 2
 #endif
 #ifndef LA_EARLY
-#define LA_EARLY (!OUT)
+#define LA_EARLY true
 #endif
 constexpr int CHUNK = 64; // tokens; the pairs of a chunk cost 64 (ka + nc) multiplications a token, the state 2 ka nc
 
@@ -184,7 +184,7 @@ template <int N> __device__ inline void row_frag(Frag (&x)[N], const bf16 *p, in
 }
 
 // rows t0 + 8 (lane / 16) + 0 .. 7 of one column: column c0 + (i / 4) cs + i % 4 for i = lane % 16
-template <int PITCH, int N> __device__ inline void col_frag(Frag (&x)[N], const bf16 *tile, int t0, int c0, int cs, int lane)
+template <int PITCH, int N> __device__ inline void col_frag(Frag (&x)[N], const bf16 *tile, int plane, int t0, int c0, int cs, int lane)
 {
     // the transposing read: of each 16 lanes, lane s gives the address of four columns of row s / 4, and lane i gets
     // the four rows of column i
@@ -192,7 +192,7 @@ template <int PITCH, int N> __device__ inline void col_frag(Frag (&x)[N], const 
     typedef __attribute__((address_space(3))) s16x4 *lds;
 #pragma unroll
     for (int k = 0; k < N; k++) {
-        const bf16 *const p = tile + k * CHUNK * PITCH + row * PITCH + col;
+        const bf16 *const p = tile + k * plane + row * PITCH + col;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(p + 4 * PITCH));
         x[k] = __builtin_bit_cast(Frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
@@ -203,35 +203,48 @@ __device__ inline void split_in(bf16x8 v, Frag (&p)[1]) { p[0] = v; }
 __device__ inline void split_in(f16x8 v, Frag (&p)[2]) { split(__builtin_convertvector(v, f32x8), p); }
 __device__ inline void split_in(f32x8 v, Frag (&p)[3]) { split(v, p); }
 
-// Rows 0 .. n-1 of `d` entries, on their way from memory into a tile of 64 rows of D entries with zeros elsewhere: fetched into
+// Rows 0 .. n-1 of `d` entries, on their way from memory into a tile of CH rows of D entries with zeros elsewhere: fetched into
 // registers, all loads in flight at once (rows and columns that are not there are read from ones that are), and put into LDS
-// where the walk gets to them.
-template <typename S, int D, int THREADS> struct Rows64 {
+// where the walk gets to them.  A thread's units of eight entries lie in one column, STEP rows apart.
+template <typename S, int D, int THREADS, int CH> struct TileRows {
     typedef typename Vec<S, 8>::type SV;
-    static constexpr int UNITS = CHUNK * D / 8, N = (UNITS + THREADS - 1) / THREADS;
+    static constexpr int UNITS = CH * D / 8, N = (UNITS + THREADS - 1) / THREADS, STEP = THREADS / (D / 8);
+    static_assert(THREADS % (D / 8) == 0, "units of a thread in one column");
     SV x[N];
 
-    // a thread's units lie in one column, STEP rows apart
-    static constexpr int STEP = THREADS / (D / 8);
-    static_assert(THREADS % (D / 8) == 0, "units of a thread in one column");
     __device__ static inline int row0() { return threadIdx.x / (D / 8); }
     __device__ static inline int col0() { return threadIdx.x % (D / 8) * 8; }
 
-    __device__ inline void fetch(const S *src, long long stride, int n, int d)
+    // vec: units are aligned to their size (d a multiple of eight); else element by element
+    __device__ inline void fetch(const S *src, long long stride, int n, int d, bool vec)
     {
-        // byte offsets within the chunk, 32 bits (the host has longer strides taken element by element)
+        // byte offsets within the chunk, 32 bits (checked by the host)
         const unsigned col = (col0() < d ? col0() : 0) * sizeof(S), bytes = (unsigned)stride * sizeof(S);
         const char *const p = reinterpret_cast<const char *>(src);
-        if (n == CHUNK) {
-            const unsigned at = row0() * bytes + col, step = STEP * bytes;
+        if (vec) {
+            if (n == CH) {
+                const unsigned at = row0() * bytes + col, step = STEP * bytes;
 #pragma unroll
-            for (int k = 0; k < N; k++)
-                if (UNITS % THREADS == 0 || row0() + k * STEP < CHUNK) x[k] = *reinterpret_cast<const SV *>(p + (at + k * step));
+                for (int k = 0; k < N; k++)
+                    if (UNITS % THREADS == 0 || row0() + k * STEP < CH) x[k] = *reinterpret_cast<const SV *>(p + (at + k * step));
+            } else {
+#pragma unroll
+                for (int k = 0; k < N; k++) {
+                    const int row = row0() + k * STEP;
+                    x[k] = *reinterpret_cast<const SV *>(p + ((row < n ? row : n - 1) * bytes + col));
+                }
+            }
         } else {
+            const int left = col0() < d ? d - col0() : 0; // entries from this unit's first on
 #pragma unroll
             for (int k = 0; k < N; k++) {
                 const int row = row0() + k * STEP;
-                x[k] = *reinterpret_cast<const SV *>(p + ((row < n ? row : n - 1) * bytes + col));
+                const S *const q = reinterpret_cast<const S *>(p + ((row < n ? row : n - 1) * bytes + col));
+                S e[8];
+#pragma unroll
+                for (int c = 0; c < 8; c++) e[c] = q[c < left ? c : 0];
+#pragma unroll
+                for (int c = 0; c < 8; c++) x[k][c] = c < left ? e[c] : (S)0.0f;
             }
         }
     }
@@ -242,44 +255,21 @@ template <typename S, int D, int THREADS> struct Rows64 {
 #pragma unroll
         for (int k = 0; k < N; k++) {
             SV v = x[k];
-            if (!there || (n != CHUNK && row0() + k * STEP >= n)) v = SV{};
+            if (!there || (n != CH && row0() + k * STEP >= n)) v = SV{};
             Frag p[Parts<S>::IN];
             split_in(v, p);
 #pragma unroll
             for (int q = 0; q < Parts<S>::IN; q++)
-                if (UNITS % THREADS == 0 || row0() + k * STEP < CHUNK) *reinterpret_cast<Frag *>(to0 + (q * CHUNK + k * STEP) * PITCH) = p[q];
+                if (UNITS % THREADS == 0 || row0() + k * STEP < CH) *reinterpret_cast<Frag *>(to0 + (q * CH + k * STEP) * PITCH) = p[q];
         }
     }
 };
 
-// the same for rows whose vectors are not aligned: straight into LDS, element by element
-template <typename S, int D, int PITCH, int THREADS> __device__ inline void stage_elements(bf16 *tile, const S *src, long long stride, int n, int d)
-{
-#pragma unroll 1
-    for (int u0 = threadIdx.x; u0 < CHUNK * D; u0 += 16 * THREADS) {
-        S x[16];
-#pragma unroll
-        for (int k = 0; k < 16; k++) {
-            const int u = u0 + k * THREADS, row = u / D, col = u % D;
-            x[k] = src[(row < n ? row : n - 1) * stride + (col < d ? col : 0)];
-        }
-#pragma unroll
-        for (int k = 0; k < 16; k++) {
-            const int u = u0 + k * THREADS, row = u / D, col = u % D;
-            float v = row < n && col < d ? (float)x[k] : 0.0f;
-#pragma unroll
-            for (int q = 0; q < Parts<S>::IN; q++) {
-                const bf16 part = (bf16)v;
-                v -= (float)part;
-                if (u < CHUNK * D) tile[(q * CHUNK + row) * PITCH + col] = part;
-            }
-        }
-    }
-}
-
 template <typename S, int DK, int DV, int NW, bool OUT> struct WalkLds {
+    // tokens of a step: where only the state is wanted, twice as many: more loads in flight for each barrier
+    static constexpr int CH = OUT || Parts<S>::IN > 1 ? CHUNK : 2 * CHUNK;
     static constexpr int PK = DK + PITCH_PAD, PV = DV + PITCH_PAD;
-    static constexpr int K_TILE = CHUNK * PK * Parts<S>::IN, V_TILE = CHUNK * PV * Parts<S>::IN; // elements
+    static constexpr int K_TILE = CH * PK * Parts<S>::IN, V_TILE = CH * PV * Parts<S>::IN; // elements
     static constexpr int P_FRAGS = OUT ? 6 * Parts<S>::OUT * 64 : 0; // the six 16 x 32 blocks of P with pairs in them
     static constexpr size_t bytes = (K_TILE * (OUT ? 2 : 1) + V_TILE) * sizeof(bf16) + P_FRAGS * sizeof(Frag);
     // workgroups of a CU: as many as its LDS holds, and no more than leave their waves the registers for the state (DK DV / 64 NW
@@ -300,7 +290,7 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
     typedef WalkLds<S, DK, DV, NW, OUT> Lds;
     constexpr int THREADS = NW * 64, NT = DV / 16 / NW, KS = DK / 32, CS = NT == 2 ? 8 : 4;
     constexpr int IP = Parts<S>::IN, OP = Parts<S>::OUT, SP = Parts<S>::STATE;
-    constexpr int KP = CHUNK * Lds::PK; // elements from part to part
+    constexpr int CH = Lds::CH, KP = CH * Lds::PK, VP = CH * Lds::PV; // tokens of a step, elements from part to part
     static_assert(NT == 1 || NT == 2, "a wave has one or two column tiles");
     Frag *const p_lds = reinterpret_cast<Frag *>(lds);
     bf16 *const b_lds = reinterpret_cast<bf16 *>(p_lds + Lds::P_FRAGS);
@@ -342,18 +332,18 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
     const S *const b = reinterpret_cast<const S *>(r.b) + at.start * r.b_tok + h / r.b_group * r.b_head;
     const S *const c = reinterpret_cast<const S *>(r.c) + at.start * r.c_tok + h / r.c_group * r.c_head + part * DV;
     const long long seg0 = at.seg * w.seg_len, seg1 = seg0 + w.seg_len < at.len ? seg0 + w.seg_len : at.len;
-    const int nchunks = (int)((seg1 - seg0 + CHUNK - 1) / CHUNK);
+    const int nchunks = (int)((seg1 - seg0 + CH - 1) / CH);
     const bool a_vec = r.a_vec, b_vec = r.b_vec, c_vec = r.c_vec;
-    Rows64<S, DK, THREADS> ax, bx;
-    Rows64<S, DV, THREADS> cx;
-    auto chunk_at = [&](int step) { return seg0 + (long long)(REV ? nchunks - 1 - step : step) * CHUNK; };
-    auto chunk_rows = [&](long long t0) { return seg1 - t0 < CHUNK ? (int)(seg1 - t0) : CHUNK; };
+    TileRows<S, DK, THREADS, CH> ax, bx;
+    TileRows<S, DV, THREADS, CH> cx;
+    auto chunk_at = [&](int step) { return seg0 + (long long)(REV ? nchunks - 1 - step : step) * CH; };
+    auto chunk_rows = [&](long long t0) { return seg1 - t0 < CH ? (int)(seg1 - t0) : CH; };
     auto fetch = [&](int step) {
         const long long t0 = chunk_at(step);
         const int n = chunk_rows(t0);
-        if (OUT && a_vec) ax.fetch(a + t0 * r.a_tok, r.a_tok, n, r.ka);
-        if (b_vec) bx.fetch(b + t0 * r.b_tok, r.b_tok, n, r.ka);
-        if (c_vec) cx.fetch(c + t0 * r.c_tok, r.c_tok, n, nc);
+        if (OUT) ax.fetch(a + t0 * r.a_tok, r.a_tok, n, r.ka, a_vec);
+        bx.fetch(b + t0 * r.b_tok, r.b_tok, n, r.ka, b_vec);
+        cx.fetch(c + t0 * r.c_tok, r.c_tok, n, nc, c_vec);
     };
     constexpr bool EARLY = LA_EARLY;
     if (EARLY && nchunks > 0) fetch(0);
@@ -364,14 +354,9 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
         asm volatile("" : "+v"(g2)); // the chunk's weights are formed anew for each: kept, they would take some 50 registers
         __syncthreads();
         if (!EARLY) fetch(step);
-        if (OUT) {
-            if (a_vec) ax.template put<Lds::PK>(a_lds, n, r.ka);
-            else stage_elements<S, DK, Lds::PK, THREADS>(a_lds, a + t0 * r.a_tok, r.a_tok, n, r.ka);
-        }
-        if (b_vec) bx.template put<Lds::PK>(b_lds, n, r.ka);
-        else stage_elements<S, DK, Lds::PK, THREADS>(b_lds, b + t0 * r.b_tok, r.b_tok, n, r.ka);
-        if (c_vec) cx.template put<Lds::PV>(c_lds, n, nc);
-        else stage_elements<S, DV, Lds::PV, THREADS>(c_lds, c + t0 * r.c_tok, r.c_tok, n, nc);
+        if (OUT) ax.template put<Lds::PK>(a_lds, n, r.ka);
+        bx.template put<Lds::PK>(b_lds, n, r.ka);
+        cx.template put<Lds::PV>(c_lds, n, nc);
         __syncthreads();
         if (EARLY && step + 1 < nchunks) fetch(step + 1); // while this chunk is worked on
 
@@ -411,12 +396,12 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
             __syncthreads();
         }
 
-        Frag cf[2][NT][IP];
+        Frag cf[CH / 32][NT][IP];
         auto load_columns = [&] {
 #pragma unroll
-            for (int ks = 0; ks < 2; ks++)
+            for (int ks = 0; ks < CH / 32; ks++)
 #pragma unroll
-                for (int nt = 0; nt < NT; nt++) col_frag<Lds::PV>(cf[ks][nt], c_lds, ks * 32, col0 + 4 * nt, CS, lane);
+                for (int nt = 0; nt < NT; nt++) col_frag<Lds::PV>(cf[ks][nt], c_lds, VP, ks * 32, col0 + 4 * nt, CS, lane);
         };
         if (!OUT) load_columns();
         if (OUT) {
@@ -497,11 +482,11 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
 #pragma unroll
             for (int nt = 0; nt < NT; nt++) R[t][nt] *= whole;
 #pragma unroll
-        for (int ks = 0; ks < 2; ks++) {
+        for (int ks = 0; ks < CH / 32; ks++) {
             f32x8 wt; // u g^(n - j'); rows past the end, where it would grow, are zeros
             const int first = REV ? ks * 32 + g * 8 + 1 : n - ahead - ks * 32 - g * 8;
             const float at = g2 * (float)first, by = REV ? g2 : -g2;
-            if (n == CHUNK) {
+            if (n == CH) {
 #pragma unroll
                 for (int e = 0; e < 8; e++) wt[e] = r.u_scale * __builtin_amdgcn_exp2f(at + by * (float)e);
             } else {
@@ -513,7 +498,7 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
             for (int nt = 0; nt < NT; nt++) split(widen(cf[ks][nt]) * wt, cd[nt]);
             constexpr int AHEAD = IP == 1 ? 2 : 1;
             Frag bf[AHEAD][IP];
-            auto load_rows = [&](int t) { col_frag<Lds::PK>(bf[t % AHEAD], b_lds, ks * 32, t / 2 * 32 + t % 2 * 4, 8, lane); };
+            auto load_rows = [&](int t) { col_frag<Lds::PK>(bf[t % AHEAD], b_lds, KP, ks * 32, t / 2 * 32 + t % 2 * 4, 8, lane); };
             if (AHEAD > 1) load_rows(0);
 #pragma unroll
             for (int t = 0; t < DK / 16; t++) {
@@ -792,11 +777,10 @@ static int launch_walks(goom_ctx *ctx, int type, const WalkArgs &w, int roles, l
     });
 }
 
-// rows of `d` entries whose vectors of 8 elements are aligned to 16 bytes (32 for floats: read as two); a chunk's offsets
-// within 32 bits
+// rows of `d` entries whose vectors of 8 elements are aligned to 16 bytes (32 for floats: read as two)
 static int vec_rows(const void *p, long long tok, long long head, int d, size_t size)
 {
-    return d % 8 == 0 && tok % 8 == 0 && head % 8 == 0 && goom::aligned(p, 8 * size) && tok < (1ll << 24);
+    return d % 8 == 0 && tok % 8 == 0 && head % 8 == 0 && goom::aligned(p, 8 * size);
 }
 
 static WalkArgs walk_args(const goom_attention_shape &sh, const float *log_decay, const int64_t *offsets, const Segments &g)
@@ -853,11 +837,13 @@ static int check_shape(goom_ctx *ctx, const goom_attention_shape *given, goom_at
     if (sh.seqs > (1 << 26) / sh.heads || sh.tokens > (1ll << 40) || sh.tokens / CHUNK > (1 << 26) / sh.heads) return goom::fail(ctx, GOOM_EUNSUPPORTED, "too many sequences, heads or tokens");
     const int64_t rows[3][3] = {{sh.q_token, sh.q_head, sh.dk}, {sh.k_token, sh.k_head, sh.dk}, {sh.v_token, sh.v_head, sh.dv}};
     for (auto &x : rows)
-        if (x[0] < 0 || x[1] < 0 || ((x[0] || x[1]) && (x[0] < x[2] || x[1] < x[2])) || x[0] > (1ll << 32) || x[1] > (1ll << 32))
+        if (x[0] < 0 || x[1] < 0 || ((x[0] || x[1]) && (x[0] < x[2] || x[1] < x[2])) || x[0] > (1ll << 40) || x[1] > (1ll << 40))
             return goom::fail(ctx, GOOM_EINVAL, "strides of tokens and heads must be 0 (both: contiguous) or at least a head's entries");
     if (!sh.q_token) { sh.q_token = (int64_t)sh.heads * sh.dk; sh.q_head = sh.dk; }
     if (!sh.k_token) { sh.k_token = (int64_t)sh.kv_heads * sh.dk; sh.k_head = sh.dk; }
     if (!sh.v_token) { sh.v_token = (int64_t)sh.kv_heads * sh.dv; sh.v_head = sh.dv; }
+    if (!need_equal && (sh.q_token > (1 << 22) || sh.k_token > (1 << 22) || sh.v_token > (1 << 22) || (int64_t)sh.heads * sh.dv > (1 << 22))) // 32-bit offsets within a chunk
+        return goom::fail(ctx, GOOM_EUNSUPPORTED, "more than 2^22 elements from token to token");
     return GOOM_OK;
 }
 
