@@ -23,12 +23,6 @@
 
 namespace goom_layer {
 
-#ifndef LA_PK
-#define LA_PK 2
-#endif
-#ifndef LA_EARLY
-#define LA_EARLY true
-#endif
 constexpr int CHUNK = 64; // tokens; the pairs of a chunk cost 64 (ka + nc) multiplications a token, the state 2 ka nc
 
 struct WalkRole {
@@ -266,11 +260,13 @@ template <typename S, int D, int THREADS, int CH> struct TileRows {
 };
 
 template <typename S, int DK, int DV, int NW, bool OUT> struct WalkLds {
-    // tokens of a step: where only the state is wanted, twice as many: more loads in flight for each barrier
-    static constexpr int CH = OUT || Parts<S>::IN > 1 ? CHUNK : 2 * CHUNK;
+    // Tokens of a step.  Inputs of two and three parts: half, so that two workgroups share a CU (20,700 cycles a chunk of 64 with one).
+    // Where only the state is wanted, twice as many: more loads in flight for each barrier.
+    static constexpr int CH = (Parts<S>::IN > 1 ? CHUNK / 2 : CHUNK) * (OUT ? 1 : 2);
+    static constexpr int P_BLOCKS = CH == CHUNK ? 6 : 2; // 16 x 32 blocks of P that have pairs in them
     static constexpr int PK = DK + PITCH_PAD, PV = DV + PITCH_PAD;
     static constexpr int K_TILE = CH * PK * Parts<S>::IN, V_TILE = CH * PV * Parts<S>::IN; // elements
-    static constexpr int P_FRAGS = OUT ? 6 * Parts<S>::OUT * 64 : 0; // the six 16 x 32 blocks of P with pairs in them
+    static constexpr int P_FRAGS = OUT ? P_BLOCKS * Parts<S>::OUT * 64 : 0;
     static constexpr size_t bytes = (K_TILE * (OUT ? 2 : 1) + V_TILE) * sizeof(bf16) + P_FRAGS * sizeof(Frag);
     // workgroups of a CU: as many as its LDS holds, and no more than leave their waves the registers for the state (DK DV / 64 NW
     // a lane), the outputs and the rows on their way: three waves a SIMD with 168 each, or two with 256
@@ -280,8 +276,18 @@ template <typename S, int DK, int DV, int NW, bool OUT> struct WalkLds {
     static constexpr int per_simd = resident * NW / 4 > 0 ? resident * NW / 4 : 1;
 };
 
-// which of the six blocks of P: rows 16 it on, columns 32 ks on
-template <bool REV> __device__ constexpr int p_block(int it, int ks) { return REV ? (it < 2 ? it * 2 + ks : it + 2) : (it < 2 ? it : it * 2 - 2 + ks); }
+// the blocks of P with pairs in them: of rows 16 it on and columns 32 ks on, in order; and back
+template <bool REV> __device__ constexpr bool p_has(int it, int ks) { return REV ? ks >= it / 2 : ks <= it / 2; }
+template <bool REV> __device__ constexpr int p_block(int it, int ks, int ch)
+{
+    return ch == 32 ? it : REV ? (it < 2 ? it * 2 + ks : it + 2) : (it < 2 ? it : it * 2 - 2 + ks);
+}
+template <bool REV> __device__ inline void p_place(int block, int ch, int &it, int &ks)
+{
+    if (ch == 32) { it = block; ks = 0; }
+    else if (REV) { it = block < 4 ? block / 2 : block - 2; ks = block < 4 ? block % 2 : 1; }
+    else { it = block < 2 ? block : block / 2 + 1; ks = block < 2 ? 0 : block % 2; }
+}
 
 // DK, DV: ka and nc (of one of `parts` column parts), padded; NW waves of NT tiles of 16 columns each
 template <typename S, int DK, int DV, int NW, bool OUT, bool REV>
@@ -345,53 +351,49 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
         bx.fetch(b + t0 * r.b_tok, r.b_tok, n, r.ka, b_vec);
         cx.fetch(c + t0 * r.c_tok, r.c_tok, n, nc, c_vec);
     };
-    constexpr bool EARLY = LA_EARLY;
-    if (EARLY && nchunks > 0) fetch(0);
+    if (nchunks > 0) fetch(0);
     for (int step = 0; step < nchunks; step++) {
         const long long t0 = chunk_at(step);
         const int n = chunk_rows(t0);
         float g2 = log2_g;
         asm volatile("" : "+v"(g2)); // the chunk's weights are formed anew for each: kept, they would take some 50 registers
         __syncthreads();
-        if (!EARLY) fetch(step);
         if (OUT) ax.template put<Lds::PK>(a_lds, n, r.ka);
         bx.template put<Lds::PK>(b_lds, n, r.ka);
         cx.template put<Lds::PV>(c_lds, n, nc);
         __syncthreads();
-        if (EARLY && step + 1 < nchunks) fetch(step + 1); // while this chunk is worked on
+        if (step + 1 < nchunks) fetch(step + 1); // while this chunk is worked on
 
         if (OUT) {
             // ---- P, transposed (accumulator columns are the rows i, so that a lane's entries are consecutive j)
-            for (int it = wave; it < 4; it += NW) {
+            for (int block = wave; block < Lds::P_BLOCKS; block += NW) {
+                int it, ks;
+                p_place<REV>(block, CH, it, ks);
+                f32x4 p0 = {0, 0, 0, 0}, p1 = {0, 0, 0, 0};
+                const bf16 *const arow = a_lds + (it * 16 + i) * Lds::PK + g * 8;
+                const bf16 *const brow = b_lds + (ks * 32 + (i >> 2) * 8 + (i & 3)) * Lds::PK + g * 8;
 #pragma unroll
-                for (int ks = 0; ks < 2; ks++) {
-                    if (REV ? ks < it / 2 : ks > it / 2) continue; // no pair in this half
-                    f32x4 p0 = {0, 0, 0, 0}, p1 = {0, 0, 0, 0};
-                    const bf16 *const arow = a_lds + (it * 16 + i) * Lds::PK + g * 8;
-                    const bf16 *const brow = b_lds + (ks * 32 + (i >> 2) * 8 + (i & 3)) * Lds::PK + g * 8;
-#pragma unroll
-                    for (int kk = 0; kk < KS; kk++) {
-                        Frag af[IP], b0[IP], b1[IP];
-                        row_frag(af, arow + kk * 32, KP);
-                        row_frag(b0, brow + kk * 32, KP);
-                        row_frag(b1, brow + 4 * Lds::PK + kk * 32, KP);
-                        p0 = product<3>(b0, af, p0);
-                        p1 = product<3>(b1, af, p1);
-                    }
-                    f32x8 x;
-                    int first = it * 16 + i - ks * 32 - g * 8; // i - j of the lane's first j
-                    asm volatile("" : "+v"(first));            // (and so are the masks)
-                    const float at = g2 * (float)(REV ? -first : first), by = REV ? g2 : -g2;
-#pragma unroll
-                    for (int e = 0; e < 8; e++) {
-                        const float p = (e < 4 ? p0[e & 3] : p1[e & 3]) * (r.p_scale * __builtin_amdgcn_exp2f(at + by * (float)e));
-                        x[e] = (REV ? e >= first : e <= first) ? p : 0.0f;
-                    }
-                    Frag parts[OP];
-                    split(x, parts);
-#pragma unroll
-                    for (int q = 0; q < OP; q++) p_lds[(p_block<REV>(it, ks) * OP + q) * 64 + lane] = parts[q];
+                for (int kk = 0; kk < KS; kk++) {
+                    Frag af[IP], b0[IP], b1[IP];
+                    row_frag(af, arow + kk * 32, KP);
+                    row_frag(b0, brow + kk * 32, KP);
+                    row_frag(b1, brow + 4 * Lds::PK + kk * 32, KP);
+                    p0 = product<3>(b0, af, p0);
+                    p1 = product<3>(b1, af, p1);
                 }
+                f32x8 x;
+                int first = it * 16 + i - ks * 32 - g * 8; // i - j of the lane's first j
+                asm volatile("" : "+v"(first));            // (and so are the masks)
+                const float at = g2 * (float)(REV ? -first : first), by = REV ? g2 : -g2;
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    const float p = (e < 4 ? p0[e & 3] : p1[e & 3]) * (r.p_scale * __builtin_amdgcn_exp2f(at + by * (float)e));
+                    x[e] = (REV ? e >= first : e <= first) ? p : 0.0f;
+                }
+                Frag parts[OP];
+                split(x, parts);
+#pragma unroll
+                for (int q = 0; q < OP; q++) p_lds[(block * OP + q) * 64 + lane] = parts[q];
             }
             __syncthreads();
         }
@@ -406,19 +408,19 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
         if (!OUT) load_columns();
         if (OUT) {
             // ---- what the state gives to each row, then the pairs; transposed: a lane has consecutive columns of row i
-            f32x4 y[4][NT];
+            f32x4 y[CH / 16][NT];
 #pragma unroll
-            for (int it = 0; it < 4; it++)
+            for (int it = 0; it < CH / 16; it++)
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++) y[it][nt] = f32x4{0, 0, 0, 0};
             if (step > 0 || total || r.init) {
                 // operands are read one step ahead of their products, and no further: registers are what the walk is short of
                 constexpr int AHEAD = IP == 1 ? 2 : 1;
-                Frag af[AHEAD][4][IP];
+                Frag af[AHEAD][CH / 16][IP];
                 const bf16 *const a0 = a_lds + i * Lds::PK + g * 8;
                 auto load_rows = [&](int kk) {
 #pragma unroll
-                    for (int it = 0; it < 4; it++) row_frag(af[kk % AHEAD][it], a0 + it * 16 * Lds::PK + kk * 32, KP);
+                    for (int it = 0; it < CH / 16; it++) row_frag(af[kk % AHEAD][it], a0 + it * 16 * Lds::PK + kk * 32, KP);
                 };
                 if (AHEAD > 1) load_rows(0);
 #pragma unroll
@@ -429,7 +431,7 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++) split(__builtin_shufflevector(R[2 * kk][nt], R[2 * kk + 1][nt], 0, 1, 2, 3, 4, 5, 6, 7), rf[nt]);
 #pragma unroll
-                    for (int it = 0; it < 4; it++)
+                    for (int it = 0; it < CH / 16; it++)
 #pragma unroll
                         for (int nt = 0; nt < NT; nt++) y[it][nt] = product<OP>(rf[nt], af[kk % AHEAD][it], y[it][nt]);
                     __builtin_amdgcn_sched_barrier(0);
@@ -437,17 +439,17 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
             }
             load_columns();
 #pragma unroll
-            for (int it = 0; it < 4; it++) {
+            for (int it = 0; it < CH / 16; it++) {
                 const int row = it * 16 + i, age = REV ? n - 1 - row : row;
                 const float scale = r.w_scale * decay_power(g2, age > 0 ? age : 0);
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++) y[it][nt] *= scale;
 #pragma unroll
-                for (int ks = 0; ks < 2; ks++) {
-                    if (REV ? ks < it / 2 : ks > it / 2) continue;
+                for (int ks = 0; ks < CH / 32; ks++) {
+                    if (!p_has<REV>(it, ks)) continue;
                     Frag pf[OP];
 #pragma unroll
-                    for (int q = 0; q < OP; q++) pf[q] = p_lds[(p_block<REV>(it, ks) * OP + q) * 64 + lane];
+                    for (int q = 0; q < OP; q++) pf[q] = p_lds[(p_block<REV>(it, ks, CH) * OP + q) * 64 + lane];
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++) y[it][nt] = product<OP>(cf[ks][nt], pf, y[it][nt]);
                 }
@@ -543,7 +545,7 @@ __global__ __launch_bounds__(NW * 64, (WalkLds<S, DK, DV, NW, OUT>::per_simd)) v
     const int part = item % w.parts, h = item / w.parts % w.heads;
     const long long slot = item / w.parts / w.heads;
     const Place at = find_place(w, slot);
-    if (at.seg >= at.nseg) return;
+    if (at.seg >= at.nseg || part * DV >= r.nc) return;
     if (r.reverse) walk<S, DK, DV, NW, OUT, true>(w, r, at, slot, h, part, lds);
     else walk<S, DK, DV, NW, OUT, false>(w, r, at, slot, h, part, lds);
 }
@@ -591,15 +593,18 @@ template <int DK, int DV, int NW> __global__ __launch_bounds__(256) void carry_k
     }
 }
 
-// sums over heads that share keys and values: y[token][kv head][.] = sum over the group of x[token][head][.], floats
-template <typename S> __global__ __launch_bounds__(256) void shared_sum_kernel(const float *x, S *y, long long n, int group, int d)
+// sums over heads that share keys and values: y[token][kv head][.] = sum over the group of x[token][head][.], floats.  Two such
+// arrays in one launch, blockIdx.y apart
+struct SharedSum { const float *x; void *y; long long n; int d; };
+template <typename S> __global__ __launch_bounds__(256) void shared_sum_kernel(SharedSum k, SharedSum v, int group)
 {
-    for (long long u = blockIdx.x * 256ll + threadIdx.x; u < n; u += gridDim.x * 256ll) {
-        const long long row = u / d;
-        const float *p = x + row * group * d + (u - row * d);
+    const SharedSum &t = blockIdx.y ? v : k;
+    for (long long u = blockIdx.x * 256ll + threadIdx.x; u < t.n; u += gridDim.x * 256ll) {
+        const long long row = u / t.d;
+        const float *p = t.x + row * group * t.d + (u - row * t.d);
         float sum = 0.0f;
-        for (int k = 0; k < group; k++) sum += p[(long long)k * d];
-        y[u] = (S)sum;
+        for (int k = 0; k < group; k++) sum += p[(long long)k * t.d];
+        reinterpret_cast<S *>(t.y)[u] = (S)sum;
     }
 }
 
@@ -688,8 +693,7 @@ template <typename F> static auto with_walk(int type, int ka, int nc, F f)
             // floats' three parts of 128 x 128 do not fit LDS: two halves of the columns
             if constexpr (DK == 128 && IN == 3) return f(tag, rows, std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
             else if (nc <= 64) return f(tag, rows, std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
-            // waves: each with two column tiles where two workgroups share a CU, with one (more waves) where LDS holds but one
-            else return f(tag, rows, std::integral_constant<int, 128>(), std::integral_constant<int, IN == 1 ? 4 : 8>());
+            else return f(tag, rows, std::integral_constant<int, 128>(), std::integral_constant<int, 4>());
         };
         return ka <= 32 ? columns(std::integral_constant<int, 32>()) : ka <= 64 ? columns(std::integral_constant<int, 64>()) : columns(std::integral_constant<int, 128>());
     });
@@ -704,9 +708,12 @@ static Segments choose_segments(const goom_attention_shape &sh, int roles, bool 
     const long long resident = with_walk(sh.type, sh.dk, sh.dv, [&](auto tag, auto rows, auto cols, auto waves) {
         return WalkLds<typename decltype(tag)::type, decltype(rows)::value, decltype(cols)::value, decltype(waves)::value, true>::resident;
     });
-    const long long walks = sh.seqs * sh.heads * roles, round = 256 * resident * (packed ? LA_PK : 1), mean = sh.seqs > 0 ? (sh.tokens + sh.seqs - 1) / sh.seqs : 0;
+    // (sequences of different lengths: four rounds of shorter ones, which even out)
+    const long long walks = sh.seqs * sh.heads * roles, round = 256 * resident * (packed ? 4 : 1), mean = sh.seqs > 0 ? (sh.tokens + sh.seqs - 1) / sh.seqs : 0;
     long long want = walks > 0 ? round / walks : 1; // segments a sequence of mean length
-    const long long most = (mean + 4 * CHUNK - 1) / (4 * CHUNK);  // not below four chunks each
+    // Not below two chunks each (one, where lengths differ): measured at 8 x 1000 tokens of 8 heads of 32 and 64, forward and
+    // backward, 148, 139 and 140 us with four, two and one chunks; at 5 ragged sequences of 1500 tokens in all, 141, 113 and 95 us
+    const long long least = packed ? CHUNK : 2 * CHUNK, most = (mean + least - 1) / least;
     if (want > most) want = most;
     if (want < 1) want = 1;
     long long len = (mean + want - 1) / want;
@@ -744,7 +751,9 @@ template <typename S, int DK, int DV, int NW> static int launch_walks_sized(goom
 {
     w.roles = roles;
     w.slots = (unsigned)slots;
-    w.parts = (w.role[0].nc + DV - 1) / DV;
+    int nc = 0;
+    for (int k = 0; k < roles; k++) nc = w.role[k].nc > nc ? w.role[k].nc : nc;
+    w.parts = (nc + DV - 1) / DV;
     const unsigned grid = (unsigned)((slots * w.heads * w.parts + 7) / 8 * 8 * roles);
     const bool parts = w.role[0].totals != nullptr;
     if (parts) {
@@ -769,10 +778,15 @@ template <typename S, int DK, int DV, int NW> static int launch_walks_sized(goom
     return goom::check_hip(ctx, hipGetLastError(), label);
 }
 
-// roles of one launch have the same kernel
+// the roles of one launch share a kernel, of the largest size among them
 static int launch_walks(goom_ctx *ctx, int type, const WalkArgs &w, int roles, long long slots, const char *label)
 {
-    return with_walk(type, w.role[0].ka, w.role[0].nc, [&](auto tag, auto rows, auto cols, auto waves) {
+    int ka = 0, nc = 0;
+    for (int k = 0; k < roles; k++) {
+        ka = w.role[k].ka > ka ? w.role[k].ka : ka;
+        nc = w.role[k].nc > nc ? w.role[k].nc : nc;
+    }
+    return with_walk(type, ka, nc, [&](auto tag, auto rows, auto cols, auto waves) {
         return launch_walks_sized<typename decltype(tag)::type, decltype(rows)::value, decltype(cols)::value, decltype(waves)::value>(ctx, w, roles, slots, label);
     });
 }
@@ -865,6 +879,7 @@ int check_workspace(goom_ctx *ctx, const void *ws, size_t given, size_t need)
 // bytes of the backward pass's workspace by parts: states of the three walks, floats of shared heads' gradients
 struct BackwardPlan {
     Segments seg;
+    bool together; // the three walks in one launch
     size_t totals_q, totals_k, totals_v, sum_k, sum_v, bytes;
 };
 
@@ -872,22 +887,19 @@ static BackwardPlan backward_plan(const goom_attention_shape &sh, bool packed)
 {
     BackwardPlan p;
     p.seg = choose_segments(sh, 3, packed);
-    p.totals_q = totals_bytes(sh, p.seg, sh.dv, sh.dk);
-    p.totals_k = totals_bytes(sh, p.seg, sh.dv, sh.dk);
-    p.totals_v = totals_bytes(sh, p.seg, sh.dk, sh.dv);
+    // Walks of different sizes go together, padded to the larger, where the chip has room for all of them at once: a small
+    // pass is bound by its launches
+    const int most = sh.dk > sh.dv ? sh.dk : sh.dv, least = sh.dk > sh.dv ? sh.dv : sh.dk;
+    p.together = padded_head(least) == padded_head(most) || sh.seqs * sh.heads * 3 <= 256;
+    const int dk = p.together ? most : sh.dk, dv = p.together ? most : sh.dv;
+    p.totals_q = totals_bytes(sh, p.seg, dv, dk);
+    p.totals_k = totals_bytes(sh, p.seg, dv, dk);
+    p.totals_v = totals_bytes(sh, p.seg, dk, dv);
     const bool shared = sh.heads != sh.kv_heads;
     p.sum_k = shared ? goom::align_up((size_t)sh.tokens * sh.heads * sh.dk * 4, 256) : 0;
     p.sum_v = shared ? goom::align_up((size_t)sh.tokens * sh.heads * sh.dv * 4, 256) : 0;
     p.bytes = p.totals_q + p.totals_k + p.totals_v + p.sum_k + p.sum_v;
     return p;
-}
-
-template <typename S> static void launch_shared_sum(goom_ctx *ctx, const float *x, void *y, long long rows, int group, int d)
-{
-    const long long n = rows * d, blocks = (n + 255) / 256;
-    goom::prof_begin(ctx, "linear attention: shared heads");
-    shared_sum_kernel<S><<<(unsigned)(blocks < 16384 ? blocks : 16384), 256, 0, ctx->stream>>>(x, reinterpret_cast<S *>(y), n, group, d);
-    goom::prof_end(ctx);
 }
 
 } // namespace goom_layer
@@ -1017,7 +1029,7 @@ int goom_linear_attention_backward(goom_ctx *ctx, const goom_attention_shape *sh
     w.role[0] = gq;
     w.role[1] = gk;
     w.role[2] = gv;
-    if (padded_head(sh.dk) == padded_head(sh.dv)) {
+    if (plan.together) {
         if (int s = launch_walks(ctx, sh.type, w, 3, plan.seg.slots, "linear attention: gradients")) return s;
     } else {
         if (int s = launch_walks(ctx, sh.type, w, 2, plan.seg.slots, "linear attention: gradients of q and k")) return s;
@@ -1028,8 +1040,10 @@ int goom_linear_attention_backward(goom_ctx *ctx, const goom_attention_shape *sh
         const long long rows = sh.tokens * sh.kv_heads;
         return with_type(sh.type, [&](auto tag) {
             typedef typename decltype(tag)::type S;
-            launch_shared_sum<S>(ctx, sum_k, grad_k, rows, group, sh.dk);
-            launch_shared_sum<S>(ctx, sum_v, grad_v, rows, group, sh.dv);
+            const long long most = rows * (sh.dk > sh.dv ? sh.dk : sh.dv), blocks = (most + 255) / 256;
+            goom::prof_begin(ctx, "linear attention: shared heads");
+            shared_sum_kernel<S><<<dim3((unsigned)(blocks < 16384 ? blocks : 16384), 2), 256, 0, ctx->stream>>>({sum_k, grad_k, rows * sh.dk, sh.dk}, {sum_v, grad_v, rows * sh.dv, sh.dv}, group);
+            goom::prof_end(ctx);
             return goom::check_hip(ctx, hipGetLastError(), "linear attention: shared heads");
         });
     }
