@@ -72,7 +72,7 @@ def test_linear_attention_step_and_backward_refuse(lib):
         assert back(attention(), **{x: None}) == EINVAL and "null" in err(lib), x
     assert back(attention(), gk=C.c_void_p(0x1001)) == EINVAL and "aligned" in err(lib)
     need = lib.goom_linear_attention_backward_workspace_bytes(C.byref(attention()), 0)
-    assert need > 2 * 256 * 4 * (32 + 64) * 2  # the shared heads' sums are in it
+    assert need >= 4 * 256 * 4 * (32 + 64)  # floats of 256 tokens' 4 heads, to be summed where they share keys and values
     assert back(attention(), wsn=need - 1) == EWS
     assert lib.goom_linear_attention_workspace_bytes(C.byref(attention(dk=0)), 0) == 0
 
