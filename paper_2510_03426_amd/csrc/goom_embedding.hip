@@ -39,18 +39,52 @@ template <typename S, int V> __global__ __launch_bounds__(256) void embedding_ke
 struct SortPass {
     const int64_t *tokens; // first pass: keys come from here, positions are the indices
     const unsigned *keys, *values;
-    unsigned *out_keys, *out_values, *counts; // counts: [tiles][bins]
+    unsigned *out_keys, *out_values;
+    unsigned *counts; // [tiles][bins]
     unsigned n, vocab, tile;
     int shift, bits;
 };
 
-__device__ inline unsigned sort_key(const SortPass &p, unsigned i)
+__device__ inline unsigned token_key(long long t, unsigned vocab) { return t >= 0 && t < vocab ? (unsigned)t : vocab; }
+
+// keys of the lane's entries i, i + 64, ..., all loads at once; entries from `end` on have none
+template <int N> __device__ inline void load_keys(const SortPass &p, unsigned i, unsigned end, unsigned (&key)[N])
 {
-    if (!p.tokens) return p.keys[i];
-    const long long t = p.tokens[i];
-    return t >= 0 && t < p.vocab ? (unsigned)t : p.vocab;
+    if (p.tokens) {
+        long long t[N];
+#pragma unroll
+        for (int k = 0; k < N; k++) t[k] = p.tokens[i + k * 64 < end ? i + k * 64 : 0];
+#pragma unroll
+        for (int k = 0; k < N; k++) key[k] = token_key(t[k], p.vocab);
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; k++) key[k] = p.keys[i + k * 64 < end ? i + k * 64 : 0];
+    }
 }
 
+// lanes whose digit equals this lane's, among those that are live
+__device__ inline unsigned long long same_digit(unsigned digit, int bits, bool live)
+{
+    unsigned long long same = __ballot(live);
+    for (int b = 0; b < bits; b++) {
+        const unsigned long long m = __ballot(digit >> b & 1);
+        same &= digit >> b & 1 ? m : ~m;
+    }
+    return same;
+}
+
+// one addition a wave and digit: frequent tokens' digits would have the lanes wait for each other
+__device__ inline unsigned long long add_count(unsigned *count, unsigned digit, int bits, bool live)
+{
+    const unsigned long long same = same_digit(digit, bits, live);
+    if (live && !(same & ((1ull << (threadIdx.x & 63)) - 1))) atomicAdd(&count[digit], (unsigned)__popcll(same));
+    return same;
+}
+
+constexpr int ROUNDS = 4; // entries of a lane that are loaded at once
+
+// counts of the digits by tiles (counted by the scattering pass before, with atomics in memory, frequent tokens' counts made it
+// twice as long: 16 us for 8)
 __global__ __launch_bounds__(256) void sort_count_kernel(SortPass p)
 {
     __shared__ unsigned count[MAX_BINS];
@@ -58,7 +92,12 @@ __global__ __launch_bounds__(256) void sort_count_kernel(SortPass p)
     for (int d = threadIdx.x; d < bins; d += 256) count[d] = 0;
     __syncthreads();
     const unsigned begin = blockIdx.x * p.tile, end = p.n - begin < p.tile ? p.n : begin + p.tile;
-    for (unsigned i = begin + threadIdx.x; i < end; i += 256) atomicAdd(&count[sort_key(p, i) >> p.shift & (bins - 1)], 1u);
+    for (unsigned i = begin + (threadIdx.x >> 6) * 64 * ROUNDS + (threadIdx.x & 63); i < end; i += 256 * ROUNDS) {
+        unsigned key[ROUNDS];
+        load_keys<ROUNDS>(p, i, end, key);
+#pragma unroll
+        for (int k = 0; k < ROUNDS; k++) add_count(count, key[k] >> p.shift & (bins - 1), p.bits, i + k * 64 < end);
+    }
     __syncthreads();
     for (int d = threadIdx.x; d < bins; d += 256) p.counts[blockIdx.x * (unsigned)bins + d] = count[d];
 }
@@ -67,39 +106,51 @@ __global__ __launch_bounds__(256) void sort_count_kernel(SortPass p)
 __global__ __launch_bounds__(256) void sort_scatter_kernel(SortPass p)
 {
     __shared__ unsigned at[4][MAX_BINS]; // counts of the waves' quarters, then where each wave's next entry of a digit goes
-    __shared__ unsigned sums[256];
+    __shared__ unsigned waves[4];
     const int bins = 1 << p.bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int d = threadIdx.x; d < 4 * MAX_BINS; d += 256) at[d / MAX_BINS][d % MAX_BINS] = 0;
-    __syncthreads();
     const unsigned begin = blockIdx.x * p.tile + wave * (p.tile / 4), limit = (p.n < (blockIdx.x + 1u) * p.tile ? p.n : (blockIdx.x + 1u) * p.tile);
     const unsigned end = begin + p.tile / 4 < limit ? begin + p.tile / 4 : limit;
-    for (unsigned i = begin + lane; i < end; i += 64) atomicAdd(&at[wave][sort_key(p, i) >> p.shift & (bins - 1)], 1u);
+    unsigned key[ROUNDS]; // the first entries; they stay here in tiles of 1024
+    if (begin < end) load_keys<ROUNDS>(p, begin + lane, end, key);
+    for (int d = threadIdx.x; d < 4 * MAX_BINS; d += 256) at[d / MAX_BINS][d % MAX_BINS] = 0;
     // entries of each digit in all tiles, and in the tiles before this one; a thread has two neighbouring digits
     unsigned total[2] = {0, 0}, before[2] = {0, 0};
+    if ((int)threadIdx.x * 2 < bins)
+        for (unsigned t0 = 0; t0 < gridDim.x; t0 += 32) {
+            unsigned long long c[32];
 #pragma unroll
-    for (int k = 0; k < 2; k++) {
-        const int d = threadIdx.x * 2 + k;
-        if (d < bins)
-            for (unsigned t0 = 0; t0 < gridDim.x; t0 += 16) {
-                unsigned c[16];
+            for (int t = 0; t < 32; t++) c[t] = t0 + t < gridDim.x ? *reinterpret_cast<const unsigned long long *>(p.counts + (t0 + t) * (unsigned)bins + threadIdx.x * 2) : 0;
 #pragma unroll
-                for (int t = 0; t < 16; t++) c[t] = t0 + t < gridDim.x ? p.counts[(t0 + t) * (unsigned)bins + d] : 0;
-#pragma unroll
-                for (int t = 0; t < 16; t++) {
-                    total[k] += c[t];
-                    before[k] += t0 + t < blockIdx.x ? c[t] : 0;
+            for (int t = 0; t < 32; t++) {
+                total[0] += (unsigned)c[t];
+                total[1] += (unsigned)(c[t] >> 32);
+                if (t0 + t < blockIdx.x) {
+                    before[0] += (unsigned)c[t];
+                    before[1] += (unsigned)(c[t] >> 32);
                 }
             }
+        }
+    unsigned sum = total[0] + total[1]; // running sums over the digits: of the wave, then of the waves
+    for (int s = 1; s < 64; s *= 2) {
+        const unsigned x = __shfl_up(sum, s);
+        sum += lane >= s ? x : 0;
     }
-    sums[threadIdx.x] = total[0] + total[1];
+    if (lane == 63) waves[wave] = sum;
     __syncthreads();
-    for (int s = 1; s < 256; s *= 2) { // running sums over the digits
-        const unsigned x = (int)threadIdx.x >= s ? sums[threadIdx.x - s] : 0;
-        __syncthreads();
-        sums[threadIdx.x] += x;
-        __syncthreads();
+    unsigned long long same[ROUNDS]; // of the first entries, too
+    for (unsigned i0 = begin; i0 < end; i0 += 64 * ROUNDS) {
+        unsigned more[ROUNDS];
+        if (i0 != begin) load_keys<ROUNDS>(p, i0 + lane, end, more);
+#pragma unroll
+        for (int k = 0; k < ROUNDS; k++) {
+            const unsigned digit = (i0 != begin ? more[k] : key[k]) >> p.shift & (bins - 1);
+            const unsigned long long m = add_count(at[wave], digit, p.bits, i0 + lane + k * 64 < end);
+            if (i0 == begin) same[k] = m;
+        }
     }
-    unsigned base = sums[threadIdx.x] - total[0] - total[1];
+    __syncthreads();
+    unsigned base = sum - total[0] - total[1];
+    for (int v = 0; v < wave; v++) base += waves[v];
 #pragma unroll
     for (int k = 0; k < 2; k++) {
         const int d = threadIdx.x * 2 + k;
@@ -113,52 +164,113 @@ __global__ __launch_bounds__(256) void sort_scatter_kernel(SortPass p)
         base += total[k];
     }
     __syncthreads();
-    for (unsigned i0 = begin; i0 < end; i0 += 64) {
-        const unsigned i = i0 + lane;
-        const bool live = i < end;
-        const unsigned key = live ? sort_key(p, i) : 0, digit = key >> p.shift & (bins - 1);
-        unsigned long long same = __ballot(live);
-        for (int b = 0; b < p.bits; b++) {
-            const unsigned long long m = __ballot(digit >> b & 1);
-            same &= digit >> b & 1 ? m : ~m;
+    for (unsigned i0 = begin; i0 < end; i0 += 64 * ROUNDS) {
+        if (i0 != begin) load_keys<ROUNDS>(p, i0 + lane, end, key);
+        unsigned value[ROUNDS];
+#pragma unroll
+        for (int k = 0; k < ROUNDS; k++) {
+            const unsigned i = i0 + k * 64 + lane;
+            value[k] = p.tokens ? i : p.values[i < end ? i : 0];
         }
-        const unsigned rank = __popcll(same & ((1ull << lane) - 1));
-        unsigned to = 0;
-        if (live) to = at[wave][digit] + rank;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); // all lanes have read before a digit's first lane moves it on
-        if (live) {
-            if (rank == 0) at[wave][digit] += __popcll(same);
-            p.out_keys[to] = key;
-            p.out_values[to] = p.tokens ? i : p.values[i];
+#pragma unroll
+        for (int k = 0; k < ROUNDS; k++) {
+            if (i0 + k * 64 >= end) break;
+            const bool live = i0 + k * 64 + lane < end;
+            const unsigned digit = key[k] >> p.shift & (bins - 1);
+            const unsigned long long mine = i0 == begin ? same[k] : same_digit(digit, p.bits, live);
+            const unsigned rank = __popcll(mine & ((1ull << lane) - 1));
+            unsigned to = 0;
+            if (live) to = at[wave][digit] + rank;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); // all lanes have read before a digit's first lane moves it on
+            if (live) {
+                if (rank == 0) at[wave][digit] += __popcll(mine);
+                p.out_keys[to] = key[k];
+                p.out_values[to] = value[k];
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
-// start[t] = first sorted position whose token is at least t, t = 0 .. vocab.  A thread writes the tokens from its left
-// neighbour's on up to its own; gaps of more than 64 (few positions, many tokens) are written by the whole workgroup.
-__global__ __launch_bounds__(256) void run_start_kernel(const unsigned *keys, unsigned *start, unsigned n, unsigned vocab)
+// The whole sort of up to SMALL positions by one workgroup, in LDS: five launches fewer, and as fast up to here.
+constexpr int SMALL = 4096;
+__global__ __launch_bounds__(1024) void sort_small_kernel(const int64_t *tokens, unsigned *out_keys, unsigned *out_values, unsigned n, unsigned vocab, int passes, int bits)
 {
-    __shared__ unsigned gaps[256][2];
-    __shared__ int count;
-    if (threadIdx.x == 0) count = 0;
-    __syncthreads();
-    const unsigned i = blockIdx.x * 256 + threadIdx.x;
-    if (i <= n) {
-        const unsigned from = i == 0 ? 0 : keys[i - 1] + 1, to = i == n ? vocab : keys[i];
-        if (from <= to && to - from > 64) {
-            const int at = atomicAdd(&count, 1);
-            gaps[at][0] = i;
-            gaps[at][1] = from;
-        } else {
-            for (unsigned t = from; t <= to; t++) start[t] = i;
+    __shared__ unsigned keys[SMALL];
+    __shared__ unsigned short values[SMALL];
+    __shared__ unsigned at[16][MAX_BINS];
+    __shared__ unsigned waves[16];
+    constexpr int N = SMALL / 1024;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bins = 1 << bits;
+    const unsigned begin = wave * 64 * N + lane; // a wave has 64 N entries in order, a lane every 64th of them
+    unsigned key[N], value[N];
+    long long t[N];
+#pragma unroll
+    for (int k = 0; k < N; k++) t[k] = tokens[begin + k * 64 < n ? begin + k * 64 : 0];
+#pragma unroll
+    for (int k = 0; k < N; k++) {
+        key[k] = token_key(t[k], vocab);
+        value[k] = begin + k * 64;
+    }
+    for (int pass = 0; pass < passes; pass++) {
+        const int shift = pass * bits;
+        for (int d = threadIdx.x; d < 16 * MAX_BINS; d += 1024) at[d / MAX_BINS][d % MAX_BINS] = 0;
+        __syncthreads();
+        unsigned long long same[N];
+#pragma unroll
+        for (int k = 0; k < N; k++) same[k] = add_count(at[wave], key[k] >> shift & (bins - 1), bits, begin + k * 64 < n);
+        __syncthreads();
+        unsigned total = 0;
+        const int d = threadIdx.x;
+        if (d < bins)
+#pragma unroll
+            for (int v = 0; v < 16; v++) total += at[v][d];
+        unsigned sum = total;
+        for (int s = 1; s < 64; s *= 2) {
+            const unsigned x = __shfl_up(sum, s);
+            sum += lane >= s ? x : 0;
+        }
+        if (lane == 63) waves[wave] = sum;
+        __syncthreads();
+        if (d < bins) {
+            unsigned next = sum - total;
+            for (int v = 0; v < wave; v++) next += waves[v];
+#pragma unroll
+            for (int v = 0; v < 16; v++) {
+                const unsigned c = at[v][d];
+                at[v][d] = next;
+                next += c;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; k++) {
+            const bool live = begin + k * 64 < n;
+            const unsigned digit = key[k] >> shift & (bins - 1);
+            const unsigned rank = __popcll(same[k] & ((1ull << lane) - 1));
+            unsigned to = 0;
+            if (live) to = at[wave][digit] + rank;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (live) {
+                if (rank == 0) at[wave][digit] += __popcll(same[k]);
+                keys[to] = key[k];
+                values[to] = (unsigned short)value[k];
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; k++) {
+            key[k] = keys[begin + k * 64];
+            value[k] = values[begin + k * 64];
         }
     }
-    __syncthreads();
-    for (int k = 0; k < count; k++) {
-        const unsigned at = gaps[k][0], to = at == n ? vocab : keys[at];
-        for (unsigned t = gaps[k][1] + threadIdx.x; t <= to; t += 256) start[t] = at;
-    }
+#pragma unroll
+    for (int k = 0; k < N; k++)
+        if (begin + k * 64 < n) {
+            out_keys[begin + k * 64] = key[k];
+            out_values[begin + k * 64] = value[k];
+        }
 }
 
 // x += rows of grad at sorted positions [i, end), in order
@@ -181,17 +293,51 @@ template <typename S, int V> __device__ inline void add_rows(float (&x)[V], cons
     }
 }
 
-// sums of the blocks of RUN sorted positions that belong to one token; grid: (blocks, parts of 64 V columns)
-template <typename S, int V> __global__ __launch_bounds__(64) void run_block_kernel(const S *grad, const unsigned *keys, const unsigned *values, float *sums, unsigned vocab, int width)
+// start[t] = first sorted position whose token is at least t, t = 0 .. vocab.  A thread writes the tokens from its left
+// neighbour's on up to its own; gaps of more than 64 (few positions, many tokens) are written by the whole workgroup.
+__device__ inline void run_starts(const unsigned *keys, unsigned *start, unsigned n, unsigned vocab, unsigned block)
 {
-    const unsigned i = blockIdx.x * RUN;
+    __shared__ unsigned gaps[256][3];
+    __shared__ int count;
+    if (threadIdx.x == 0) count = 0;
+    __syncthreads();
+    const unsigned i = block * 256 + threadIdx.x;
+    if (i <= n) {
+        const unsigned from = i == 0 ? 0 : keys[i - 1] + 1, to = i == n ? vocab : keys[i];
+        if (from <= to && to - from > 64) {
+            const int at = atomicAdd(&count, 1);
+            gaps[at][0] = i;
+            gaps[at][1] = from;
+            gaps[at][2] = to;
+        } else {
+            for (unsigned t = from; t <= to; t++) start[t] = i;
+        }
+    }
+    __syncthreads();
+    for (int k = 0; k < count; k++) {
+        const unsigned at = gaps[k][0], to = gaps[k][2];
+        for (unsigned t = gaps[k][1] + threadIdx.x; t <= to; t += 256) start[t] = at;
+    }
+}
+
+// The first n / 256 + 1 workgroups: run starts.  The others: sums of the blocks of RUN sorted positions that belong to one token, a
+// wave each 64 V columns of a block.
+template <typename S, int V> __global__ __launch_bounds__(256) void runs_kernel(const S *grad, const unsigned *keys, const unsigned *values, unsigned *start, float *sums, unsigned n, unsigned vocab, int width, int parts)
+{
+    if (blockIdx.x <= n / 256) {
+        run_starts(keys, start, n, vocab, blockIdx.x);
+        return;
+    }
+    const unsigned task = (blockIdx.x - n / 256 - 1) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), block = task / parts;
+    const unsigned i = block * RUN;
+    if (block >= n / RUN) return;
     const unsigned key = keys[i];
     if (key != keys[i + RUN - 1] || key >= vocab) return;
-    const int col = (blockIdx.y * 64 + threadIdx.x) * V;
+    const int col = ((int)(task - block * parts) * 64 + (threadIdx.x & 63)) * V;
     if (col >= width) return;
     float x[V] = {};
     add_rows<S, V>(x, grad, values, i, i + RUN, width, col);
-    store_floats<float, V>(sums + (long long)blockIdx.x * width + col, x);
+    store_floats<float, V>(sums + (long long)block * width + col, x);
 }
 
 // 64 V columns of a table row a wave: the run's head, its whole blocks, its tail.  grid: vocab parts / 4
@@ -231,8 +377,36 @@ template <typename S, typename W, int V> __global__ __launch_bounds__(256) void 
     store_floats<W, V>(table + row * width + col, x);
 }
 
+// Up to FEW positions need no sorting: every row's waves look at all tokens themselves.  One launch.
+constexpr int FEW = 256;
+template <typename S, typename W, int V> __global__ __launch_bounds__(256) void few_rows_kernel(const S *grad, const int64_t *tokens, W *table, unsigned n, long long vocab, int width, int parts, float scale)
+{
+    const long long task = blockIdx.x * 4ll + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = task / parts;
+    const int lane = threadIdx.x & 63, col = ((int)(task - row * parts) * 64 + lane) * V;
+    if (row >= vocab) return;
+    unsigned long long mine[FEW / 64]; // positions of this row's token
+#pragma unroll
+    for (int k = 0; k < FEW / 64; k++) mine[k] = __ballot(k * 64 + lane < (int)n && tokens[k * 64 + lane < (int)n ? k * 64 + lane : 0] == row);
+    if (col >= width) return;
+    float x[V] = {};
+#pragma unroll
+    for (int k = 0; k < FEW / 64; k++)
+        while (mine[k]) {
+            const int i = k * 64 + __builtin_ctzll(mine[k]);
+            mine[k] &= mine[k] - 1;
+            float y[V];
+            load_floats<S, V>(grad + (long long)i * width + col, y);
+#pragma unroll
+            for (int e = 0; e < V; e++) x[e] += y[e];
+        }
+#pragma unroll
+    for (int e = 0; e < V; e++) x[e] *= scale;
+    store_floats<W, V>(table + row * width + col, x);
+}
+
 struct EmbeddingPlan {
     int passes, bits;
+    bool small;
     unsigned tile, tiles;
     size_t counts, list, start, sums, bytes; // bytes of each part: counts, one list of n (four of them), run starts, block sums
 };
@@ -248,7 +422,8 @@ static EmbeddingPlan embedding_plan(long long n, long long vocab, int width)
     p.tile = n <= 65536 ? 1024 : n <= (1 << 20) ? 8192 : 65536;
     p.tiles = (unsigned)((n + p.tile - 1) / p.tile);
     auto up = [](size_t b) { return goom::align_up(b, 256); };
-    p.counts = up((size_t)p.tiles * (1u << p.bits) * 4);
+    p.small = n <= SMALL;
+    p.counts = p.small ? 0 : up((size_t)p.tiles * (1u << p.bits) * 4);
     p.list = up((size_t)n * 4);
     p.start = up((size_t)(vocab + 1) * 4);
     p.sums = up((size_t)(n / RUN) * width * 4);
@@ -349,16 +524,21 @@ int goom_embedding_backward(goom_ctx *ctx, const int64_t *tokens, const void *gr
     float *const sums = reinterpret_cast<float *>(take(plan.sums));
 
     const unsigned *keys = lists[0][0], *values = lists[0][1];
-    goom::prof_begin(ctx, "embedding gradient: sort");
-    for (int k = 0; n > 0 && k < plan.passes; k++) {
-        SortPass p = {k == 0 ? tokens : nullptr, keys, values, lists[k & 1][0], lists[k & 1][1], counts, (unsigned)n, (unsigned)vocab, plan.tile, k * plan.bits, plan.bits};
-        sort_count_kernel<<<plan.tiles, 256, 0, ctx->stream>>>(p);
-        sort_scatter_kernel<<<plan.tiles, 256, 0, ctx->stream>>>(p);
-        keys = p.out_keys;
-        values = p.out_values;
+    if (n > FEW) goom::prof_begin(ctx, "embedding gradient: sort");
+    if (n <= FEW) {
+        // no sorting
+    } else if (plan.small) {
+        sort_small_kernel<<<1, 1024, 0, ctx->stream>>>(tokens, lists[0][0], lists[0][1], (unsigned)n, (unsigned)vocab, plan.passes, plan.bits);
+    } else {
+        for (int k = 0; k < plan.passes; k++) {
+            SortPass p = {k == 0 ? tokens : nullptr, keys, values, lists[k & 1][0], lists[k & 1][1], counts, (unsigned)n, (unsigned)vocab, plan.tile, k * plan.bits, plan.bits};
+            sort_count_kernel<<<plan.tiles, 256, 0, ctx->stream>>>(p);
+            sort_scatter_kernel<<<plan.tiles, 256, 0, ctx->stream>>>(p);
+            keys = p.out_keys;
+            values = p.out_values;
+        }
     }
-    run_start_kernel<<<(unsigned)(n / 256 + 1), 256, 0, ctx->stream>>>(keys, start, (unsigned)n, (unsigned)vocab);
-    goom::prof_end(ctx);
+    if (n > FEW) goom::prof_end(ctx);
     const int v = vector_of(width, {{grad, size}, {grad_table, wsize}, {sums, 4}});
     const int rc = with_type(type, [&](auto tag) {
         typedef typename decltype(tag)::type S;
@@ -366,16 +546,19 @@ int goom_embedding_backward(goom_ctx *ctx, const int64_t *tokens, const void *gr
             constexpr int V = decltype(vec)::value;
             if constexpr (V <= 4) {
                 const S *const gr = reinterpret_cast<const S *>(grad);
-                if (n >= RUN) {
-                    goom::prof_begin(ctx, "embedding gradient: frequent tokens");
-                    run_block_kernel<S, V><<<dim3((unsigned)(n / RUN), (width + 64 * V - 1) / (64 * V)), 64, 0, ctx->stream>>>(gr, keys, values, sums, (unsigned)vocab, width);
+                const int parts = (width + 64 * V - 1) / (64 * V);
+                const unsigned row_groups = (unsigned)((vocab * parts + 3) / 4);
+                if (n > FEW) {
+                    goom::prof_begin(ctx, "embedding gradient: runs");
+                    runs_kernel<S, V><<<(unsigned)(n / 256 + 1 + (n / RUN * parts + 3) / 4), 256, 0, ctx->stream>>>(gr, keys, values, start, sums, (unsigned)n, (unsigned)vocab, width, parts);
                     goom::prof_end(ctx);
                 }
                 goom::prof_begin(ctx, "embedding gradient: rows");
                 with_type(table_type, [&](auto wtag) {
                     typedef typename decltype(wtag)::type W;
-                    const int parts = (width + 64 * V - 1) / (64 * V);
-                    table_row_kernel<S, W, V><<<(unsigned)((vocab * parts + 3) / 4), 256, 0, ctx->stream>>>(gr, values, start, sums, reinterpret_cast<W *>(grad_table), vocab, width, parts, (float)scale);
+                    W *const out = reinterpret_cast<W *>(grad_table);
+                    if (n > FEW) table_row_kernel<S, W, V><<<row_groups, 256, 0, ctx->stream>>>(gr, values, start, sums, out, vocab, width, parts, (float)scale);
+                    else few_rows_kernel<S, W, V><<<row_groups, 256, 0, ctx->stream>>>(gr, tokens, out, (unsigned)n, vocab, width, parts, (float)scale);
                     return 0;
                 });
                 goom::prof_end(ctx);

@@ -64,7 +64,7 @@ def test_rows_and_gradient(g, dtype, gtype, kind, n, vocab, width):
     assert torch.equal(out, g.embedding_backward(tokens, grad.cuda(), vocab, scale=scale, dtype=_types()[gtype]))  # a fixed order
 
 
-@pytest.mark.parametrize("n", [65536, 65537, 200001])
+@pytest.mark.parametrize("n", [31, 256, 257, 4095, 4096, 4097, 65536, 65537, 200001])
 def test_many_positions(g, n):
     """Whole numbers, whose sums are exact in any order: every position has to be counted once."""
     import torch
@@ -74,6 +74,9 @@ def test_many_positions(g, n):
     grad = torch.randint(-8, 9, (n, 4), device="cuda", generator=gen).float()
     want = torch.zeros(vocab, 4, device="cuda", dtype=torch.float64).index_add_(0, tokens, grad.double())
     assert torch.equal(g.embedding_backward(tokens, grad, vocab).double(), want)
+    if n > 65000:  # and with three sorting passes
+        wide = tokens * 60
+        assert torch.equal(g.embedding_backward(wide, grad, 60 * vocab)[::60].double(), want)
 
 
 def test_odd_addresses_and_nothing(g):
