@@ -65,10 +65,25 @@ template <int V> __device__ inline void params(const void *p, int type, int i, f
 // is near e^z): library exp and division were 25 of the 40 instructions an element and took longer than its bytes
 __device__ inline float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504088896341f)); }
 
+// Phi(z) = (1 + erf(z / sqrt 2)) / 2 and phi(z) = Phi'(z), from one exponential: the rational approximation 7.1.26 of Abramowitz
+// and Stegun, Handbook of Mathematical Functions (absolute error of erf at most 1.5e-7, about one unit of a float near 1).  With
+// the library's erf and exp the kernels were bound by some 80 instructions an element.
+__device__ inline void normal(float z, float &cdf, float &density)
+{
+    const float x = fabsf(z) * 0.70710678118654752f, e = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f), t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * x);
+    const float tail = 0.5f * e * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    cdf = z < 0.0f ? tail : 1.0f - tail; // (a NaN stays one)
+    density = e * 0.39894228040143268f;
+}
+
 __device__ inline float activate(float z, int act)
 {
     if (act == GOOM_ACT_SILU) return z * logistic(z);
-    if (act == GOOM_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    if (act == GOOM_ACT_GELU) {
+        float cdf, density;
+        normal(z, cdf, density);
+        return z * cdf;
+    }
     return z;
 }
 
@@ -78,7 +93,11 @@ __device__ inline float activate_slope(float z, int act)
         const float p = logistic(z);
         return p * (1.0f + z * (1.0f - p));
     }
-    if (act == GOOM_ACT_GELU) return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * expf(-0.5f * z * z);
+    if (act == GOOM_ACT_GELU) {
+        float cdf, density;
+        normal(z, cdf, density);
+        return cdf + z * density;
+    }
     return 1.0f;
 }
 
@@ -242,16 +261,19 @@ __global__ __launch_bounds__(1024) void norm_weight_kernel(const float *partial,
     }
 }
 
-// ---- long groups.  Thread (tx, ty): units tx, tx + columns, ... of the slab's V-element units, positions ty, ty + rows_at_once,
-// ... of the chunk.  A slab of several groups has at most as many units as a workgroup has columns.  grid: (items chunks, slabs)
-struct Slab { int group0, ngroups, units, columns, tx, ty; long long item, chunk, row0, row1; bool live; };
+// ---- long groups.  Thread (tx, ty): units tx, tx + columns, ... of the slab's V-element units (whatever groups their channels
+// belong to), positions ty, ty + rows_at_once, ... of the chunk, DEEP of them loaded at once.  A slab of several groups has at
+// most as many units as a workgroup has columns.  grid: (items chunks, slabs)
+constexpr int DEEP = 4;
+struct Slab { int group0, ngroups, chan0, units, columns, tx, ty; long long item, chunk, row0, row1; bool live; };
 
 template <int V> __device__ inline Slab slab_of(const NormArgs &a)
 {
     Slab s;
     s.group0 = blockIdx.y * a.gps;
     s.ngroups = a.groups - s.group0 < a.gps ? a.groups - s.group0 : a.gps;
-    s.units = s.ngroups * (a.cg / V);
+    s.chan0 = s.group0 * a.cg;
+    s.units = s.ngroups * a.cg / V;
     s.columns = a.threads / a.rows_at_once;
     s.tx = threadIdx.x % s.columns;
     s.ty = threadIdx.x / s.columns;
@@ -263,47 +285,72 @@ template <int V> __device__ inline Slab slab_of(const NormArgs &a)
     return s;
 }
 
-template <typename S, int V> __global__ __launch_bounds__(512) void norm_stats_kernel(NormArgs a)
+typedef double f64x2 __attribute__((ext_vector_type(2)));
+
+// lanes that add up one group's sums: a power of two, at most a wave
+__device__ inline int lanes_of(int ngroups)
 {
-    __shared__ double meet[2][512];
-    const Slab s = slab_of<V>(a);
-    const S *const x = reinterpret_cast<const S *>(a.x) + s.item * a.length * a.channels + s.group0 * a.cg;
-    const int cu = a.cg / V;
-    double sum = 0.0, square = 0.0;
-    for (int u = s.tx; s.live && u < s.units; u += s.columns) {
-        const double pivot = (double)(float)x[u / cu * a.cg]; // first element of the group
-        for (long long row = s.row0 + s.ty; row < s.row1; row += a.rows_at_once) {
-            float v[V];
-            load_floats<S, V>(x + row * a.channels + u * V, v);
+    int lanes = 64;
+    while (lanes > 1 && lanes * ngroups > (int)blockDim.x) lanes /= 2;
+    return lanes;
+}
+
+// f(row, x, y) for the thread's rows, DEEP loads of x (and of y, unless NULL) ahead
+template <typename S, int V, typename F> __device__ inline void rows_of(const NormArgs &a, const Slab &s, const S *x, const S *y, int u, F f)
+{
+    typedef typename Vec<S, V>::type SV;
+    for (long long row0 = s.row0 + s.ty; row0 < s.row1; row0 += (long long)DEEP * a.rows_at_once) {
+        SV p[DEEP], q[DEEP];
 #pragma unroll
-            for (int e = 0; e < V; e++) {
-                const double d = (double)v[e] - pivot;
-                sum += d;
-                square += d * d;
-            }
+        for (int k = 0; k < DEEP; k++) {
+            const long long row = row0 + k * a.rows_at_once, from = (row < s.row1 ? row : row0) * a.channels + u * V;
+            p[k] = *reinterpret_cast<const SV *>(x + from);
+            if (y) q[k] = *reinterpret_cast<const SV *>(y + from);
+        }
+#pragma unroll
+        for (int k = 0; k < DEEP; k++) {
+            const long long row = row0 + k * a.rows_at_once;
+            if (row < s.row1) f(row, p[k], q[k]);
         }
     }
-    meet[0][threadIdx.x] = sum;
-    meet[1][threadIdx.x] = square;
-    __syncthreads();
-    // a wave a group: its threads are the columns [g cu, (g + 1) cu) in every row, or (one group) all
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = (blockDim.x + 63) / 64;
-    for (int g = wave; g < s.ngroups; g += waves) {
-        const int width = s.ngroups == 1 ? s.columns : cu, total = width * a.rows_at_once;
-        double p = 0.0, q = 0.0;
-        for (int k = lane; k < total; k += 64) {
-            const int t = k / width * s.columns + (s.ngroups == 1 ? 0 : g * cu) + k % width;
-            p += meet[0][t];
-            q += meet[1][t];
-        }
-        for (int m = 1; m < 64; m *= 2) {
-            p += __shfl_xor(p, m);
-            q += __shfl_xor(q, m);
-        }
-        if (lane == 0) {
-            double *to = a.stats + ((s.item * a.chunks + s.chunk) * a.groups + s.group0 + g) * 2;
-            to[0] = p;
-            to[1] = q;
+}
+
+template <typename S, int V> __global__ __launch_bounds__(512) void norm_stats_kernel(NormArgs a)
+{
+    __shared__ double meet[V][512];
+    const Slab s = slab_of<V>(a);
+    const S *const x = reinterpret_cast<const S *>(a.x) + s.item * a.length * a.channels + s.chan0;
+    double sum[V] = {}, square[V] = {}; // of the thread's channels; of all its units where the slab is one group
+    for (int u = s.tx; s.live && u < s.units; u += s.columns) {
+        double pivot[V];
+#pragma unroll
+        for (int e = 0; e < V; e++) pivot[e] = (double)(float)x[(u * V + e) / a.cg * a.cg]; // first element of the channel's group
+        rows_of<S, V>(a, s, x, (const S *)nullptr, u, [&](long long, const auto &v, const auto &) {
+#pragma unroll
+            for (int e = 0; e < V; e++) {
+                const double d = (double)(float)v[e] - pivot[e];
+                sum[e] += d;
+                square[e] += d * d;
+            }
+        });
+    }
+    const int lanes = lanes_of(s.ngroups), per = blockDim.x / lanes, lane = threadIdx.x % lanes;
+    for (int which = 0; which < 2; which++) {
+        if (which) __syncthreads();
+#pragma unroll
+        for (int e = 0; e < V; e++) meet[e][threadIdx.x] = which ? square[e] : sum[e];
+        __syncthreads();
+        for (int g0 = 0; g0 < s.ngroups; g0 += per) {
+            const int g = g0 + threadIdx.x / lanes;
+            const int width = s.ngroups == 1 ? s.columns * V : a.cg;
+            double p = 0.0;
+            if (g < s.ngroups)
+                for (int k = lane; k < width; k += lanes) {
+                    const int c = g * a.cg + k;
+                    for (int row = 0; row < a.rows_at_once; row++) p += meet[c % V][row * s.columns + c / V];
+                }
+            for (int m = 1; m < lanes; m *= 2) p += __shfl_xor(p, m);
+            if (g < s.ngroups && lane == 0) a.stats[((s.item * a.chunks + s.chunk) * a.groups + s.group0 + g) * 2 + which] = p;
         }
     }
 }
@@ -312,21 +359,24 @@ template <typename S, int V> __global__ __launch_bounds__(512) void norm_apply_k
 {
     __shared__ float stat[512][2];
     const Slab s = slab_of<V>(a);
-    const long long base = s.item * a.length * a.channels + s.group0 * a.cg;
+    const long long base = s.item * a.length * a.channels + s.chan0;
     const S *const x = reinterpret_cast<const S *>(a.x) + base;
     S *const y = reinterpret_cast<S *>(a.y) + base;
-    const int cu = a.cg / V;
-    int lanes = 64; // of a group, for its chunks' sums
-    while (lanes > 1 && lanes * s.ngroups > (int)blockDim.x) lanes /= 2;
-    const int per = blockDim.x / lanes;
+    const int lanes = lanes_of(s.ngroups), per = blockDim.x / lanes;
     for (int g0 = 0; g0 < s.ngroups; g0 += per) {
         const int g = g0 + threadIdx.x / lanes;
         double p = 0.0, q = 0.0;
         if (g < s.ngroups)
-            for (long long k = threadIdx.x % lanes; k < a.chunks; k += lanes) {
-                const double *from = a.stats + ((s.item * a.chunks + k) * a.groups + s.group0 + g) * 2;
-                p += from[0];
-                q += from[1];
+            for (long long k0 = threadIdx.x % lanes; k0 < a.chunks; k0 += 16ll * lanes) { // 16 chunks' sums at once
+                f64x2 v[16];
+#pragma unroll
+                for (int k = 0; k < 16; k++) v[k] = *reinterpret_cast<const f64x2 *>(a.stats + ((s.item * a.chunks + (k0 + k * lanes < a.chunks ? k0 + k * lanes : k0)) * a.groups + s.group0 + g) * 2);
+#pragma unroll
+                for (int k = 0; k < 16; k++)
+                    if (k0 + k * lanes < a.chunks) {
+                        p += v[k][0];
+                        q += v[k][1];
+                    }
             }
         for (int m = 1; m < lanes; m *= 2) {
             p += __shfl_xor(p, m);
@@ -344,17 +394,20 @@ template <typename S, int V> __global__ __launch_bounds__(512) void norm_apply_k
     }
     __syncthreads();
     for (int u = s.tx; s.live && u < s.units; u += s.columns) {
-        const float mean = stat[u / cu][0], rstd = stat[u / cu][1];
-        float w[V], b[V];
-        params<V>(a.weight, a.type_w, s.group0 * a.cg + u * V, 1.0f, w);
-        params<V>(a.bias, a.type_w, s.group0 * a.cg + u * V, 0.0f, b);
-        for (long long row = s.row0 + s.ty; row < s.row1; row += a.rows_at_once) {
-            float v[V];
-            load_floats<S, V>(x + row * a.channels + u * V, v);
+        float mean[V], rstd[V], w[V], b[V];
+        params<V>(a.weight, a.type_w, s.chan0 + u * V, 1.0f, w);
+        params<V>(a.bias, a.type_w, s.chan0 + u * V, 0.0f, b);
 #pragma unroll
-            for (int e = 0; e < V; e++) v[e] = activate((v[e] - mean) * rstd * w[e] + b[e], a.act);
-            store_floats<S, V>(y + row * a.channels + u * V, v);
+        for (int e = 0; e < V; e++) {
+            mean[e] = stat[(u * V + e) / a.cg][0];
+            rstd[e] = stat[(u * V + e) / a.cg][1];
         }
+        rows_of<S, V>(a, s, x, (const S *)nullptr, u, [&](long long row, const auto &v, const auto &) {
+            float z[V];
+#pragma unroll
+            for (int e = 0; e < V; e++) z[e] = activate(((float)v[e] - mean[e]) * rstd[e] * w[e] + b[e], a.act);
+            store_floats<S, V>(y + row * a.channels + u * V, z);
+        });
     }
 }
 
@@ -363,29 +416,30 @@ template <typename S, int V> __global__ __launch_bounds__(512) void norm_sums_ke
 {
     __shared__ float meet[2 * V][512];
     const Slab s = slab_of<V>(a);
-    const long long base = s.item * a.length * a.channels + s.group0 * a.cg;
+    const long long base = s.item * a.length * a.channels + s.chan0;
     const S *const x = reinterpret_cast<const S *>(a.x) + base;
     const S *const gy = reinterpret_cast<const S *>(a.gy) + base;
-    const int cu = a.cg / V;
     for (int u0 = 0; u0 < s.units; u0 += s.columns) {
         const int u = u0 + s.tx;
         float sw[V] = {}, sb[V] = {};
         if (s.live && u < s.units) {
-            const float mean = a.mean[s.item * a.groups + s.group0 + u / cu], rstd = a.rstd[s.item * a.groups + s.group0 + u / cu];
-            float w[V], b[V];
-            params<V>(a.weight, a.type_w, s.group0 * a.cg + u * V, 1.0f, w);
-            params<V>(a.bias, a.type_w, s.group0 * a.cg + u * V, 0.0f, b);
-            for (long long row = s.row0 + s.ty; row < s.row1; row += a.rows_at_once) {
-                float v[V], g[V];
-                load_floats<S, V>(x + row * a.channels + u * V, v);
-                load_floats<S, V>(gy + row * a.channels + u * V, g);
+            float mean[V], rstd[V], w[V], b[V];
+            params<V>(a.weight, a.type_w, s.chan0 + u * V, 1.0f, w);
+            params<V>(a.bias, a.type_w, s.chan0 + u * V, 0.0f, b);
+#pragma unroll
+            for (int e = 0; e < V; e++) {
+                const long long at = s.item * a.groups + s.group0 + (u * V + e) / a.cg;
+                mean[e] = a.mean[at];
+                rstd[e] = a.rstd[at];
+            }
+            rows_of<S, V>(a, s, x, gy, u, [&](long long, const auto &v, const auto &g) {
 #pragma unroll
                 for (int e = 0; e < V; e++) {
-                    const float xhat = (v[e] - mean) * rstd, dz = g[e] * activate_slope(xhat * w[e] + b[e], a.act);
+                    const float xhat = ((float)v[e] - mean[e]) * rstd[e], dz = (float)g[e] * activate_slope(xhat * w[e] + b[e], a.act);
                     sw[e] += dz * xhat;
                     sb[e] += dz;
                 }
-            }
+            });
         }
         __syncthreads();
 #pragma unroll
@@ -395,7 +449,7 @@ template <typename S, int V> __global__ __launch_bounds__(512) void norm_sums_ke
         }
         __syncthreads();
         if (s.ty == 0 && u < s.units) {
-            float *const to = a.sums + (s.item * a.chunks + s.chunk) * 2 * a.channels + s.group0 * a.cg + u * V;
+            float *const to = a.sums + (s.item * a.chunks + s.chunk) * 2 * a.channels + s.chan0 + u * V;
 #pragma unroll
             for (int e = 0; e < 2 * V; e++) {
                 float sum = 0.0f;
@@ -439,28 +493,31 @@ __global__ __launch_bounds__(256) void norm_means_kernel(NormArgs a)
 template <typename S, int V> __global__ __launch_bounds__(512) void norm_grad_kernel(NormArgs a)
 {
     const Slab s = slab_of<V>(a);
-    const long long base = s.item * a.length * a.channels + s.group0 * a.cg;
+    const long long base = s.item * a.length * a.channels + s.chan0;
     const S *const x = reinterpret_cast<const S *>(a.x) + base;
     const S *const gy = reinterpret_cast<const S *>(a.gy) + base;
     S *const gx = reinterpret_cast<S *>(a.y) + base;
-    const int cu = a.cg / V;
     for (int u = s.tx; s.live && u < s.units; u += s.columns) {
-        const long long at = s.item * a.groups + s.group0 + u / cu;
-        const float mean = a.mean[at], rstd = a.rstd[at], m1 = a.means[at * 2], m2 = a.means[at * 2 + 1];
-        float w[V], b[V];
-        params<V>(a.weight, a.type_w, s.group0 * a.cg + u * V, 1.0f, w);
-        params<V>(a.bias, a.type_w, s.group0 * a.cg + u * V, 0.0f, b);
-        for (long long row = s.row0 + s.ty; row < s.row1; row += a.rows_at_once) {
-            float v[V], g[V];
-            load_floats<S, V>(x + row * a.channels + u * V, v);
-            load_floats<S, V>(gy + row * a.channels + u * V, g);
+        float mean[V], rstd[V], m1[V], m2[V], w[V], b[V];
+        params<V>(a.weight, a.type_w, s.chan0 + u * V, 1.0f, w);
+        params<V>(a.bias, a.type_w, s.chan0 + u * V, 0.0f, b);
+#pragma unroll
+        for (int e = 0; e < V; e++) {
+            const long long at = s.item * a.groups + s.group0 + (u * V + e) / a.cg;
+            mean[e] = a.mean[at];
+            rstd[e] = a.rstd[at];
+            m1[e] = a.means[at * 2];
+            m2[e] = a.means[at * 2 + 1];
+        }
+        rows_of<S, V>(a, s, x, gy, u, [&](long long row, const auto &v, const auto &g) {
+            float z[V];
 #pragma unroll
             for (int e = 0; e < V; e++) {
-                const float xhat = (v[e] - mean) * rstd, dz = g[e] * activate_slope(xhat * w[e] + b[e], a.act);
-                v[e] = rstd * (dz * w[e] - m1 - xhat * m2);
+                const float xhat = ((float)v[e] - mean[e]) * rstd[e], dz = (float)g[e] * activate_slope(xhat * w[e] + b[e], a.act);
+                z[e] = rstd[e] * (dz * w[e] - m1[e] - xhat * m2[e]);
             }
-            store_floats<S, V>(gx + row * a.channels + u * V, v);
-        }
+            store_floats<S, V>(gx + row * a.channels + u * V, z);
+        });
     }
 }
 
@@ -474,8 +531,8 @@ struct NormPlan {
     size_t stats, sums, means, partial;  // bytes in the workspace
 };
 
-// v: elements of an access.  Short if a group's units fit a wave with TEAM_ELEMENTS elements a lane.
-static NormPlan norm_plan(const goom_norm_shape &sh, int v, bool back)
+// cap: elements of an access that addresses and types allow.  Short if a group's units fit a wave with TEAM_ELEMENTS elements a lane.
+static NormPlan norm_plan(const goom_norm_shape &sh, int cap, bool back)
 {
     NormPlan p = {};
     NormArgs &a = p.a;
@@ -487,6 +544,8 @@ static NormPlan norm_plan(const goom_norm_shape &sh, int v, bool back)
     a.type_w = sh.param_type;
     a.act = sh.activation;
     a.eps = (float)sh.eps;
+    int v = cap;
+    while (a.cg % v) v /= 2;
     p.v = v;
     const long long units = (long long)sh.length * (a.cg / v);
     const int most = TEAM_ELEMENTS / v < 8 ? TEAM_ELEMENTS / v : 8;
@@ -509,10 +568,18 @@ static NormPlan norm_plan(const goom_norm_shape &sh, int v, bool back)
         p.partial = back ? goom::align_up((size_t)p.blocks * 2 * sh.channels * 4, 256) : 0;
         return p;
     }
-    const int cu = a.cg / v;
-    a.gps = cu >= 256 ? 1 : 256 / cu;
+    // a slab: whole groups whose channels make whole units, 256 of these at most (or one group)
+    int least = 1;
+    for (v = cap; v > 1; v /= 2) {
+        for (least = 1; least * a.cg % v; least *= 2) {}
+        if (sh.channels % v == 0 && (least == 1 || least * a.cg / v <= 256)) break;
+        least = 1;
+    }
+    p.v = v;
+    a.gps = (int)(256ll * v / ((long long)a.cg * least) * least);
+    if (a.gps < least) a.gps = least;
     if (a.gps > sh.groups) a.gps = sh.groups;
-    const int columns = a.gps * cu < 256 ? a.gps * cu : 256;
+    const int columns = a.gps * a.cg / v < 256 ? a.gps * a.cg / v : 256;
     a.rows_at_once = 512 / columns > 0 ? 512 / columns : 1;
     if (columns * a.rows_at_once > 320 && a.rows_at_once > 1) { // 256 to 320 threads where that wastes fewer lanes
         const int half = a.rows_at_once / 2;
@@ -537,21 +604,19 @@ static NormPlan norm_plan(const goom_norm_shape &sh, int v, bool back)
 static size_t norm_bytes(const goom_norm_shape &sh, bool back)
 {
     size_t most = 0;
-    for (int v = 1; v <= 8; v *= 2)
-        if ((sh.channels / sh.groups) % v == 0 && v * real_bytes(sh.type) <= 16) {
-            const NormPlan p = norm_plan(sh, v, back);
-            const size_t need = p.stats + p.sums + p.means + p.partial;
-            if (need > most) most = need;
-        }
+    for (int cap = 1; cap * real_bytes(sh.type) <= 16; cap *= 2) {
+        const NormPlan p = norm_plan(sh, cap, back);
+        const size_t need = p.stats + p.sums + p.means + p.partial;
+        if (need > most) most = need;
+    }
     return most;
 }
 
-static int norm_width(const goom_norm_shape &sh, const void *a, const void *b, const void *c)
+static int norm_cap(const goom_norm_shape &sh, const void *a, const void *b, const void *c)
 {
     const size_t size = real_bytes(sh.type);
-    const int cg = sh.channels / sh.groups;
-    int v = 8;
-    while (v > 1 && (v * size > 16 || cg % v || !goom::aligned(a, v * size) || !goom::aligned(b, v * size) || !goom::aligned(c, v * size))) v /= 2;
+    int v = (int)(16 / size);
+    while (v > 1 && (sh.channels % v || !goom::aligned(a, v * size) || !goom::aligned(b, v * size) || !goom::aligned(c, v * size))) v /= 2;
     return v;
 }
 
@@ -616,7 +681,7 @@ int goom_group_norm(goom_ctx *ctx, const goom_norm_shape *shape, const void *x, 
         return fail(ctx, GOOM_EINVAL, "misaligned data pointer");
     if (int s = check_workspace(ctx, workspace, workspace_bytes, norm_bytes(*shape, false))) return s;
     if (int s = enter(ctx)) return s;
-    NormPlan p = norm_plan(*shape, norm_width(*shape, x, y, nullptr), false);
+    NormPlan p = norm_plan(*shape, norm_cap(*shape, x, y, nullptr), false);
     NormArgs &a = p.a;
     a.x = x;
     a.weight = weight;
@@ -672,7 +737,7 @@ int goom_group_norm_backward(goom_ctx *ctx, const goom_norm_shape *shape, const 
     const float *partial = nullptr;
     long long partials = 0;
     if (shape->items > 0) {
-        p = norm_plan(*shape, norm_width(*shape, x, grad_y, grad_x), true);
+        p = norm_plan(*shape, norm_cap(*shape, x, grad_y, grad_x), true);
         NormArgs &a = p.a;
         a.x = x;
         a.gy = grad_y;

@@ -84,7 +84,7 @@ def test_short_groups(g, dtype, act, items, length, channels, groups):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("items,length,channels,groups", [(2, 500, 320, 32), (1, 1, 5000, 1), (1, 70, 2600, 1), (3, 257, 9, 3), (2, 33, 1024, 2), (1, 4000, 8, 8), (40, 65, 96, 2)])
+@pytest.mark.parametrize("items,length,channels,groups", [(2, 100, 4100, 4), (3, 700, 36, 6), (2, 500, 320, 32), (1, 1, 5000, 1), (1, 70, 2600, 1), (3, 257, 9, 3), (2, 33, 1024, 2), (1, 4000, 8, 8), (40, 65, 96, 2)])
 @pytest.mark.parametrize("act", ["none", "gelu"])
 def test_long_groups(g, dtype, items, length, channels, groups, act):
     _check(g, dtype, items, length, channels, groups, act, seed=length)
