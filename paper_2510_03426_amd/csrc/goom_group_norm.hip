@@ -234,33 +234,6 @@ template <typename S, int V, int J, bool BACK> __global__ __launch_bounds__(256)
     }
 }
 
-// gw[c] = sum of partial[k][0][c], gb[c] = sum of partial[k][1][c] over k < n; 32 channels a workgroup, 32 runs of k each
-__global__ __launch_bounds__(1024) void norm_weight_kernel(const float *partial, long long n, int channels, void *gw, void *gb, int type_w)
-{
-    __shared__ double meet[32][32];
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
-    const long long len = (n + 31) / 32, begin = part * len, end = begin + len < n ? begin + len : n;
-    double sum = 0.0;
-    if (c < channels)
-        for (long long k0 = begin; k0 < end; k0 += 32) {
-            float x[32];
-#pragma unroll
-            for (int k = 0; k < 32; k++) x[k] = partial[((k0 + k < end ? k0 + k : begin) * 2 + blockIdx.y) * channels + c];
-#pragma unroll
-            for (int k = 0; k < 32; k++) sum += k0 + k < end ? (double)x[k] : 0.0;
-        }
-    meet[part][threadIdx.x & 31] = sum;
-    __syncthreads();
-    void *out = blockIdx.y ? gb : gw;
-    if (part == 0 && c < channels && out) {
-#pragma unroll
-        for (int k = 1; k < 32; k++) sum += meet[k][threadIdx.x];
-        if (type_w == GOOM_REAL_F32) reinterpret_cast<float *>(out)[c] = (float)sum;
-        else if (type_w == GOOM_REAL_BF16) reinterpret_cast<bf16 *>(out)[c] = (bf16)(float)sum;
-        else reinterpret_cast<f16 *>(out)[c] = (f16)(float)sum;
-    }
-}
-
 // ---- long groups.  Thread (tx, ty): units tx, tx + columns, ... of the slab's V-element units (whatever groups their channels
 // belong to), positions ty, ty + rows_at_once, ... of the chunk, DEEP of them loaded at once.  A slab of several groups has at
 // most as many units as a workgroup has columns.  grid: (items chunks, slabs)
@@ -460,33 +433,62 @@ template <typename S, int V> __global__ __launch_bounds__(512) void norm_sums_ke
     }
 }
 
-// means over a group of dz w and of dz w xhat; a workgroup a group.  grid: items groups
-__global__ __launch_bounds__(256) void norm_means_kernel(NormArgs a)
+// The first `groups` workgroups (items groups, or none): means over a group of dz w and of dz w xhat.  The others:
+// gw[c] = sum of partial[k][0][c], gb[c] = sum of partial[k][1][c] over k < n; 32 channels a workgroup, 32 runs of k each.
+struct WeightArgs { const float *partial; long long n; void *gw, *gb; };
+__global__ __launch_bounds__(1024) void norm_finish_kernel(NormArgs a, unsigned groups, WeightArgs t)
 {
-    __shared__ double meet[2][4];
-    const long long item = blockIdx.x / a.groups;
-    const int group = blockIdx.x % a.groups;
-    double m1 = 0.0, m2 = 0.0;
-    for (long long u = threadIdx.x; u < a.chunks * a.cg; u += 256) {
-        const long long k = u / a.cg;
-        const int ch = group * a.cg + (int)(u - k * a.cg);
-        const float *from = a.sums + (item * a.chunks + k) * 2 * a.channels + ch;
-        const double w = (double)param(a.weight, a.type_w, ch, 1.0f);
-        m2 += w * (double)from[0];
-        m1 += w * (double)from[a.channels];
+    __shared__ double meet[32][32];
+    if (blockIdx.x < groups) {
+        const long long item = blockIdx.x / a.groups;
+        const int group = blockIdx.x % a.groups, wave = threadIdx.x >> 6;
+        double m1 = 0.0, m2 = 0.0;
+        for (long long u = threadIdx.x; u < a.chunks * a.cg; u += 1024) {
+            const long long k = u / a.cg;
+            const int ch = group * a.cg + (int)(u - k * a.cg);
+            const float *from = a.sums + (item * a.chunks + k) * 2 * a.channels + ch;
+            const double w = (double)param(a.weight, a.type_w, ch, 1.0f);
+            m2 += w * (double)from[0];
+            m1 += w * (double)from[a.channels];
+        }
+        for (int m = 1; m < 64; m *= 2) {
+            m1 += __shfl_xor(m1, m);
+            m2 += __shfl_xor(m2, m);
+        }
+        if ((threadIdx.x & 63) == 0) {
+            meet[0][wave] = m1;
+            meet[1][wave] = m2;
+        }
+        __syncthreads();
+        if (threadIdx.x < 2) {
+            double sum = 0.0;
+#pragma unroll
+            for (int k = 0; k < 16; k++) sum += meet[threadIdx.x][k];
+            a.means[blockIdx.x * 2ll + threadIdx.x] = (float)(sum / ((double)a.length * a.cg));
+        }
+        return;
     }
-    for (int m = 1; m < 64; m *= 2) {
-        m1 += __shfl_xor(m1, m);
-        m2 += __shfl_xor(m2, m);
-    }
-    if ((threadIdx.x & 63) == 0) {
-        meet[0][threadIdx.x >> 6] = m1;
-        meet[1][threadIdx.x >> 6] = m2;
-    }
+    const unsigned at = blockIdx.x - groups;
+    const int c = at / 2 * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
+    const long long len = (t.n + 31) / 32, begin = part * len, end = begin + len < t.n ? begin + len : t.n;
+    double sum = 0.0;
+    if (c < a.channels)
+        for (long long k0 = begin; k0 < end; k0 += 32) {
+            float x[32];
+#pragma unroll
+            for (int k = 0; k < 32; k++) x[k] = t.partial[((k0 + k < end ? k0 + k : begin) * 2 + at % 2) * a.channels + c];
+#pragma unroll
+            for (int k = 0; k < 32; k++) sum += k0 + k < end ? (double)x[k] : 0.0;
+        }
+    meet[part][threadIdx.x & 31] = sum;
     __syncthreads();
-    if (threadIdx.x < 2) {
-        const double n = (double)a.length * a.cg;
-        a.means[blockIdx.x * 2ll + threadIdx.x] = (float)(((meet[threadIdx.x][0] + meet[threadIdx.x][1]) + (meet[threadIdx.x][2] + meet[threadIdx.x][3])) / n);
+    void *out = at % 2 ? t.gb : t.gw;
+    if (part == 0 && c < a.channels && out) {
+#pragma unroll
+        for (int k = 1; k < 32; k++) sum += meet[k][threadIdx.x];
+        if (a.type_w == GOOM_REAL_F32) reinterpret_cast<float *>(out)[c] = (float)sum;
+        else if (a.type_w == GOOM_REAL_BF16) reinterpret_cast<bf16 *>(out)[c] = (bf16)(float)sum;
+        else reinterpret_cast<f16 *>(out)[c] = (f16)(float)sum;
     }
 }
 
@@ -734,58 +736,62 @@ int goom_group_norm_backward(goom_ctx *ctx, const goom_norm_shape *shape, const 
     if (int s = check_workspace(ctx, workspace, workspace_bytes, shape->items ? norm_bytes(*shape, true) : 0)) return s;
     if (int s = enter(ctx)) return s;
     NormPlan p = {};
-    const float *partial = nullptr;
-    long long partials = 0;
     if (shape->items > 0) {
         p = norm_plan(*shape, norm_cap(*shape, x, grad_y, grad_x), true);
-        NormArgs &a = p.a;
-        a.x = x;
-        a.gy = grad_y;
-        a.weight = weight;
-        a.bias = bias;
-        a.y = grad_x;
-        a.mean = const_cast<float *>(mean);
-        a.rstd = const_cast<float *>(rstd);
-        a.partial = a.sums = reinterpret_cast<float *>(workspace);
-        a.means = reinterpret_cast<float *>(reinterpret_cast<unsigned char *>(workspace) + p.sums);
-        partial = a.partial;
-        partials = p.blocks; // workgroups along the items, or items chunks: [partials][2][channels] either way
-        const int rc = with_type(shape->type, [&](auto tag) {
-            typedef typename decltype(tag)::type S;
-            const dim3 grid((unsigned)p.blocks, (unsigned)p.parts);
-            if (p.team) {
+    } else { // sums over nothing
+        p.team = true;
+        p.a.channels = shape->channels;
+        p.a.type_w = shape->param_type;
+    }
+    NormArgs &a = p.a;
+    a.x = x;
+    a.gy = grad_y;
+    a.weight = weight;
+    a.bias = bias;
+    a.y = grad_x;
+    a.mean = const_cast<float *>(mean);
+    a.rstd = const_cast<float *>(rstd);
+    a.partial = a.sums = reinterpret_cast<float *>(workspace);
+    a.means = reinterpret_cast<float *>(reinterpret_cast<unsigned char *>(workspace) + p.sums);
+    // p.blocks: workgroups along the items, or items chunks: [blocks][2][channels] partial sums either way
+    const WeightArgs weights = {a.sums, p.blocks, grad_weight, grad_bias};
+    const unsigned wants_weights = grad_weight || grad_bias ? (unsigned)((shape->channels + 31) / 32 * 2) : 0;
+    return with_type(shape->type, [&](auto tag) {
+        typedef typename decltype(tag)::type S;
+        const dim3 grid((unsigned)p.blocks, (unsigned)p.parts);
+        if (p.team) {
+            if (shape->items > 0) {
                 goom::prof_begin(ctx, "group norm gradient");
                 with_team<S>(p.v, p.j, [&](auto vec, auto units) {
                     norm_team_kernel<S, decltype(vec)::value, decltype(units)::value, true><<<grid, 256, 0, ctx->stream>>>(a);
                     return 0;
                 });
                 goom::prof_end(ctx);
-            } else {
-                const int threads = (a.threads + 63) / 64 * 64;
-                goom::prof_begin(ctx, "group norm gradient: sums");
-                with_width<S>(p.v, [&](auto vec) {
-                    norm_sums_kernel<S, decltype(vec)::value><<<grid, threads, 0, ctx->stream>>>(a);
-                    return 0;
-                });
-                norm_means_kernel<<<(unsigned)(a.items * a.groups), 256, 0, ctx->stream>>>(a);
-                goom::prof_end(ctx);
-                goom::prof_begin(ctx, "group norm gradient");
-                with_width<S>(p.v, [&](auto vec) {
-                    norm_grad_kernel<S, decltype(vec)::value><<<grid, threads, 0, ctx->stream>>>(a);
-                    return 0;
-                });
+            }
+            if (wants_weights) {
+                goom::prof_begin(ctx, "group norm gradient: weights");
+                norm_finish_kernel<<<wants_weights, 1024, 0, ctx->stream>>>(a, 0, weights);
                 goom::prof_end(ctx);
             }
-            return goom::check_hip(ctx, hipGetLastError(), "group norm gradient");
-        });
-        if (rc) return rc;
-    }
-    if (grad_weight || grad_bias) {
-        goom::prof_begin(ctx, "group norm gradient: weights");
-        norm_weight_kernel<<<dim3((shape->channels + 31) / 32, 2), 1024, 0, ctx->stream>>>(partial, partials, shape->channels, grad_weight, grad_bias, shape->param_type);
-        goom::prof_end(ctx);
-    }
-    return goom::check_hip(ctx, hipGetLastError(), "group norm gradient: weights");
+        } else {
+            const int threads = (a.threads + 63) / 64 * 64;
+            const unsigned groups = (unsigned)(a.items * a.groups);
+            goom::prof_begin(ctx, "group norm gradient: sums");
+            with_width<S>(p.v, [&](auto vec) {
+                norm_sums_kernel<S, decltype(vec)::value><<<grid, threads, 0, ctx->stream>>>(a);
+                return 0;
+            });
+            norm_finish_kernel<<<groups + wants_weights, 1024, 0, ctx->stream>>>(a, groups, weights);
+            goom::prof_end(ctx);
+            goom::prof_begin(ctx, "group norm gradient");
+            with_width<S>(p.v, [&](auto vec) {
+                norm_grad_kernel<S, decltype(vec)::value><<<grid, threads, 0, ctx->stream>>>(a);
+                return 0;
+            });
+            goom::prof_end(ctx);
+        }
+        return goom::check_hip(ctx, hipGetLastError(), "group norm gradient");
+    });
 }
 
 } // extern "C"
