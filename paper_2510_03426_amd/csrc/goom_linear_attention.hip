@@ -244,12 +244,12 @@ template <typename S, int D, int THREADS, int CH> struct TileRows {
     }
     template <int PITCH> __device__ inline void put(bf16 *tile, int n, int d) const
     {
-        const bool there = col0() < d;
+        const bool there = col0() < d, whole = n == CH && d == D;
         bf16 *const to0 = tile + row0() * PITCH + col0();
 #pragma unroll
         for (int k = 0; k < N; k++) {
             SV v = x[k];
-            if (!there || (n != CH && row0() + k * STEP >= n)) v = SV{};
+            if (!whole && (!there || row0() + k * STEP >= n)) v = SV{};
             Frag p[Parts<S>::IN];
             split_in(v, p);
 #pragma unroll
@@ -259,6 +259,10 @@ template <typename S, int D, int THREADS, int CH> struct TileRows {
     }
 };
 
+// Powers of the decay in LDS, written once a walk: formed in every chunk anew they were a quarter of its instructions.  PAIRS: the
+// weights of eight neighbouring j (zeros where there is no pair) for each i - j of the first of them
+constexpr int PAIRS = 96;
+
 template <typename S, int DK, int DV, int NW, bool OUT> struct WalkLds {
     // Tokens of a step.  Inputs of two and three parts: half, so that two workgroups share a CU (20,700 cycles a chunk of 64 with one).
     // Where only the state is wanted, twice as many: more loads in flight for each barrier.
@@ -267,7 +271,8 @@ template <typename S, int DK, int DV, int NW, bool OUT> struct WalkLds {
     static constexpr int PK = DK + PITCH_PAD, PV = DV + PITCH_PAD;
     static constexpr int K_TILE = CH * PK * Parts<S>::IN, V_TILE = CH * PV * Parts<S>::IN; // elements
     static constexpr int P_FRAGS = OUT ? P_BLOCKS * Parts<S>::OUT * 64 : 0;
-    static constexpr size_t bytes = (K_TILE * (OUT ? 2 : 1) + V_TILE) * sizeof(bf16) + P_FRAGS * sizeof(Frag);
+    static constexpr int WEIGHTS = CH + (OUT ? CH + 8 * PAIRS : 0); // floats
+    static constexpr size_t bytes = (K_TILE * (OUT ? 2 : 1) + V_TILE) * sizeof(bf16) + P_FRAGS * sizeof(Frag) + WEIGHTS * sizeof(float);
     // workgroups of a CU: as many as its LDS holds, and no more than leave their waves the registers for the state (DK DV / 64 NW
     // a lane), the outputs and the rows on their way: three waves a SIMD with 168 each, or two with 256
     static constexpr int waves = DK * DV / (64 * NW) > 16 ? 2 : 3;
@@ -298,7 +303,10 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
     constexpr int IP = Parts<S>::IN, OP = Parts<S>::OUT, SP = Parts<S>::STATE;
     constexpr int CH = Lds::CH, KP = CH * Lds::PK, VP = CH * Lds::PV; // tokens of a step, elements from part to part
     static_assert(NT == 1 || NT == 2, "a wave has one or two column tiles");
-    Frag *const p_lds = reinterpret_cast<Frag *>(lds);
+    f32x8 *const pair_weights = reinterpret_cast<f32x8 *>(lds);                      // (OUT)
+    float *const row_weights = reinterpret_cast<float *>(lds) + (OUT ? 8 * PAIRS : 0); // (OUT) w g^x
+    float *const state_weights = row_weights + (OUT ? CH : 0);                         // u g^(CH - j')
+    Frag *const p_lds = reinterpret_cast<Frag *>(reinterpret_cast<float *>(lds) + Lds::WEIGHTS);
     bf16 *const b_lds = reinterpret_cast<bf16 *>(p_lds + Lds::P_FRAGS);
     bf16 *const c_lds = b_lds + Lds::K_TILE;
     bf16 *const a_lds = c_lds + Lds::V_TILE;
@@ -306,7 +314,7 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
     const bool last = REV ? at.seg == 0 : at.seg == at.nseg - 1; // in walking order
     if (!OUT && last) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-    const float log2_g = log2_decay(w.log_decay[h]);
+    const float g2 = log2_decay(w.log_decay[h]);
     const int col0 = wave * NT * 16; // the wave's columns: col0 + (i / 4) CS + 4 nt + i % 4
 
     // ---- the incoming state
@@ -323,7 +331,7 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
             if (OUT && total && !empty) {
                 x = *reinterpret_cast<const f32x4 *>(total + (nt * (DK / 16) + t) * 256);
             } else if (OUT && r.init) {
-                const float scale = REV || empty ? 1.0f : decay_power(log2_g, 1);
+                const float scale = REV || empty ? 1.0f : decay_power(g2, 1);
                 const int col = col0 + (i >> 2) * CS + 4 * nt + (i & 3);
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
@@ -352,11 +360,17 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
         cx.fetch(c + t0 * r.c_tok, r.c_tok, n, nc, c_vec);
     };
     if (nchunks > 0) fetch(0);
+    if (OUT) {
+        for (int u = threadIdx.x; u < 8 * PAIRS; u += THREADS) {
+            const int first = REV ? 31 - u / 8 : u / 8 - 32, age = REV ? u % 8 - first : first - u % 8; // i - j of the eight's first j
+            reinterpret_cast<float *>(pair_weights)[u] = age >= 0 ? r.p_scale * decay_power(g2, age) : 0.0f;
+        }
+        for (int x = threadIdx.x; x < CH; x += THREADS) row_weights[x] = r.w_scale * decay_power(g2, x);
+    }
+    for (int x = threadIdx.x; x < CH; x += THREADS) state_weights[x] = r.u_scale * decay_power(g2, REV ? x + 1 : CH - x);
     for (int step = 0; step < nchunks; step++) {
         const long long t0 = chunk_at(step);
         const int n = chunk_rows(t0);
-        float g2 = log2_g;
-        asm volatile("" : "+v"(g2)); // the chunk's weights are formed anew for each: kept, they would take some 50 registers
         __syncthreads();
         if (OUT) ax.template put<Lds::PK>(a_lds, n, r.ka);
         bx.template put<Lds::PK>(b_lds, n, r.ka);
@@ -381,15 +395,8 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
                     p0 = product<3>(b0, af, p0);
                     p1 = product<3>(b1, af, p1);
                 }
-                f32x8 x;
-                int first = it * 16 + i - ks * 32 - g * 8; // i - j of the lane's first j
-                asm volatile("" : "+v"(first));            // (and so are the masks)
-                const float at = g2 * (float)(REV ? -first : first), by = REV ? g2 : -g2;
-#pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    const float p = (e < 4 ? p0[e & 3] : p1[e & 3]) * (r.p_scale * __builtin_amdgcn_exp2f(at + by * (float)e));
-                    x[e] = (REV ? e >= first : e <= first) ? p : 0.0f;
-                }
+                const int first = it * 16 + i - ks * 32 - g * 8; // i - j of the lane's first j
+                const f32x8 x = __builtin_shufflevector(p0, p1, 0, 1, 2, 3, 4, 5, 6, 7) * pair_weights[REV ? 31 - first : first + 32];
                 Frag parts[OP];
                 split(x, parts);
 #pragma unroll
@@ -441,7 +448,7 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
 #pragma unroll
             for (int it = 0; it < CH / 16; it++) {
                 const int row = it * 16 + i, age = REV ? n - 1 - row : row;
-                const float scale = r.w_scale * decay_power(g2, age > 0 ? age : 0);
+                const float scale = row_weights[age > 0 ? age : 0];
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++) y[it][nt] *= scale;
 #pragma unroll
@@ -486,14 +493,12 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
 #pragma unroll
         for (int ks = 0; ks < CH / 32; ks++) {
             f32x8 wt; // u g^(n - j'); rows past the end, where it would grow, are zeros
-            const int first = REV ? ks * 32 + g * 8 + 1 : n - ahead - ks * 32 - g * 8;
-            const float at = g2 * (float)first, by = REV ? g2 : -g2;
-            if (n == CH) {
-#pragma unroll
-                for (int e = 0; e < 8; e++) wt[e] = r.u_scale * __builtin_amdgcn_exp2f(at + by * (float)e);
+            if (REV || (n == CH && !ahead)) {
+                wt = *reinterpret_cast<const f32x8 *>(state_weights + ks * 32 + g * 8);
             } else {
+                const int first = n - ahead - ks * 32 - g * 8;
 #pragma unroll
-                for (int e = 0; e < 8; e++) wt[e] = !REV && first - e < 0 ? 0.0f : r.u_scale * __builtin_amdgcn_exp2f(at + by * (float)e);
+                for (int e = 0; e < 8; e++) wt[e] = first - e < 0 ? 0.0f : r.u_scale * decay_power(g2, first - e);
             }
             Frag cd[NT][SP];
 #pragma unroll
