@@ -502,8 +502,9 @@ typedef struct goom_attention_shape {
  * is cut off); state: NULL (zero) or [seqs, heads, dk, dv] floats, S before the first token; final_state: NULL or the same
  * shape, S after the last one (the state itself for a sequence without tokens; it may be the array `state`).
  * The sequences are cut into segments where they are few: segment totals, their carries, then every segment walked from its
- * incoming state, 64 tokens at a time on the matrix instructions.  bfloat16: operands computed on the way are held in two
- * bf16 parts (16 bits; three, 24 bits, where they enter a state); others run on float operands throughout.
+ * incoming state, 64 tokens at a time on the matrix instructions.  All of them are sums of one
+ * (bfloat16), two (half) or three (float) bf16 parts; operands computed on the way are held in two parts (16 bits), or three (24
+ * bits) for floats and where they enter a state that is returned.
  * A NaN or an infinity among q, k, v may show in all outputs of its head in its sequence.
  * workspace: goom_linear_attention_workspace_bytes(shape, offsets != NULL) bytes (may be 0).
  * Errors: GOOM_EINVAL (null or misaligned pointers, sizes, types), GOOM_EUNSUPPORTED (dk or dv above GOOM_MAX_DIM),
