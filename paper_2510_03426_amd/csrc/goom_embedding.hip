@@ -434,7 +434,8 @@ static EmbeddingPlan embedding_plan(long long n, long long vocab, int width)
 static int check_embedding(goom_ctx *ctx, long long n, long long vocab, int width)
 {
     if (n < 0 || vocab <= 0 || width <= 0) return goom::fail(ctx, GOOM_EINVAL, "n must not be negative, vocab and width positive");
-    if (n >= (1ll << 31) || vocab >= (1ll << 31) || (double)vocab * width > 1e12) return goom::fail(ctx, GOOM_EUNSUPPORTED, "up to 2^31 - 1 tokens and table rows, and 10^12 entries");
+    if (n >= (1ll << 31) || vocab >= (1ll << 31) || (double)vocab * width > 1e11 || (double)n * width > 1e12)
+        return goom::fail(ctx, GOOM_EUNSUPPORTED, "up to 2^31 - 1 tokens and table rows, 10^11 entries of the table and 10^12 of the rows");
     return GOOM_OK;
 }
 

@@ -115,13 +115,14 @@ template <typename S, int V, int J, bool BACK> __global__ __launch_bounds__(256)
     const bool live = ti < a.ipw && group < a.groups;
     const int cu = a.cg / V, units = cu * (int)a.length;
     const float count = (float)a.cg * (float)a.length;
-    int off[J], chan[J];     // of this lane's units: element offsets within the item, channels
+    unsigned off[J]; // of this lane's units: element offsets within the item (2^31 at most), channels
+    int chan[J];
     float w[J][V], b[J][V], sw[J][V], sb[J][V];
 #pragma unroll
     for (int j = 0; j < J; j++) {
         const int u = lane + j * a.team;
         chan[j] = live && u < units ? group * a.cg + u % cu * V : -1;
-        off[j] = chan[j] >= 0 ? u / cu * a.channels + chan[j] : 0;
+        off[j] = chan[j] >= 0 ? (unsigned)(u / cu) * (unsigned)a.channels + chan[j] : 0u;
         params<V>(a.weight, a.type_w, chan[j] >= 0 ? chan[j] : 0, 1.0f, w[j]);
         params<V>(a.bias, a.type_w, chan[j] >= 0 ? chan[j] : 0, 0.0f, b[j]);
 #pragma unroll
@@ -636,6 +637,12 @@ static int check_norm(goom_ctx *ctx, const goom_norm_shape *sh)
     return GOOM_OK;
 }
 
+static int check_grid(goom_ctx *ctx, const NormPlan &p)
+{
+    if (p.blocks > 0x7fffffffll || p.parts > 65535) return goom::fail(ctx, GOOM_EUNSUPPORTED, "too many items or groups");
+    return GOOM_OK;
+}
+
 // f(vector width, units a lane)
 template <typename S, typename F> static int with_team(int v, int j, F f)
 {
@@ -684,6 +691,7 @@ int goom_group_norm(goom_ctx *ctx, const goom_norm_shape *shape, const void *x, 
     if (int s = check_workspace(ctx, workspace, workspace_bytes, norm_bytes(*shape, false))) return s;
     if (int s = enter(ctx)) return s;
     NormPlan p = norm_plan(*shape, norm_cap(*shape, x, y, nullptr), false);
+    if (int s = check_grid(ctx, p)) return s;
     NormArgs &a = p.a;
     a.x = x;
     a.weight = weight;
@@ -738,6 +746,7 @@ int goom_group_norm_backward(goom_ctx *ctx, const goom_norm_shape *shape, const 
     NormPlan p = {};
     if (shape->items > 0) {
         p = norm_plan(*shape, norm_cap(*shape, x, grad_y, grad_x), true);
+        if (int s = check_grid(ctx, p)) return s;
     } else { // sums over nothing
         p.team = true;
         p.a.channels = shape->channels;

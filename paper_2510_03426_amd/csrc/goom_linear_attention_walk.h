@@ -551,7 +551,7 @@ __global__ __launch_bounds__(NW * 64, (WalkLds<S, DK, DV, NW, OUT>::per_simd)) v
     const int part = item % w.parts, h = item / w.parts % w.heads;
     const long long slot = item / w.parts / w.heads;
     const Place at = find_place(w, slot);
-    if (at.seg >= at.nseg || part * DV >= r.nc) return;
+    if (at.seg < 0 || at.seg >= at.nseg || part * DV >= r.nc) return; // a slot that no sequence has
     constexpr int FULL = Parts<S>::STATE, SHORT = Parts<S>::OUT;
     if (FULL == SHORT || r.fin) {
         if (r.reverse) walk<S, DK, DV, NW, OUT, true, FULL>(w, r, at, slot, h, part, lds);

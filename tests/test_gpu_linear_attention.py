@@ -208,6 +208,36 @@ def test_final_state_may_replace_the_first(g):
     assert torch.equal(o2, o) and torch.equal(state, last)
 
 
+@pytest.mark.parametrize("offsets", [[100, 700, 1400], [700, 200, 1100], [1500, 1500, -3], [5, 5000, 9]])
+def test_offsets_that_are_none(g, offsets):
+    """Offsets that reach outside 0 .. tokens are cut off there; what they name is computed.  Offsets that fall promise no results, but
+    nothing outside the sequences they name is touched either."""
+    torch, _ = _torch()
+    from oracle import layer_oracle as lo
+    import ctypes as C
+    q, k, v, do, ld, s0, _ = (x.cuda() for x in _inputs("f32", 1500, 1, 1, 32, 32, 2, 3))
+    off = torch.tensor(offsets, device="cuda")
+    cut = [(min(max(a, 0), 1500), min(max(b, min(max(a, 0), 1500)), 1500)) for a, b in zip(offsets, offsets[1:])]
+    shape, pq, pk, pv = g._attention(q, k, v, ld, off, 1.0)
+    need = g.lib.goom_linear_attention_workspace_bytes(C.byref(shape), 1)
+    ws = torch.full((need + 4096,), 9, dtype=torch.uint8, device="cuda")
+    held, last = torch.full((1500 + 128, 1, 32), 7.0, device="cuda"), torch.empty(2, 1, 32, 32, device="cuda")
+    o = held[64:-64]
+    p = lambda t: C.c_void_p(t.data_ptr())  # noqa: E731
+    assert g.lib.goom_linear_attention(g._ctx, C.byref(shape), pq, pk, pv, p(ld), p(off), p(s0), p(o), p(last), p(ws), need) == 0
+    inside = torch.zeros(1500, dtype=torch.bool)
+    rising = all(a <= b for a, b in zip([a for a, _ in cut], [a for a, _ in cut][1:]))
+    for s, (a, b) in enumerate(cut):
+        inside[a:b] = True
+        if not rising:
+            continue
+        want, wl = lo.attention(_f64(q)[a:b], _f64(k)[a:b], _f64(v)[a:b], _f64(ld), _f64(s0)[s:s + 1])
+        mag, ml = lo.attention(*(np.abs(_f64(x)[a:b]) for x in (q, k, v)), _f64(ld), np.abs(_f64(s0)[s:s + 1]))
+        _near(last[s:s + 1], wl, ml, "f32", 160, False, "state")
+        _near(o[a:b], want, mag, "f32", 160, False, "o")
+    assert (o.cpu()[~inside] == 7).all() and (held[:64] == 7).all() and (held[-64:] == 7).all() and (ws[need:] == 9).all()
+
+
 def test_another_stream_and_graph(g):
     """Work follows the context's stream; a captured call, replayed on new inputs, gives what an eager one gives."""
     torch, _ = _torch()
