@@ -499,7 +499,7 @@ typedef struct goom_attention_shape {
 /* All tokens of all sequences.  q: [tokens, heads, dk], k: [tokens, kv_heads, dk], v: [tokens, kv_heads, dv];
  * o: [tokens, heads, dv], contiguous; log_decay: [heads] floats; offsets: NULL, or seqs + 1 int64 (device, rising from 0 to
  * tokens): sequence s has the tokens offsets[s] .. offsets[s + 1] - 1, none if they are equal (what lies outside 0 .. tokens
- * is cut off; outputs of tokens that no sequence has are not written); state: NULL (zero) or [seqs, heads, dk, dv] floats, S before the first token; final_state: NULL or the same
+ * is cut off; outputs of tokens that no sequence has are not written; falling offsets have no meaning, and touch nothing else); state: NULL (zero) or [seqs, heads, dk, dv] floats, S before the first token; final_state: NULL or the same
  * shape, S after the last one (the state itself for a sequence without tokens; it may be the array `state`).
  * The sequences are cut into segments where they are few: segment totals, their carries, then every segment walked from its
  * incoming state, 64 tokens at a time on the matrix instructions.  All of them are sums of one

@@ -23,6 +23,7 @@ template <typename S> __global__ __launch_bounds__(256) void shared_sum_kernel(S
 
 // ---- single tokens: S <- g S + k v^T, o = scale q^T S.  One pass over the state, bound by its bytes.  A workgroup has 32
 // columns of a head's state (eight groups of four) and its threads every 32nd row; their sums meet in LDS in a fixed order.
+// 256 sequences of 16 heads of 128 x 128: 109 us, 5.0 TB/s.
 template <typename S, bool VEC> __global__ __launch_bounds__(256) void step_kernel(goom_attention_shape sh, const S *q, const S *k, const S *v, const float *log_decay,
                                                                                   const float *state, S *o, float *next)
 {
