@@ -502,7 +502,7 @@ typedef struct goom_attention_shape {
  * is cut off; outputs of tokens that no sequence has are not written; falling offsets have no meaning, and touch nothing else); state: NULL (zero) or [seqs, heads, dk, dv] floats, S before the first token; final_state: NULL or the same
  * shape, S after the last one (the state itself for a sequence without tokens; it may be the array `state`).
  * The sequences are cut into segments where they are few: segment totals, their carries, then every segment walked from its
- * incoming state, 64 tokens at a time on the matrix instructions.  All of them are sums of one
+ * incoming state, 64 tokens (32 for halves and floats) at a time on the matrix instructions.  All of them are sums of one
  * (bfloat16), two (half) or three (float) bf16 parts; operands computed on the way are held in two parts (16 bits), or three (24
  * bits) for floats and where they enter a state that is returned.
  * A NaN or an infinity among q, k, v may show in all outputs of its head in its sequence.
@@ -525,7 +525,7 @@ int goom_linear_attention_step(goom_ctx *ctx, const goom_attention_shape *shape,
  *     grad_q_i = u sum_{j <= i} gamma^(i-j) (grad_o_i . v_j) k_j,   grad_k_j = u sum_{i >= j} gamma^(i-j) (v_j . grad_o_i) q_i,
  *     grad_v_j = u sum_{i >= j} gamma^(i-j) (k_j . q_i) grad_o_i,
  * and the terms of the first and the final state: three walks of the forward kind, two of them backwards in time.
- * Everything else as for goom_linear_attention, whose inputs are given again.
+ * The decays are given: there is no gradient for them.  Everything else as for goom_linear_attention, whose inputs are given again.
  * workspace: goom_linear_attention_backward_workspace_bytes(shape, offsets != NULL) bytes (may be 0). */
 int goom_linear_attention_backward(goom_ctx *ctx, const goom_attention_shape *shape, const void *q, const void *k, const void *v,
                                    const float *log_decay, const int64_t *offsets, const float *state, const void *grad_o,

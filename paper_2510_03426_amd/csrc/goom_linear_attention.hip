@@ -8,16 +8,22 @@ namespace goom_layer {
 
 // sums over heads that share keys and values: y[token][kv head][.] = sum over the group of x[token][head][.], floats.  Two such
 // arrays in one launch, blockIdx.y apart
-struct SharedSum { const float *x; void *y; long long n; int d; };
-template <typename S> __global__ __launch_bounds__(256) void shared_sum_kernel(SharedSum k, SharedSum v, int group)
+struct SharedSum { const float *x; void *y; long long n; int d; }; // n: units of V entries
+template <typename S, int V> __global__ __launch_bounds__(256) void shared_sum_kernel(SharedSum k, SharedSum v, int group)
 {
     const SharedSum &t = blockIdx.y ? v : k;
+    const int units = t.d / V;
     for (long long u = blockIdx.x * 256ll + threadIdx.x; u < t.n; u += gridDim.x * 256ll) {
-        const long long row = u / t.d;
-        const float *p = t.x + row * group * t.d + (u - row * t.d);
-        float sum = 0.0f;
-        for (int k = 0; k < group; k++) sum += p[(long long)k * t.d];
-        reinterpret_cast<S *>(t.y)[u] = (S)sum;
+        const long long row = t.n < (1ll << 31) ? (unsigned)u / (unsigned)units : u / units;
+        const float *const p = t.x + row * group * t.d + (u - row * units) * V;
+        float sum[V] = {};
+        for (int h = 0; h < group; h++) {
+            float x[V];
+            load_floats<float, V>(p + (long long)h * t.d, x);
+#pragma unroll
+            for (int e = 0; e < V; e++) sum[e] += x[e];
+        }
+        store_floats<S, V>(reinterpret_cast<S *>(t.y) + u * V, sum);
     }
 }
 
@@ -110,8 +116,10 @@ static Segments choose_segments(const goom_attention_shape &sh, int roles, bool 
         typedef typename decltype(tag)::type S;
         return with_walk<S>(sh.dk, sh.dv, [](auto rows, auto cols, auto waves) { return WalkLds<S, decltype(rows)::value, decltype(cols)::value, decltype(waves)::value, true>::resident; });
     });
-    // (sequences of different lengths: four rounds of shorter ones, which even out)
-    const long long walks = sh.seqs * sh.heads * roles, round = 256 * resident * (packed ? 4 : 1), mean = sh.seqs > 0 ? (sh.tokens + sh.seqs - 1) / sh.seqs : 0;
+    // (sequences of different lengths: two rounds of shorter ones, which even out.  Two, three, four and six rounds: 7 sequences of 9000
+    // tokens in all, 8 heads of 128, both directions 235, 276, 293 and 292 us; 20 of 30,000, 16 heads of 64 411, 386, 407 and 426;
+    // 37 of 30,011, 12 float heads of 50 and 72, forward 309, 307, 299 and 304)
+    const long long walks = sh.seqs * sh.heads * roles, round = 256 * resident * (packed ? 2 : 1), mean = sh.seqs > 0 ? (sh.tokens + sh.seqs - 1) / sh.seqs : 0;
     long long want = walks > 0 ? round / walks : 1; // segments a sequence of mean length
     // Not below two chunks each (one, where lengths differ): measured at 8 x 1000 tokens of 8 heads of 32 and 64, forward and
     // backward, 148, 139 and 140 us with four, two and one chunks; at 5 ragged sequences of 1500 tokens in all, 141, 113 and 95 us
@@ -388,9 +396,13 @@ int goom_linear_attention_backward(goom_ctx *ctx, const goom_attention_shape *sh
         const long long rows = sh.tokens * sh.kv_heads;
         return with_type(sh.type, [&](auto tag) {
             typedef typename decltype(tag)::type S;
-            const long long most = rows * (sh.dk > sh.dv ? sh.dk : sh.dv), blocks = (most + 255) / 256;
+            const bool vec = sh.dk % 4 == 0 && sh.dv % 4 == 0 && aligned(grad_k, 4 * size) && aligned(grad_v, 4 * size);
+            const int V = vec ? 4 : 1;
+            const long long most = rows * (sh.dk > sh.dv ? sh.dk : sh.dv) / V, blocks = (most + 255) / 256;
+            const SharedSum ks = {sum_k, grad_k, rows * sh.dk / V, sh.dk}, vs = {sum_v, grad_v, rows * sh.dv / V, sh.dv};
+            auto *kernel = vec ? shared_sum_kernel<S, 4> : shared_sum_kernel<S, 1>;
             goom::prof_begin(ctx, "linear attention: shared heads");
-            shared_sum_kernel<S><<<dim3((unsigned)(blocks < 16384 ? blocks : 16384), 2), 256, 0, ctx->stream>>>({sum_k, grad_k, rows * sh.dk, sh.dk}, {sum_v, grad_v, rows * sh.dv, sh.dv}, group);
+            kernel<<<dim3((unsigned)(blocks < 16384 ? blocks : 16384), 2), 256, 0, ctx->stream>>>(ks, vs, group);
             goom::prof_end(ctx);
             return goom::check_hip(ctx, hipGetLastError(), "linear attention: shared heads");
         });
