@@ -437,42 +437,59 @@ template <typename S, int V> __global__ __launch_bounds__(512) void norm_sums_ke
     }
 }
 
-// The first `groups` workgroups (items groups, or none): means over a group of dz w and of dz w xhat.  The others:
-// gw[c] = sum of partial[k][0][c], gb[c] = sum of partial[k][1][c] over k < n; 32 channels a workgroup, 32 runs of k each.
+// means over a group of dz w and of dz w xhat; a workgroup (of 256 or 1024 threads) a group.  grid: items groups
+__global__ __launch_bounds__(1024) void norm_means_kernel(NormArgs a)
+{
+    __shared__ double meet[2][16];
+    const long long item = blockIdx.x / a.groups;
+    const int group = blockIdx.x % a.groups, wave = threadIdx.x >> 6, threads = blockDim.x;
+    double m1 = 0.0, m2 = 0.0;
+    // a thread has one channel (or every threads-th) and every rows-th chunk, eight chunks' sums at once
+    const int cols = a.cg < threads ? a.cg : threads, rows = threads / cols, row = threadIdx.x / cols;
+    for (int c = threadIdx.x % cols; row < rows && c < a.cg; c += cols) {
+        const float *const from = a.sums + item * a.chunks * 2 * a.channels + group * a.cg + c;
+        double p = 0.0, q = 0.0;
+        for (long long k0 = row; k0 < a.chunks; k0 += 8ll * rows) {
+            float x[8], y[8];
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+                const float *const at = from + (k0 + k * rows < a.chunks ? k0 + k * rows : k0) * 2 * a.channels;
+                x[k] = at[0];
+                y[k] = at[a.channels];
+            }
+#pragma unroll
+            for (int k = 0; k < 8; k++)
+                if (k0 + k * rows < a.chunks) {
+                    q += (double)x[k];
+                    p += (double)y[k];
+                }
+        }
+        const double w = (double)param(a.weight, a.type_w, group * a.cg + c, 1.0f);
+        m1 += w * p;
+        m2 += w * q;
+    }
+    for (int m = 1; m < 64; m *= 2) {
+        m1 += __shfl_xor(m1, m);
+        m2 += __shfl_xor(m2, m);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        meet[0][wave] = m1;
+        meet[1][wave] = m2;
+    }
+    __syncthreads();
+    if (threadIdx.x < 2) {
+        double sum = 0.0;
+        for (int k = 0; k < threads / 64; k++) sum += meet[threadIdx.x][k];
+        a.means[blockIdx.x * 2ll + threadIdx.x] = (float)(sum / ((double)a.length * a.cg));
+    }
+}
+
+// gw[c] = sum of partial[k][0][c], gb[c] = sum of partial[k][1][c] over k < n; 32 channels a workgroup, 32 runs of k each
 struct WeightArgs { const float *partial; long long n; void *gw, *gb; };
-__global__ __launch_bounds__(1024) void norm_finish_kernel(NormArgs a, unsigned groups, WeightArgs t)
+__global__ __launch_bounds__(1024) void norm_weight_kernel(NormArgs a, WeightArgs t)
 {
     __shared__ double meet[32][32];
-    if (blockIdx.x < groups) {
-        const long long item = blockIdx.x / a.groups;
-        const int group = blockIdx.x % a.groups, wave = threadIdx.x >> 6;
-        double m1 = 0.0, m2 = 0.0;
-        for (long long u = threadIdx.x; u < a.chunks * a.cg; u += 1024) {
-            const long long k = u / a.cg;
-            const int ch = group * a.cg + (int)(u - k * a.cg);
-            const float *from = a.sums + (item * a.chunks + k) * 2 * a.channels + ch;
-            const double w = (double)param(a.weight, a.type_w, ch, 1.0f);
-            m2 += w * (double)from[0];
-            m1 += w * (double)from[a.channels];
-        }
-        for (int m = 1; m < 64; m *= 2) {
-            m1 += __shfl_xor(m1, m);
-            m2 += __shfl_xor(m2, m);
-        }
-        if ((threadIdx.x & 63) == 0) {
-            meet[0][wave] = m1;
-            meet[1][wave] = m2;
-        }
-        __syncthreads();
-        if (threadIdx.x < 2) {
-            double sum = 0.0;
-#pragma unroll
-            for (int k = 0; k < 16; k++) sum += meet[threadIdx.x][k];
-            a.means[blockIdx.x * 2ll + threadIdx.x] = (float)(sum / ((double)a.length * a.cg));
-        }
-        return;
-    }
-    const unsigned at = blockIdx.x - groups;
+    const unsigned at = blockIdx.x;
     const int c = at / 2 * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
     const long long len = (t.n + 31) / 32, begin = part * len, end = begin + len < t.n ? begin + len : t.n;
     double sum = 0.0;
@@ -782,7 +799,7 @@ int goom_group_norm_backward(goom_ctx *ctx, const goom_norm_shape *shape, const 
             }
             if (wants_weights) {
                 goom::prof_begin(ctx, "group norm gradient: weights");
-                norm_finish_kernel<<<wants_weights, 1024, 0, ctx->stream>>>(a, 0, weights);
+                norm_weight_kernel<<<wants_weights, 1024, 0, ctx->stream>>>(a, weights);
                 goom::prof_end(ctx);
             }
         } else {
@@ -793,7 +810,7 @@ int goom_group_norm_backward(goom_ctx *ctx, const goom_norm_shape *shape, const 
                 norm_sums_kernel<S, decltype(vec)::value><<<grid, threads, 0, ctx->stream>>>(a);
                 return 0;
             });
-            norm_finish_kernel<<<groups + wants_weights, 1024, 0, ctx->stream>>>(a, groups, weights);
+            norm_means_kernel<<<groups, a.chunks * a.cg <= 4096 ? 256 : 1024, 0, ctx->stream>>>(a);
             goom::prof_end(ctx);
             goom::prof_begin(ctx, "group norm gradient");
             with_width<S>(p.v, [&](auto vec) {
@@ -801,6 +818,11 @@ int goom_group_norm_backward(goom_ctx *ctx, const goom_norm_shape *shape, const 
                 return 0;
             });
             goom::prof_end(ctx);
+            if (wants_weights) {
+                goom::prof_begin(ctx, "group norm gradient: weights");
+                norm_weight_kernel<<<wants_weights, 1024, 0, ctx->stream>>>(a, weights);
+                goom::prof_end(ctx);
+            }
         }
         return goom::check_hip(ctx, hipGetLastError(), "group norm gradient");
     });
