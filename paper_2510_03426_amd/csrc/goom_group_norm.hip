@@ -10,7 +10,7 @@
 // Weight gradients: one partial sum per workgroup and channel, added up in a fixed order by a last launch.
 // Measured: 32,768 tokens of 16 groups of 128 (bfloat16, SiLU) 60 us forward (4.5 TB/s), 109 + 7 us backward (3.7 TB/s; as many
 // workgroups again, and as many partial sums, took 13 us longer); 8 x 4096 positions of 32 groups of 10 (float, GELU) 11 + 22 us
-// forward, 20 + 10 + 22 us backward.
+// forward, 20 + 5 + 22 + 6 us backward.
 #include <cmath>
 
 #include "goom_real.h"
