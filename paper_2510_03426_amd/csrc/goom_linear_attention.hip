@@ -30,7 +30,7 @@ template <typename S, int V> __global__ __launch_bounds__(256) void shared_sum_k
 // ---- single tokens: S <- g S + k v^T, o = scale q^T S.  One pass over the state, bound by its bytes.  A workgroup has 32
 // columns of a head's state (eight groups of four) and its threads every 32nd row; their sums meet in LDS in a fixed order.
 // 256 sequences of 16 heads of 128 x 128: 109 us, 5.0 TB/s.
-template <typename S, bool VEC> __global__ __launch_bounds__(256) void step_kernel(goom_attention_shape sh, const S *q, const S *k, const S *v, const float *log_decay,
+template <typename S> __global__ __launch_bounds__(256) void step_kernel(goom_attention_shape sh, const S *q, const S *k, const S *v, const float *log_decay,
                                                                                   const float *state, S *o, float *next)
 {
     const int h = blockIdx.x % sh.heads, col = blockIdx.y * 32 + (threadIdx.x & 7) * 4, row0 = threadIdx.x >> 3;
@@ -54,12 +54,14 @@ template <typename S, bool VEC> __global__ __launch_bounds__(256) void step_kern
             kr[u] = (float)kh[row];
             qr[u] = (float)qh[row];
             const float *p = state ? state + base + (long long)row * sh.dv + col : nullptr;
-            if (VEC) {
-                if (p && col < sh.dv) load_floats<float, 4>(p, st[u]);
-            } else {
+            if (p && col + 4 <= sh.dv) {
+                const f32x4 four = load_unaligned<float, 4>(p);
+#pragma unroll
+                for (int e = 0; e < 4; e++) st[u][e] = four[e];
+            } else if (p) {
 #pragma unroll
                 for (int e = 0; e < 4; e++)
-                    if (p && col + e < sh.dv) st[u][e] = p[e];
+                    if (col + e < sh.dv) st[u][e] = p[e];
             }
         }
     }
@@ -73,8 +75,8 @@ template <typename S, bool VEC> __global__ __launch_bounds__(256) void step_kern
                 y[e] += qr[u] * st[u][e];
             }
             float *p = next + base + (long long)row * sh.dv + col;
-            if (VEC) {
-                if (col < sh.dv) store_floats<float, 4>(p, st[u]);
+            if (col + 4 <= sh.dv) {
+                store_floats_unaligned<float, 4>(p, st[u]);
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; e++)
@@ -147,12 +149,6 @@ static size_t totals_bytes(const goom_attention_shape &sh, const Segments &g, in
     return goom::align_up((size_t)(g.slots * sh.heads) * padded_head(ka) * padded_head(nc) * 4, 256);
 }
 
-// rows of `d` entries whose vectors of 8 elements are aligned to 16 bytes (32 for floats: read as two)
-static int vec_rows(const void *p, long long tok, long long head, int d, size_t size)
-{
-    return d % 8 == 0 && tok % 8 == 0 && head % 8 == 0 && goom::aligned(p, 8 * size);
-}
-
 static WalkArgs walk_args(const goom_attention_shape &sh, const float *log_decay, const int64_t *offsets, const Segments &g)
 {
     WalkArgs w = {};
@@ -169,19 +165,18 @@ static WalkArgs walk_args(const goom_attention_shape &sh, const float *log_decay
 
 struct Rows { const void *p; long long tok, head; int group, d; }; // one of q, k, v, grad_o
 
-static WalkRole role(const Rows &a, const Rows &b, const Rows &c, void *y, int y_float, int heads, int reverse, size_t size)
+static WalkRole role(const Rows &a, const Rows &b, const Rows &c, void *y, int y_float, int heads, int reverse)
 {
     WalkRole r = {};
-    r.a = a.p; r.a_tok = a.tok; r.a_head = a.head; r.a_group = a.group; r.a_vec = vec_rows(a.p, a.tok, a.head, a.d, size);
-    r.b = b.p; r.b_tok = b.tok; r.b_head = b.head; r.b_group = b.group; r.b_vec = vec_rows(b.p, b.tok, b.head, b.d, size);
-    r.c = c.p; r.c_tok = c.tok; r.c_head = c.head; r.c_group = c.group; r.c_vec = vec_rows(c.p, c.tok, c.head, c.d, size);
+    r.a = a.p; r.a_tok = a.tok; r.a_head = a.head; r.a_group = a.group;
+    r.b = b.p; r.b_tok = b.tok; r.b_head = b.head; r.b_group = b.group;
+    r.c = c.p; r.c_tok = c.tok; r.c_head = c.head; r.c_group = c.group;
     r.ka = a.d;
     r.nc = c.d;
     r.y = y;
     r.y_float = y_float;
     r.y_head = c.d;
     r.y_tok = (long long)heads * c.d;
-    r.y_vec = vec_rows(y, r.y_tok, r.y_head, c.d, y_float ? 4 : size);
     r.reverse = reverse;
     r.p_scale = r.w_scale = r.u_scale = 1.0f;
     r.state_row = c.d;
@@ -292,7 +287,7 @@ int goom_linear_attention(goom_ctx *ctx, const goom_attention_shape *shape, cons
     const int group = sh.heads / sh.kv_heads;
     const Rows rq = {q, sh.q_token, sh.q_head, 1, sh.dk}, rk = {k, sh.k_token, sh.k_head, group, sh.dk}, rv = {v, sh.v_token, sh.v_head, group, sh.dv};
     WalkRole &r = w.role[0];
-    r = role(rq, rk, rv, o, 0, sh.heads, 0, size);
+    r = role(rq, rk, rv, o, 0, sh.heads, 0);
     r.p_scale = r.w_scale = (float)sh.scale;
     r.init = state;
     r.fin = final_state;
@@ -312,12 +307,10 @@ int goom_linear_attention_step(goom_ctx *ctx, const goom_attention_shape *shape,
         return fail(ctx, GOOM_EINVAL, "misaligned data pointer");
     if (int s = enter(ctx)) return s;
     const dim3 grid((unsigned)(sh.seqs * sh.heads), (sh.dv + 31) / 32);
-    const bool vec = sh.dv % 4 == 0 && aligned(state, 16) && aligned(next_state, 16);
     goom::prof_begin(ctx, "linear attention: one token");
     const int rc = with_type(sh.type, [&](auto tag) {
         typedef typename decltype(tag)::type S;
-        auto *kernel = vec ? step_kernel<S, true> : step_kernel<S, false>;
-        kernel<<<grid, 256, 0, ctx->stream>>>(sh, reinterpret_cast<const S *>(q), reinterpret_cast<const S *>(k), reinterpret_cast<const S *>(v), log_decay, state,
+        step_kernel<S><<<grid, 256, 0, ctx->stream>>>(sh, reinterpret_cast<const S *>(q), reinterpret_cast<const S *>(k), reinterpret_cast<const S *>(v), log_decay, state,
                                               reinterpret_cast<S *>(o), next_state);
         return goom::check_hip(ctx, hipGetLastError(), "linear attention step");
     });
@@ -363,19 +356,19 @@ int goom_linear_attention_backward(goom_ctx *ctx, const goom_attention_shape *sh
     const Rows rq = {q, sh.q_token, sh.q_head, 1, sh.dk}, rk = {k, sh.k_token, sh.k_head, group, sh.dk}, rv = {v, sh.v_token, sh.v_head, group, sh.dv},
                rg = {grad_o, (long long)sh.heads * sh.dv, sh.dv, 1, sh.dv};
     const float scale = (float)sh.scale;
-    WalkRole gq = role(rg, rv, rk, grad_q, 0, sh.heads, 0, size);
+    WalkRole gq = role(rg, rv, rk, grad_q, 0, sh.heads, 0);
     gq.p_scale = gq.w_scale = scale;
     gq.init = state;
     gq.state_row = 1;
     gq.state_col = sh.dv;
     gq.totals = totals_q;
-    WalkRole gk = role(rv, rg, rq, shared ? (void *)sum_k : grad_k, shared, sh.heads, 1, size);
+    WalkRole gk = role(rv, rg, rq, shared ? (void *)sum_k : grad_k, shared, sh.heads, 1);
     gk.p_scale = gk.u_scale = scale;
     gk.init = grad_final;
     gk.state_row = 1;
     gk.state_col = sh.dv;
     gk.totals = totals_k;
-    WalkRole gv = role(rk, rq, rg, shared ? (void *)sum_v : grad_v, shared, sh.heads, 1, size);
+    WalkRole gv = role(rk, rq, rg, shared ? (void *)sum_v : grad_v, shared, sh.heads, 1);
     gv.p_scale = gv.u_scale = scale;
     gv.init = grad_final;
     gv.fin = grad_state;

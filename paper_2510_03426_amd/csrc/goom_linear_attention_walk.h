@@ -34,7 +34,6 @@ struct WalkRole {
     void *y;                 // NULL in walks without outputs
     long long a_tok, a_head, b_tok, b_head, c_tok, c_head, y_tok, y_head; // elements
     int a_group, b_group, c_group; // heads that share a row set: 1, or heads / kv_heads
-    int a_vec, b_vec, c_vec, y_vec; // 16-byte accesses are aligned
     int ka, nc;
     int reverse;
     int y_float;             // y holds floats, whatever the type
@@ -213,47 +212,60 @@ template <typename S, int D, int THREADS, int CH> struct TileRows {
     __device__ static inline int row0() { return threadIdx.x / (D / 8); }
     __device__ static inline int col0() { return threadIdx.x % (D / 8) * 8; }
 
-    // vec: units are aligned to their size (d a multiple of eight); else element by element
-    __device__ inline void fetch(const S *src, long long stride, int n, int d, bool vec)
+    // Units are read whole, whatever their alignment; the last one of a row whose entries make no whole units from eight entries
+    // before the row's end, and put() moves it into place.  Rows of fewer than eight entries: element by element.
+    __device__ static inline int shift(int d) { return -d & 7; }
+    __device__ inline void fetch(const S *src, long long stride, int n, int d)
     {
         // byte offsets within the chunk, 32 bits (checked by the host)
-        const unsigned col = (col0() < d ? col0() : 0) * sizeof(S), bytes = (unsigned)stride * sizeof(S);
+        const unsigned bytes = (unsigned)stride * sizeof(S), first = col0() + 8 <= d ? col0() : col0() < d && d >= 8 ? d - 8 : 0, col = first * sizeof(S);
         const char *const p = reinterpret_cast<const char *>(src);
-        if (vec) {
+        if (d >= 8) {
             if (n == CH) {
                 const unsigned at = row0() * bytes + col, step = STEP * bytes;
 #pragma unroll
                 for (int k = 0; k < N; k++)
-                    if (UNITS % THREADS == 0 || row0() + k * STEP < CH) x[k] = *reinterpret_cast<const SV *>(p + (at + k * step));
+                    if (UNITS % THREADS == 0 || row0() + k * STEP < CH) x[k] = load_unaligned<S, 8>(reinterpret_cast<const S *>(p + (at + k * step)));
             } else {
 #pragma unroll
                 for (int k = 0; k < N; k++) {
                     const int row = row0() + k * STEP;
-                    x[k] = *reinterpret_cast<const SV *>(p + ((row < n ? row : n - 1) * bytes + col));
+                    x[k] = load_unaligned<S, 8>(reinterpret_cast<const S *>(p + ((row < n ? row : n - 1) * bytes + col)));
                 }
             }
         } else {
-            const int left = col0() < d ? d - col0() : 0; // entries from this unit's first on
 #pragma unroll
             for (int k = 0; k < N; k++) {
                 const int row = row0() + k * STEP;
-                const S *const q = reinterpret_cast<const S *>(p + ((row < n ? row : n - 1) * bytes + col));
-                S e[8];
+                const S *const q = reinterpret_cast<const S *>(p + (row < n ? row : n - 1) * bytes);
 #pragma unroll
-                for (int c = 0; c < 8; c++) e[c] = q[c < left ? c : 0];
-#pragma unroll
-                for (int c = 0; c < 8; c++) x[k][c] = c < left ? e[c] : (S)0.0f;
+                for (int c = 0; c < 8; c++) x[k][c] = c < d ? q[c < d ? c : 0] : (S)0.0f;
             }
         }
     }
     template <int PITCH> __device__ inline void put(bf16 *tile, int n, int d) const
     {
-        const bool there = col0() < d, whole = n == CH && d == D;
+        if (n == CH && d == D) put_units<PITCH, false, false>(tile, n, d);
+        else if (d < 8 || !shift(d)) put_units<PITCH, true, false>(tile, n, d);
+        else put_units<PITCH, true, true>(tile, n, d);
+    }
+    // CUT: rows or columns may be missing; MOVE: the rows' last units are to be moved
+    template <int PITCH, bool CUT, bool MOVE> __device__ inline void put_units(bf16 *tile, int n, int d) const
+    {
+        const bool there = col0() < d;
         bf16 *const to0 = tile + row0() * PITCH + col0();
 #pragma unroll
         for (int k = 0; k < N; k++) {
             SV v = x[k];
-            if (!whole && (!there || row0() + k * STEP >= n)) v = SV{};
+            if (MOVE) {
+                const SV z = {};
+                SV w = v;
+                if (shift(d) & 4) w = __builtin_shufflevector(w, z, 4, 5, 6, 7, 8, 9, 10, 11);
+                if (shift(d) & 2) w = __builtin_shufflevector(w, z, 2, 3, 4, 5, 6, 7, 8, 9);
+                if (shift(d) & 1) w = __builtin_shufflevector(w, z, 1, 2, 3, 4, 5, 6, 7, 8);
+                if (col0() + 8 > d) v = w;
+            }
+            if (CUT && (!there || row0() + k * STEP >= n)) v = SV{};
             Frag p[Parts<S>::IN];
             split_in(v, p);
 #pragma unroll
@@ -351,7 +363,6 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
     const S *const c = reinterpret_cast<const S *>(r.c) + at.start * r.c_tok + h / r.c_group * r.c_head + part * DV;
     const long long seg0 = at.seg * w.seg_len, seg1 = seg0 + w.seg_len < at.len ? seg0 + w.seg_len : at.len;
     const int nchunks = (int)((seg1 - seg0 + CH - 1) / CH);
-    const bool a_vec = r.a_vec, b_vec = r.b_vec, c_vec = r.c_vec;
     TileRows<S, DK, THREADS, CH> ax, bx;
     TileRows<S, DV, THREADS, CH> cx;
     auto chunk_at = [&](int step) { return seg0 + (long long)(REV ? nchunks - 1 - step : step) * CH; };
@@ -359,9 +370,9 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
     auto fetch = [&](int step) {
         const long long t0 = chunk_at(step);
         const int n = chunk_rows(t0);
-        if (OUT) ax.fetch(a + t0 * r.a_tok, r.a_tok, n, r.ka, a_vec);
-        bx.fetch(b + t0 * r.b_tok, r.b_tok, n, r.ka, b_vec);
-        cx.fetch(c + t0 * r.c_tok, r.c_tok, n, nc, c_vec);
+        if (OUT) ax.fetch(a + t0 * r.a_tok, r.a_tok, n, r.ka);
+        bx.fetch(b + t0 * r.b_tok, r.b_tok, n, r.ka);
+        cx.fetch(c + t0 * r.c_tok, r.c_tok, n, nc);
     };
     if (nchunks > 0) fetch(0);
     if (OUT) {
@@ -471,9 +482,9 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
                     float x[NT * 4];
 #pragma unroll
                     for (int e = 0; e < NT * 4; e++) x[e] = y[it][e / 4][e % 4];
-                    if (r.y_vec && col + NT * 4 <= nc) {
-                        if (r.y_float) store_floats<float, NT * 4>(reinterpret_cast<float *>(r.y) + to + col, x);
-                        else store_floats<S, NT * 4>(reinterpret_cast<S *>(r.y) + to + col, x);
+                    if (col + NT * 4 <= nc) {
+                        if (r.y_float) store_floats_unaligned<float, NT * 4>(reinterpret_cast<float *>(r.y) + to + col, x);
+                        else store_floats_unaligned<S, NT * 4>(reinterpret_cast<S *>(r.y) + to + col, x);
                     } else {
 #pragma unroll
                         for (int e = 0; e < NT * 4; e++)

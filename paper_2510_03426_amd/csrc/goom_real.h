@@ -40,6 +40,21 @@ template <typename T, int N> __device__ inline void store_floats(T *p, const flo
     *reinterpret_cast<typename Vec<T, N>::type *>(p) = v;
 }
 
+// the same from addresses aligned to one element only (the hardware takes them, as one access)
+template <typename T, int N> __device__ inline typename Vec<T, N>::type load_unaligned(const T *p)
+{
+    typedef typename Vec<T, N>::type V __attribute__((aligned(sizeof(T))));
+    return *reinterpret_cast<const V *>(p);
+}
+template <typename T, int N> __device__ inline void store_floats_unaligned(T *p, const float (&x)[N])
+{
+    typedef typename Vec<T, N>::type V __attribute__((aligned(sizeof(T))));
+    typename Vec<T, N>::type v;
+#pragma unroll
+    for (int i = 0; i < N; i++) v[i] = (T)x[i];
+    *reinterpret_cast<V *>(p) = v;
+}
+
 // f(type tag) with the element type that `type` (GOOM_REAL_*) names
 template <typename T> struct Tag { typedef T type; };
 template <typename F> int with_type(int type, F f)
