@@ -17,23 +17,27 @@ namespace goom_layer {
 constexpr int RUN = 32;       // sorted positions of a block that is summed beforehand
 constexpr int MAX_BINS = 512; // digits of a sorting pass
 
+// Rows are taken in units of V columns, whatever the width: the last unit ends at the row's end and overlaps the one before it (both
+// write the same values).
+__device__ inline int column(int col, int width, int v) { return col + v <= width ? col : width - v; }
+
 template <typename S, int V> __global__ __launch_bounds__(256) void embedding_kernel(const S *table, const int64_t *tokens, S *rows, long long n, long long vocab, int width, float scale)
 {
-    const int units = width / V;
+    const int units = (width + V - 1) / V;
     for (long long u = blockIdx.x * 256ll + threadIdx.x; u < n * units; u += gridDim.x * 256ll) {
         const long long row = u / units;
-        const int col = (int)(u - row * units) * V;
+        const int col = column((int)(u - row * units) * V, width, V);
         const long long t = tokens[row];
         float x[V];
         if (t >= 0 && t < vocab) {
-            load_floats<S, V>(table + t * width + col, x);
+            load_floats_unaligned<S, V>(table + t * width + col, x);
 #pragma unroll
             for (int e = 0; e < V; e++) x[e] *= scale;
         } else {
 #pragma unroll
             for (int e = 0; e < V; e++) x[e] = 0.0f;
         }
-        store_floats<S, V>(rows + row * width + col, x);
+        store_floats_unaligned<S, V>(rows + row * width + col, x);
     }
 }
 
@@ -281,7 +285,7 @@ template <typename S, int V> __device__ inline void add_rows(float (&x)[V], cons
     for (; i + 8 <= end; i += 8) { // eight rows in flight
         float y[8][V];
 #pragma unroll
-        for (int k = 0; k < 8; k++) load_floats<S, V>(grad + (long long)values[i + k] * width + col, y[k]);
+        for (int k = 0; k < 8; k++) load_floats_unaligned<S, V>(grad + (long long)values[i + k] * width + col, y[k]);
 #pragma unroll
         for (int k = 0; k < 8; k++)
 #pragma unroll
@@ -289,7 +293,7 @@ template <typename S, int V> __device__ inline void add_rows(float (&x)[V], cons
     }
     for (; i < end; i++) {
         float y[V];
-        load_floats<S, V>(grad + (long long)values[i] * width + col, y);
+        load_floats_unaligned<S, V>(grad + (long long)values[i] * width + col, y);
 #pragma unroll
         for (int e = 0; e < V; e++) x[e] += y[e];
     }
@@ -335,22 +339,24 @@ template <typename S, int V> __global__ __launch_bounds__(256) void runs_kernel(
     if (block >= n / RUN) return;
     const unsigned key = keys[i];
     if (key != keys[i + RUN - 1] || key >= vocab) return;
-    const int col = ((int)(task - block * parts) * 64 + (threadIdx.x & 63)) * V;
+    int col = ((int)(task - block * parts) * 64 + (threadIdx.x & 63)) * V;
     if (col >= width) return;
+    col = column(col, width, V);
     float x[V] = {};
     add_rows<S, V>(x, grad, values, i, i + RUN, width, col);
-    store_floats<float, V>(sums + (long long)block * width + col, x);
+    store_floats_unaligned<float, V>(sums + (long long)block * width + col, x);
 }
 
 // 64 V columns of a table row a wave: the run's head, its whole blocks, its tail.  grid: vocab parts / 4
 template <typename S, typename W, int V> __global__ __launch_bounds__(256) void table_row_kernel(const S *grad, const unsigned *values, const unsigned *start, const float *sums, W *table, long long vocab, int width, int parts, float scale)
 {
     const long long task = blockIdx.x * 4ll + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = task / parts;
-    const int col = ((int)(task - row * parts) * 64 + (threadIdx.x & 63)) * V;
+    int col = ((int)(task - row * parts) * 64 + (threadIdx.x & 63)) * V;
     if (row >= vocab) return;
     const unsigned begin = start[row], end = start[row + 1];
     const unsigned first = (begin + RUN - 1) / RUN, last = end / RUN; // whole blocks: first .. last - 1
     if (col >= width) return;
+    col = column(col, width, V);
     float x[V] = {};
     if (first < last) {
         add_rows<S, V>(x, grad, values, begin, first * RUN, width, col);
@@ -358,7 +364,7 @@ template <typename S, typename W, int V> __global__ __launch_bounds__(256) void 
         for (; b + 8 <= last; b += 8) {
             float y[8][V];
 #pragma unroll
-            for (int k = 0; k < 8; k++) load_floats<float, V>(sums + (long long)(b + k) * width + col, y[k]);
+            for (int k = 0; k < 8; k++) load_floats_unaligned<float, V>(sums + (long long)(b + k) * width + col, y[k]);
 #pragma unroll
             for (int k = 0; k < 8; k++)
 #pragma unroll
@@ -366,7 +372,7 @@ template <typename S, typename W, int V> __global__ __launch_bounds__(256) void 
         }
         for (; b < last; b++) {
             float y[V];
-            load_floats<float, V>(sums + (long long)b * width + col, y);
+            load_floats_unaligned<float, V>(sums + (long long)b * width + col, y);
 #pragma unroll
             for (int e = 0; e < V; e++) x[e] += y[e];
         }
@@ -376,7 +382,7 @@ template <typename S, typename W, int V> __global__ __launch_bounds__(256) void 
     }
 #pragma unroll
     for (int e = 0; e < V; e++) x[e] *= scale;
-    store_floats<W, V>(table + row * width + col, x);
+    store_floats_unaligned<W, V>(table + row * width + col, x);
 }
 
 // Up to FEW positions need no sorting: every row's waves look at all tokens themselves.  One launch.
@@ -384,12 +390,14 @@ constexpr int FEW = 256;
 template <typename S, typename W, int V> __global__ __launch_bounds__(256) void few_rows_kernel(const S *grad, const int64_t *tokens, W *table, unsigned n, long long vocab, int width, int parts, float scale)
 {
     const long long task = blockIdx.x * 4ll + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = task / parts;
-    const int lane = threadIdx.x & 63, col = ((int)(task - row * parts) * 64 + lane) * V;
+    const int lane = threadIdx.x & 63;
+    int col = ((int)(task - row * parts) * 64 + lane) * V;
     if (row >= vocab) return;
     unsigned long long mine[FEW / 64]; // positions of this row's token
 #pragma unroll
     for (int k = 0; k < FEW / 64; k++) mine[k] = __ballot(k * 64 + lane < (int)n && tokens[k * 64 + lane < (int)n ? k * 64 + lane : 0] == row);
     if (col >= width) return;
+    col = column(col, width, V);
     float x[V] = {};
 #pragma unroll
     for (int k = 0; k < FEW / 64; k++)
@@ -397,13 +405,13 @@ template <typename S, typename W, int V> __global__ __launch_bounds__(256) void 
             const int i = k * 64 + __builtin_ctzll(mine[k]);
             mine[k] &= mine[k] - 1;
             float y[V];
-            load_floats<S, V>(grad + (long long)i * width + col, y);
+            load_floats_unaligned<S, V>(grad + (long long)i * width + col, y);
 #pragma unroll
             for (int e = 0; e < V; e++) x[e] += y[e];
         }
 #pragma unroll
     for (int e = 0; e < V; e++) x[e] *= scale;
-    store_floats<W, V>(table + row * width + col, x);
+    store_floats_unaligned<W, V>(table + row * width + col, x);
 }
 
 struct EmbeddingPlan {
@@ -441,12 +449,11 @@ static int check_embedding(goom_ctx *ctx, long long n, long long vocab, int widt
     return GOOM_OK;
 }
 
-// elements of a vector access that widths and addresses allow, up to 16 bytes of the larger type
-static int vector_of(int width, std::initializer_list<std::pair<const void *, size_t>> arrays)
+// columns of a unit: 16 bytes of the larger type, no more than a row has
+static int vector_of(int width, size_t size)
 {
-    int v = 8;
-    for (auto &a : arrays)
-        while (v > 1 && (width % v || v * a.second > 16 || !goom::aligned(a.first, v * a.second))) v /= 2;
+    int v = (int)(16 / size);
+    while (v > width) v /= 2;
     return v;
 }
 
@@ -478,8 +485,8 @@ int goom_embedding(goom_ctx *ctx, const void *table, const int64_t *tokens, void
     const size_t size = real_bytes(type);
     if (!aligned(table, size) || !aligned(rows, size) || !aligned(tokens, 8)) return fail(ctx, GOOM_EINVAL, "misaligned data pointer");
     if (int s = enter(ctx)) return s;
-    const int v = vector_of(width, {{table, size}, {rows, size}});
-    const long long blocks = (n * (width / v) + 255) / 256;
+    const int v = vector_of(width, size);
+    const long long blocks = (n * ((width + v - 1) / v) + 255) / 256;
     goom::prof_begin(ctx, "embedding");
     const int rc = with_type(type, [&](auto tag) {
         typedef typename decltype(tag)::type S;
@@ -542,7 +549,7 @@ int goom_embedding_backward(goom_ctx *ctx, const int64_t *tokens, const void *gr
         }
     }
     if (n > FEW) goom::prof_end(ctx);
-    const int v = vector_of(width, {{grad, size}, {grad_table, wsize}, {sums, 4}});
+    const int v = vector_of(width, 4); // (block sums are floats)
     const int rc = with_type(type, [&](auto tag) {
         typedef typename decltype(tag)::type S;
         return with_vector(v, [&](auto vec) {

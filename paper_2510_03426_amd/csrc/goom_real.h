@@ -46,6 +46,12 @@ template <typename T, int N> __device__ inline typename Vec<T, N>::type load_una
     typedef typename Vec<T, N>::type V __attribute__((aligned(sizeof(T))));
     return *reinterpret_cast<const V *>(p);
 }
+template <typename T, int N> __device__ inline void load_floats_unaligned(const T *p, float (&x)[N])
+{
+    const typename Vec<T, N>::type v = load_unaligned<T, N>(p);
+#pragma unroll
+    for (int i = 0; i < N; i++) x[i] = (float)v[i];
+}
 template <typename T, int N> __device__ inline void store_floats_unaligned(T *p, const float (&x)[N])
 {
     typedef typename Vec<T, N>::type V __attribute__((aligned(sizeof(T))));
