@@ -46,15 +46,15 @@ __device__ inline float param(const void *p, int type, int i, float otherwise)
     return type == GOOM_REAL_F32 ? reinterpret_cast<const float *>(p)[i] : type == GOOM_REAL_BF16 ? (float)reinterpret_cast<const bf16 *>(p)[i] : (float)reinterpret_cast<const f16 *>(p)[i];
 }
 
-// V parameters of neighbouring channels from a multiple of V on
+// V parameters of neighbouring channels
 template <int V> __device__ inline void params(const void *p, int type, int i, float otherwise, float (&x)[V])
 {
-    if (p && type == GOOM_REAL_F32 && V > 1 && (reinterpret_cast<uintptr_t>(p) & (V > 4 ? 15 : 4 * V - 1)) == 0) {
+    if (p && type == GOOM_REAL_F32) {
         constexpr int N = V > 4 ? 4 : V;
 #pragma unroll
         for (int e = 0; e < V; e += N) {
             float y[N];
-            load_floats<float, N>(reinterpret_cast<const float *>(p) + i + e, y);
+            load_floats_unaligned<float, N>(reinterpret_cast<const float *>(p) + i + e, y);
 #pragma unroll
             for (int k = 0; k < N; k++) x[e + k] = y[k];
         }
@@ -110,21 +110,25 @@ __device__ inline float team_sum(float v, int team)
     return v;
 }
 
-// ---- short groups.  Unit u of a group (u < length cg / V): position u / (cg / V), channels V (u % (cg / V)) on; lane l of the
-// team has the units l, l + team, ...  grid: (workgroups over items, parts of the groups)
-template <typename S, int V, int J, bool BACK> __global__ __launch_bounds__(256) void norm_team_kernel(NormArgs a)
+// ---- short groups.  A position's channels of a group are cu = ceil(cg / V) units of V; unit u of a group: position u / cu, unit
+// u % cu of it; lane l of the team has the units l, l + team, ...  TAIL: V does not divide cg; a position's last unit ends at its last
+// channel and shares its first `skip` channels with the unit before, which count there.  grid: (workgroups over items, parts of
+// the groups)
+template <typename S, int V, int J, bool BACK, bool TAIL> __global__ __launch_bounds__(256) void norm_team_kernel(NormArgs a)
 {
     const int lane = threadIdx.x % a.team, team = threadIdx.x / a.team, ti = team / a.gpw, group = blockIdx.y * a.gpw + team % a.gpw;
     const bool live = ti < a.ipw && group < a.groups;
-    const int cu = a.cg / V, units = cu * (int)a.length;
+    const int cu = (a.cg + V - 1) / V, units = cu * (int)a.length;
     const float count = (float)a.cg * (float)a.length;
     unsigned off[J]; // of this lane's units: element offsets within the item (2^31 at most), channels
-    int chan[J];
+    int chan[J], skip[J];
     float w[J][V], b[J][V], sw[J][V], sb[J][V];
 #pragma unroll
     for (int j = 0; j < J; j++) {
         const int u = lane + j * a.team;
-        chan[j] = live && u < units ? group * a.cg + u % cu * V : -1;
+        const bool end = TAIL && u % cu == cu - 1;
+        skip[j] = end ? cu * V - a.cg : 0;
+        chan[j] = live && u < units ? group * a.cg + (end ? a.cg - V : u % cu * V) : -1;
         off[j] = chan[j] >= 0 ? (unsigned)(u / cu) * (unsigned)a.channels + chan[j] : 0u;
         params<V>(a.weight, a.type_w, chan[j] >= 0 ? chan[j] : 0, 1.0f, w[j]);
         params<V>(a.bias, a.type_w, chan[j] >= 0 ? chan[j] : 0, 0.0f, b[j]);
@@ -141,8 +145,8 @@ template <typename S, int V, int J, bool BACK> __global__ __launch_bounds__(256)
         const long long from = item < a.items ? item : 0;
 #pragma unroll
         for (int j = 0; j < J; j++) {
-            next_x[j] = *reinterpret_cast<const SV *>(xs + from * size + off[j]);
-            if (BACK) next_g[j] = *reinterpret_cast<const SV *>(gs + from * size + off[j]);
+            next_x[j] = load_unaligned<S, V>(xs + from * size + off[j]);
+            if (BACK) next_g[j] = load_unaligned<S, V>(gs + from * size + off[j]);
         }
     };
     fetch((long long)blockIdx.x * a.ipw + ti);
@@ -164,7 +168,7 @@ template <typename S, int V, int J, bool BACK> __global__ __launch_bounds__(256)
 #pragma unroll
             for (int j = 0; j < J; j++)
 #pragma unroll
-                for (int e = 0; e < V; e++) sum += x[j][e];
+                for (int e = 0; e < V; e++) sum += !TAIL || e >= skip[j] ? x[j][e] : 0.0f;
             const float mean = team_sum(sum, a.team) / count;
             float square = 0.0f;
 #pragma unroll
@@ -173,7 +177,7 @@ template <typename S, int V, int J, bool BACK> __global__ __launch_bounds__(256)
 #pragma unroll
                     for (int e = 0; e < V; e++) {
                         x[j][e] -= mean;
-                        square += x[j][e] * x[j][e];
+                        square += !TAIL || e >= skip[j] ? x[j][e] * x[j][e] : 0.0f;
                     }
                 }
             const float rstd = 1.0f / sqrtf(team_sum(square, a.team) / count + a.eps);
@@ -186,7 +190,7 @@ template <typename S, int V, int J, bool BACK> __global__ __launch_bounds__(256)
                 if (here && chan[j] >= 0) {
 #pragma unroll
                     for (int e = 0; e < V; e++) x[j][e] = activate(x[j][e] * rstd * w[j][e] + b[j][e], a.act);
-                    store_floats<S, V>(ys + item * size + off[j], x[j]);
+                    store_floats_unaligned<S, V>(ys + item * size + off[j], x[j]);
                 }
         } else {
             const float mean = here ? a.mean[item * a.groups + group] : 0.0f, rstd = here ? a.rstd[item * a.groups + group] : 0.0f;
@@ -201,8 +205,8 @@ template <typename S, int V, int J, bool BACK> __global__ __launch_bounds__(256)
                         sw[j][e] += dz[j][e] * x[j][e];
                         sb[j][e] += dz[j][e];
                         dz[j][e] *= w[j][e];
-                        m1 += dz[j][e];
-                        m2 += dz[j][e] * x[j][e];
+                        m1 += !TAIL || e >= skip[j] ? dz[j][e] : 0.0f;
+                        m2 += !TAIL || e >= skip[j] ? dz[j][e] * x[j][e] : 0.0f;
                     }
                 }
             m1 = team_sum(m1, a.team) / count;
@@ -212,7 +216,7 @@ template <typename S, int V, int J, bool BACK> __global__ __launch_bounds__(256)
                 if (here && chan[j] >= 0) {
 #pragma unroll
                     for (int e = 0; e < V; e++) x[j][e] = rstd * (dz[j][e] - m1 - x[j][e] * m2);
-                    store_floats<S, V>(ys + item * size + off[j], x[j]);
+                    store_floats_unaligned<S, V>(ys + item * size + off[j], x[j]);
                 }
         }
     }
@@ -230,7 +234,7 @@ template <typename S, int V, int J, bool BACK> __global__ __launch_bounds__(256)
                 if (blockIdx.y * a.gpw + tg >= a.groups) continue;
                 float sum = 0.0f;
                 for (int t = 0; t < a.ipw; t++)
-                    for (int u = cc / V; u < units; u += cu) sum += meet[(u / a.team * V + cc % V) * 256 + (t * a.gpw + tg) * a.team + u % a.team];
+                    for (int u = cc / V; u < units; u += cu) sum += meet[(u / a.team * V + (TAIL && cc / V == cu - 1 ? cc - (a.cg - V) : cc % V)) * 256 + (t * a.gpw + tg) * a.team + u % a.team];
                 a.partial[((long long)blockIdx.x * 2 + which) * a.channels + (blockIdx.y * a.gpw) * a.cg + c] = sum;
             }
             __syncthreads();
@@ -567,10 +571,10 @@ static NormPlan norm_plan(const goom_norm_shape &sh, int cap, bool back)
     a.type_w = sh.param_type;
     a.act = sh.activation;
     a.eps = (float)sh.eps;
-    int v = cap;
-    while (a.cg % v) v /= 2;
+    int v = (int)(16 / real_bytes(sh.type)); // (whatever the addresses' alignment)
+    while (v > a.cg) v /= 2;
     p.v = v;
-    const long long units = (long long)sh.length * (a.cg / v);
+    const long long units = (long long)sh.length * ((a.cg + v - 1) / v);
     const int most = TEAM_ELEMENTS / v < 8 ? TEAM_ELEMENTS / v : 8;
     p.team = units <= 64ll * most;
     if (p.team) {
@@ -663,17 +667,22 @@ static int check_grid(goom_ctx *ctx, const NormPlan &p)
     return GOOM_OK;
 }
 
-// f(vector width, units a lane)
-template <typename S, typename F> static int with_team(int v, int j, F f)
+// f(vector width, units a lane, whether cg leaves a rest)
+template <typename S, typename F> static int with_team(int v, int j, int cg, F f)
 {
     auto units = [&](auto vec) {
         constexpr int V = decltype(vec)::value;
         if constexpr (V * sizeof(S) <= 16) {
-            if constexpr (V <= 4)
-                if (j == 8) return f(vec, std::integral_constant<int, 8>());
-            if (j == 4) return f(vec, std::integral_constant<int, 4>());
-            if (j == 2) return f(vec, std::integral_constant<int, 2>());
-            return f(vec, std::integral_constant<int, 1>());
+            auto lanes = [&](auto tail) {
+                if constexpr (V <= 4)
+                    if (j == 8) return f(vec, std::integral_constant<int, 8>(), tail);
+                if (j == 4) return f(vec, std::integral_constant<int, 4>(), tail);
+                if (j == 2) return f(vec, std::integral_constant<int, 2>(), tail);
+                return f(vec, std::integral_constant<int, 1>(), tail);
+            };
+            if constexpr (V > 1)
+                if (cg % V) return lanes(std::true_type());
+            return lanes(std::false_type());
         }
         return 0;
     };
@@ -725,8 +734,8 @@ int goom_group_norm(goom_ctx *ctx, const goom_norm_shape *shape, const void *x, 
         const dim3 grid((unsigned)p.blocks, (unsigned)p.parts);
         if (p.team) {
             goom::prof_begin(ctx, "group norm");
-            with_team<S>(p.v, p.j, [&](auto vec, auto units) {
-                norm_team_kernel<S, decltype(vec)::value, decltype(units)::value, false><<<grid, 256, 0, ctx->stream>>>(a);
+            with_team<S>(p.v, p.j, a.cg, [&](auto vec, auto units, auto tail) {
+                norm_team_kernel<S, decltype(vec)::value, decltype(units)::value, false, decltype(tail)::value><<<grid, 256, 0, ctx->stream>>>(a);
                 return 0;
             });
             goom::prof_end(ctx);
@@ -791,8 +800,8 @@ int goom_group_norm_backward(goom_ctx *ctx, const goom_norm_shape *shape, const 
         if (p.team) {
             if (shape->items > 0) {
                 goom::prof_begin(ctx, "group norm gradient");
-                with_team<S>(p.v, p.j, [&](auto vec, auto units) {
-                    norm_team_kernel<S, decltype(vec)::value, decltype(units)::value, true><<<grid, 256, 0, ctx->stream>>>(a);
+                with_team<S>(p.v, p.j, a.cg, [&](auto vec, auto units, auto tail) {
+                    norm_team_kernel<S, decltype(vec)::value, decltype(units)::value, true, decltype(tail)::value><<<grid, 256, 0, ctx->stream>>>(a);
                     return 0;
                 });
                 goom::prof_end(ctx);

@@ -78,7 +78,7 @@ def _check(g, dtype, items, length, channels, groups, act, wtype="f32", seed=0, 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("act", ["none", "silu", "gelu"])
-@pytest.mark.parametrize("items,length,channels,groups", [(1, 1, 2, 1), (3, 1, 64, 4), (17, 1, 53, 1), (5, 1, 1744, 16), (2, 1, 2048, 16), (9, 3, 24, 8), (300, 1, 128, 32)])
+@pytest.mark.parametrize("items,length,channels,groups", [(1, 1, 2, 1), (3, 1, 64, 4), (17, 1, 53, 1), (5, 1, 1744, 16), (2, 1, 2048, 16), (9, 3, 24, 8), (7, 5, 105, 7), (4, 40, 90, 10), (300, 1, 128, 32)])
 def test_short_groups(g, dtype, act, items, length, channels, groups):
     _check(g, dtype, items, length, channels, groups, act, seed=channels)
 
