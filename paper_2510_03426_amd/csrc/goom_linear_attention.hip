@@ -239,9 +239,10 @@ static BackwardPlan backward_plan(const goom_attention_shape &sh, bool packed)
     BackwardPlan p;
     p.seg = choose_segments(sh, 3, packed);
     // Walks of different sizes go together, padded to the larger, where the chip has room for all of them at once: a small
-    // pass is bound by its launches
+    // pass is bound by its launches.  (6000 tokens of 32 bfloat16 heads of 110 and 25: 109 us together, 124 apart; of 128 and 64 98 and
+    // 114.  Floats pay six products for the padding: heads of 110 and 25 240 and 191, of 50 and 100 176 and 170, so only up to 64.)
     const int most = sh.dk > sh.dv ? sh.dk : sh.dv, least = sh.dk > sh.dv ? sh.dv : sh.dk;
-    p.together = padded_head(least) == padded_head(most) || sh.seqs * sh.heads * 3 <= 256;
+    p.together = padded_head(least) == padded_head(most) || (sh.seqs * sh.heads * 3 <= 256 && (sh.type != GOOM_REAL_F32 || padded_head(most) <= 64));
     const int dk = p.together ? most : sh.dk, dv = p.together ? most : sh.dv;
     p.totals_q = totals_bytes(sh, p.seg, dv, dk);
     p.totals_k = totals_bytes(sh, p.seg, dv, dk);
