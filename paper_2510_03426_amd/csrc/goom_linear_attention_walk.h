@@ -116,7 +116,8 @@ __device__ inline float decay_power(float g2, int x) { return __builtin_amdgcn_e
 // ---- operands: eight consecutive entries of the contraction per lane (lane / 16 picks which eight of 32), as sums of bf16
 // parts, each 8 bits further down.  Inputs are held exactly: one part for bfloat16, two for halves (11 bits, and products and
 // states of halves may leave their range), three for floats.  Computed operands are split into as many as their result
-// needs: OUT for P and the state where outputs are formed from them, three where they enter a state that is returned, in floats.  Of a product of
+// needs: OUT for P and the state where outputs are formed from them, three where they enter the state, whether it is returned or not: outputs
+// have the same bits either way.  Of a product of
 // parts i and j those with i + j up to the number of parts matter.  (On floats' own matrix instruction a product takes eight
 // instructions of 32 cycles; six of 16 cycles here.)
 typedef bf16x8 Frag;
@@ -311,12 +312,12 @@ template <bool REV> __device__ inline void p_place(int block, int ch, int &it, i
 }
 
 // DK, DV: ka and nc (of one of `parts` column parts), padded; NW waves of NT tiles of 16 columns each
-template <typename S, int DK, int DV, int NW, bool OUT, bool REV, int SP> // SP: parts of what enters the state
+template <typename S, int DK, int DV, int NW, bool OUT, bool REV>
 __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &at, long long slot, int h, int part, unsigned char *lds)
 {
     typedef WalkLds<S, DK, DV, NW, OUT> Lds;
     constexpr int THREADS = NW * 64, NT = DV / 16 / NW, KS = DK / 32, CS = NT == 2 ? 8 : 4;
-    constexpr int IP = Parts<S>::IN, OP = Parts<S>::OUT;
+    constexpr int IP = Parts<S>::IN, OP = Parts<S>::OUT, SP = Parts<S>::STATE;
     constexpr int CH = Lds::CH, KP = CH * Lds::PK, VP = CH * Lds::PV; // tokens of a step, elements from part to part
     static_assert(NT == 1 || NT == 2, "a wave has one or two column tiles");
     f32x8 *const pair_weights = reinterpret_cast<f32x8 *>(lds);                      // (OUT)
@@ -566,14 +567,8 @@ __global__ __launch_bounds__(NW * 64, (WalkLds<S, DK, DV, NW, OUT>::per_simd)) v
     const long long slot = item / w.parts / w.heads;
     const Place at = find_place(w, slot);
     if (at.seg < 0 || at.seg >= at.nseg || part * DV >= r.nc) return; // a slot that no sequence has
-    constexpr int FULL = Parts<S>::STATE, SHORT = Parts<S>::OUT;
-    if (FULL == SHORT || r.fin) {
-        if (r.reverse) walk<S, DK, DV, NW, OUT, true, FULL>(w, r, at, slot, h, part, lds);
-        else walk<S, DK, DV, NW, OUT, false, FULL>(w, r, at, slot, h, part, lds);
-    } else {
-        if (r.reverse) walk<S, DK, DV, NW, OUT, true, SHORT>(w, r, at, slot, h, part, lds);
-        else walk<S, DK, DV, NW, OUT, false, SHORT>(w, r, at, slot, h, part, lds);
-    }
+    if (r.reverse) walk<S, DK, DV, NW, OUT, true>(w, r, at, slot, h, part, lds);
+    else walk<S, DK, DV, NW, OUT, false>(w, r, at, slot, h, part, lds);
 }
 
 // Segment totals -> incoming states, in place, in walking order: a thread has four entries of one head's state and goes

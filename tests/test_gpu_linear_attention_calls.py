@@ -1,0 +1,38 @@
+"""Linear attention as training and serving programs call it, beside the forms that test_gpu_linear_attention.py takes: without a
+final state, without an initial one's gradient.  References and tolerances are those of that file (the recurrence in 64 bits)."""
+import pytest
+
+from test_gpu_linear_attention import _check, _f64, _inputs, _near, g  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n,H,G,dk,dv,with_state", [(1, 2, 1, 16, 16, True), (200, 3, 3, 40, 64, False), (1500, 1, 1, 64, 64, False), (1500, 2, 1, 128, 128, True), (700, 2, 2, 50, 100, False)])
+def test_outputs_without_a_final_state(g, dtype, n, H, G, dk, dv, with_state):  # noqa: F811
+    """The ordinary training call: outputs as the recurrence has them, and the bits of a call that asks for the state."""
+    import torch
+    import numpy as np
+    from oracle import layer_oracle as lo
+    q, k, v, _, ld, s0, _ = _inputs(dtype, n, H, G, dk, dv, 1, n + dk)
+    args = [x.cuda()[None] for x in (q, k, v)] + [ld.cuda()]
+    s = s0.cuda() if with_state else None
+    o = g.linear_attention(*args, state=s)
+    both, _ = g.linear_attention(*args, state=s, want_state=True)
+    assert torch.equal(o, both)
+    st = _f64(s0) if with_state else None
+    want, _ = lo.attention(*[_f64(x) for x in (q, k, v)], _f64(ld), st)
+    mag, _ = lo.attention(*[np.abs(_f64(x)) for x in (q, k, v)], _f64(ld), None if st is None else np.abs(st))
+    _near(o[0], want, mag, dtype, max(dk, dv) + 64 + n // 64 + 32, dtype != "f32", "o")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_gradients_without_a_state(g, dtype):  # noqa: F811
+    """grad_k and grad_v do not depend on whether the initial state's gradient is formed beside them."""
+    import torch
+    q, k, v, do, ld, _, _ = (x.cuda() for x in _inputs(dtype, 1500, 2, 1, 64, 64, 1, 21))
+    args = [x[None] for x in (q, k, v)] + [ld, do[None]]
+    a = g.linear_attention_backward(*args)
+    b = g.linear_attention_backward(*args, state=torch.zeros(1, 2, 64, 64, device="cuda"), grad_state=torch.zeros(1, 2, 64, 64, device="cuda"))
+    for x, y in zip(a[:3], b[:3]):
+        assert torch.equal(x, y)
