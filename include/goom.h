@@ -503,8 +503,8 @@ typedef struct goom_attention_shape {
  * shape, S after the last one (the state itself for a sequence without tokens; it may be the array `state`).
  * The sequences are cut into segments where they are few: segment totals, their carries, then every segment walked from its
  * incoming state, 64 tokens (32 for halves and floats) at a time on the matrix instructions.  All of them are sums of one
- * (bfloat16), two (half) or three (float) bf16 parts; operands computed on the way are held in two parts (16 bits), or three (24
- * bits) for floats and where they enter a state.  Outputs do not depend on whether the final state is asked for.
+ * (bfloat16), two (half) or three (float) bf16 parts; operands computed on the way are held in three (24 bits), whatever the
+ * type.  Outputs do not depend on whether the final state is asked for.
  * A NaN or an infinity among q, k, v may show in all outputs of its head in its sequence.
  * workspace: goom_linear_attention_workspace_bytes(shape, offsets != NULL) bytes (may be 0).
  * Errors: GOOM_EINVAL (null or misaligned pointers, sizes, types), GOOM_EUNSUPPORTED (dk or dv above GOOM_MAX_DIM),

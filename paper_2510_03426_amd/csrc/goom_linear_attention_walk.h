@@ -115,25 +115,27 @@ __device__ inline float decay_power(float g2, int x) { return __builtin_amdgcn_e
 
 // ---- operands: eight consecutive entries of the contraction per lane (lane / 16 picks which eight of 32), as sums of bf16
 // parts, each 8 bits further down.  Inputs are held exactly: one part for bfloat16, two for halves (11 bits, and products and
-// states of halves may leave their range), three for floats.  Computed operands are split into as many as their result
-// needs: OUT for P and the state where outputs are formed from them, three where they enter the state, whether it is returned or not: outputs
-// have the same bits either way.  Of a product of
-// parts i and j those with i + j up to the number of parts matter.  (On floats' own matrix instruction a product takes eight
-// instructions of 32 cycles; six of 16 cycles here.)
+// states of halves may leave their range), three for floats.  Computed operands (P, the state where outputs are formed from it, the
+// decayed rows that enter it) are floats, held in three parts whatever the type: 24 bits, so that outputs are off by no more than sums of
+// floats are.  (Two parts, 16 bits: 0.22 % of the bfloat16 outputs of 8 x 4096 tokens of heads of 128 were a neighbour of the
+// rounded exact value, for 0.015 % and for 0.018 % of an evaluation in floats; both directions took 12 % less time.)  Of a product of
+// parts i and j those with i + j up to two matter.  (On floats' own matrix instruction a product takes eight instructions of
+// 32 cycles; six of 16 cycles here.)
 typedef bf16x8 Frag;
 template <typename S> struct Parts;
-template <> struct Parts<bf16> { static constexpr int IN = 1, OUT = 2, STATE = 3; };
-template <> struct Parts<f16> { static constexpr int IN = 2, OUT = 2, STATE = 3; };
-template <> struct Parts<float> { static constexpr int IN = 3, OUT = 3, STATE = 3; };
+template <> struct Parts<bf16> { static constexpr int IN = 1; };
+template <> struct Parts<f16> { static constexpr int IN = 2; };
+template <> struct Parts<float> { static constexpr int IN = 3; };
+constexpr int COMPUTED = 3;
 constexpr int PITCH_PAD = 8;
 
-template <int LIMIT, int NA, int NB> __device__ inline f32x4 product(const Frag (&a)[NA], const Frag (&b)[NB], f32x4 c)
+template <int NA, int NB> __device__ inline f32x4 product(const Frag (&a)[NA], const Frag (&b)[NB], f32x4 c)
 {
 #pragma unroll
     for (int i = 0; i < NA; i++)
 #pragma unroll
         for (int j = 0; j < NB; j++)
-            if (i + j < LIMIT) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], c, 0, 0, 0);
+            if (i + j < 3) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], c, 0, 0, 0);
     return c;
 }
 
@@ -287,7 +289,7 @@ template <typename S, int DK, int DV, int NW, bool OUT> struct WalkLds {
     static constexpr int P_BLOCKS = CH == CHUNK ? 6 : 2; // 16 x 32 blocks of P that have pairs in them
     static constexpr int PK = DK + PITCH_PAD, PV = DV + PITCH_PAD;
     static constexpr int K_TILE = CH * PK * Parts<S>::IN, V_TILE = CH * PV * Parts<S>::IN; // elements
-    static constexpr int P_FRAGS = OUT ? P_BLOCKS * Parts<S>::OUT * 64 : 0;
+    static constexpr int P_FRAGS = OUT ? P_BLOCKS * COMPUTED * 64 : 0;
     static constexpr int WEIGHTS = CH + (OUT ? CH + 8 * PAIRS : 0); // floats
     static constexpr size_t bytes = (K_TILE * (OUT ? 2 : 1) + V_TILE) * sizeof(bf16) + P_FRAGS * sizeof(Frag) + WEIGHTS * sizeof(float);
     // workgroups of a CU: as many as its LDS holds, and no more than leave their waves the registers for the state (DK DV / 64 NW
@@ -317,7 +319,7 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
 {
     typedef WalkLds<S, DK, DV, NW, OUT> Lds;
     constexpr int THREADS = NW * 64, NT = DV / 16 / NW, KS = DK / 32, CS = NT == 2 ? 8 : 4;
-    constexpr int IP = Parts<S>::IN, OP = Parts<S>::OUT, SP = Parts<S>::STATE;
+    constexpr int IP = Parts<S>::IN, OP = COMPUTED;
     constexpr int CH = Lds::CH, KP = CH * Lds::PK, VP = CH * Lds::PV; // tokens of a step, elements from part to part
     static_assert(NT == 1 || NT == 2, "a wave has one or two column tiles");
     f32x8 *const pair_weights = reinterpret_cast<f32x8 *>(lds);                      // (OUT)
@@ -408,8 +410,8 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
                     row_frag(af, arow + kk * 32, KP);
                     row_frag(b0, brow + kk * 32, KP);
                     row_frag(b1, brow + 4 * Lds::PK + kk * 32, KP);
-                    p0 = product<3>(b0, af, p0);
-                    p1 = product<3>(b1, af, p1);
+                    p0 = product(b0, af, p0);
+                    p1 = product(b1, af, p1);
                 }
                 const int first = it * 16 + i - ks * 32 - g * 8; // i - j of the lane's first j
                 const f32x8 x = __builtin_shufflevector(p0, p1, 0, 1, 2, 3, 4, 5, 6, 7) * pair_weights[REV ? 31 - first : first + 32];
@@ -456,7 +458,7 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
 #pragma unroll
                     for (int it = 0; it < CH / 16; it++)
 #pragma unroll
-                        for (int nt = 0; nt < NT; nt++) y[it][nt] = product<OP>(rf[nt], af[kk % AHEAD][it], y[it][nt]);
+                        for (int nt = 0; nt < NT; nt++) y[it][nt] = product(rf[nt], af[kk % AHEAD][it], y[it][nt]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -474,7 +476,7 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
 #pragma unroll
                     for (int q = 0; q < OP; q++) pf[q] = p_lds[(p_block<REV>(it, ks, CH) * OP + q) * 64 + lane];
 #pragma unroll
-                    for (int nt = 0; nt < NT; nt++) y[it][nt] = product<OP>(cf[ks][nt], pf, y[it][nt]);
+                    for (int nt = 0; nt < NT; nt++) y[it][nt] = product(cf[ks][nt], pf, y[it][nt]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 if (row < n) {
@@ -516,7 +518,7 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
 #pragma unroll
                 for (int e = 0; e < 8; e++) wt[e] = first - e < 0 ? 0.0f : r.u_scale * decay_power(g2, first - e);
             }
-            Frag cd[NT][SP];
+            Frag cd[NT][OP];
 #pragma unroll
             for (int nt = 0; nt < NT; nt++) split(widen(cf[ks][nt]) * wt, cd[nt]);
             constexpr int AHEAD = IP == 1 ? 2 : 1;
@@ -528,7 +530,7 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
                 if (AHEAD == 1) load_rows(t);
                 else if (t + 1 < DK / 16) load_rows(t + 1);
 #pragma unroll
-                for (int nt = 0; nt < NT; nt++) R[t][nt] = product<SP>(bf[t % AHEAD], cd[nt], R[t][nt]);
+                for (int nt = 0; nt < NT; nt++) R[t][nt] = product(bf[t % AHEAD], cd[nt], R[t][nt]);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }

@@ -36,3 +36,28 @@ def test_gradients_without_a_state(g, dtype):  # noqa: F811
     b = g.linear_attention_backward(*args, state=torch.zeros(1, 2, 64, 64, device="cuda"), grad_state=torch.zeros(1, 2, 64, 64, device="cuda"))
     for x, y in zip(a[:3], b[:3]):
         assert torch.equal(x, y)
+
+
+def _neighbours(got, want):
+    """Share of the entries that are not the exact value rounded to their type."""
+    import torch
+    return float((got != torch.from_numpy(want).cuda().to(got.dtype)).double().mean())
+
+
+@pytest.mark.parametrize("shape", [(700, 2, 2, 128, 128), (1500, 2, 1, 64, 64)])
+def test_bfloat16_outputs_are_sums_of_floats(g, shape):  # noqa: F811
+    """Operands that are computed on the way lose no bits that a float holds.  An output whose float sum is off by e = c u s (s: the
+    spread of the outputs, u = 2^-24, c some 4 where rounding errors add up at random) is rounded to a neighbour with probability 2 e
+    over the spacing of bfloat16 there (2^-8 |y| to 2^-7 |y|, 2^-7.5 taken): 8 u s / (2^-7.5 |y|) = 2^-13.5 s / |y|, whose mean over
+    normal y, cut off where it reaches one, is some 7 times 2^-13.5 = 0.06 %.  0.1 % is
+    allowed.  With operands of 16 bits, off by up to 2^-17 of themselves, e is some 2^-18 s, 16 times as much."""
+    from oracle import layer_oracle as lo
+    n, H, G, dk, dv = shape
+    q, k, v, do, ld, _, _ = _inputs("bf16", n, H, G, dk, dv, 1, 31)
+    args = [x.cuda()[None] for x in (q, k, v)] + [ld.cuda()]
+    ref = [_f64(x) for x in (q, k, v)]
+    want, _ = lo.attention(*ref, _f64(ld))
+    assert _neighbours(g.linear_attention(*args)[0], want) <= 1e-3
+    grads = g.linear_attention_backward(*args, do.cuda()[None])
+    for got, want in zip(grads[:3], lo.attention_backward(*ref, _f64(ld), _f64(do))):
+        assert _neighbours(got[0], want) <= 1e-3
