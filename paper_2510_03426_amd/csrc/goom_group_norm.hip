@@ -19,6 +19,7 @@ namespace goom_layer {
 
 constexpr int TEAM_ELEMENTS = 32;    // of a group, per lane
 constexpr int CHUNK_ROWS = 128;      // positions a thread of the long kernels sums at most, in floats
+constexpr int SLAB_GROUPS = 512;     // groups of a slab at most: their statistics are in LDS (a multiple of every `least` below)
 
 struct NormArgs {
     const void *x, *gy;
@@ -338,7 +339,7 @@ template <typename S, int V> __global__ __launch_bounds__(512) void norm_stats_k
 
 template <typename S, int V> __global__ __launch_bounds__(512) void norm_apply_kernel(NormArgs a)
 {
-    __shared__ float stat[512][2];
+    __shared__ float stat[SLAB_GROUPS][2];
     const Slab s = slab_of<V>(a);
     const long long base = s.item * a.length * a.channels + s.chan0;
     const S *const x = reinterpret_cast<const S *>(a.x) + base;
@@ -595,7 +596,7 @@ static NormPlan norm_plan(const goom_norm_shape &sh, int cap, bool back)
         p.partial = back ? goom::align_up((size_t)p.blocks * 2 * sh.channels * 4, 256) : 0;
         return p;
     }
-    // a slab: whole groups whose channels make whole units, 256 of these at most (or one group)
+    // a slab: whole groups whose channels make whole units, 256 of these and SLAB_GROUPS groups at most (or one group)
     int least = 1;
     for (v = cap; v > 1; v /= 2) {
         for (least = 1; least * a.cg % v; least *= 2) {}
@@ -605,6 +606,7 @@ static NormPlan norm_plan(const goom_norm_shape &sh, int cap, bool back)
     p.v = v;
     a.gps = (int)(256ll * v / ((long long)a.cg * least) * least);
     if (a.gps < least) a.gps = least;
+    if (a.gps > SLAB_GROUPS) a.gps = SLAB_GROUPS; // (groups of one to three channels)
     if (a.gps > sh.groups) a.gps = sh.groups;
     const int columns = a.gps * a.cg / v < 256 ? a.gps * a.cg / v : 256;
     a.rows_at_once = 512 / columns > 0 ? 512 / columns : 1;
