@@ -213,7 +213,7 @@ def _at(t):
 
 def _rows(t, name):
     """Address and strides (token, head; 0, 0: contiguous) of [..., heads, d] whose last axis is contiguous and whose leading axes
-    follow one another in memory, as in a slice of a fused projection."""
+    follow one another in memory, as in a slice of a fused projection.  Axes that were expanded are refused."""
     if not t.is_cuda:
         raise ValueError("libgoom takes device tensors")
     if t.is_contiguous():
@@ -232,6 +232,8 @@ def _rows(t, name):
             raise ValueError(f"{name}: the tokens do not follow one another in memory")
         else:
             run *= sh[i]
+    if head < sh[-1] or (token is not None and token < sh[-1]):  # (0, 0 would be taken for contiguous)
+        raise ValueError(f"{name}: rows share memory, as those of an expanded tensor do")
     return t.data_ptr(), sh[-2] * head if token is None else token, head
 
 
