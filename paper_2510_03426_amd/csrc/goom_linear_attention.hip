@@ -7,13 +7,21 @@
 namespace goom_layer {
 
 // sums over heads that share keys and values: y[token][kv head][.] = sum over the group of x[token][head][.], floats.  Two such
-// arrays in one launch, blockIdx.y apart
+// arrays in one launch, blockIdx.y apart.  Tokens before the first sequence and after the last one have no sums, and none are written.
 struct SharedSum { const float *x; void *y; long long n; int d; }; // n: units of V entries
-template <typename S, int V> __global__ __launch_bounds__(256) void shared_sum_kernel(SharedSum k, SharedSum v, int group)
+template <typename S, int V>
+__global__ __launch_bounds__(256) void shared_sum_kernel(SharedSum k, SharedSum v, int group, int kv_heads, const int64_t *offsets, long long seqs, long long tokens)
 {
     const SharedSum &t = blockIdx.y ? v : k;
     const int units = t.d / V;
-    for (long long u = blockIdx.x * 256ll + threadIdx.x; u < t.n; u += gridDim.x * 256ll) {
+    long long begin = 0, end = t.n;
+    if (offsets) {
+        auto cut = [&](long long at) { return at < 0 ? 0 : at > tokens ? tokens : at; };
+        const long long first = cut(offsets[0]), start = cut(offsets[seqs - 1]), last = cut(offsets[seqs]);
+        begin = first * kv_heads * units;
+        end = (last > start ? last : start) * kv_heads * units; // (the last sequence has no tokens if its end is before its start)
+    }
+    for (long long u = begin + blockIdx.x * 256ll + threadIdx.x; u < end; u += gridDim.x * 256ll) {
         const long long row = t.n < (1ll << 31) ? (unsigned)u / (unsigned)units : u / units;
         const float *const p = t.x + row * group * t.d + (u - row * units) * V;
         float sum[V] = {};
@@ -396,7 +404,7 @@ int goom_linear_attention_backward(goom_ctx *ctx, const goom_attention_shape *sh
             const SharedSum ks = {sum_k, grad_k, rows * sh.dk / V, sh.dk}, vs = {sum_v, grad_v, rows * sh.dv / V, sh.dv};
             auto *kernel = vec ? shared_sum_kernel<S, 4> : shared_sum_kernel<S, 1>;
             goom::prof_begin(ctx, "linear attention: shared heads");
-            kernel<<<dim3((unsigned)(blocks < 16384 ? blocks : 16384), 2), 256, 0, ctx->stream>>>(ks, vs, group);
+            kernel<<<dim3((unsigned)(blocks < 16384 ? blocks : 16384), 2), 256, 0, ctx->stream>>>(ks, vs, group, sh.kv_heads, offsets, sh.seqs, sh.tokens);
             goom::prof_end(ctx);
             return goom::check_hip(ctx, hipGetLastError(), "linear attention: shared heads");
         });

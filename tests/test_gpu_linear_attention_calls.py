@@ -61,3 +61,43 @@ def test_bfloat16_outputs_are_sums_of_floats(g, shape):  # noqa: F811
     grads = g.linear_attention_backward(*args, do.cuda()[None])
     for got, want in zip(grads[:3], lo.attention_backward(*ref, _f64(ld), _f64(do))):
         assert _neighbours(got[0], want) <= 1e-3
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("H,G,dk,dv", [(4, 2, 32, 64), (4, 4, 32, 64), (3, 1, 20, 33)])
+@pytest.mark.parametrize("offsets", [[100, 700, 1400], [0, 700, 700, 1463], [37, 37], [1500, 1500, -3], [5, 5000, 9]])
+def test_gradients_of_tokens_without_a_sequence(g, dtype, H, G, dk, dv, offsets):  # noqa: F811
+    """Tokens before the first and after the last sequence (padding of a packed batch): their gradients are not written, whatever the
+    workspace holds."""
+    import ctypes as C
+    import torch
+    import numpy as np
+    from oracle import layer_oracle as lo
+    n, seqs = 1500, len(offsets) - 1
+    q, k, v, do, ld, s0, ds = (x.cuda() for x in _inputs(dtype, n, H, G, dk, dv, seqs, 7))
+    off = torch.tensor(offsets, device="cuda")
+    shape, pq, pk, pv = g._attention(q, k, v, ld, off, 1.0)
+    need = g.lib.goom_linear_attention_backward_workspace_bytes(C.byref(shape), 1)
+    ws = torch.full((need // 4 + 1024,), float("nan"), device="cuda")
+    grads = [torch.full_like(x, 7.0) for x in (q, k, v)]
+    gs = torch.empty_like(s0)
+    p = lambda t: C.c_void_p(t.data_ptr())  # noqa: E731
+    assert g.lib.goom_linear_attention_backward(g._ctx, C.byref(shape), pq, pk, pv, p(ld), p(off), p(s0), p(do), p(ds), p(grads[0]), p(grads[1]), p(grads[2]), p(gs),
+                                                p(ws), need) == 0
+    assert ws[need // 4:].isnan().all()
+    cut = [min(max(a, 0), n) for a in offsets]
+    inside = torch.zeros(n, dtype=torch.bool)
+    for s, (a, b) in enumerate(zip(cut, cut[1:])):
+        inside[a:b] = True
+        if b < a:
+            continue
+        args = [_f64(x[a:b]) for x in (q, k, v)]
+        st, dst = _f64(s0[s:s + 1]), _f64(ds[s:s + 1])
+        want = lo.attention_backward(*args, _f64(ld), _f64(do[a:b]), st, dst)
+        mag = lo.attention_backward(*[np.abs(x) for x in args], _f64(ld), np.abs(_f64(do[a:b])), np.abs(st), np.abs(dst))
+        terms = max(dk, dv) + 64 + n // 64 + 32 + H // G
+        for name, got, w, m in zip(("grad_q", "grad_k", "grad_v"), grads, want, mag):
+            _near(got[a:b], w, m, dtype, terms, False, name)
+        _near(gs[s:s + 1], want[3], mag[3], "f32", terms, False, "grad_state")
+    for got in grads:
+        assert (got[~inside.cuda()] == 7).all()
