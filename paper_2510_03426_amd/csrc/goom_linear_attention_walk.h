@@ -378,18 +378,25 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
         cx.fetch(c + t0 * r.c_tok, r.c_tok, n, nc);
     };
     if (nchunks > 0) fetch(0);
-    if (OUT) {
-        for (int u = threadIdx.x; u < 8 * PAIRS; u += THREADS) {
-            const int first = REV ? 31 - u / 8 : u / 8 - 32, age = REV ? u % 8 - first : first - u % 8; // i - j of the eight's first j
-            reinterpret_cast<float *>(pair_weights)[u] = age >= 0 ? r.p_scale * decay_power(g2, age) : 0.0f;
-        }
+    // Backwards the first chunk may be short.  The rows that are not there are zeros, and so must their weights be: those of a growing decay
+    // may be out of range.  (Forwards a chunk's rows meet no later ones, and the next state's weights are formed for it.)
+    auto weigh = [&](int rows) {
+        if (OUT)
+            for (int u = threadIdx.x; u < 8 * PAIRS; u += THREADS) {
+                const int first = REV ? 31 - u / 8 : u / 8 - 32, age = REV ? u % 8 - first : first - u % 8; // i - j of the eight's first j
+                reinterpret_cast<float *>(pair_weights)[u] = age >= 0 && age < rows ? r.p_scale * decay_power(g2, age) : 0.0f;
+            }
+        for (int x = threadIdx.x; x < CH; x += THREADS) state_weights[x] = !REV || x < rows ? r.u_scale * decay_power(g2, REV ? x + 1 : CH - x) : 0.0f;
+    };
+    if (OUT)
         for (int x = threadIdx.x; x < CH; x += THREADS) row_weights[x] = r.w_scale * decay_power(g2, x);
-    }
-    for (int x = threadIdx.x; x < CH; x += THREADS) state_weights[x] = r.u_scale * decay_power(g2, REV ? x + 1 : CH - x);
+    const bool cut = REV && nchunks > 0 && chunk_rows(chunk_at(0)) < CH;
+    weigh(cut ? chunk_rows(chunk_at(0)) : CH);
     for (int step = 0; step < nchunks; step++) {
         const long long t0 = chunk_at(step);
         const int n = chunk_rows(t0);
         __syncthreads();
+        if (REV && step == 1 && cut) weigh(CH);
         if (OUT) ax.template put<Lds::PK>(a_lds, n, r.ka);
         bx.template put<Lds::PK>(b_lds, n, r.ka);
         cx.template put<Lds::PV>(c_lds, n, nc);

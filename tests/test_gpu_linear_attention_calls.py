@@ -101,3 +101,29 @@ def test_gradients_of_tokens_without_a_sequence(g, dtype, H, G, dk, dv, offsets)
         _near(gs[s:s + 1], want[3], mag[3], "f32", terms, False, "grad_state")
     for got in grads:
         assert (got[~inside.cuda()] == 7).all()
+
+
+@pytest.mark.parametrize("dtype,decay,offsets", [("bf16", 1.5, [0, 40]), ("bf16", 1.5, [0, 1, 30, 70]), ("f32", 3.0, [0, 20]), ("f32", 2.9, [0, 7, 7, 24]), ("bf16", 0.75, [0, 100]),
+                                                 ("bf16", 0.7, [0, 65, 100, 190])])
+def test_growing_decays(g, dtype, decay, offsets):  # noqa: F811
+    """Decays above one, within the range of floats over the sequences' lengths but not over those of whole chunks: the chunks' missing
+    rows count for nothing.  The exponent of a power, age times log2 of the decay, is rounded three times: 3 u of itself, age |log decay|
+    times the power, beside what test_gpu_linear_attention.py allows."""
+    import torch
+    import numpy as np
+    from oracle import layer_oracle as lo
+    n, seqs, dk, dv = offsets[-1], len(offsets) - 1, 32, 40
+    q, k, v, do, ld, s0, ds = _inputs(dtype, n, 2, 1, dk, dv, seqs, 17, decays=[decay, -0.1])
+    args, st, dst = [_f64(x) for x in (q, k, v)], _f64(s0), _f64(ds)
+    mags = [np.abs(x) for x in args]
+    terms = dv + 64 + 32 + 2 + int(3 * decay * n)
+    off = torch.tensor(offsets).cuda()
+    dev = [x.cuda() for x in (q, k, v, ld)]
+    o, last = g.linear_attention(*dev, state=s0.cuda(), offsets=off, want_state=True)
+    for name, got, want, mag, t in zip(("o", "state"), (o, last), lo.attention(*args, _f64(ld), st, offsets), lo.attention(*mags, _f64(ld), np.abs(st), offsets), (dtype, "f32")):
+        _near(got, want, mag, t, terms, False, name)
+    grads = g.linear_attention_backward(*dev, do.cuda(), state=s0.cuda(), grad_state=ds.cuda(), offsets=off)
+    want = lo.attention_backward(*args, _f64(ld), _f64(do), st, dst, offsets)
+    mag = lo.attention_backward(*mags, _f64(ld), np.abs(_f64(do)), np.abs(st), np.abs(dst), offsets)
+    for name, got, w, m, t in zip(("grad_q", "grad_k", "grad_v", "grad_state"), grads, want, mag, (dtype, dtype, dtype, "f32")):
+        _near(got, w, m, t, terms, False, name)
