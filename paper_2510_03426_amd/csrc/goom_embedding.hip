@@ -330,11 +330,12 @@ __device__ inline void run_starts(const unsigned *keys, unsigned *start, unsigne
 // wave each 64 V columns of a block.
 template <typename S, int V> __global__ __launch_bounds__(256) void runs_kernel(const S *grad, const unsigned *keys, const unsigned *values, unsigned *start, float *sums, unsigned n, unsigned vocab, int width, int parts)
 {
-    if (blockIdx.x <= n / 256) {
-        run_starts(keys, start, n, vocab, blockIdx.x);
+    const long long at = block_of();
+    if (at <= n / 256) {
+        run_starts(keys, start, n, vocab, (unsigned)at);
         return;
     }
-    const unsigned task = (blockIdx.x - n / 256 - 1) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), block = task / parts;
+    const unsigned task = (unsigned)(at - n / 256 - 1) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), block = task / parts; // (below 2^29)
     const unsigned i = block * RUN;
     if (block >= n / RUN) return;
     const unsigned key = keys[i];
@@ -347,10 +348,10 @@ template <typename S, int V> __global__ __launch_bounds__(256) void runs_kernel(
     store_floats_unaligned<float, V>(sums + (long long)block * width + col, x);
 }
 
-// 64 V columns of a table row a wave: the run's head, its whole blocks, its tail.  grid: vocab parts / 4
+// 64 V columns of a table row a wave: the run's head, its whole blocks, its tail.  grid: vocab parts / 4, in one order
 template <typename S, typename W, int V> __global__ __launch_bounds__(256) void table_row_kernel(const S *grad, const unsigned *values, const unsigned *start, const float *sums, W *table, long long vocab, int width, int parts, float scale)
 {
-    const long long task = blockIdx.x * 4ll + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = task / parts;
+    const long long task = block_of() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = task / parts;
     int col = ((int)(task - row * parts) * 64 + (threadIdx.x & 63)) * V;
     if (row >= vocab) return;
     const unsigned begin = start[row], end = start[row + 1];
@@ -389,7 +390,7 @@ template <typename S, typename W, int V> __global__ __launch_bounds__(256) void 
 constexpr int FEW = 256;
 template <typename S, typename W, int V> __global__ __launch_bounds__(256) void few_rows_kernel(const S *grad, const int64_t *tokens, W *table, unsigned n, long long vocab, int width, int parts, float scale)
 {
-    const long long task = blockIdx.x * 4ll + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = task / parts;
+    const long long task = block_of() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = task / parts;
     const int lane = threadIdx.x & 63;
     int col = ((int)(task - row * parts) * 64 + lane) * V;
     if (row >= vocab) return;
@@ -557,10 +558,10 @@ int goom_embedding_backward(goom_ctx *ctx, const int64_t *tokens, const void *gr
             if constexpr (V <= 4) {
                 const S *const gr = reinterpret_cast<const S *>(grad);
                 const int parts = (width + 64 * V - 1) / (64 * V);
-                const unsigned row_groups = (unsigned)((vocab * parts + 3) / 4);
+                const dim3 row_groups = grid_of((vocab * parts + 3) / 4, 256);
                 if (n > FEW) {
                     goom::prof_begin(ctx, "embedding gradient: runs");
-                    runs_kernel<S, V><<<(unsigned)(n / 256 + 1 + (n / RUN * parts + 3) / 4), 256, 0, ctx->stream>>>(gr, keys, values, start, sums, (unsigned)n, (unsigned)vocab, width, parts);
+                    runs_kernel<S, V><<<grid_of(n / 256 + 1 + (n / RUN * parts + 3) / 4, 256), 256, 0, ctx->stream>>>(gr, keys, values, start, sums, (unsigned)n, (unsigned)vocab, width, parts);
                     goom::prof_end(ctx);
                 }
                 goom::prof_begin(ctx, "embedding gradient: rows");

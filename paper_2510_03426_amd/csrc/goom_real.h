@@ -72,6 +72,15 @@ template <typename F> int with_type(int type, F f)
     }
 }
 
+// A grid of any number of workgroups in one order.  The hardware counts the threads along an axis in 32 bits: more go on along y, and
+// the last workgroups may be beyond `blocks`.
+inline dim3 grid_of(long long blocks, int threads)
+{
+    const long long most = 0xffffffffll / threads, rows = (blocks + most - 1) / most;
+    return rows <= 1 ? dim3((unsigned)blocks) : dim3((unsigned)((blocks + rows - 1) / rows), (unsigned)rows);
+}
+__device__ inline long long block_of() { return blockIdx.y * (long long)gridDim.x + blockIdx.x; }
+
 // entry checks that the layer operators share (goom_linear_attention.hip)
 int enter(goom_ctx *ctx);
 int check_workspace(goom_ctx *ctx, const void *ws, size_t given, size_t need);

@@ -1,0 +1,35 @@
+"""The layer operators where a launch has more threads than 32 bits count along one axis of a grid.  Whole numbers, whose sums are exact,
+or parts of a large call against the same parts alone."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def g():
+    import torch
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    from paper_2510_03426_amd import Goom
+    g = Goom(0)
+    yield g
+    g._ws = None
+    g.close()
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("vocab", [(1 << 26) + 3, (1 << 31) - 1])
+@pytest.mark.parametrize("n", [100, 1000])
+def test_tables_of_many_rows(g, n, vocab):
+    """A wave for every table row: 2^32 threads from 2^26 rows on.  Up to 256 positions take one launch, more the sort and the runs."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    tokens = torch.randint(0, vocab, (n,), device="cuda", generator=gen)
+    tokens[:50] = vocab - 1
+    tokens[50:60] = 0
+    tokens[60:70] = (1 << 26) + 1
+    grad = torch.randint(1, 9, (n, 1), device="cuda", generator=gen).float()
+    out = g.embedding_backward(tokens, grad, vocab, dtype=torch.bfloat16)[:, 0]
+    rows, at = tokens.unique(return_inverse=True)
+    want = torch.zeros(rows.numel(), device="cuda").index_add_(0, at, grad[:, 0])
+    assert torch.equal(out[rows], want.bfloat16())
+    assert int((out != 0).sum()) == rows.numel()
