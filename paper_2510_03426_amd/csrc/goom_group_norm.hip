@@ -442,12 +442,14 @@ template <typename S, int V> __global__ __launch_bounds__(512) void norm_sums_ke
     }
 }
 
-// means over a group of dz w and of dz w xhat; a workgroup (of 256 or 1024 threads) a group.  grid: items groups
+// means over a group of dz w and of dz w xhat; a workgroup (of 256 or 1024 threads) a group.  grid: items groups, in one order
 __global__ __launch_bounds__(1024) void norm_means_kernel(NormArgs a)
 {
     __shared__ double meet[2][16];
-    const long long item = blockIdx.x / a.groups;
-    const int group = blockIdx.x % a.groups, wave = threadIdx.x >> 6, threads = blockDim.x;
+    const long long at_group = block_of();
+    if (at_group >= a.items * a.groups) return;
+    const long long item = (unsigned)at_group / (unsigned)a.groups; // (2 10^9 at most)
+    const int group = (unsigned)at_group % (unsigned)a.groups, wave = threadIdx.x >> 6, threads = blockDim.x;
     double m1 = 0.0, m2 = 0.0;
     // a thread has one channel (or every threads-th) and every rows-th chunk, eight chunks' sums at once
     const int cols = a.cg < threads ? a.cg : threads, rows = threads / cols, row = threadIdx.x / cols;
@@ -485,7 +487,7 @@ __global__ __launch_bounds__(1024) void norm_means_kernel(NormArgs a)
     if (threadIdx.x < 2) {
         double sum = 0.0;
         for (int k = 0; k < threads / 64; k++) sum += meet[threadIdx.x][k];
-        a.means[blockIdx.x * 2ll + threadIdx.x] = (float)(sum / ((double)a.length * a.cg));
+        a.means[at_group * 2 + threadIdx.x] = (float)(sum / ((double)a.length * a.cg));
     }
 }
 
@@ -663,9 +665,12 @@ static int check_norm(goom_ctx *ctx, const goom_norm_shape *sh)
     return GOOM_OK;
 }
 
+static int threads_of(const NormPlan &p) { return p.team ? 256 : (p.a.threads + 63) / 64 * 64; }
+
+// (a grid has fewer than 2^32 threads along its first axis)
 static int check_grid(goom_ctx *ctx, const NormPlan &p)
 {
-    if (p.blocks > 0x7fffffffll || p.parts > 65535) return goom::fail(ctx, GOOM_EUNSUPPORTED, "too many items or groups");
+    if (p.blocks > 0xffffffffll / threads_of(p) || p.parts > 65535) return goom::fail(ctx, GOOM_EUNSUPPORTED, "too many items or groups");
     return GOOM_OK;
 }
 
@@ -719,10 +724,10 @@ int goom_group_norm(goom_ctx *ctx, const goom_norm_shape *shape, const void *x, 
     const size_t size = real_bytes(shape->type), wsize = real_bytes(shape->param_type);
     if (!aligned(x, size) || !aligned(y, size) || !aligned(weight, wsize) || !aligned(bias, wsize) || !aligned(mean, 4) || !aligned(rstd, 4))
         return fail(ctx, GOOM_EINVAL, "misaligned data pointer");
-    if (int s = check_workspace(ctx, workspace, workspace_bytes, norm_bytes(*shape, false))) return s;
-    if (int s = enter(ctx)) return s;
     NormPlan p = norm_plan(*shape, norm_cap(*shape, x, y, nullptr), false);
     if (int s = check_grid(ctx, p)) return s;
+    if (int s = check_workspace(ctx, workspace, workspace_bytes, norm_bytes(*shape, false))) return s;
+    if (int s = enter(ctx)) return s;
     NormArgs &a = p.a;
     a.x = x;
     a.weight = weight;
@@ -742,7 +747,7 @@ int goom_group_norm(goom_ctx *ctx, const goom_norm_shape *shape, const void *x, 
             });
             goom::prof_end(ctx);
         } else {
-            const int threads = (a.threads + 63) / 64 * 64;
+            const int threads = threads_of(p);
             goom::prof_begin(ctx, "group norm: sums");
             with_width<S>(p.v, [&](auto vec) {
                 norm_stats_kernel<S, decltype(vec)::value><<<grid, threads, 0, ctx->stream>>>(a);
@@ -772,8 +777,6 @@ int goom_group_norm_backward(goom_ctx *ctx, const goom_norm_shape *shape, const 
     for (const void *q : params)
         if (!aligned(q, wsize)) return fail(ctx, GOOM_EINVAL, "misaligned data pointer");
     if (!aligned(mean, 4) || !aligned(rstd, 4)) return fail(ctx, GOOM_EINVAL, "misaligned data pointer");
-    if (int s = check_workspace(ctx, workspace, workspace_bytes, shape->items ? norm_bytes(*shape, true) : 0)) return s;
-    if (int s = enter(ctx)) return s;
     NormPlan p = {};
     if (shape->items > 0) {
         p = norm_plan(*shape, norm_cap(*shape, x, grad_y, grad_x), true);
@@ -783,6 +786,8 @@ int goom_group_norm_backward(goom_ctx *ctx, const goom_norm_shape *shape, const 
         p.a.channels = shape->channels;
         p.a.type_w = shape->param_type;
     }
+    if (int s = check_workspace(ctx, workspace, workspace_bytes, shape->items ? norm_bytes(*shape, true) : 0)) return s;
+    if (int s = enter(ctx)) return s;
     NormArgs &a = p.a;
     a.x = x;
     a.gy = grad_y;
@@ -814,14 +819,14 @@ int goom_group_norm_backward(goom_ctx *ctx, const goom_norm_shape *shape, const 
                 goom::prof_end(ctx);
             }
         } else {
-            const int threads = (a.threads + 63) / 64 * 64;
-            const unsigned groups = (unsigned)(a.items * a.groups);
+            const int threads = threads_of(p);
+            const int means_threads = a.chunks * a.cg <= 4096 ? 256 : 1024;
             goom::prof_begin(ctx, "group norm gradient: sums");
             with_width<S>(p.v, [&](auto vec) {
                 norm_sums_kernel<S, decltype(vec)::value><<<grid, threads, 0, ctx->stream>>>(a);
                 return 0;
             });
-            norm_means_kernel<<<groups, a.chunks * a.cg <= 4096 ? 256 : 1024, 0, ctx->stream>>>(a);
+            norm_means_kernel<<<grid_of(a.items * a.groups, means_threads), means_threads, 0, ctx->stream>>>(a);
             goom::prof_end(ctx);
             goom::prof_begin(ctx, "group norm gradient");
             with_width<S>(p.v, [&](auto vec) {

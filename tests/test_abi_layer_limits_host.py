@@ -1,0 +1,26 @@
+"""Sizes that no launch takes are refused before anything is enqueued, through the C ABI and without a GPU: with a null context, what
+is in order ends in GOOM_EINVAL for the context."""
+import ctypes as C
+
+import pytest
+
+from test_abi_layer_host import EINVAL, EUNSUP, P, attention, err, lib  # noqa: F401
+
+
+def norm(**kw):
+    from paper_2510_03426_amd.binding import NormShape
+    f = dict(items=4, length=1000, channels=64, groups=8, type=16, param_type=16, activation=1, flags=0, eps=1e-5)
+    f.update(kw)
+    return NormShape(**f)
+
+
+@pytest.mark.parametrize("kw", [dict(items=1 << 24, length=600, channels=8), dict(items=1 << 30, length=3, channels=2048, groups=1), dict(items=1 << 25, length=2100, channels=1, groups=1)])
+def test_group_norm(lib, kw):  # noqa: F811
+    """Long groups: a workgroup an item at least, of 192 threads or more."""
+    many = norm(**kw)
+    few = norm(**{**kw, "items": 1 << 20})
+    forward = lambda s: lib.goom_group_norm(None, C.byref(s), P, None, None, P, None, None, P, 1 << 60)  # noqa: E731
+    back = lambda s: lib.goom_group_norm_backward(None, C.byref(s), *[P] * 9, P, 1 << 60)  # noqa: E731
+    for call in (forward, back):
+        assert call(many) == EUNSUP and "too many" in err(lib)
+        assert call(few) == EINVAL and "context" in err(lib)

@@ -33,3 +33,19 @@ def test_tables_of_many_rows(g, n, vocab):
     want = torch.zeros(rows.numel(), device="cuda").index_add_(0, at, grad[:, 0])
     assert torch.equal(out[rows], want.bfloat16())
     assert int((out != 0).sum()) == rows.numel()
+
+
+def test_group_norm_gradient_of_many_groups(g):
+    """A workgroup for the means of every item and group: 2^24 of them are 2^32 threads."""
+    import torch
+    items, length, C = 9 * 8192, 513, 256
+    x = torch.empty(items, length, C, dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(4))
+    _, mean, rstd = g.group_norm(x, C, activation="silu", want_stats=True)
+    gx, gw, _ = g.group_norm_backward(x, x, mean, rstd, C, activation="silu")
+    total = torch.zeros(C, dtype=torch.float64, device="cuda")
+    for a in range(0, items, 8192):
+        part = x[a:a + 8192]
+        px, pw, _ = g.group_norm_backward(part, part, mean[a:a + 8192], rstd[a:a + 8192], C, activation="silu")
+        assert torch.equal(px, gx[a:a + 8192])
+        total += pw.double()
+    assert torch.allclose(gw.double(), total, rtol=1e-5)
