@@ -208,6 +208,7 @@ static int check_shape(goom_ctx *ctx, const goom_attention_shape *given, goom_at
     if (!packed && sh.seqs > 0 && sh.tokens % sh.seqs) return goom::fail(ctx, GOOM_EINVAL, "without offsets the sequences have tokens / seqs tokens each");
     if (need_equal && sh.seqs != sh.tokens) return goom::fail(ctx, GOOM_EINVAL, "one token a sequence");
     if (sh.seqs > (1 << 24) / sh.heads || sh.tokens > (1ll << 40) || sh.tokens / CHUNK > (1 << 24) / sh.heads) return goom::fail(ctx, GOOM_EUNSUPPORTED, "too many sequences, heads or tokens");
+    if (need_equal && sh.seqs * sh.heads > 0xffffffffll / 256) return goom::fail(ctx, GOOM_EUNSUPPORTED, "too many sequences or heads"); // threads of a grid's first axis
     const int64_t rows[3][3] = {{sh.q_token, sh.q_head, sh.dk}, {sh.k_token, sh.k_head, sh.dk}, {sh.v_token, sh.v_head, sh.dv}};
     for (auto &x : rows)
         if (x[0] < 0 || x[1] < 0 || ((x[0] || x[1]) && (x[0] < x[2] || x[1] < x[2])) || x[0] > (1ll << 40) || x[1] > (1ll << 40))

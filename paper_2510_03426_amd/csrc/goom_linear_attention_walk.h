@@ -562,13 +562,13 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
     }
 }
 
-// grid: slots heads parts roles; the roles of a head and segment run on one XCD (of 8, dealt round robin), whose L2 has the rows
+// grid: slots heads parts roles, in one order; the roles of a head and segment run on one XCD (of 8, dealt round robin), whose L2 has the rows
 // they share
 template <typename S, int DK, int DV, int NW, bool OUT>
 __global__ __launch_bounds__(NW * 64, (WalkLds<S, DK, DV, NW, OUT>::per_simd)) void walk_kernel(WalkArgs w)
 {
     extern __shared__ __align__(16) unsigned char lds[];
-    const unsigned group = blockIdx.x / (8 * w.roles), in = blockIdx.x % (8 * w.roles);
+    const unsigned block = (unsigned)block_of(), group = block / (8 * w.roles), in = block % (8 * w.roles); // (2^28 at most)
     const unsigned item = group * 8 + in % 8;
     if (item >= w.slots * w.heads * w.parts) return;
     const WalkRole &r = w.role[in / 8];
@@ -640,7 +640,7 @@ template <typename S, int DK, int DV, int NW> static int launch_walks_sized(goom
     int nc = 0;
     for (int k = 0; k < roles; k++) nc = w.role[k].nc > nc ? w.role[k].nc : nc;
     w.parts = (nc + DV - 1) / DV;
-    const unsigned grid = (unsigned)((slots * w.heads * w.parts + 7) / 8 * 8 * roles);
+    const dim3 grid = grid_of((slots * w.heads * w.parts + 7) / 8 * 8 * roles, NW * 64);
     const bool parts = w.role[0].totals != nullptr;
     if (parts) {
         auto *totals = walk_kernel<S, DK, DV, NW, false>;

@@ -24,3 +24,11 @@ def test_group_norm(lib, kw):  # noqa: F811
     for call in (forward, back):
         assert call(many) == EUNSUP and "too many" in err(lib)
         assert call(few) == EINVAL and "context" in err(lib)
+
+
+def test_linear_attention_step(lib):  # noqa: F811
+    """256 threads for every head of every sequence: fewer than 2^24 of them."""
+    step = lambda n, heads: lib.goom_linear_attention_step(None, C.byref(attention(seqs=n, tokens=n, heads=heads, kv_heads=heads)), *[P] * 7)  # noqa: E731
+    for heads in (1, 16):
+        assert step((1 << 24) // heads, heads) == EUNSUP and "too many" in err(lib)
+        assert step((1 << 24) // heads - 1, heads) == EINVAL and "context" in err(lib)

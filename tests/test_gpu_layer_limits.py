@@ -49,3 +49,19 @@ def test_group_norm_gradient_of_many_groups(g):
         assert torch.equal(px, gx[a:a + 8192])
         total += pw.double()
     assert torch.allclose(gw.double(), total, rtol=1e-5)
+
+
+def test_linear_attention_of_many_short_sequences(g):
+    """2^20 sequences of one token and 16 heads of one entry: three walks each, 2^32.6 threads.  One token: o = scale q (k v + decay s), and
+    the gradients are products of the others, all of small whole numbers and exact."""
+    import torch
+    n, H = 1 << 20, 16
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    q, k, v, do, s0, ds = (torch.randint(-3, 4, (n, 1, H, 1), device="cuda", generator=gen).float() for _ in range(6))
+    ld = torch.zeros(H, device="cuda")
+    state, dstate = s0.reshape(n, H, 1, 1), ds.reshape(n, H, 1, 1)
+    o, last = g.linear_attention(q, k, v, ld, state=state, scale=2.0, want_state=True)
+    assert torch.equal(last.reshape(q.shape), k * v + s0) and torch.equal(o, 2 * q * (k * v + s0))
+    gq, gk, gv, gs = g.linear_attention_backward(q, k, v, ld, do, state=state, grad_state=dstate, scale=2.0)
+    u = 2 * q * do + ds  # the state's adjoint
+    assert torch.equal(gq, 2 * do * (k * v + s0)) and torch.equal(gk, u * v) and torch.equal(gv, u * k) and torch.equal(gs.reshape(q.shape), u)
