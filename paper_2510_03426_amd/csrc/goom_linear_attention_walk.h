@@ -378,8 +378,8 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
         cx.fetch(c + t0 * r.c_tok, r.c_tok, n, nc);
     };
     if (nchunks > 0) fetch(0);
-    // Backwards the first chunk may be short.  The rows that are not there are zeros, and so must their weights be: those of a growing decay
-    // may be out of range.  (Forwards a chunk's rows meet no later ones, and the next state's weights are formed for it.)
+    // Backwards the first chunk may be short.  The rows that are not there are zeros, and so their weights must be finite: those of a growing
+    // decay, which may be out of range, are zeros in that chunk.  (Forwards a chunk's rows meet no later ones, and the next state's weights are formed for it.)
     auto weigh = [&](int rows) {
         if (OUT)
             for (int u = threadIdx.x; u < 8 * PAIRS; u += THREADS) {
@@ -390,7 +390,7 @@ __device__ inline void walk(const WalkArgs &w, const WalkRole &r, const Place &a
     };
     if (OUT)
         for (int x = threadIdx.x; x < CH; x += THREADS) row_weights[x] = r.w_scale * decay_power(g2, x);
-    const bool cut = REV && nchunks > 0 && chunk_rows(chunk_at(0)) < CH;
+    const bool cut = REV && g2 > 0.0f && nchunks > 0 && chunk_rows(chunk_at(0)) < CH;
     weigh(cut ? chunk_rows(chunk_at(0)) : CH);
     for (int step = 0; step < nchunks; step++) {
         const long long t0 = chunk_at(step);
