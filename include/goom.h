@@ -490,7 +490,7 @@ typedef struct goom_attention_shape {
     int32_t dk, dv;    /* entries of a head's q and k, and of its v and o; 1 <= dk, dv <= GOOM_MAX_DIM */
     int32_t type;      /* GOOM_REAL_*, of q, k, v, o and their gradients */
     int32_t flags;     /* 0 */
-    double scale;      /* of the outputs; finite */
+    double scale;      /* of the outputs; finite, within the range of floats */
     int64_t q_token, q_head; /* elements from one token, and from one head, to the next in q, k and v (the last axis is */
     int64_t k_token, k_head; /* contiguous, tokens of all sequences follow one another): slices of a fused projection */
     int64_t v_token, v_head; /* need no copy.  Both 0: contiguous, [tokens, heads, d] */
@@ -546,7 +546,7 @@ typedef struct goom_norm_shape {
     int32_t param_type;       /* GOOM_REAL_* of weight, bias and their gradients */
     int32_t activation;       /* GOOM_ACT_* */
     int32_t flags;            /* 0 */
-    double eps;               /* >= 0 */
+    double eps;               /* >= 0, within the range of floats */
 } goom_norm_shape;
 
 /* weight, bias: NULL (1 and 0) or [channels]; y: of x's shape; mean, rstd: NULL or [items, groups] floats, what the backward
@@ -566,7 +566,7 @@ int goom_group_norm_backward(goom_ctx *ctx, const goom_norm_shape *shape, const 
 size_t goom_group_norm_backward_workspace_bytes(const goom_norm_shape *shape);
 
 /* Token embeddings: rows[i] = scale table[tokens[i]].  table: [vocab, width], rows: [n, width] of one type; tokens: [n] int64
- * (device); a token outside 0 .. vocab - 1 (padding) gives a row of zeros and takes no gradient. */
+ * (device); a token outside 0 .. vocab - 1 (padding) gives a row of zeros and takes no gradient.  scale: within the range of floats. */
 int goom_embedding(goom_ctx *ctx, const void *table, const int64_t *tokens, void *rows, int64_t n, int64_t vocab, int width,
                    int type, double scale);
 

@@ -480,7 +480,7 @@ int goom_embedding(goom_ctx *ctx, const void *table, const int64_t *tokens, void
 {
     if (!real_type(type)) return fail(ctx, GOOM_EINVAL, "unknown element type %d", type);
     if (int s = check_embedding(ctx, n, vocab, width)) return s;
-    if (!std::isfinite(scale)) return fail(ctx, GOOM_EINVAL, "scale must be finite");
+    if (!std::isfinite((float)scale)) return fail(ctx, GOOM_EINVAL, "scale must be finite, and a float");
     if (n == 0) return ctx ? GOOM_OK : fail(nullptr, GOOM_EINVAL, "null context");
     if (!table || !tokens || !rows) return fail(ctx, GOOM_EINVAL, "null data pointer");
     const size_t size = real_bytes(type);
@@ -514,7 +514,7 @@ int goom_embedding_backward(goom_ctx *ctx, const int64_t *tokens, const void *gr
 {
     if (!real_type(type) || !real_type(table_type)) return fail(ctx, GOOM_EINVAL, "unknown element type %d", real_type(type) ? table_type : type);
     if (int s = check_embedding(ctx, n, vocab, width)) return s;
-    if (!std::isfinite(scale)) return fail(ctx, GOOM_EINVAL, "scale must be finite");
+    if (!std::isfinite((float)scale)) return fail(ctx, GOOM_EINVAL, "scale must be finite, and a float");
     if (!grad_table || (n > 0 && (!tokens || !grad))) return fail(ctx, GOOM_EINVAL, "null data pointer");
     const size_t size = real_bytes(type), wsize = real_bytes(table_type);
     if (!aligned(grad, size) || !aligned(grad_table, wsize) || !aligned(tokens, 8)) return fail(ctx, GOOM_EINVAL, "misaligned data pointer");

@@ -659,7 +659,7 @@ static int check_norm(goom_ctx *ctx, const goom_norm_shape *sh)
     if (sh->items < 0 || sh->length <= 0 || sh->channels <= 0) return goom::fail(ctx, GOOM_EINVAL, "items must not be negative, length and channels positive");
     if (sh->groups <= 0 || sh->channels % sh->groups) return goom::fail(ctx, GOOM_EINVAL, "groups must be positive and divide channels");
     if (sh->activation < GOOM_ACT_NONE || sh->activation > GOOM_ACT_GELU) return goom::fail(ctx, GOOM_EINVAL, "unknown activation %d", sh->activation);
-    if (!(sh->eps >= 0.0) || !std::isfinite(sh->eps)) return goom::fail(ctx, GOOM_EINVAL, "eps must be finite and not negative");
+    if (!(sh->eps >= 0.0) || !std::isfinite((float)sh->eps) || (sh->eps > 0.0 && (float)sh->eps == 0.0f)) return goom::fail(ctx, GOOM_EINVAL, "eps must be finite and not negative, and a float");
     if (sh->items > (1ll << 31) || sh->length > (1ll << 31) || sh->channels > (1 << 20) || (double)sh->items * sh->length * sh->channels > 1e15 || (double)sh->items * sh->groups > 2e9)
         return goom::fail(ctx, GOOM_EUNSUPPORTED, "too many items, positions or channels");
     return GOOM_OK;

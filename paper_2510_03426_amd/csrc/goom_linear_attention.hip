@@ -203,7 +203,7 @@ static int check_shape(goom_ctx *ctx, const goom_attention_shape *given, goom_at
     if (sh.heads <= 0 || sh.kv_heads <= 0 || sh.heads % sh.kv_heads) return goom::fail(ctx, GOOM_EINVAL, "kv_heads must be positive and divide heads");
     if (sh.dk <= 0 || sh.dv <= 0) return goom::fail(ctx, GOOM_EINVAL, "dk and dv must be positive");
     if (sh.dk > GOOM_MAX_DIM || sh.dv > GOOM_MAX_DIM) return goom::fail(ctx, GOOM_EUNSUPPORTED, "dk and dv go up to %d", GOOM_MAX_DIM);
-    if (!std::isfinite(sh.scale)) return goom::fail(ctx, GOOM_EINVAL, "scale must be finite");
+    if (!std::isfinite((float)sh.scale)) return goom::fail(ctx, GOOM_EINVAL, "scale must be finite, and a float");
     if (sh.seqs == 0 && sh.tokens > 0) return goom::fail(ctx, GOOM_EINVAL, "tokens without a sequence");
     if (!packed && sh.seqs > 0 && sh.tokens % sh.seqs) return goom::fail(ctx, GOOM_EINVAL, "without offsets the sequences have tokens / seqs tokens each");
     if (need_equal && sh.seqs != sh.tokens) return goom::fail(ctx, GOOM_EINVAL, "one token a sequence");

@@ -32,3 +32,14 @@ def test_linear_attention_step(lib):  # noqa: F811
     for heads in (1, 16):
         assert step((1 << 24) // heads, heads) == EUNSUP and "too many" in err(lib)
         assert step((1 << 24) // heads - 1, heads) == EINVAL and "context" in err(lib)
+
+
+def test_scales_that_no_float_holds(lib):  # noqa: F811
+    """They would be infinities, or an eps of zero, on the device."""
+    for scale in (1e39, -1e300):
+        assert lib.goom_linear_attention(None, C.byref(attention(scale=scale)), P, P, P, P, None, None, P, None, P, 1 << 40) == EINVAL and "scale" in err(lib)
+        assert lib.goom_embedding(None, P, P, P, 5, 10, 8, 16, scale) == EINVAL and "scale" in err(lib)
+        assert lib.goom_embedding_backward(None, P, P, P, 5, 10, 8, 16, 17, scale, P, 1 << 40) == EINVAL and "scale" in err(lib)
+    for eps in (1e39, 1e-60):
+        assert lib.goom_group_norm(None, C.byref(norm(eps=eps)), P, None, None, P, None, None, P, 1 << 40) == EINVAL and "eps" in err(lib)
+    assert lib.goom_group_norm(None, C.byref(norm(eps=0.0)), P, None, None, P, None, None, P, 1 << 40) == EINVAL and "context" in err(lib)
