@@ -505,7 +505,7 @@ typedef struct goom_attention_shape {
  * incoming state, 64 tokens (32 for halves and floats) at a time on the matrix instructions.  All of them are sums of one
  * (bfloat16), two (half) or three (float) bf16 parts; operands computed on the way are held in three (24 bits), whatever the
  * type.  Outputs do not depend on whether the final state is asked for.
- * A NaN or an infinity among q, k, v may show in all outputs of its head in its sequence.
+ * A NaN or an infinity among q, k, v (a float above 3.39e38 counts as one) may show in all outputs of its head in its sequence.
  * workspace: goom_linear_attention_workspace_bytes(shape, offsets != NULL) bytes (may be 0).
  * Errors: GOOM_EINVAL (null or misaligned pointers, sizes, types), GOOM_EUNSUPPORTED (dk or dv above GOOM_MAX_DIM),
  * GOOM_EWORKSPACE. */
@@ -538,7 +538,8 @@ size_t goom_linear_attention_backward_workspace_bytes(const goom_attention_shape
  *     y = act((x - mean) rstd weight + bias),    rstd = 1 / sqrt(variance + eps). */
 #define GOOM_ACT_NONE 0
 #define GOOM_ACT_SILU 1 /* z / (1 + e^-z) */
-#define GOOM_ACT_GELU 2 /* z (1 + erf(z / sqrt 2)) / 2 */
+#define GOOM_ACT_GELU 2 /* z (1 + erf(z / sqrt 2)) / 2; erf is off by 1.5e-7 at most, so that far below zero, where the value vanishes, it
+                           * has fewer correct digits: relative 5e-5 at z = -3, 2e-3 at -5, 1e-2 at -8 */
 typedef struct goom_norm_shape {
     int64_t items, length;
     int32_t channels, groups; /* groups divides channels */
@@ -550,8 +551,9 @@ typedef struct goom_norm_shape {
 } goom_norm_shape;
 
 /* weight, bias: NULL (1 and 0) or [channels]; y: of x's shape; mean, rstd: NULL or [items, groups] floats, what the backward
- * pass takes.  Groups of up to 2048 elements are held in registers and read once; longer ones (length above 1) are read a
- * second time for the output.  workspace: goom_group_norm_workspace_bytes(shape) bytes (may be 0). */
+ * pass takes.  Short groups are held in registers and read once: those of up to 512 vectors of 4 entries (float) or 256 of 8, 2048
+ * entries at most.  A vector lies in one position and has no more entries than the group has channels (narrow groups: 512 vectors of 1,
+ * 2 or 4); a position's last one counts whole.  Longer groups are read a second time for the output.  workspace: goom_group_norm_workspace_bytes(shape) bytes (may be 0). */
 int goom_group_norm(goom_ctx *ctx, const goom_norm_shape *shape, const void *x, const void *weight, const void *bias, void *y,
                     float *mean, float *rstd, void *workspace, size_t workspace_bytes);
 size_t goom_group_norm_workspace_bytes(const goom_norm_shape *shape);

@@ -686,7 +686,7 @@ class Goom:
     def linear_attention(self, q, k, v, log_decay, state=None, offsets=None, scale: float = 1.0, want_state: bool = False):
         """o_t = scale q_t^T S_t, S_t = exp(log_decay) S_{t-1} + k_t v_t^T for every head.  q: [batch, T, heads, dk], k: [batch, T,
         kv_heads, dk], v: [batch, T, kv_heads, dv], or without the batch axis and with offsets (int64 [sequences + 1]) where
-        sequences of different lengths lie behind one another; state, and the final one that want_state adds: float32 [sequences,
+        sequences of different lengths lie behind one another (what is returned for tokens that no sequence has is not set); state, and the final one that want_state adds: float32 [sequences,
         heads, dk, dv].  q, k, v may be slices of one projection's output."""
         torch = self.torch
         shape, pq, pk, pv = self._attention(q, k, v, log_decay, offsets, scale)
@@ -712,7 +712,7 @@ class Goom:
 
     def linear_attention_backward(self, q, k, v, log_decay, grad_o, state=None, grad_state=None, offsets=None, scale: float = 1.0):
         """Gradients with respect to q, k, v and (None without one) the initial state, given those with respect to the outputs and
-        (None: none) the final state."""
+        (None: none) the final state.  Tokens that no sequence has: as above."""
         empty = self.torch.empty
         shape, pq, pk, pv = self._attention(q, k, v, log_decay, offsets, scale)
         if grad_o.shape != q.shape[:-1] + (shape.dv,) or grad_o.dtype != q.dtype:
