@@ -470,7 +470,8 @@ size_t goom_affine_scan_backward_workspace_bytes(int64_t T, int d, int64_t batch
 /* ---- operators around the recurrences in a layer of a language model ------------------------------------------------ */
 
 /* Element types of the real tensors below (none of them a goom_dtype).  Sums, statistics and states are held in 32 bits or
- * more whatever the type; a result is rounded once, when it is stored. */
+ * more whatever the type; a result is rounded once, when it is stored.  Outputs overlap neither inputs nor each other, unless it is said
+ * that they may. */
 typedef enum goom_real {
     GOOM_REAL_F32 = 16,
     GOOM_REAL_BF16 = 17,
@@ -521,7 +522,7 @@ int goom_linear_attention_step(goom_ctx *ctx, const goom_attention_shape *shape,
 
 /* Gradients of a loss L, given grad_o = dL / do ([tokens, heads, dv], contiguous, of the shape's type) and, unless NULL,
  * grad_final = dL / d final_state: grad_q, grad_k, grad_v (contiguous, of the shape's type; heads that share k and v are
- * summed in float, in a fixed order) and, unless NULL, grad_state (floats).  With u = scale (the adjoint of a state),
+ * summed in float, in a fixed order) and, unless NULL, grad_state (floats; not the array grad_final).  With u = scale (the adjoint of a state),
  *     grad_q_i = u sum_{j <= i} gamma^(i-j) (grad_o_i . v_j) k_j,   grad_k_j = u sum_{i >= j} gamma^(i-j) (v_j . grad_o_i) q_i,
  *     grad_v_j = u sum_{i >= j} gamma^(i-j) (k_j . q_i) grad_o_i,
  * and the terms of the first and the final state: three walks of the forward kind, two of them backwards in time.

@@ -65,3 +65,26 @@ def test_linear_attention_of_many_short_sequences(g):
     gq, gk, gv, gs = g.linear_attention_backward(q, k, v, ld, do, state=state, grad_state=dstate, scale=2.0)
     u = 2 * q * do + ds  # the state's adjoint
     assert torch.equal(gq, 2 * do * (k * v + s0)) and torch.equal(gk, u * v) and torch.equal(gv, u * k) and torch.equal(gs.reshape(q.shape), u)
+
+
+def test_linear_attention_past_32_bit_offsets(g):
+    """The last of 4.3e9 elements against the recurrence in 64 bits, with the tolerances of test_gpu_linear_attention.py."""
+    import numpy as np
+    import torch
+    from oracle import layer_oracle as lo
+    from test_gpu_linear_attention import _f64, _near
+    n, H, d, T = 530000, 64, 128, 300
+    assert (n - T) * H * d > 2 ** 32
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    q, k, v, do = (torch.empty(n, H, d, dtype=torch.bfloat16, device="cuda").normal_(generator=gen) for _ in range(4))
+    ld = torch.linspace(-0.5, -0.02, H, device="cuda")
+    offsets = torch.tensor([0, 1000, n - T, n], device="cuda")
+    o = g.linear_attention(q, k, v, ld, offsets=offsets)
+    grads = g.linear_attention_backward(q, k, v, ld, do, offsets=offsets)[:3]
+    args = [_f64(x[n - T:]) for x in (q, k, v)]
+    mags = [np.abs(x) for x in args]
+    terms = d + 64 + T // 64 + 32
+    _near(o[n - T:], lo.attention(*args, _f64(ld))[0], lo.attention(*mags, _f64(ld))[0], "bf16", terms, False, "o")
+    want, mag = lo.attention_backward(*args, _f64(ld), _f64(do[n - T:])), lo.attention_backward(*mags, _f64(ld), np.abs(_f64(do[n - T:])))
+    for name, got, w, m in zip(("grad_q", "grad_k", "grad_v"), grads, want, mag):
+        _near(got[n - T:], w, m, "bf16", terms, False, name)
