@@ -127,12 +127,13 @@ static Segments choose_segments(const goom_attention_shape &sh, int roles, bool 
         return with_walk<S>(sh.dk, sh.dv, [](auto rows, auto cols, auto waves) { return WalkLds<S, decltype(rows)::value, decltype(cols)::value, decltype(waves)::value, true>::resident; });
     });
     // (sequences of different lengths: two rounds of shorter ones, which even out.  Two, three, four and six rounds: 7 sequences of 9000
-    // tokens in all, 8 heads of 128, both directions 235, 276, 293 and 292 us; 20 of 30,000, 16 heads of 64 411, 386, 407 and 426;
-    // 37 of 30,011, 12 float heads of 50 and 72, forward 309, 307, 299 and 304)
+    // tokens in all, 8 heads of 128, bfloat16, both directions 237, 272, 282 and 280 us; 20 of 30,000, 16 heads of 64 437, 396, 412 and 435;
+    // 37 of 30,011, 12 float heads of 50 and 72, forward 278, 279, 273 and 275.  Places are counted for (dk, dv) also where walks of different
+    // sizes go together, padded to the larger.)
     const long long walks = sh.seqs * sh.heads * roles, round = 256 * resident * (packed ? 2 : 1), mean = sh.seqs > 0 ? (sh.tokens + sh.seqs - 1) / sh.seqs : 0;
     long long want = walks > 0 ? round / walks : 1; // segments a sequence of mean length
-    // Not below two chunks each (one, where lengths differ): measured at 8 x 1000 tokens of 8 heads of 32 and 64, forward and
-    // backward, 148, 139 and 140 us with four, two and one chunks; at 5 ragged sequences of 1500 tokens in all, 141, 113 and 95 us
+    // Not below two chunks each (one, where lengths differ): measured at 8 x 1000 float tokens of 8 heads of 32 and 64, forward and
+    // backward, 141, 132 and 132 us with four, two and one chunks; at 5 ragged sequences of 1500 tokens in all, 86, 73 and 70 us
     const long long least = packed ? CHUNK : 2 * CHUNK, most = (mean + least - 1) / least;
     if (want > most) want = most;
     if (want < 1) want = 1;
@@ -247,9 +248,11 @@ static BackwardPlan backward_plan(const goom_attention_shape &sh, bool packed)
 {
     BackwardPlan p;
     p.seg = choose_segments(sh, 3, packed);
-    // Walks of different sizes go together, padded to the larger, where the chip has room for all of them at once: a small
-    // pass is bound by its launches.  (6000 tokens of 32 bfloat16 heads of 110 and 25: 109 us together, 124 apart; of 128 and 64 98 and
-    // 114.  Floats pay six products for the padding: heads of 110 and 25 240 and 191, of 50 and 100 176 and 170, so only up to 64.)
+    // Walks of different sizes go together, padded to the larger, where they are, before they are cut into segments, no more than the
+    // chip has CUs: a small pass is bound by its launches.  (Both directions, together and apart: one sequence of 6000 tokens, 32 bfloat16 heads
+    // of 110 and 25, 401 and 459 us, of 128 and 64, 330 and 377; two of 600 142 and 161.  Floats pay six products for the padding: 8295 tokens, 4 heads of
+    // 110 and 25, packed from 7 sequences 243 and 202 us, from 15 236 and 189, 15 equal ones 219 and 235; of 50 and 100, 15 packed, 234 and
+    // 208; of 64 and 30, 15 equal, 101 and 126.  So only up to 64.)
     const int most = sh.dk > sh.dv ? sh.dk : sh.dv, least = sh.dk > sh.dv ? sh.dv : sh.dk;
     p.together = padded_head(least) == padded_head(most) || (sh.seqs * sh.heads * 3 <= 256 && (sh.type != GOOM_REAL_F32 || padded_head(most) <= 64));
     const int dk = p.together ? most : sh.dk, dv = p.together ? most : sh.dv;

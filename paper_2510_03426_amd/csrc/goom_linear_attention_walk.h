@@ -13,9 +13,10 @@
 // touches memory.  Where there are fewer walks than the chip holds at once, every sequence is cut into segments: segment totals
 // (the walk without outputs), carries, then all segments at once.
 //
-// Measured (bfloat16; a copy reaches 5.09 TB/s): 65,536 tokens of 16 heads of 64: totals 72 us (3.7 TB/s), carries 10, walk 135
-// (4.0 TB/s); 8 x 4096 tokens of 16 heads of 128: 66 + 11 + 157 us, the three walks of the backward pass 497.  What bounds it: the
-// issue of 780 vector and 190 matrix instructions a wave and chunk, by two waves a SIMD (three for heads of 64).
+// Measured (bfloat16; a copy reaches 5.09 TB/s): 65,536 tokens of 16 heads of 64: totals 71 us (3.8 TB/s), carries 10, walk 141
+// (3.8 TB/s); 8 x 4096 tokens of 16 heads of 128: 69 + 11 + 177 us, the three walks of the backward pass 592.  What bounds it: no one
+// unit.  Of a wave's 19,100 cycles a chunk (950 other vector and 236 matrix instructions, two waves a SIMD) 25 % issue vector
+// instructions, in 31 % it is ready and waits to issue, in 34 % it waits for LDS, memory and barriers; the matrix unit is busy for 39 %.
 //
 // A workgroup walks one head of one segment.  Each wave owns nc / NW columns of the state, which stay in its registers as
 // accumulators of the matrix instruction for the whole walk; the rows of the tiles are numbered such that a lane's
