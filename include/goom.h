@@ -534,6 +534,52 @@ int goom_linear_attention_backward(goom_ctx *ctx, const goom_attention_shape *sh
                                    void *workspace, size_t workspace_bytes);
 size_t goom_linear_attention_backward_workspace_bytes(const goom_attention_shape *shape, int packed);
 
+/* The gated delta rule: linear attention whose state forgets by its data.  Every token decays its head's state by a factor of its own
+ * and, before it adds its value, takes off beta times what the state already holds for its key:
+ *     S_t = a_t (S_{t-1} - beta_t k_t (k_t^T S_{t-1})) + beta_t k_t v_t^T,      o_t = scale q_t^T S_t,      a_t = exp(log_decay_t).
+ * -inf, a decay of zero, forgets everything before the token; logarithms below -110 count as that.  Keys are usually of length one and beta
+ * between 0 and 1, or 2: with beta |k|^2 above 2 the recurrence itself grows, and its rounding errors with it. */
+typedef struct goom_delta_shape {
+    int64_t seqs;      /* sequences */
+    int64_t tokens;    /* tokens of all sequences; without offsets every sequence has tokens / seqs of them */
+    int32_t heads;     /* heads of v, o, the decays, beta and the states */
+    int32_t qk_heads;  /* heads of q and k, a divisor of heads: head h reads q and k of head h / (heads / qk_heads) */
+    int32_t dk, dv;    /* entries of a head's q and k, and of its v and o; 1 <= dk, dv <= GOOM_MAX_DIM */
+    int32_t type;      /* GOOM_REAL_*, of q, k, v, o and their gradients */
+    int32_t flags;     /* 0 */
+    double scale;      /* of the outputs; finite, within the range of floats */
+    int64_t q_token, q_head; /* elements from one token, and from one head, to the next in q, k and v (the last axis is */
+    int64_t k_token, k_head; /* contiguous, tokens of all sequences follow one another): slices of a fused projection */
+    int64_t v_token, v_head; /* need no copy.  Both 0: contiguous, [tokens, heads, d] */
+} goom_delta_shape;
+
+/* All tokens of all sequences.  q, k: [tokens, qk_heads, dk], v: [tokens, heads, dv]; log_decay, beta: [tokens, heads] floats;
+ * o: [tokens, heads, dv], contiguous; offsets, state, final_state: as for goom_linear_attention (final_state may be the array `state`;
+ * outputs of tokens that no sequence has are not written).  Chunks of 64 tokens (32 for halves and floats): what lies within them is
+ * solved for all chunks at once, then every head's state walks along its sequence, which is cut into segments, chained as affine maps of
+ * the state, where sequences and heads are few.  Operands are held as for goom_linear_attention (24 bits where they are computed); sums of
+ * logarithms take 64 bits.  A NaN or an infinity in an input may show in all outputs of its head in its sequence.
+ * workspace: goom_gated_delta_workspace_bytes(shape, offsets != NULL) bytes: some 0.6 KB a token and head in bfloat16, 0.4 KB in the
+ * other types, and the segments' maps. */
+int goom_gated_delta(goom_ctx *ctx, const goom_delta_shape *shape, const void *q, const void *k, const void *v, const float *log_decay, const float *beta,
+                     const int64_t *offsets, const float *state, void *o, float *final_state, void *workspace, size_t workspace_bytes);
+size_t goom_gated_delta_workspace_bytes(const goom_delta_shape *shape, int packed);
+
+/* One token of each sequence, for decoding: seqs = tokens; reads every state once (NULL: zeros) and writes it once.  next_state: [seqs, heads,
+ * dk, dv], required; it may be the array `state`.  No workspace. */
+int goom_gated_delta_step(goom_ctx *ctx, const goom_delta_shape *shape, const void *q, const void *k, const void *v, const float *log_decay, const float *beta,
+                          const float *state, void *o, float *next_state);
+
+/* Gradients of a loss, given grad_o ([tokens, heads, dv], contiguous, of the shape's type) and, unless NULL, grad_final, that with respect to the
+ * final state: grad_q, grad_k, grad_v (contiguous, of the shape's type; those of heads that share q and k are summed in float, in a fixed order),
+ * grad_log_decay and grad_beta ([tokens, heads] floats; a decay of zero has no slope) and, unless NULL, grad_state (floats; not the array grad_final).
+ * The forward pass's inputs are given again.  workspace: goom_gated_delta_backward_workspace_bytes(shape, offsets != NULL) bytes: two states and
+ * two chunks of rows in floats for each chunk and head (in bfloat16 with heads of 128, 4 KB a token and head). */
+int goom_gated_delta_backward(goom_ctx *ctx, const goom_delta_shape *shape, const void *q, const void *k, const void *v, const float *log_decay, const float *beta,
+                              const int64_t *offsets, const float *state, const void *grad_o, const float *grad_final, void *grad_q, void *grad_k, void *grad_v,
+                              float *grad_log_decay, float *grad_beta, float *grad_state, void *workspace, size_t workspace_bytes);
+size_t goom_gated_delta_backward_workspace_bytes(const goom_delta_shape *shape, int packed);
+
 /* Group norm with an activation, channels last.  x: [items, length, channels]; a group is channels / groups neighbouring
  * channels over the whole length of an item (length 1: over one position, as after the heads of a recurrence):
  *     y = act((x - mean) rstd weight + bias),    rstd = 1 / sqrt(variance + eps). */

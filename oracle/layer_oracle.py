@@ -122,3 +122,63 @@ def embedding_backward(tokens, grad, vocab, scale=1.0):
     ok = (tokens >= 0) & (tokens < vocab)
     np.add.at(out, tokens[ok], grad[ok] * scale)
     return out
+
+
+# ---- the gated delta rule, token after token
+
+def gated_delta(q, k, v, log_decay, beta, state=None, offsets=None, scale=1.0):
+    """q, k: [tokens, Q, dk], v: [tokens, H, dv], log_decay, beta: [tokens, H], state: [sequences, H, dk, dv]; returns (o, final states,
+    the largest norm of each head's states)."""
+    q, k, v, log_decay, beta = (np.asarray(x, dtype=np.float64) for x in (q, k, v, log_decay, beta))
+    n, H, dv = v.shape
+    share = np.arange(H) // (H // q.shape[1])
+    spans = _spans(n, offsets)
+    o, last, most = np.zeros((n, H, dv)), np.zeros((len(spans), H, q.shape[2], dv)), np.zeros(H)
+    for s, (a, b) in enumerate(spans):
+        S = np.zeros(last.shape[1:]) if state is None else np.array(state[s], dtype=np.float64)
+        for t in range(a, b):
+            most = np.maximum(most, np.sqrt((S * S).sum((1, 2))))
+            S = _delta_step(S, k[t, share], v[t], log_decay[t], beta[t])[0]
+            o[t] = scale * np.einsum("hk,hkv->hv", q[t, share], S)
+        most = np.maximum(most, np.sqrt((S * S).sum((1, 2))))
+        last[s] = S
+    return o, last, most
+
+
+def _delta_step(S, k, v, log_decay, beta):
+    S = np.exp(log_decay)[:, None, None] * S
+    e = v - np.einsum("hk,hkv->hv", k, S)
+    return S + k[:, :, None] * (beta[:, None] * e)[:, None, :], e
+
+
+def gated_delta_backward(q, k, v, log_decay, beta, grad_o, state=None, grad_state=None, offsets=None, scale=1.0):
+    """Adjoints of the recurrence, walked backwards: returns (grad_q, grad_k, grad_v, grad_log_decay, grad_beta, grad_state or None, the
+    largest norm of each head's adjoints)."""
+    q, k, v, log_decay, beta, grad_o = (np.asarray(x, dtype=np.float64) for x in (q, k, v, log_decay, beta, grad_o))
+    n, H, dv = v.shape
+    share = np.arange(H) // (H // q.shape[1])
+    spans = _spans(n, offsets)
+    gq, gk, gv, ga, gb = (np.zeros_like(x) for x in (q, k, v, log_decay, beta))
+    gs, most = np.zeros((len(spans), H, q.shape[2], dv)), np.zeros(H)
+    for s, (a, b) in enumerate(spans):
+        S = np.zeros(gs.shape[1:]) if state is None else np.array(state[s], dtype=np.float64)
+        before, errors = [], []
+        for t in range(a, b):
+            before.append(S)
+            S, e = _delta_step(S, k[t, share], v[t], log_decay[t], beta[t])
+            errors.append(e)
+        before.append(S)
+        D = np.zeros(gs.shape[1:]) if grad_state is None else np.array(grad_state[s], dtype=np.float64)
+        for t in range(b - 1, a - 1, -1):
+            old, new, e, decay = before[t - a], before[t - a + 1], errors[t - a], np.exp(log_decay[t])[:, None]
+            np.add.at(gq[t], share, scale * np.einsum("hkv,hv->hk", new, grad_o[t]))
+            D = D + scale * q[t, share][:, :, None] * grad_o[t][:, None, :]
+            most = np.maximum(most, np.sqrt((D * D).sum((1, 2))))
+            w = np.einsum("hk,hkv->hv", k[t, share], D)
+            gb[t] = (w * e).sum(-1)
+            gv[t] = beta[t][:, None] * w
+            np.add.at(gk[t], share, np.einsum("hkv,hv->hk", D, beta[t][:, None] * e) - decay * np.einsum("hkv,hv->hk", old, gv[t]))
+            D = decay[:, :, None] * (D - k[t, share][:, :, None] * gv[t][:, None, :])
+            ga[t] = (D * old).sum((1, 2))
+        gs[s] = D
+    return gq, gk, gv, ga, gb, gs if state is not None else None, most

@@ -37,6 +37,7 @@ EXPORTS = [
     "goom_lmme_backward", "goom_lmme_backward_workspace_bytes", "goom_scan_backward", "goom_scan_backward_workspace_bytes", "goom_scaled_exp_backward",
     "goom_linear_attention", "goom_linear_attention_workspace_bytes", "goom_linear_attention_step",
     "goom_linear_attention_backward", "goom_linear_attention_backward_workspace_bytes",
+    "goom_gated_delta", "goom_gated_delta_workspace_bytes", "goom_gated_delta_step", "goom_gated_delta_backward", "goom_gated_delta_backward_workspace_bytes",
     "goom_group_norm", "goom_group_norm_workspace_bytes", "goom_group_norm_backward", "goom_group_norm_backward_workspace_bytes",
     "goom_embedding", "goom_embedding_backward", "goom_embedding_backward_workspace_bytes",
 ]
@@ -58,6 +59,12 @@ class ResetOpts(C.Structure):
 
 class AttentionShape(C.Structure):
     _fields_ = [("seqs", C.c_int64), ("tokens", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("dk", C.c_int32), ("dv", C.c_int32),
+                ("type", C.c_int32), ("flags", C.c_int32), ("scale", C.c_double), ("q_token", C.c_int64), ("q_head", C.c_int64),
+                ("k_token", C.c_int64), ("k_head", C.c_int64), ("v_token", C.c_int64), ("v_head", C.c_int64)]
+
+
+class DeltaShape(C.Structure):
+    _fields_ = [("seqs", C.c_int64), ("tokens", C.c_int64), ("heads", C.c_int32), ("qk_heads", C.c_int32), ("dk", C.c_int32), ("dv", C.c_int32),
                 ("type", C.c_int32), ("flags", C.c_int32), ("scale", C.c_double), ("q_token", C.c_int64), ("q_head", C.c_int64),
                 ("k_token", C.c_int64), ("k_head", C.c_int64), ("v_token", C.c_int64), ("v_head", C.c_int64)]
 
@@ -156,6 +163,13 @@ def load_library():
     lib.goom_linear_attention_backward.argtypes = [vp, pa, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz]
     lib.goom_linear_attention_backward_workspace_bytes.argtypes = [pa, i32]
     lib.goom_linear_attention_backward_workspace_bytes.restype = sz
+    pd = C.POINTER(DeltaShape)
+    lib.goom_gated_delta.argtypes = [vp, pd, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz]
+    lib.goom_gated_delta_step.argtypes = [vp, pd, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.goom_gated_delta_backward.argtypes = [vp, pd] + [vp] * 16 + [sz]
+    for f in (lib.goom_gated_delta_workspace_bytes, lib.goom_gated_delta_backward_workspace_bytes):
+        f.argtypes = [pd, i32]
+        f.restype = sz
     pn = C.POINTER(NormShape)
     lib.goom_group_norm.argtypes = [vp, pn, vp, vp, vp, vp, vp, vp, vp, sz]
     lib.goom_group_norm_backward.argtypes = [vp, pn, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz]
@@ -724,6 +738,72 @@ class Goom:
         self._check(self.lib.goom_linear_attention_backward(self._ctx, C.byref(shape), pq, pk, pv, _at(log_decay), _at(offsets), ps, _at(grad_o), pg,
                                                             gq.data_ptr(), gk.data_ptr(), gv.data_ptr(), _at(gs), _at(ws), wsn))
         return gq, gk, gv, gs
+
+    # ---- the gated delta rule
+    def _delta(self, q, k, v, log_decay, beta, offsets, scale, step=False):
+        """The shape structure and the addresses of q, k, v."""
+        code = _real_code(q)
+        if k.dtype != q.dtype or v.dtype != q.dtype or log_decay.dtype != self.torch.float32 or beta.dtype != self.torch.float32:
+            raise TypeError("q, k, v have one type, log_decay and beta are float32")
+        sq, sv = tuple(q.shape), tuple(v.shape)
+        lead, (qk_heads, dk), (heads, dv) = sq[:-2], sq[-2:], sv[-2:]
+        if len(sq) < 3 or tuple(k.shape) != sq or sv[:-2] != lead or tuple(log_decay.shape) != lead + (heads,) or tuple(beta.shape) != lead + (heads,):
+            raise ValueError("shapes of q, k, v, log_decay, beta do not fit")
+        tokens = math.prod(lead)
+        if offsets is not None:
+            if offsets.dtype != self.torch.int64 or offsets.dim() != 1 or offsets.numel() < 1 or len(lead) != 1:
+                raise ValueError("offsets: int64 [sequences + 1], with q, k, v [tokens, heads, d]")
+            seqs = offsets.numel() - 1
+        elif step:
+            seqs = tokens
+        else:
+            seqs = math.prod(lead[:-1])
+        pq, q_token, q_head = _rows(q, "q")
+        pk, k_token, k_head = _rows(k, "k")
+        pv, v_token, v_head = _rows(v, "v")
+        return DeltaShape(seqs, tokens, heads, qk_heads, dk, dv, code, 0, scale, q_token, q_head, k_token, k_head, v_token, v_head), pq, pk, pv
+
+    def gated_delta(self, q, k, v, log_decay, beta, state=None, offsets=None, scale: float = 1.0, want_state: bool = False):
+        """o_t = scale q_t^T S_t, S_t = a_t (S_{t-1} - beta_t k_t k_t^T S_{t-1}) + beta_t k_t v_t^T for every head, a_t = exp(log_decay_t).
+        q, k: [batch, T, qk_heads, dk], v: [batch, T, heads, dv], log_decay, beta: float32 [batch, T, heads], or without the batch axis and with
+        offsets (int64 [sequences + 1]) where sequences of different lengths lie behind one another (what is returned for tokens that no
+        sequence has is not set); state, and the final one that want_state adds: float32 [sequences, heads, dk, dv].  q, k, v may be slices
+        of one projection's output."""
+        torch = self.torch
+        shape, pq, pk, pv = self._delta(q, k, v, log_decay, beta, offsets, scale)
+        ps = self._state(state, shape, "state")
+        o = torch.empty(v.shape, dtype=v.dtype, device=v.device)
+        last = torch.empty((shape.seqs, shape.heads, shape.dk, shape.dv), dtype=torch.float32, device=q.device) if want_state else None
+        ws, wsn = self.workspace(self.lib.goom_gated_delta_workspace_bytes(C.byref(shape), int(offsets is not None)))
+        self._check(self.lib.goom_gated_delta(self._ctx, C.byref(shape), pq, pk, pv, _at(log_decay), _at(beta), _at(offsets), ps, o.data_ptr(), _at(last), _at(ws), wsn))
+        return (o, last) if want_state else o
+
+    def gated_delta_step(self, q, k, v, log_decay, beta, state, scale: float = 1.0, out_state=None):
+        """One token of each sequence: q, k: [batch, qk_heads, dk], v: [batch, heads, dv], log_decay, beta: [batch, heads]; state: float32
+        [batch, heads, dk, dv], replaced by the next one, or left as it is if out_state receives that."""
+        if q.dim() != 3:
+            raise ValueError("q: [batch, qk_heads, dk]")
+        shape, pq, pk, pv = self._delta(q, k, v, log_decay, beta, None, scale, step=True)
+        ps = self._state(state, shape, "state")
+        pn = ps if out_state is None else self._state(out_state, shape, "out_state")
+        o = self.torch.empty(v.shape, dtype=v.dtype, device=v.device)
+        self._check(self.lib.goom_gated_delta_step(self._ctx, C.byref(shape), pq, pk, pv, _at(log_decay), _at(beta), ps, o.data_ptr(), pn))
+        return o
+
+    def gated_delta_backward(self, q, k, v, log_decay, beta, grad_o, state=None, grad_state=None, offsets=None, scale: float = 1.0):
+        """Gradients with respect to q, k, v, log_decay, beta and (None without one) the initial state, given those with respect to the outputs
+        and (None: none) the final state.  Tokens that no sequence has: as above."""
+        empty = self.torch.empty
+        shape, pq, pk, pv = self._delta(q, k, v, log_decay, beta, offsets, scale)
+        if grad_o.shape != v.shape or grad_o.dtype != v.dtype:
+            raise ValueError("grad_o: of o's shape and type")
+        gq, gk, gv, ga, gb = (empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v, log_decay, beta))
+        ps, pg = self._state(state, shape, "state"), self._state(grad_state, shape, "grad_state")
+        gs = empty(state.shape, dtype=state.dtype, device=state.device) if state is not None else None
+        ws, wsn = self.workspace(self.lib.goom_gated_delta_backward_workspace_bytes(C.byref(shape), int(offsets is not None)))
+        self._check(self.lib.goom_gated_delta_backward(self._ctx, C.byref(shape), pq, pk, pv, _at(log_decay), _at(beta), _at(offsets), ps, _at(grad_o), pg, gq.data_ptr(),
+                                                       gk.data_ptr(), gv.data_ptr(), ga.data_ptr(), gb.data_ptr(), _at(gs), _at(ws), wsn))
+        return gq, gk, gv, ga, gb, gs
 
     # ---- group norm with an activation, channels last
     def _norm(self, x, groups, weight, bias, eps, activation):

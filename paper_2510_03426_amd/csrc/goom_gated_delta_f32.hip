@@ -1,0 +1,13 @@
+// The gated delta rule: what lies within chunks, and the forward walks, for float.
+#include "goom_gated_delta_walk.h"
+
+namespace goom_layer {
+
+template <> int launch_delta_within<float>(goom_ctx *ctx, const DeltaArgs &w, long long slots) { return launch_delta_within_typed<float>(ctx, w, slots); }
+
+template <> int launch_delta_walk<float>(goom_ctx *ctx, const DeltaArgs &w, int mode, long long slots, const char *label)
+{
+    return launch_delta_walk_typed<float, FORWARD, MAPS, KEEP>(ctx, w, mode, slots, label);
+}
+
+} // namespace goom_layer

@@ -237,6 +237,24 @@ int check_workspace(goom_ctx *ctx, const void *ws, size_t given, size_t need)
     return GOOM_OK;
 }
 
+int launch_shared_sums(goom_ctx *ctx, int type, const float *x0, void *y0, int d0, const float *x1, void *y1, int d1, long long tokens, int shared_heads, int group,
+                       const int64_t *offsets, long long seqs, const char *label)
+{
+    const long long rows = tokens * shared_heads;
+    return with_type(type, [&](auto tag) {
+        typedef typename decltype(tag)::type S;
+        const bool vec = d0 % 4 == 0 && d1 % 4 == 0 && goom::aligned(y0, 4 * sizeof(S)) && goom::aligned(y1, 4 * sizeof(S));
+        const int V = vec ? 4 : 1;
+        const long long most = rows * (d0 > d1 ? d0 : d1) / V, blocks = (most + 255) / 256;
+        const SharedSum a = {x0, y0, rows * d0 / V, d0}, b = {x1, y1, rows * d1 / V, d1};
+        auto *kernel = vec ? shared_sum_kernel<S, 4> : shared_sum_kernel<S, 1>;
+        goom::prof_begin(ctx, label);
+        kernel<<<dim3((unsigned)(blocks < 16384 ? blocks : 16384), 2), 256, 0, ctx->stream>>>(a, b, group, shared_heads, offsets, seqs, tokens);
+        goom::prof_end(ctx);
+        return goom::check_hip(ctx, hipGetLastError(), label);
+    });
+}
+
 // bytes of the backward pass's workspace by parts: states of the three walks, floats of shared heads' gradients
 struct BackwardPlan {
     Segments seg;
@@ -398,21 +416,8 @@ int goom_linear_attention_backward(goom_ctx *ctx, const goom_attention_shape *sh
         w.role[0] = gv;
         if (int s = launch_walks(ctx, sh.type, w, 1, plan.seg.slots, "linear attention: gradient of v")) return s;
     }
-    if (shared && sh.tokens > 0) {
-        const long long rows = sh.tokens * sh.kv_heads;
-        return with_type(sh.type, [&](auto tag) {
-            typedef typename decltype(tag)::type S;
-            const bool vec = sh.dk % 4 == 0 && sh.dv % 4 == 0 && aligned(grad_k, 4 * size) && aligned(grad_v, 4 * size);
-            const int V = vec ? 4 : 1;
-            const long long most = rows * (sh.dk > sh.dv ? sh.dk : sh.dv) / V, blocks = (most + 255) / 256;
-            const SharedSum ks = {sum_k, grad_k, rows * sh.dk / V, sh.dk}, vs = {sum_v, grad_v, rows * sh.dv / V, sh.dv};
-            auto *kernel = vec ? shared_sum_kernel<S, 4> : shared_sum_kernel<S, 1>;
-            goom::prof_begin(ctx, "linear attention: shared heads");
-            kernel<<<dim3((unsigned)(blocks < 16384 ? blocks : 16384), 2), 256, 0, ctx->stream>>>(ks, vs, group, sh.kv_heads, offsets, sh.seqs, sh.tokens);
-            goom::prof_end(ctx);
-            return goom::check_hip(ctx, hipGetLastError(), "linear attention: shared heads");
-        });
-    }
+    if (shared && sh.tokens > 0)
+        return launch_shared_sums(ctx, sh.type, sum_k, grad_k, sh.dk, sum_v, grad_v, sh.dv, sh.tokens, sh.kv_heads, group, offsets, sh.seqs, "linear attention: shared heads");
     return GOOM_OK;
 }
 

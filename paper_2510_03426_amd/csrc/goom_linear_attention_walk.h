@@ -58,7 +58,7 @@ struct WalkArgs {
 // at least one, and as many as it has segments, without a pass over the lengths.
 struct Place { long long seq, seg, nseg, start, len; };
 
-__device__ inline void span(const WalkArgs &w, long long s, long long &start, long long &len)
+template <typename W> __device__ inline void span(const W &w, long long s, long long &start, long long &len)
 {
     if (w.offsets) {
         long long b = w.offsets[s], e = w.offsets[s + 1];
@@ -72,7 +72,7 @@ __device__ inline void span(const WalkArgs &w, long long s, long long &start, lo
     }
 }
 
-__device__ inline long long first_slot(const WalkArgs &w, long long s)
+template <typename W> __device__ inline long long first_slot(const W &w, long long s)
 {
     if (!w.offsets) return s * w.segs;
     long long start, len;
@@ -80,7 +80,7 @@ __device__ inline long long first_slot(const WalkArgs &w, long long s)
     return start / w.seg_len + s;
 }
 
-__device__ inline Place find_place(const WalkArgs &w, long long slot)
+template <typename W> __device__ inline Place find_place(const W &w, long long slot)
 {
     Place p;
     if (!w.offsets) {
@@ -692,6 +692,11 @@ template <typename S> int launch_walks_typed(goom_ctx *ctx, const WalkArgs &w, i
         return launch_walks_sized<S, decltype(rows)::value, decltype(cols)::value, decltype(waves)::value>(ctx, w, roles, slots, label);
     });
 }
+
+// gradients of two inputs that heads share, summed over each `group` of heads: x[tokens][heads][d] floats -> y[tokens][heads / group][d]
+// (goom_linear_attention.hip)
+int launch_shared_sums(goom_ctx *ctx, int type, const float *x0, void *y0, int d0, const float *x1, void *y1, int d1, long long tokens, int shared_heads, int group,
+                       const int64_t *offsets, long long seqs, const char *label);
 
 template <typename S> int launch_walks_of(goom_ctx *ctx, const WalkArgs &w, int roles, long long slots, const char *label);
 template <> int launch_walks_of<float>(goom_ctx *ctx, const WalkArgs &w, int roles, long long slots, const char *label);
