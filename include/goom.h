@@ -614,6 +614,66 @@ int goom_group_norm_backward(goom_ctx *ctx, const goom_norm_shape *shape, const 
                              void *grad_bias, void *workspace, size_t workspace_bytes);
 size_t goom_group_norm_backward_workspace_bytes(const goom_norm_shape *shape);
 
+/* Rotary positions: of every head's dim entries the first 2 pairs are turned, pair i by the angle position frequency_i,
+ *     (x1, x2) -> scale (x1 cos a - x2 sin a, x1 sin a + x2 cos a);
+ * the entries behind them are copied as they are (without the scale).  A pair is (x[i], x[pairs + i]), or with GOOM_ROTARY_INTERLEAVED
+ * (x[2 i], x[2 i + 1]).  Longer contexts are a matter of the frequencies and the scale.  Angles are formed in 64 bits, so positions may be as large as they like
+ * below 2^53.  With GOOM_ROTARY_BACK the turn is the other way: the gradient's way back, with the same scale. */
+#define GOOM_ROTARY_INTERLEAVED 1
+#define GOOM_ROTARY_BACK 2
+typedef struct goom_rotary_shape {
+    int64_t tokens;
+    int32_t heads, kv_heads; /* of q, and of k (0: no k) */
+    int32_t dim, pairs;      /* 1 <= pairs <= dim / 2 */
+    int32_t type;            /* GOOM_REAL_* of q, k and what they become */
+    int32_t flags;           /* GOOM_ROTARY_* */
+    double scale;            /* finite, within the range of floats */
+    int64_t q_token, q_head; /* elements from one token, and from one head, to the next in q and k, as in goom_attention_shape: */
+    int64_t k_token, k_head; /* slices of a fused projection need no copy.  Both 0: contiguous */
+} goom_rotary_shape;
+
+/* q: [tokens, heads, dim], k: [tokens, kv_heads, dim]; positions: [tokens] int64 (device); frequencies: [pairs] floats (device), radians a position;
+ * q_out, k_out: contiguous.  No workspace. */
+int goom_rotary(goom_ctx *ctx, const goom_rotary_shape *shape, const void *q, const void *k, const int64_t *positions, const float *frequencies, void *q_out,
+                void *k_out);
+
+/* Norms before and after a block of a layer, with its gate and its residual stream.  Tensors are [tokens, channels]; a group is channels / groups
+ * neighbouring channels of one token (1: the whole token, heads: each head by itself), and norm(x) = (x - mean) / sqrt(variance + eps) with
+ * GOOM_NORM_MEAN, x / sqrt(mean of x^2 + eps) without:
+ *     after:  y = residual + scale (norm(x) weight + bias) act(gate),
+ *     before: h = residual + scale x act(gate),   y = norm(h) weight + bias,
+ * where x is the block's output.  h, rounded to its type, is what is normalised. */
+#define GOOM_NORM_MEAN 1
+typedef struct goom_block_norm_shape {
+    int64_t tokens;
+    int32_t channels, groups; /* groups divides channels; up to 16384 channels a group */
+    int32_t type;             /* GOOM_REAL_* of the tensors and their gradients */
+    int32_t param_type;       /* GOOM_REAL_* of weight, bias, scale and their gradients */
+    int32_t activation;       /* GOOM_ACT_* of the gate */
+    int32_t flags;            /* GOOM_NORM_MEAN */
+    double eps;               /* >= 0, within the range of floats */
+} goom_block_norm_shape;
+
+/* gate, residual: NULL (a factor of 1, and 0) or [tokens, channels]; weight, bias, scale: NULL (1, 0, 1) or [channels]; mean (with GOOM_NORM_MEAN; otherwise
+ * zeros), rstd: NULL or [tokens, groups] floats, what the backward passes take; h: NULL or [tokens, channels]. */
+int goom_norm_after(goom_ctx *ctx, const goom_block_norm_shape *shape, const void *x, const void *gate, const void *residual, const void *weight, const void *bias,
+                    const void *scale, void *y, float *mean, float *rstd);
+int goom_norm_before(goom_ctx *ctx, const goom_block_norm_shape *shape, const void *x, const void *gate, const void *residual, const void *weight, const void *bias,
+                     const void *scale, void *h, void *y, float *mean, float *rstd);
+
+/* Gradients, given those with respect to y (and, for norm_before, unless NULL, to h: what the rest of the stream makes of it).  The residual's gradient
+ * is grad_y itself after a block, grad_residual before one, and there that is the gradient of x as well where neither gate nor scale stand between (grad_x
+ * is not written then).  grad_gate: with a gate; grad_weight, grad_bias, grad_scale: NULL or [channels] of param_type, sums over the tokens in a
+ * fixed order.  x in norm_before_backward: only with a gate or a scale; mean: only with GOOM_NORM_MEAN.  workspace:
+ * goom_block_norm_backward_workspace_bytes(shape) bytes, unless no parameter's gradient is asked for. */
+int goom_norm_after_backward(goom_ctx *ctx, const goom_block_norm_shape *shape, const void *x, const void *gate, const void *grad_y, const float *mean, const float *rstd,
+                             const void *weight, const void *bias, const void *scale, void *grad_x, void *grad_gate, void *grad_weight, void *grad_bias, void *grad_scale,
+                             void *workspace, size_t workspace_bytes);
+int goom_norm_before_backward(goom_ctx *ctx, const goom_block_norm_shape *shape, const void *x, const void *gate, const void *h, const void *grad_y, const void *grad_h,
+                              const float *mean, const float *rstd, const void *weight, const void *scale, void *grad_residual, void *grad_x, void *grad_gate,
+                              void *grad_weight, void *grad_bias, void *grad_scale, void *workspace, size_t workspace_bytes);
+size_t goom_block_norm_backward_workspace_bytes(const goom_block_norm_shape *shape);
+
 /* Token embeddings: rows[i] = scale table[tokens[i]].  table: [vocab, width], rows: [n, width] of one type; tokens: [n] int64
  * (device); a token outside 0 .. vocab - 1 (padding) gives a row of zeros and takes no gradient.  scale: within the range of floats. */
 int goom_embedding(goom_ctx *ctx, const void *table, const int64_t *tokens, void *rows, int64_t n, int64_t vocab, int width,

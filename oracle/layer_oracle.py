@@ -182,3 +182,63 @@ def gated_delta_backward(q, k, v, log_decay, beta, grad_o, state=None, grad_stat
             ga[t] = (D * old).sum((1, 2))
         gs[s] = D
     return gq, gk, gv, ga, gb, gs if state is not None else None, most
+
+
+# ---- rotary positions
+
+def rotary(x, positions, frequencies, interleaved=False, scale=1.0, back=False):
+    """x: [tokens, heads, dim]: pairs as complex numbers, times scale e^(+-i position frequency)."""
+    x = np.array(x, dtype=np.float64)
+    p = len(frequencies)
+    turn = scale * np.exp((-1j if back else 1j) * np.asarray(positions, np.float64)[:, None] * np.asarray(frequencies, np.float64))[:, None, :]
+    one, two = (slice(0, 2 * p, 2), slice(1, 2 * p, 2)) if interleaved else (slice(0, p), slice(p, 2 * p))
+    z = (x[..., one] + 1j * x[..., two]) * turn
+    x[..., one], x[..., two] = z.real, z.imag
+    return x
+
+
+# ---- norms before and after a block
+
+def _groups_norm(x, groups, eps, kind):
+    xg = x.reshape(len(x), groups, -1)
+    mean = xg.mean(-1) if kind == "layer" else np.zeros(xg.shape[:2])
+    rstd = 1 / np.sqrt(((xg - mean[..., None]) ** 2).mean(-1) + eps)
+    return ((xg - mean[..., None]) * rstd[..., None]).reshape(x.shape), mean, rstd
+
+
+def _or(x, otherwise):
+    return otherwise if x is None else np.asarray(x, np.float64)
+
+
+def block_norm(x, groups, weight=None, bias=None, scale=None, gate=None, residual=None, kind="rms", act="silu", eps=1e-5, before=False, rounded=None):
+    """x: [tokens, channels]; returns (y, h or None, mean, rstd).  rounded: takes h to the type that it is held in."""
+    x = np.asarray(x, np.float64)
+    a = 1.0 if gate is None else activation(np.asarray(gate, np.float64), act)[0]
+    w, b, s, r = _or(weight, 1.0), _or(bias, 0.0), _or(scale, 1.0), _or(residual, 0.0)
+    if before:
+        h = r + s * x * a
+        if rounded is not None:
+            h = rounded(h)
+        n, mean, rstd = _groups_norm(h, groups, eps, kind)
+        return n * w + b, h, mean, rstd
+    n, mean, rstd = _groups_norm(x, groups, eps, kind)
+    return r + s * (n * w + b) * a, None, mean, rstd
+
+
+def block_norm_backward(x, grad_y, groups, weight=None, bias=None, scale=None, gate=None, kind="rms", act="silu", eps=1e-5, h=None, grad_h=None):
+    """Returns a dict of the gradients of x, residual, gate, weight, bias, scale; h: what was normalised, before a block."""
+    x, gy = np.asarray(x, np.float64), np.asarray(grad_y, np.float64)
+    a, slope = (1.0, 0.0) if gate is None else activation(np.asarray(gate, np.float64), act)
+    w, b, s = _or(weight, 1.0), _or(bias, 0.0), _or(scale, 1.0)
+    before = h is not None
+    xhat, _, rstd = _groups_norm(np.asarray(h if before else x, np.float64), groups, eps, kind)
+    n = xhat * w + b
+    dn = gy if before else gy * s * a
+    d = (dn * w).reshape(len(x), groups, -1)
+    t = xhat.reshape(d.shape)
+    m1 = d.mean(-1, keepdims=True) if kind == "layer" else 0.0
+    dx = (rstd[..., None] * (d - m1 - t * (d * t).mean(-1, keepdims=True))).reshape(x.shape)
+    if before:
+        total = dx + _or(grad_h, 0.0)
+        return dict(residual=total, x=total * s * a, gate=total * s * x * slope, weight=(dn * xhat).sum(0), bias=dn.sum(0), scale=(total * x * a).sum(0))
+    return dict(residual=gy, x=dx, gate=gy * s * n * slope, weight=(dn * xhat).sum(0), bias=dn.sum(0), scale=(gy * n * a).sum(0))

@@ -22,6 +22,8 @@ RESET_ALWAYS, RESET_COLINEAR, RESET_NEVER = 1, 0, -1
 AFFINE_TIME_INVARIANT = 1
 REAL_F32, REAL_BF16, REAL_F16 = 16, 17, 18
 ACTIVATIONS = {"none": 0, "silu": 1, "gelu": 2}
+ROTARY_INTERLEAVED, ROTARY_BACK = 1, 2
+NORM_KINDS = {"rms": 0, "layer": 1}
 
 EXPORTS = [
     "goom_version", "goom_create", "goom_destroy", "goom_set_stream", "goom_last_error",
@@ -39,6 +41,7 @@ EXPORTS = [
     "goom_linear_attention_backward", "goom_linear_attention_backward_workspace_bytes",
     "goom_gated_delta", "goom_gated_delta_workspace_bytes", "goom_gated_delta_step", "goom_gated_delta_backward", "goom_gated_delta_backward_workspace_bytes",
     "goom_group_norm", "goom_group_norm_workspace_bytes", "goom_group_norm_backward", "goom_group_norm_backward_workspace_bytes",
+    "goom_rotary", "goom_norm_after", "goom_norm_before", "goom_norm_after_backward", "goom_norm_before_backward", "goom_block_norm_backward_workspace_bytes",
     "goom_embedding", "goom_embedding_backward", "goom_embedding_backward_workspace_bytes",
 ]
 
@@ -72,6 +75,16 @@ class DeltaShape(C.Structure):
 class NormShape(C.Structure):
     _fields_ = [("items", C.c_int64), ("length", C.c_int64), ("channels", C.c_int32), ("groups", C.c_int32), ("type", C.c_int32),
                 ("param_type", C.c_int32), ("activation", C.c_int32), ("flags", C.c_int32), ("eps", C.c_double)]
+
+
+class RotaryShape(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("dim", C.c_int32), ("pairs", C.c_int32), ("type", C.c_int32), ("flags", C.c_int32),
+                ("scale", C.c_double), ("q_token", C.c_int64), ("q_head", C.c_int64), ("k_token", C.c_int64), ("k_head", C.c_int64)]
+
+
+class BlockNormShape(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("channels", C.c_int32), ("groups", C.c_int32), ("type", C.c_int32), ("param_type", C.c_int32), ("activation", C.c_int32),
+                ("flags", C.c_int32), ("eps", C.c_double)]
 
 
 def library_path() -> str:
@@ -163,6 +176,14 @@ def load_library():
     lib.goom_linear_attention_backward.argtypes = [vp, pa, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz]
     lib.goom_linear_attention_backward_workspace_bytes.argtypes = [pa, i32]
     lib.goom_linear_attention_backward_workspace_bytes.restype = sz
+    lib.goom_rotary.argtypes = [vp, C.POINTER(RotaryShape)] + [vp] * 6
+    pb = C.POINTER(BlockNormShape)
+    lib.goom_norm_after.argtypes = [vp, pb] + [vp] * 9
+    lib.goom_norm_before.argtypes = [vp, pb] + [vp] * 10
+    lib.goom_norm_after_backward.argtypes = [vp, pb] + [vp] * 14 + [sz]
+    lib.goom_norm_before_backward.argtypes = [vp, pb] + [vp] * 16 + [sz]
+    lib.goom_block_norm_backward_workspace_bytes.argtypes = [pb]
+    lib.goom_block_norm_backward_workspace_bytes.restype = sz
     pd = C.POINTER(DeltaShape)
     lib.goom_gated_delta.argtypes = [vp, pd, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz]
     lib.goom_gated_delta_step.argtypes = [vp, pd, vp, vp, vp, vp, vp, vp, vp, vp]
@@ -257,6 +278,32 @@ def _ptr(t):
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError("libgoom takes contiguous device tensors")
     return C.c_void_p(t.data_ptr())
+
+
+def rotary_frequencies(pairs: int, base: float = 10000.0, factor: float = 1.0, method: str = "none", trained: int = 0, low: float = 1.0, high: float = 32.0,
+                       device="cpu"):
+    """Frequencies for Goom.rotary, float32 [pairs], base^(-i / pairs) radians a position, and the scale that goes with them.  For contexts
+    `factor` times as long as the `trained` one a method other than "none" (which leaves them and 1.0):
+        "linear": all of them divided by the factor;
+        "base":   base times factor^(pairs / (pairs - 1)), so that the first stays and the last is divided by the factor;
+        "parts":  waves that turn at least `high` times within the trained context stay, those that turn at most `low` times are divided by the factor, the ones
+                  between in proportion; the scale is 0.1 log(factor) + 1, on q and on k."""
+    import torch
+    if pairs < 1 or not base > 1 or not factor >= 1 or method not in ("none", "linear", "base", "parts"):
+        raise ValueError('pairs >= 1, base > 1, factor >= 1, method "none", "linear", "base" or "parts"')
+    if method == "base":
+        base *= factor ** (pairs / max(1, pairs - 1))
+    f = torch.pow(torch.tensor(base, dtype=torch.float64), -torch.arange(pairs, dtype=torch.float64) / pairs)
+    scale = 1.0
+    if method == "linear":
+        f = f / factor
+    elif method == "parts":
+        if trained < 1 or not high > low:
+            raise ValueError("parts: the trained context's length, and low < high")
+        stay = ((trained * f / (2 * math.pi) - low) / (high - low)).clamp(0, 1)
+        f = f * stay + f / factor * (1 - stay)
+        scale = 0.1 * math.log(factor) + 1.0
+    return f.to(torch.float32).to(device), scale
 
 
 class Goom:
@@ -854,6 +901,117 @@ class Goom:
         self._check(self.lib.goom_group_norm_backward(self._ctx, C.byref(shape), px, _at(grad_y), _at(mean), _at(rstd), _at(weight), _at(bias), gx.data_ptr(),
                                                       gw.data_ptr(), gb.data_ptr(), _at(ws), wsn))
         return gx, gw, gb
+
+    # ---- rotary positions
+    def _rotary(self, q, k, positions, frequencies, interleaved, scale, flags):
+        torch = self.torch
+        code = _real_code(q)
+        lead, (heads, dim) = tuple(q.shape[:-2]), tuple(q.shape[-2:])
+        if q.dim() < 3 or positions.dtype != torch.int64 or tuple(positions.shape) != lead or frequencies.dtype != torch.float32 or frequencies.dim() != 1:
+            raise ValueError("q: [..., heads, dim]; positions: int64 of q's leading shape; frequencies: float32 [pairs]")
+        pq, q_token, q_head = _rows(q, "q")
+        kv_heads, pk, k_token, k_head, out_k = 0, None, 0, 0, None
+        if k is not None:
+            if k.dtype != q.dtype or k.dim() != q.dim() or tuple(k.shape[:-2]) != lead or k.shape[-1] != dim or k.shape[-2] < 1:
+                raise ValueError("k: [..., kv_heads, dim] of q's leading shape and type")
+            kv_heads = k.shape[-2]
+            pk, k_token, k_head = _rows(k, "k")
+            out_k = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        out_q = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        shape = RotaryShape(math.prod(lead), heads, kv_heads, dim, frequencies.numel(), code, flags | (ROTARY_INTERLEAVED if interleaved else 0), scale, q_token, q_head, k_token, k_head)
+        self._check(self.lib.goom_rotary(self._ctx, C.byref(shape), pq, pk, _at(positions), _at(frequencies), out_q.data_ptr(), _at(out_k)))
+        return out_q, out_k
+
+    def rotary(self, q, k, positions, frequencies, interleaved: bool = False, scale: float = 1.0):
+        """q [..., heads, dim] and (unless None) k [..., kv_heads, dim] with their first 2 pairs entries turned by position times frequency, times
+        scale; positions: int64 [...]; frequencies: float32 [pairs] (rotary_frequencies).  Pairs are (i, pairs + i), or (2 i, 2 i + 1) if interleaved;
+        entries behind them are copied.  q and k may be slices of one projection's output."""
+        return self._rotary(q, k, positions, frequencies, interleaved, scale, 0)
+
+    def rotary_backward(self, grad_q, grad_k, positions, frequencies, interleaved: bool = False, scale: float = 1.0):
+        """Gradients with respect to rotary's q and k."""
+        return self._rotary(grad_q, grad_k, positions, frequencies, interleaved, scale, ROTARY_BACK)
+
+    # ---- norms before and after a block
+    def _block_norm(self, x, groups, weight, bias, scale, gate, residual, kind, activation, eps):
+        act = ACTIVATIONS.get(activation)
+        if x.dim() < 1 or act is None or kind not in NORM_KINDS:
+            raise ValueError("x: [..., channels]; kind: one of " + ", ".join(NORM_KINDS) + "; activation: one of " + ", ".join(ACTIVATIONS))
+        channels, code, first = x.shape[-1], REAL_F32, None
+        for p in (weight, bias, scale):
+            if p is None:
+                continue
+            if tuple(p.shape) != (channels,):
+                raise ValueError("weight, bias and scale: [channels]")
+            if first is not None and p.dtype != first.dtype:
+                raise TypeError("weight, bias and scale have one type")
+            first, code = p, _real_code(p)
+        for t in (gate, residual):
+            if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
+                raise ValueError("gate and residual: of x's shape and type")
+        return BlockNormShape(math.prod(x.shape[:-1]), channels, groups, _real_code(x), code, act, NORM_KINDS[kind], eps), self.torch.float32 if first is None else first.dtype
+
+    def _stats(self, x, groups, kind, want):
+        if not want:
+            return None, None
+        rstd = self.torch.empty(x.shape[:-1] + (groups,), dtype=self.torch.float32, device=x.device)
+        return self.torch.empty_like(rstd) if kind == "layer" else None, rstd
+
+    def norm_after(self, x, groups: int = 1, weight=None, bias=None, scale=None, gate=None, residual=None, kind: str = "rms", activation: str = "silu", eps: float = 1e-5,
+                   want_stats: bool = False):
+        """residual + scale * (norm(x) * weight + bias) * act(gate): what closes a block whose output is x, [..., channels].  Every group of channels /
+        groups neighbouring channels is normalised by itself, by its root mean square ("rms") or, less its mean, by its deviation ("layer").
+        weight, bias, scale: [channels]; gate, residual: of x's shape.  want_stats: also mean (None for "rms") and rstd, float32 [..., groups]."""
+        shape, _ = self._block_norm(x, groups, weight, bias, scale, gate, residual, kind, activation, eps)
+        px = _at(x)
+        y = self.torch.empty_like(x)
+        mean, rstd = self._stats(x, groups, kind, want_stats)
+        self._check(self.lib.goom_norm_after(self._ctx, C.byref(shape), px, _at(gate), _at(residual), _at(weight), _at(bias), _at(scale), y.data_ptr(), _at(mean), _at(rstd)))
+        return (y, mean, rstd) if want_stats else y
+
+    def norm_before(self, x, groups: int = 1, weight=None, bias=None, scale=None, gate=None, residual=None, kind: str = "rms", activation: str = "silu", eps: float = 1e-5,
+                    want_stats: bool = False):
+        """h = residual + scale * x * act(gate), y = norm(h) * weight + bias: what opens the next block, x being the last one's output.  Returns y and
+        h (x itself where there is nothing to add), with want_stats also mean (None for "rms") and rstd.  Arguments as for norm_after."""
+        shape, _ = self._block_norm(x, groups, weight, bias, scale, gate, residual, kind, activation, eps)
+        px = _at(x)
+        y = self.torch.empty_like(x)
+        h = x if scale is None and gate is None and residual is None else self.torch.empty_like(x)
+        mean, rstd = self._stats(x, groups, kind, want_stats)
+        self._check(self.lib.goom_norm_before(self._ctx, C.byref(shape), px, _at(gate), _at(residual), _at(weight), _at(bias), _at(scale), None if h is x else h.data_ptr(),
+                                              y.data_ptr(), _at(mean), _at(rstd)))
+        return (y, h, mean, rstd) if want_stats else (y, h)
+
+    def _norm_grads(self, x, grads, mean, rstd, groups, kind, params, dtype, gate):
+        for t in grads:
+            if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
+                raise ValueError("gradients and h: of x's shape and type")
+        for t in (mean, rstd) if kind == "layer" else (rstd,):
+            if t is None or tuple(t.shape) != tuple(x.shape[:-1]) + (groups,) or t.dtype != self.torch.float32:
+                raise ValueError("mean (for layer), rstd: float32 [..., groups]")
+        new = [None if p is None else self.torch.empty(x.shape[-1], dtype=dtype, device=x.device) for p in params]
+        return self.torch.empty_like(x), None if gate is None else self.torch.empty_like(x), new
+
+    def norm_after_backward(self, x, grad_y, mean, rstd, groups: int = 1, weight=None, bias=None, scale=None, gate=None, kind: str = "rms", activation: str = "silu"):
+        """Gradients with respect to x, gate, weight, bias and scale (None for those that there are not); the residual's is grad_y."""
+        shape, dtype = self._block_norm(x, groups, weight, bias, scale, gate, None, kind, activation, 0.0)
+        gx, ggate, (gw, gb, gs) = self._norm_grads(x, (grad_y,), mean, rstd, groups, kind, (weight, bias, scale), dtype, gate)
+        ws, wsn = self.workspace(self.lib.goom_block_norm_backward_workspace_bytes(C.byref(shape)))
+        self._check(self.lib.goom_norm_after_backward(self._ctx, C.byref(shape), _at(x), _at(gate), _at(grad_y), _at(mean), _at(rstd), _at(weight), _at(bias), _at(scale),
+                                                      gx.data_ptr(), _at(ggate), _at(gw), _at(gb), _at(gs), _at(ws), wsn))
+        return gx, ggate, gw, gb, gs
+
+    def norm_before_backward(self, x, h, grad_y, mean, rstd, grad_h=None, groups: int = 1, weight=None, bias=None, scale=None, gate=None, kind: str = "rms",
+                             activation: str = "silu"):
+        """Gradients with respect to residual, x, gate, weight, bias and scale (None for those that there are not; without gate and scale residual's and
+        x's are one tensor), given those with respect to y and (None: none) to h."""
+        shape, dtype = self._block_norm(x, groups, weight, bias, scale, gate, None, kind, activation, 0.0)
+        gres, ggate, (gw, gb, gs) = self._norm_grads(x, (h, grad_y, grad_h), mean, rstd, groups, kind, (weight, bias, scale), dtype, gate)
+        gx = gres if gate is None and scale is None else self.torch.empty_like(x)
+        ws, wsn = self.workspace(self.lib.goom_block_norm_backward_workspace_bytes(C.byref(shape)))
+        self._check(self.lib.goom_norm_before_backward(self._ctx, C.byref(shape), _at(x), _at(gate), _at(h), _at(grad_y), _at(grad_h), _at(mean), _at(rstd), _at(weight), _at(scale),
+                                                       gres.data_ptr(), None if gx is gres else gx.data_ptr(), _at(ggate), _at(gw), _at(gb), _at(gs), _at(ws), wsn))
+        return gres, gx, ggate, gw, gb, gs
 
     # ---- token embeddings
     def embedding(self, table, tokens, scale: float = 1.0, out=None):
