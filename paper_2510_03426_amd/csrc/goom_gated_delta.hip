@@ -137,7 +137,7 @@ struct DeltaPlan {
     Pieces chunk, seg;
     bool maps;      // sequences are cut into segments
     int dk, cols, pitch, parts, map_parts, ch;
-    size_t frags, vecs, totals, map, state, rows, sum, bytes; // state, rows, sum: two each
+    size_t m, vecs, totals, map, state, rows, sum, bytes; // state, rows, sum: two each
 };
 
 static DeltaPlan plan_of(const goom_delta_shape &sh, bool packed, bool backward)
@@ -150,24 +150,25 @@ static DeltaPlan plan_of(const goom_delta_shape &sh, bool packed, bool backward)
     p.map_parts = (p.dk + p.cols - 1) / p.cols; // (zeros past dk)
     p.pitch = p.parts * p.cols;
     p.chunk = pieces_of(sh, packed, p.ch);
-    // Segments where the walks are fewer than the chip holds: as many as fill it.  A cut costs a walk without outputs over the columns of A and B.
+    // Segments where the walks are fewer than the chip has CUs: as many as make two a CU.  A cut costs a walk without outputs over the columns of A and B:
+    // with 256 walks of 64 chunks (8 x 4096 tokens, 16 heads of 128, bfloat16) both directions took 2120 us uncut, 2450 us in two segments each.
     const long long walks = sh.seqs * sh.heads * p.parts, mean = sh.seqs > 0 ? (sh.tokens + sh.seqs - 1) / sh.seqs : 0, least = 4 * p.ch;
-    long long want = walks > 0 ? 512 / walks : 1;
+    
+    long long want = walks > 0 && walks < 256 ? 512 / walks : 1;
     if (want > mean / least) want = mean / least;
     p.maps = want > 1;
     const long long len = p.maps ? ((mean + want - 1) / want + p.ch - 1) / p.ch * p.ch : (sh.tokens / p.ch + 1) * p.ch; // (no sequence is longer)
     p.seg = pieces_of(sh, packed, len);
     if (!p.maps) p.seg = {len, sh.seqs, 1};
     const size_t records = (size_t)p.chunk.slots * sh.heads, cuts = (size_t)p.seg.slots * sh.heads;
-    const int kinds = backward ? 3 : 2;
-    p.frags = goom::align_up(records * kinds * kind_frags(p.ch) * sizeof(Frag), 256);
+    p.m = goom::align_up(records * m_floats(p.ch) * sizeof(float), 256);
     p.vecs = goom::align_up(records * (p.ch == 64 ? sizeof(ChunkVec<64>) : sizeof(ChunkVec<32>)), 256);
     p.totals = p.maps ? goom::align_up(cuts * p.dk * p.pitch * 4, 256) : 0;
     p.map = p.maps ? goom::align_up(cuts * p.dk * p.dk * 4, 256) : 0;
     p.state = backward ? goom::align_up(records * p.dk * p.pitch * 4, 256) : 0;
     p.rows = backward ? goom::align_up(records * p.ch * p.pitch * 4, 256) : 0;
     p.sum = backward && sh.heads != sh.qk_heads ? goom::align_up((size_t)sh.tokens * sh.heads * sh.dk * 4, 256) : 0;
-    p.bytes = p.frags + p.vecs + p.totals + p.map + 2 * (p.state + p.rows + p.sum);
+    p.bytes = p.m + p.vecs + p.totals + p.map + 2 * (p.state + p.rows + p.sum);
     return p;
 }
 
@@ -193,7 +194,6 @@ static DeltaArgs delta_args(const goom_delta_shape &sh, const DeltaPlan &p, cons
     w.dk = sh.dk;
     w.dv = sh.dv;
     w.scale = (float)sh.scale;
-    w.m = w.p = w.mt = w.pt = -1;
     w.pitch = p.pitch;
     w.parts = p.parts;
     w.map_parts = p.map_parts;
@@ -202,12 +202,12 @@ static DeltaArgs delta_args(const goom_delta_shape &sh, const DeltaPlan &p, cons
 
 template <typename S> static int launch_carry(goom_ctx *ctx, const goom_delta_shape &sh, const DeltaArgs &w, bool back)
 {
-    return with_delta(sh.dk, sh.dv, [&](auto rows, auto cols, auto waves) {
-        constexpr int DK = decltype(rows)::value, DV = decltype(cols)::value, NW = decltype(waves)::value, NT = DV / 16 / NW;
-        const dim3 grid = grid_of(sh.seqs * sh.heads * w.parts, NW * 64);
+    return with_delta(sh.dk, sh.dv, [&](auto rows, auto cols) {
+        constexpr int DK = decltype(rows)::value, DV = decltype(cols)::value;
+        const dim3 grid = grid_of(sh.seqs * sh.heads * w.parts, DV * 4);
         goom::prof_begin(ctx, "gated delta rule: carries");
-        if (back) delta_carry_kernel<DK, DV, NW, NT, true><<<grid, NW * 64, 0, ctx->stream>>>(w);
-        else delta_carry_kernel<DK, DV, NW, NT, false><<<grid, NW * 64, 0, ctx->stream>>>(w);
+        if (back) delta_carry_kernel<DK, DV, true><<<grid, DV * 4, 0, ctx->stream>>>(w);
+        else delta_carry_kernel<DK, DV, false><<<grid, DV * 4, 0, ctx->stream>>>(w);
         goom::prof_end(ctx);
         return goom::check_hip(ctx, hipGetLastError(), "gated delta rule: carries");
     });
@@ -298,13 +298,10 @@ int goom_gated_delta(goom_ctx *ctx, const goom_delta_shape *shape, const void *q
     if (int s = enter(ctx)) return s;
     DeltaArgs w = delta_args(sh, p, offsets, q, k, v, log_decay, beta);
     unsigned char *ws = reinterpret_cast<unsigned char *>(workspace);
-    w.frags = reinterpret_cast<Frag *>(ws);
-    w.vecs = ws + p.frags;
-    w.totals = p.maps ? reinterpret_cast<float *>(ws + p.frags + p.vecs) : nullptr;
-    w.maps = reinterpret_cast<float *>(ws + p.frags + p.vecs + p.totals);
-    w.kinds = 2;
-    w.m = 0;
-    w.p = 1;
+    w.m = reinterpret_cast<float *>(ws);
+    w.vecs = ws + p.m;
+    w.totals = p.maps ? reinterpret_cast<float *>(ws + p.m + p.vecs) : nullptr;
+    w.maps = reinterpret_cast<float *>(ws + p.m + p.vecs + p.totals);
     w.init = state;
     w.fin = final_state;
     w.o = o;
@@ -368,16 +365,13 @@ int goom_gated_delta_backward(goom_ctx *ctx, const goom_delta_shape *shape, cons
         ws += bytes;
         return reinterpret_cast<float *>(at);
     };
-    w.frags = reinterpret_cast<Frag *>(take(p.frags));
+    w.m = take(p.m);
     w.vecs = take(p.vecs);
     w.totals = take(p.totals);
     w.maps = take(p.map);
     float *const kept_s = take(p.state), *const kept_d = take(p.state), *const rows_e = take(p.rows), *const rows_w = take(p.rows);
     float *const sum_q = take(p.sum), *const sum_k = take(p.sum);
-    w.kinds = 3;
-    w.m = 0;
-    w.mt = 1;
-    w.pt = 2;
+    w.back = 1;
     const BackPointers b = {grad_o, state, grad_final, grad_state, grad_q, grad_k, grad_v, grad_log_decay, grad_beta};
     if (int s = with_type(sh.type, [&](auto tag) { return run_backward<typename decltype(tag)::type>(ctx, sh, p, w, b, kept_s, kept_d, rows_e, rows_w, sum_q, sum_k); })) return s;
     if (p.sum && sh.tokens > 0)

@@ -27,7 +27,13 @@ struct Cut { const int64_t *offsets; long long tokens, seqs, seq_len, seg_len, s
 // tokens of a chunk
 template <typename S> constexpr int chunk_of() { return Parts<S>::IN > 1 ? 32 : 64; }
 constexpr int pair_blocks(int ch) { return ch == 64 ? 6 : 2; }
-constexpr int kind_frags(int ch) { return pair_blocks(ch) * COMPUTED * 64; }
+constexpr int pair_frags(int ch) { return pair_blocks(ch) * COMPUTED * 64; }
+// M of a chunk, floats in memory: rows of 32 entries, behind the first 32 rows of 64; eight of them a unit
+constexpr int m_floats(int ch) { return ch == 64 ? 32 * 32 + 32 * 64 : 32 * 32; }
+constexpr int m_units(int ch) { return m_floats(ch) / 8; }
+// in LDS in parts, planes of rows of pitches of their own
+constexpr int M_LOW = 32 + PITCH_PAD, M_HIGH = 64 + PITCH_PAD;
+constexpr int m_plane(int ch) { return 32 * M_LOW + (ch == 64 ? 32 * M_HIGH : 0); }
 
 // of a chunk and head: powers and betas, zeros past the end of the sequence
 template <int CH> struct ChunkVec {
@@ -41,26 +47,24 @@ struct DeltaArgs {
     const void *q, *k, *v, *go;
     long long q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok; // elements
     const float *log_decay, *beta;
-    int heads, share, dk, dv;
-    float scale;
-    Frag *frags;             // [chunk slots][heads][kinds][blocks][parts][64]
+    float *m;                // M, [chunk slots][heads][m_floats]
     void *vecs;              // ChunkVec [chunk slots][heads]
-    int kinds, m, mt, p, pt; // which kind of fragments is which; -1: none
     const float *init;       // NULL or [seqs][heads][dk][dv]: the state before the first token, or (backwards) its adjoint after the last
     float *fin;              // NULL or the same: the last state, or the first one's adjoint
     void *o;
     float *totals;           // NULL: one segment a sequence; [slots][heads][parts][state registers]: B, then the incoming states
     float *maps;             // A, [slots][heads][DK][DK]
     float *kept, *rows;      // KEEP: states before, BACK: adjoints after each chunk [chunk slots][heads][DK][pitch]; E or W [chunk slots][heads][CH][pitch]
-    int pitch;
     void *gv;
-    int parts, map_parts;    // workgroups' column parts of the state, and of A
-    unsigned slots;
     // gradients
     const float *kept_s, *kept_d, *rows_e, *rows_w;
     void *gq, *gk;           // [tokens][heads][dk], floats where heads share q and k
-    int grad_float;
     float *g_log_decay, *g_beta;
+    int heads, share, dk, dv, pitch;
+    int parts, map_parts;    // workgroups' column parts of the state, and of A
+    unsigned slots;
+    int back, grad_float;    // back: of a backward pass
+    float scale;
 };
 
 // log2 of a decay; below 2^-160, which is zero as a float whatever it is divided by, finite (a NaN stays one)
@@ -78,7 +82,9 @@ __device__ inline int turned_row(int t, int i) { return t / 2 * 32 + (i >> 2) * 
 
 template <typename S, int DK> struct WithinLds {
     static constexpr int CH = chunk_of<S>(), PK = DK + PITCH_PAD, TILE = CH * PK * Parts<S>::IN, PM = CH + 4;
-    static constexpr size_t bytes = 2 * TILE * sizeof(bf16) + 2 * CH * PM * sizeof(float) + CH * (sizeof(double) + sizeof(float));
+    static constexpr size_t tiles = TILE * sizeof(bf16), squares = 2 * CH * PM * sizeof(float); // first the rows, then their products
+    static constexpr size_t bytes = (tiles > squares ? tiles : squares) + CH * (sizeof(double) + sizeof(float));
+    static constexpr int fit = (int)((160 << 10) / bytes), resident = fit > 4 ? 4 : fit;
 };
 
 // M21 = (I - M22 beta2) G21 (I - beta1 M11) for the pairs of diagonal blocks of SIZE: every wave has tiles of 16 x 16
@@ -108,14 +114,14 @@ template <int SIZE, int CH> __device__ inline void join_blocks(float *m, const f
     }
 }
 
-template <typename S, int DK> __global__ __launch_bounds__(256) void within_kernel(DeltaArgs w)
+template <typename S, int DK> __global__ __launch_bounds__(256, (WithinLds<S, DK>::resident)) void within_kernel(DeltaArgs w)
 {
     typedef WithinLds<S, DK> Lds;
-    constexpr int CH = Lds::CH, PK = Lds::PK, PM = Lds::PM, IP = Parts<S>::IN, KP = CH * PK, BLOCKS = pair_blocks(CH);
+    constexpr int CH = Lds::CH, PK = Lds::PK, PM = Lds::PM, IP = Parts<S>::IN, KP = CH * PK;
     extern __shared__ __align__(16) unsigned char lds[];
-    bf16 *const k_lds = reinterpret_cast<bf16 *>(lds), *const q_lds = k_lds + Lds::TILE;
-    float *const kk = reinterpret_cast<float *>(q_lds + Lds::TILE), *const m = kk + CH * PM;
-    double *const b2 = reinterpret_cast<double *>(m + CH * PM);
+    bf16 *const k_lds = reinterpret_cast<bf16 *>(lds);
+    float *const kk = reinterpret_cast<float *>(lds), *const m = kk + CH * PM;
+    double *const b2 = reinterpret_cast<double *>(lds + (Lds::tiles > Lds::squares ? Lds::tiles : Lds::squares));
     float *const beta = reinterpret_cast<float *>(b2 + CH);
     const int qk_heads = w.heads / w.share;
     const long long block = block_of();
@@ -127,61 +133,44 @@ template <typename S, int DK> __global__ __launch_bounds__(256) void within_kern
     const long long t0 = at.seg * CH, tok = at.start + t0;
     const int n = at.len - t0 < CH ? (int)(at.len - t0) : CH;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-    const bool pairs = w.p >= 0 || w.pt >= 0;
 
-    TileRows<S, DK, 256, CH> kx, qx;
-    kx.fetch(reinterpret_cast<const S *>(w.k) + tok * w.k_tok + kh * w.k_head, w.k_tok, n, w.dk);
-    if (pairs) qx.fetch(reinterpret_cast<const S *>(w.q) + tok * w.q_tok + kh * w.q_head, w.q_tok, n, w.dk);
-    kx.template put<PK>(k_lds, n, w.dk);
-    if (pairs) qx.template put<PK>(q_lds, n, w.dk);
+    {
+        TileRows<S, DK, 256, CH> kx;
+        kx.fetch(reinterpret_cast<const S *>(w.k) + tok * w.k_tok + kh * w.k_head, w.k_tok, n, w.dk);
+        kx.template put_any<PK>(k_lds, n, w.dk);
+    }
     __syncthreads();
 
-    // k_i . k_j, by tiles on and below the diagonal; q_i . k_j by fragments, which their waves keep
-    constexpr int SIDE = CH / 16;
-    for (int tile = wave; tile < SIDE * (SIDE + 1) / 2; tile += 4) {
-        int r = 0, c = tile;
+    // k_i . k_j, by tiles on and below the diagonal
+    constexpr int SIDE = CH / 16, TILES = SIDE * (SIDE + 1) / 2, TURNS = (TILES + 3) / 4;
+    f32x4 square[TURNS];
+    auto tile_of = [&](int u, int &r, int &c) {
+        c = wave + u * 4;
+        r = 0;
         while (c > r) c -= ++r;
-        f32x4 acc = {0, 0, 0, 0};
+    };
+#pragma unroll
+    for (int u = 0; u < TURNS; u++) {
+        square[u] = f32x4{0, 0, 0, 0};
+        if (wave + u * 4 >= TILES) continue;
+        int r, c;
+        tile_of(u, r, c);
 #pragma unroll
         for (int x = 0; x < DK / 32; x++) {
             Frag a[IP], b[IP];
             row_frag(a, k_lds + (r * 16 + i) * PK + x * 32 + g * 8, KP);
             row_frag(b, k_lds + (c * 16 + i) * PK + x * 32 + g * 8, KP);
-            acc = product(a, b, acc);
+            square[u] = product(a, b, square[u]);
         }
-#pragma unroll
-        for (int e = 0; e < 4; e++) kk[(r * 16 + g * 4 + e) * PM + c * 16 + i] = acc[e];
     }
-    constexpr int MINE = (BLOCKS + 3) / 4;
-    f32x8 dots[MINE], dots_t[MINE];
-    auto rows_dot = [&](const bf16 *lane_row, const bf16 *turned, int ks) { // the lane's row against eight consecutive ones from ks 32 + g 8 on
-        f32x4 p0 = {0, 0, 0, 0}, p1 = {0, 0, 0, 0};
-        const bf16 *const other = turned + turned_row(2 * ks, i) * PK + g * 8;
+    __syncthreads();
 #pragma unroll
-        for (int x = 0; x < DK / 32; x++) {
-            Frag a[IP], b0[IP], b1[IP];
-            row_frag(a, lane_row + g * 8 + x * 32, KP);
-            row_frag(b0, other + x * 32, KP);
-            row_frag(b1, other + 4 * PK + x * 32, KP);
-            p0 = product(b0, a, p0);
-            p1 = product(b1, a, p1);
-        }
-        return f32x8(__builtin_shufflevector(p0, p1, 0, 1, 2, 3, 4, 5, 6, 7));
-    };
+    for (int u = 0; u < TURNS; u++) {
+        if (wave + u * 4 >= TILES) continue;
+        int r, c;
+        tile_of(u, r, c);
 #pragma unroll
-    for (int u = 0; u < MINE; u++) {
-        const int block = wave + u * 4;
-        int t, ks;
-        if (block < BLOCKS) {
-            if (w.p >= 0) {
-                p_place<false>(block, CH, t, ks);
-                dots[u] = rows_dot(q_lds + (t * 16 + i) * PK, k_lds, ks);
-            }
-            if (w.pt >= 0) {
-                p_place<true>(block, CH, t, ks);
-                dots_t[u] = rows_dot(k_lds + turned_row(t, i) * PK, q_lds, ks);
-            }
-        }
+        for (int e = 0; e < 4; e++) kk[(r * 16 + g * 4 + e) * PM + c * 16 + i] = square[u][e];
     }
 
     for (int s = 0; s < w.share; s++) {
@@ -234,45 +223,12 @@ template <typename S, int DK> __global__ __launch_bounds__(256) void within_kern
         join_blocks<16, CH>(m, beta);
         if constexpr (CH == 64) join_blocks<32, CH>(m, beta);
 
-        auto put = [&](int kind, int block, const f32x8 &x) {
-            Frag parts[COMPUTED];
-            split(x, parts);
-            Frag *const to = w.frags + ((record * w.kinds + kind) * BLOCKS + block) * (COMPUTED * 64) + lane;
-#pragma unroll
-            for (int q = 0; q < COMPUTED; q++) to[q * 64] = parts[q];
-        };
-#pragma unroll
-        for (int u = 0; u < MINE; u++) {
-            const int block = wave + u * 4;
-            if (block >= BLOCKS) continue;
-            int t, ks;
-            f32x8 x;
-            p_place<false>(block, CH, t, ks);
-            if (w.m >= 0) {
-                const int row = turned_row(t, i), col = ks * 32 + g * 8;
-                const f32x4 *const from = reinterpret_cast<const f32x4 *>(m + row * PM + col);
-                x = __builtin_shufflevector(from[0], from[1], 0, 1, 2, 3, 4, 5, 6, 7);
-                put(w.m, block, x);
-            }
-            if (w.p >= 0) {
-                const int row = t * 16 + i, col = ks * 32 + g * 8;
-#pragma unroll
-                for (int e = 0; e < 8; e++) x[e] = col + e <= row ? w.scale * dots[u][e] * power2(b2[row] - b2[col + e]) : 0.0f;
-                put(w.p, block, x);
-            }
-            p_place<true>(block, CH, t, ks);
-            if (w.mt >= 0) {
-                const int row = turned_row(t, i), col = ks * 32 + g * 8;
-#pragma unroll
-                for (int e = 0; e < 8; e++) x[e] = m[(col + e) * PM + row];
-                put(w.mt, block, x);
-            }
-            if (w.pt >= 0) {
-                const int row = turned_row(t, i), col = ks * 32 + g * 8;
-#pragma unroll
-                for (int e = 0; e < 8; e++) x[e] = row <= col + e ? w.scale * dots_t[u][e] * power2(b2[col + e] - b2[row]) : 0.0f;
-                put(w.pt, block, x);
-            }
+        float *const to = w.m + record * m_floats(CH);
+        for (int u = threadIdx.x; u < m_units(CH); u += 256) {
+            const int row = u < 128 ? u / 4 : 32 + (u - 128) / 8, col = (u < 128 ? u % 4 : u % 8) * 8;
+            const f32x4 *const from = reinterpret_cast<const f32x4 *>(m + row * PM + col);
+            reinterpret_cast<f32x4 *>(to + u * 8)[0] = from[0];
+            reinterpret_cast<f32x4 *>(to + u * 8)[1] = from[1];
         }
     }
 }
@@ -287,373 +243,407 @@ enum DeltaMode {
     BACK          // adjoints after the chunks, W, the gradient of v
 };
 
-template <typename S, int DK, int DV, int NW, int MODE> struct DeltaLds {
-    static constexpr int CH = chunk_of<S>(), PK = DK + PITCH_PAD, PV = DV + PITCH_PAD;
-    static constexpr bool REV = MODE == BACK_MAPS || MODE == BACK, OUT = MODE == FORWARD, Q = OUT || REV, P = OUT || REV;
-    static constexpr int K_TILE = CH * PK * Parts<S>::IN, V_TILE = CH * PV * Parts<S>::IN; // elements
-    static constexpr int FRAGS = kind_frags(CH) * (P ? 2 : 1);
-    static constexpr size_t bytes = FRAGS * sizeof(Frag) + (K_TILE * (Q ? 2 : 1) + V_TILE) * sizeof(bf16) + 4 * CH * sizeof(float);
-    static constexpr int fit = (int)((160 << 10) / bytes), most = 8 / NW;
-    static constexpr int resident = fit < 1 ? 1 : fit > most ? most : fit;
-    static constexpr int per_simd = (resident * NW + 3) / 4;
+// Waves that load for the others: they fetch the next chunk's rows and M, form P of this chunk, and put what was fetched into LDS, while
+// the walking waves do nothing but multiply.  (With every wave at both, one chunk after another, a chunk of 64 tokens and heads of 128 took
+// 17,500 cycles, half of them waits.)
+constexpr int LOADERS = 4;
+
+template <typename S, int DK, int DV, int MODE> struct DeltaLds {
+    static constexpr int CH = chunk_of<S>(), PK = DK + PITCH_PAD, PV = DV + PITCH_PAD, NW = DV / 16, WAVES = NW + LOADERS;
+    static constexpr bool REV = MODE == BACK_MAPS || MODE == BACK, OUT = MODE == FORWARD, P = OUT || REV;
+    static constexpr int K_TILE = CH * PK * Parts<S>::IN, V_TILE = CH * PV * Parts<S>::IN, M_TILE = m_plane(CH) * COMPUTED; // elements
+    // Two buffers in turn for what is read until a chunk's end; one for what is read before the barrier in the middle of it, behind which the
+    // next chunk's comes (forwards Q, V and M)
+    static constexpr int Q_BUFFERS = OUT ? 1 : REV ? 2 : 0, OTHERS = OUT ? 1 : 2;
+    static constexpr int FRAGS = P ? pair_frags(CH) : 0, VEC = 3 * CH + 4; // up, down, beta, whole
+    static constexpr size_t bytes = FRAGS * sizeof(Frag) + (K_TILE * (2 + Q_BUFFERS) + (V_TILE + M_TILE) * OTHERS) * sizeof(bf16) + CH * sizeof(double) + 2 * VEC * sizeof(float);
+    static constexpr int fit = (int)((160 << 10) / bytes), resident = fit > 2 ? 2 : fit;
+    static constexpr int per_simd = (resident * WAVES + 3) / 4;
 };
 
-// DK: dk, padded; NW waves of one or two tiles of 16 of the DV columns
-template <typename S, int DK, int DV, int NW, int MODE>
-__device__ inline void delta_walk(const DeltaArgs &w, const Place &at, long long slot, int h, int part, unsigned char *lds)
+struct WalkPlace { long long start, len, seg0, seg1, chunk0; int h, kh, col_part, nc, nchunks; bool map, last; long long state0; };
+
+// the loading waves
+template <typename S, int DK, int DV, int MODE> __device__ inline void delta_load(const DeltaArgs &w, const WalkPlace at, unsigned char *lds)
 {
-    typedef DeltaLds<S, DK, DV, NW, MODE> Lds;
-    constexpr int THREADS = NW * 64, NT = DV / 16 / NW, KS = DK / 32, CS = NT == 2 ? 8 : 4, TT = Lds::CH / 16;
-    constexpr int IP = Parts<S>::IN, CH = Lds::CH, KP = CH * Lds::PK, VP = CH * Lds::PV, HALVES = CH / 32;
-    constexpr bool REV = Lds::REV, OUT = Lds::OUT, TOTAL = MODE == MAPS || MODE == BACK_MAPS;
-    static_assert(NT == 1 || NT == 2, "a wave has one or two column tiles");
-    Frag *const m_lds = reinterpret_cast<Frag *>(lds), *const p_lds = m_lds + kind_frags(CH);
-    bf16 *const k_lds = reinterpret_cast<bf16 *>(m_lds + Lds::FRAGS), *const v_lds = k_lds + Lds::K_TILE, *const q_lds = v_lds + Lds::V_TILE;
-    float *const vec_lds = reinterpret_cast<float *>(q_lds + (Lds::Q ? Lds::K_TILE : 0)); // up, down, beta
-
-    const bool last = REV ? at.seg == 0 : at.seg == at.nseg - 1; // in walking order
-    const bool map = MODE == MAPS && part >= w.parts; // columns of A
-    if (TOTAL && last && !(map && w.mt >= 0)) return; // (the way back goes through the last segment's A as well)
+    typedef DeltaLds<S, DK, DV, MODE> Lds;
+    constexpr int THREADS = LOADERS * 64, KS = DK / 32, IP = Parts<S>::IN, CH = Lds::CH, KP = CH * Lds::PK;
+    constexpr bool REV = Lds::REV;
+    Frag *const p_lds = reinterpret_cast<Frag *>(lds);
+    bf16 *const k_lds = reinterpret_cast<bf16 *>(p_lds + Lds::FRAGS), *const q_lds = k_lds + 2 * Lds::K_TILE, *const v_lds = q_lds + Lds::Q_BUFFERS * Lds::K_TILE,
+               *const m_lds = v_lds + Lds::OTHERS * Lds::V_TILE;
+    double *const b2_lds = reinterpret_cast<double *>(m_lds + Lds::OTHERS * Lds::M_TILE);
+    float *const vec_lds = reinterpret_cast<float *>(b2_lds + CH);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-    const int col0 = wave * NT * 16; // the wave's columns: col0 + (i / 4) CS + 4 nt + i % 4
-    const int col_part = (map ? part - w.parts : part) * DV, nc_all = map ? w.dk : w.dv, nc = nc_all - col_part < DV ? nc_all - col_part : DV;
-    const int kh = h / w.share;
-    const bool empty = at.len == 0;
-    auto row_of = [&](int t, int e) { return t / 2 * 32 + g * 8 + t % 2 * 4 + e; };
-    auto col_of = [&](int nt) { return col0 + (i >> 2) * CS + 4 * nt + (i & 3); };
 
-    // ---- the incoming state
-    f32x4 R[DK / 16][NT];
-    float *const total = w.totals && !map ? w.totals + ((slot * w.heads + h) * w.parts + part) * (long long)(DK * DV) + (long long)wave * NT * (DK / 16) * 256 + lane * 4 : nullptr;
-    const long long state0 = (at.seq * w.heads + h) * (long long)w.dk * w.dv + col_part;
-#pragma unroll
-    for (int t = 0; t < DK / 16; t++)
-#pragma unroll
-        for (int nt = 0; nt < NT; nt++) {
-            f32x4 x = {0, 0, 0, 0};
-            const int col = col_of(nt);
-            if (TOTAL) {
-                if (map)
-#pragma unroll
-                    for (int e = 0; e < 4; e++) x[e] = row_of(t, e) == col_part + col && col < nc ? 1.0f : 0.0f;
-            } else if (total && !empty) {
-                x = *reinterpret_cast<const f32x4 *>(total + (nt * (DK / 16) + t) * 256);
-            } else if (w.init) {
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const int row = row_of(t, e);
-                    if (row < w.dk && col < nc) x[e] = w.init[state0 + (long long)row * w.dv + col];
-                }
-            }
-            R[t][nt] = x;
-        }
-
-    const S *const k = reinterpret_cast<const S *>(w.k) + at.start * w.k_tok + kh * w.k_head;
-    const S *const q = reinterpret_cast<const S *>(w.q) + at.start * w.q_tok + kh * w.q_head;
-    const S *const v = REV ? reinterpret_cast<const S *>(w.go) + at.start * w.o_tok + h * (long long)w.dv + col_part
-                           : reinterpret_cast<const S *>(w.v) + at.start * w.v_tok + h * w.v_head + col_part;
+    const S *const k = reinterpret_cast<const S *>(w.k) + at.start * w.k_tok + at.kh * w.k_head;
+    const S *const q = reinterpret_cast<const S *>(w.q) + at.start * w.q_tok + at.kh * w.q_head;
+    const S *const v = REV ? reinterpret_cast<const S *>(w.go) + at.start * w.o_tok + at.h * (long long)w.dv + at.col_part
+                           : reinterpret_cast<const S *>(w.v) + at.start * w.v_tok + at.h * w.v_head + at.col_part;
     const long long v_tok = REV ? w.o_tok : w.v_tok;
-    const long long seg0 = at.seg * w.seg.seg_len, seg1 = seg0 + w.seg.seg_len < at.len ? seg0 + w.seg.seg_len : at.len;
-    const int nchunks = (int)((seg1 - seg0 + CH - 1) / CH);
-    const long long chunk0 = empty ? 0 : (first_slot(w.chunk, at.seq) + seg0 / CH);
     TileRows<S, DK, THREADS, CH> kx, qx;
     TileRows<S, DV, THREADS, CH> vx;
-    constexpr int KIND = kind_frags(CH), MF = (KIND + THREADS - 1) / THREADS;
-    Frag mx[MF], px[MF];
-    float vec[3];
-    float whole = 0;
-    auto chunk_at = [&](int step) { return REV ? nchunks - 1 - step : step; };
+    constexpr int UNITS = m_units(CH), MU = (UNITS + THREADS - 1) / THREADS;
+    f32x8 mx[MU];
+    double b2 = 0;
+    float vec[3], whole = 0;
+    auto chunk_at = [&](int step) { return REV ? at.nchunks - 1 - step : step; };
+    auto rows_at = [&](int c) {
+        const long long t0 = at.seg0 + (long long)c * CH;
+        return at.seg1 - t0 < CH ? (int)(at.seg1 - t0) : CH;
+    };
     auto fetch = [&](int step) {
-        const int c = chunk_at(step);
-        const long long t0 = seg0 + (long long)c * CH, record = (chunk0 + c) * w.heads + h;
-        const int n = seg1 - t0 < CH ? (int)(seg1 - t0) : CH;
+        const int c = chunk_at(step), n = rows_at(c);
+        const long long t0 = at.seg0 + (long long)c * CH, record = (at.chunk0 + c) * w.heads + at.h;
         kx.fetch(k + t0 * w.k_tok, w.k_tok, n, w.dk);
-        if (Lds::Q) qx.fetch(q + t0 * w.q_tok, w.q_tok, n, w.dk);
-        if (!map) vx.fetch(v + t0 * v_tok, v_tok, n, nc);
-        const Frag *const frags = w.frags + record * w.kinds * KIND;
+        if (!at.map) vx.fetch(v + t0 * v_tok, v_tok, n, at.nc);
+        const float *const from = w.m + record * m_floats(CH);
 #pragma unroll
-        for (int u = 0; u < MF; u++) {
-            const int at = u * THREADS + threadIdx.x < KIND ? u * THREADS + threadIdx.x : KIND - 1;
-            mx[u] = frags[(REV ? w.mt : w.m) * KIND + at];
-            if (Lds::P) px[u] = frags[(REV ? w.pt : w.p) * KIND + at];
+        for (int u = 0; u < MU; u++) {
+            const int x = u * THREADS + threadIdx.x < UNITS ? u * THREADS + threadIdx.x : UNITS - 1;
+            mx[u] = *reinterpret_cast<const f32x8 *>(from + x * 8);
         }
         const ChunkVec<CH> &cv = reinterpret_cast<const ChunkVec<CH> *>(w.vecs)[record];
-        if (threadIdx.x < CH) {
-            vec[0] = cv.up[threadIdx.x];
-            vec[1] = cv.down[threadIdx.x];
-            vec[2] = cv.beta[threadIdx.x];
-        }
+        const int x = threadIdx.x & (CH - 1);
+        b2 = cv.b2[x];
+        vec[0] = cv.up[x];
+        vec[1] = cv.down[x];
+        vec[2] = cv.beta[x];
         whole = cv.whole;
+        if (Lds::Q_BUFFERS) qx.fetch(q + t0 * w.q_tok, w.q_tok, n, w.dk);
     };
-    if (nchunks > 0) fetch(0);
-    for (int step = 0; step < nchunks; step++) {
-        const int c = chunk_at(step);
-        const long long t0 = seg0 + (long long)c * CH, record = (chunk0 + c) * w.heads + h;
-        const int n = seg1 - t0 < CH ? (int)(seg1 - t0) : CH;
-        const float decay = whole;
-        __syncthreads();
-        kx.template put<Lds::PK>(k_lds, n, w.dk);
-        if (Lds::Q) qx.template put<Lds::PK>(q_lds, n, w.dk);
-        if (!map) vx.template put<Lds::PV>(v_lds, n, nc);
+    auto put = [&](int step) {
+        const int n = rows_at(chunk_at(step)), two = step & 1, other = Lds::OTHERS == 2 ? two : 0;
+        kx.template put_any<Lds::PK>(k_lds + two * Lds::K_TILE, n, w.dk);
+        if (!at.map) vx.template put_any<Lds::PV>(v_lds + other * Lds::V_TILE, n, at.nc);
 #pragma unroll
-        for (int u = 0; u < MF; u++)
-            if (u * THREADS + threadIdx.x < KIND) {
-                m_lds[u * THREADS + threadIdx.x] = mx[u];
-                if (Lds::P) p_lds[u * THREADS + threadIdx.x] = px[u];
+        for (int u = 0; u < MU; u++) {
+            const int x = u * THREADS + threadIdx.x;
+            if (UNITS % THREADS && x >= UNITS) continue;
+            Frag parts[COMPUTED];
+            split(mx[u], parts);
+            bf16 *const to = m_lds + other * Lds::M_TILE + (x < 128 ? x / 4 * M_LOW + x % 4 * 8 : 32 * M_LOW + (x - 128) / 8 * M_HIGH + x % 8 * 8);
+#pragma unroll
+            for (int p = 0; p < COMPUTED; p++) *reinterpret_cast<Frag *>(to + p * m_plane(CH)) = parts[p];
+        }
+        if (threadIdx.x < CH) {
+            float *const to = vec_lds + two * Lds::VEC;
+#pragma unroll
+            for (int x = 0; x < 3; x++) to[x * CH + threadIdx.x] = vec[x];
+            if (threadIdx.x == 0) to[3 * CH] = whole;
+            b2_lds[threadIdx.x] = b2;
+        }
+        if (Lds::Q_BUFFERS) qx.template put_any<Lds::PK>(q_lds + (Lds::Q_BUFFERS == 2 ? two : 0) * Lds::K_TILE, n, w.dk);
+    };
+    fetch(0);
+    put(0);
+    if (at.nchunks > 1) fetch(1);
+    __syncthreads();
+    for (int step = 0; step < at.nchunks; step++) {
+        if (Lds::P) {
+            // P: a lane has eight consecutive j of row i, or (backwards) eight consecutive i of row j
+            const bf16 *const kt = k_lds + (step & 1) * Lds::K_TILE, *const qt = q_lds + (Lds::Q_BUFFERS == 2 ? step & 1 : 0) * Lds::K_TILE;
+            for (int block = wave; block < pair_blocks(CH); block += LOADERS) {
+                int t, ks;
+                p_place<REV>(block, CH, t, ks);
+                const int row = REV ? turned_row(t, i) : t * 16 + i, col = ks * 32 + g * 8;
+                const bf16 *const one = (REV ? kt : qt) + row * Lds::PK + g * 8, *const other = (REV ? qt : kt) + turned_row(2 * ks, i) * Lds::PK + g * 8;
+                f32x4 p0 = {0, 0, 0, 0}, p1 = {0, 0, 0, 0};
+#pragma unroll
+                for (int kk = 0; kk < KS; kk++) {
+                    Frag a[IP], b0[IP], b1[IP];
+                    row_frag(a, one + kk * 32, KP);
+                    row_frag(b0, other + kk * 32, KP);
+                    row_frag(b1, other + 4 * Lds::PK + kk * 32, KP);
+                    p0 = product(b0, a, p0);
+                    p1 = product(b1, a, p1);
+                }
+                f32x8 p8 = __builtin_shufflevector(p0, p1, 0, 1, 2, 3, 4, 5, 6, 7);
+                const double mine = b2_lds[row];
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    const double age = REV ? b2_lds[col + e] - mine : mine - b2_lds[col + e];
+                    p8[e] = (REV ? row <= col + e : col + e <= row) ? w.scale * p8[e] * power2(age) : 0.0f;
+                }
+                Frag parts[COMPUTED];
+                split(p8, parts);
+#pragma unroll
+                for (int p = 0; p < COMPUTED; p++) p_lds[(block * COMPUTED + p) * 64 + lane] = parts[p];
             }
-        if (threadIdx.x < CH)
-#pragma unroll
-            for (int x = 0; x < 3; x++) vec_lds[x * CH + threadIdx.x] = vec[x];
+            __syncthreads();
+        }
+        if (step + 1 < at.nchunks) put(step + 1); // on its way since the last chunk
+        if (step + 2 < at.nchunks) fetch(step + 2);
         __syncthreads();
-        if (step + 1 < nchunks) fetch(step + 1); // while this chunk is worked on
+    }
+}
+
+// the walking waves: each has 16 of the DV columns of the state
+template <typename S, int DK, int DV, int MODE> __device__ inline void delta_walk(const DeltaArgs &w, const WalkPlace at, float *total, unsigned char *lds)
+{
+    typedef DeltaLds<S, DK, DV, MODE> Lds;
+    constexpr int KS = DK / 32, TT = Lds::CH / 16, IP = Parts<S>::IN, CH = Lds::CH, KP = CH * Lds::PK, VP = CH * Lds::PV, HALVES = CH / 32;
+    constexpr bool REV = Lds::REV, OUT = Lds::OUT, TOTAL = MODE == MAPS || MODE == BACK_MAPS;
+    const Frag *const p_lds = reinterpret_cast<const Frag *>(lds);
+    const bf16 *const k_lds = reinterpret_cast<const bf16 *>(p_lds + Lds::FRAGS), *const q_lds = k_lds + 2 * Lds::K_TILE, *const v_lds = q_lds + Lds::Q_BUFFERS * Lds::K_TILE,
+                     *const m_lds = v_lds + Lds::OTHERS * Lds::V_TILE;
+    const float *const vec_lds = reinterpret_cast<const float *>(reinterpret_cast<const double *>(m_lds + Lds::OTHERS * Lds::M_TILE) + CH);
+    const int lane = threadIdx.x & 63, wave = (threadIdx.x >> 6) - LOADERS, i = lane & 15, g = lane >> 4, col0 = wave * 16, col = col0 + i;
+    auto row_of = [&](int t, int e) { return t / 2 * 32 + g * 8 + t % 2 * 4 + e; };
+    const bool here = col < at.nc;
+
+    // ---- the incoming state
+    f32x4 R[DK / 16];
+    if (total) total += (long long)wave * (DK / 16) * 256 + lane * 4;
+#pragma unroll
+    for (int t = 0; t < DK / 16; t++) {
+        f32x4 x = {0, 0, 0, 0};
+        if (TOTAL) {
+            if (at.map)
+#pragma unroll
+                for (int e = 0; e < 4; e++) x[e] = row_of(t, e) == at.col_part + col && here ? 1.0f : 0.0f;
+        } else if (total && at.len) {
+            x = *reinterpret_cast<const f32x4 *>(total + t * 256);
+        } else if (w.init) {
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (row_of(t, e) < w.dk && here) x[e] = w.init[at.state0 + (long long)row_of(t, e) * w.dv + col];
+        }
+        R[t] = x;
+    }
+    if (at.nchunks > 0) __syncthreads();
+    for (int step = 0; step < at.nchunks; step++) {
+        const int c = REV ? at.nchunks - 1 - step : step, two = step & 1, other = Lds::OTHERS == 2 ? two : 0;
+        const long long t0 = at.seg0 + (long long)c * CH, record = (at.chunk0 + c) * w.heads + at.h;
+        const int n = at.seg1 - t0 < CH ? (int)(at.seg1 - t0) : CH;
+        const bf16 *const kt = k_lds + two * Lds::K_TILE, *const qt = q_lds + (Lds::Q_BUFFERS == 2 ? two : 0) * Lds::K_TILE, *const vt = v_lds + other * Lds::V_TILE,
+                         *const mt = m_lds + other * Lds::M_TILE;
+        const float *const vec = vec_lds + two * Lds::VEC;
+        auto eight = [&](int which, int half) { return *reinterpret_cast<const f32x8 *>(vec + which * CH + half * 32 + g * 8); };
 
         if (MODE == KEEP || MODE == BACK) {
-            float *const to = w.kept + record * (DK * (long long)w.pitch) + col_part;
+            float *const to = w.kept + record * (DK * (long long)w.pitch) + at.col_part + col;
 #pragma unroll
             for (int t = 0; t < DK / 16; t++)
 #pragma unroll
-                for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                    for (int e = 0; e < 4; e++) to[row_of(t, e) * w.pitch + col_of(nt)] = R[t][nt][e];
+                for (int e = 0; e < 4; e++) to[row_of(t, e) * w.pitch] = R[t][e];
         }
 
         // ---- K against the state, a lane with eight consecutive tokens of a column; Q with consecutive columns of a token
-        f32x4 x[TT][NT], y[OUT ? TT : 1][NT];
+        f32x4 x[TT], y[OUT ? TT : 1];
 #pragma unroll
-        for (int t = 0; t < TT; t++)
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++) {
-                x[t][nt] = f32x4{0, 0, 0, 0};
-                if (OUT) y[t][nt] = f32x4{0, 0, 0, 0};
-            }
+        for (int t = 0; t < TT; t++) {
+            x[t] = f32x4{0, 0, 0, 0};
+            if (OUT) y[t] = f32x4{0, 0, 0, 0};
+        }
 #pragma unroll
         for (int kk = 0; kk < KS; kk++) {
-            Frag rf[NT][COMPUTED];
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++) split(__builtin_shufflevector(R[2 * kk][nt], R[2 * kk + 1][nt], 0, 1, 2, 3, 4, 5, 6, 7), rf[nt]);
+            Frag rf[COMPUTED];
+            split(__builtin_shufflevector(R[2 * kk], R[2 * kk + 1], 0, 1, 2, 3, 4, 5, 6, 7), rf);
 #pragma unroll
             for (int t = 0; t < TT; t++) {
                 Frag kf[IP];
-                row_frag(kf, k_lds + turned_row(t, i) * Lds::PK + kk * 32 + g * 8, KP);
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++) x[t][nt] = product(kf, rf[nt], x[t][nt]);
+                row_frag(kf, kt + turned_row(t, i) * Lds::PK + kk * 32 + g * 8, KP);
+                x[t] = product(kf, rf, x[t]);
                 if (OUT) {
                     Frag qf[IP];
-                    row_frag(qf, q_lds + (t * 16 + i) * Lds::PK + kk * 32 + g * 8, KP);
-#pragma unroll
-                    for (int nt = 0; nt < NT; nt++) y[t][nt] = product(rf[nt], qf, y[t][nt]);
+                    row_frag(qf, qt + (t * 16 + i) * Lds::PK + kk * 32 + g * 8, KP);
+                    y[t] = product(rf, qf, y[t]);
                 }
             }
         }
-        auto eight = [&](int which, int half) { return *reinterpret_cast<const f32x8 *>(vec_lds + which * CH + half * 32 + g * 8); };
-        auto pair = [&](const f32x4 &a, const f32x4 &b) { return f32x8(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)); };
+        auto get = [&](int half) { return f32x8(__builtin_shufflevector(x[2 * half], x[2 * half + 1], 0, 1, 2, 3, 4, 5, 6, 7)); };
+        auto set = [&](int half, const f32x8 &y8) {
+            x[2 * half] = __builtin_shufflevector(y8, y8, 0, 1, 2, 3);
+            x[2 * half + 1] = __builtin_shufflevector(y8, y8, 4, 5, 6, 7);
+        };
+        if (REV) __syncthreads(); // P is there
         // ---- Y (or dU), and with M the rows E (or W)
-        f32x8 r8[HALVES][NT], go8[REV ? HALVES : 1][NT];
-        if (REV) {
-            f32x4 local[TT][NT];
+        f32x8 go8[REV ? HALVES : 1];
 #pragma unroll
-            for (int t = 0; t < TT; t++)
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++) local[t][nt] = f32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int half = 0; half < HALVES; half++)
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++) {
-                    Frag gf[IP];
-                    col_frag<Lds::PV>(gf, v_lds, VP, half * 32, col0 + 4 * nt, CS, lane);
-                    go8[half][nt] = widen(gf);
-#pragma unroll
-                    for (int t = 0; t < TT; t++) {
-                        if (!p_has<true>(t, half)) continue;
-                        Frag pf[COMPUTED];
-#pragma unroll
-                        for (int u = 0; u < COMPUTED; u++) pf[u] = p_lds[(p_block<true>(t, half, CH) * COMPUTED + u) * 64 + lane];
-                        local[t][nt] = product(pf, gf, local[t][nt]);
-                    }
+        for (int half = 0; half < HALVES; half++) {
+            if (REV) {
+                set(half, eight(1, half) * get(half));
+            } else {
+                f32x8 in = {0, 0, 0, 0, 0, 0, 0, 0};
+                if (!at.map) {
+                    Frag vf[IP];
+                    col_frag<Lds::PV>(vf, vt, VP, half * 32, col0, 4, lane);
+                    in = widen(vf);
                 }
-#pragma unroll
-            for (int half = 0; half < HALVES; half++)
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++)
-                    r8[half][nt] = pair(local[2 * half][nt], local[2 * half + 1][nt]) + eight(1, half) * pair(x[2 * half][nt], x[2 * half + 1][nt]);
-        } else {
-#pragma unroll
-            for (int half = 0; half < HALVES; half++)
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++) {
-                    f32x8 in = {0, 0, 0, 0, 0, 0, 0, 0};
-                    if (!map) {
-                        Frag vf[IP];
-                        col_frag<Lds::PV>(vf, v_lds, VP, half * 32, col0 + 4 * nt, CS, lane);
-                        in = widen(vf);
-                    }
-                    r8[half][nt] = in - eight(0, half) * pair(x[2 * half][nt], x[2 * half + 1][nt]);
-                }
+                set(half, in - eight(0, half) * get(half));
+            }
         }
-        {
-            f32x4 acc[TT][NT];
-#pragma unroll
-            for (int t = 0; t < TT; t++)
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++) acc[t][nt] = f32x4{0, 0, 0, 0};
+        if (REV) {
 #pragma unroll
             for (int half = 0; half < HALVES; half++) {
-                Frag bf[NT][COMPUTED];
+                Frag gf[IP];
+                col_frag<Lds::PV>(gf, vt, VP, half * 32, col0, 4, lane);
+                go8[half] = widen(gf);
 #pragma unroll
-                for (int nt = 0; nt < NT; nt++) split(eight(2, half) * r8[half][nt], bf[nt]);
+                for (int t = 0; t < TT; t++) {
+                    if (!p_has<true>(t, half)) continue;
+                    Frag pf[COMPUTED];
+#pragma unroll
+                    for (int u = 0; u < COMPUTED; u++) pf[u] = p_lds[(p_block<true>(t, half, CH) * COMPUTED + u) * 64 + lane];
+                    x[t] = product(pf, gf, x[t]);
+                }
+            }
+        }
+        {
+            Frag bf[HALVES][COMPUTED];
+#pragma unroll
+            for (int half = 0; half < HALVES; half++) split(-(eight(2, half) * get(half)), bf[half]);
+#pragma unroll
+            for (int half = 0; half < HALVES; half++)
 #pragma unroll
                 for (int t = 0; t < TT; t++) {
                     if (!p_has<REV>(t, half)) continue;
                     Frag mf[COMPUTED];
-#pragma unroll
-                    for (int u = 0; u < COMPUTED; u++) mf[u] = m_lds[(p_block<REV>(t, half, CH) * COMPUTED + u) * 64 + lane];
-#pragma unroll
-                    for (int nt = 0; nt < NT; nt++) acc[t][nt] = product(mf, bf[nt], acc[t][nt]);
+                    if (REV && half == 0) col_frag<M_LOW>(mf, mt, m_plane(CH), 0, t % 2 * 4, 8, lane);
+                    else if (REV) col_frag<M_HIGH>(mf, mt + 32 * M_LOW, m_plane(CH), 0, t / 2 * 32 + t % 2 * 4, 8, lane);
+                    else if (t < 2) row_frag(mf, mt + turned_row(t, i) * M_LOW + g * 8, m_plane(CH));
+                    else row_frag(mf, mt + 32 * M_LOW + (turned_row(t, i) - 32) * M_HIGH + half * 32 + g * 8, m_plane(CH));
+                    x[t] = product(mf, bf[half], x[t]);
                 }
-            }
-#pragma unroll
-            for (int half = 0; half < HALVES; half++)
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++) r8[half][nt] -= pair(acc[2 * half][nt], acc[2 * half + 1][nt]);
         }
+        if (OUT) __syncthreads(); // P is there, and Q, V and M are read
         if (MODE == KEEP || MODE == BACK) {
-            float *const to = w.rows + record * (CH * (long long)w.pitch) + col_part;
+            float *const to = w.rows + record * (CH * (long long)w.pitch) + at.col_part + col;
 #pragma unroll
             for (int half = 0; half < HALVES; half++)
 #pragma unroll
-                for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                    for (int e = 0; e < 8; e++) to[(half * 32 + g * 8 + e) * w.pitch + col_of(nt)] = r8[half][nt][e];
+                for (int e = 0; e < 8; e++) to[(half * 32 + g * 8 + e) * w.pitch] = get(half)[e];
         }
         // ---- U (or dV)
 #pragma unroll
-        for (int half = 0; half < HALVES; half++)
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++) r8[half][nt] *= eight(2, half);
-        if (MODE == BACK) {
+        for (int half = 0; half < HALVES; half++) set(half, get(half) * eight(2, half));
+        if (MODE == BACK && here) {
+            S *const to = reinterpret_cast<S *>(w.gv) + (at.start + t0) * w.o_tok + at.h * (long long)w.dv + at.col_part + col;
 #pragma unroll
             for (int half = 0; half < HALVES; half++)
 #pragma unroll
-                for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                    for (int e = 0; e < 8; e++) {
-                        const int row = half * 32 + g * 8 + e;
-                        if (row < n && col_of(nt) < nc)
-                            reinterpret_cast<S *>(w.gv)[(at.start + t0 + row) * w.o_tok + h * (long long)w.dv + col_part + col_of(nt)] = (S)r8[half][nt][e];
-                    }
+                for (int e = 0; e < 8; e++) {
+                    const int row = half * 32 + g * 8 + e;
+                    if (row < n) to[row * w.o_tok] = (S)get(half)[e];
+                }
         }
         if (OUT) {
+            Frag uf[HALVES][COMPUTED];
 #pragma unroll
-            for (int half = 0; half < HALVES; half++) {
-                Frag uf[NT][COMPUTED];
+            for (int half = 0; half < HALVES; half++) split(get(half), uf[half]);
 #pragma unroll
-                for (int nt = 0; nt < NT; nt++) split(r8[half][nt], uf[nt]);
+            for (int t = 0; t < TT; t++) {
+                y[t] *= w.scale * vec[t * 16 + i];
 #pragma unroll
-                for (int t = 0; t < TT; t++) {
-                    if (half == 0) {
-                        const float scale = w.scale * vec_lds[t * 16 + i];
-#pragma unroll
-                        for (int nt = 0; nt < NT; nt++) y[t][nt] *= scale;
-                    }
+                for (int half = 0; half < HALVES; half++) {
                     if (!p_has<false>(t, half)) continue;
                     Frag pf[COMPUTED];
 #pragma unroll
                     for (int u = 0; u < COMPUTED; u++) pf[u] = p_lds[(p_block<false>(t, half, CH) * COMPUTED + u) * 64 + lane];
-#pragma unroll
-                    for (int nt = 0; nt < NT; nt++) y[t][nt] = product(uf[nt], pf, y[t][nt]);
+                    y[t] = product(uf[half], pf, y[t]);
                 }
             }
 #pragma unroll
             for (int t = 0; t < TT; t++) {
-                const int row = t * 16 + i, col = col0 + g * CS;
+                const int row = t * 16 + i, first = col0 + g * 4;
                 if (row < n) {
-                    S *const to = reinterpret_cast<S *>(w.o) + (at.start + t0 + row) * w.o_tok + h * (long long)w.dv + col_part + col;
-                    float out[NT * 4];
-#pragma unroll
-                    for (int e = 0; e < NT * 4; e++) out[e] = y[t][e / 4][e % 4];
-                    if (col + NT * 4 <= nc) store_floats_unaligned<S, NT * 4>(to, out);
+                    S *const to = reinterpret_cast<S *>(w.o) + (at.start + t0 + row) * w.o_tok + at.h * (long long)w.dv + at.col_part + first;
+                    float out[4] = {y[t][0], y[t][1], y[t][2], y[t][3]};
+                    if (first + 4 <= at.nc) store_floats_unaligned<S, 4>(to, out);
                     else
 #pragma unroll
-                        for (int e = 0; e < NT * 4; e++)
-                            if (col + e < nc) to[e] = (S)out[e];
+                        for (int e = 0; e < 4; e++)
+                            if (first + e < at.nc) to[e] = (S)out[e];
                 }
             }
         }
-        if (!TOTAL && step == nchunks - 1 && !(last && w.fin)) break; // nobody needs the next state
-        // ---- the next state
+        // ---- the next state, unless nobody needs it
+        if (TOTAL || step + 1 < at.nchunks || (at.last && w.fin)) {
+            const float decay = vec[3 * CH];
 #pragma unroll
-        for (int t = 0; t < DK / 16; t++)
+            for (int t = 0; t < DK / 16; t++) R[t] *= decay;
 #pragma unroll
-            for (int nt = 0; nt < NT; nt++) R[t][nt] *= decay;
-#pragma unroll
-        for (int half = 0; half < HALVES; half++) {
-            Frag uf[NT][COMPUTED], gf[REV ? NT : 1][COMPUTED];
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++) {
+            for (int half = 0; half < HALVES; half++) {
+                Frag uf[COMPUTED], gf[COMPUTED];
                 if (REV) {
-                    split(-(eight(0, half) * r8[half][nt]), uf[nt]);
-                    split(w.scale * (eight(0, half) * go8[half][nt]), gf[nt]);
+                    split(-(eight(0, half) * get(half)), uf);
+                    split(w.scale * (eight(0, half) * go8[half]), gf);
                 } else {
-                    split(eight(1, half) * r8[half][nt], uf[nt]);
+                    split(eight(1, half) * get(half), uf);
                 }
-            }
 #pragma unroll
-            for (int t = 0; t < DK / 16; t++) {
-                Frag kf[IP];
-                col_frag<Lds::PK>(kf, k_lds, KP, half * 32, t / 2 * 32 + t % 2 * 4, 8, lane);
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++) R[t][nt] = product(kf, uf[nt], R[t][nt]);
-                if (REV) {
-                    Frag qf[IP];
-                    col_frag<Lds::PK>(qf, q_lds, KP, half * 32, t / 2 * 32 + t % 2 * 4, 8, lane);
-#pragma unroll
-                    for (int nt = 0; nt < NT; nt++) R[t][nt] = product(qf, gf[nt], R[t][nt]);
+                for (int t = 0; t < DK / 16; t++) {
+                    Frag kf[IP];
+                    col_frag<Lds::PK>(kf, kt, KP, half * 32, t / 2 * 32 + t % 2 * 4, 8, lane);
+                    R[t] = product(kf, uf, R[t]);
+                    if (REV) {
+                        Frag qf[IP];
+                        col_frag<Lds::PK>(qf, qt, KP, half * 32, t / 2 * 32 + t % 2 * 4, 8, lane);
+                        R[t] = product(qf, gf, R[t]);
+                    }
                 }
             }
         }
+        __syncthreads();
     }
 
 #pragma unroll
-    for (int t = 0; t < DK / 16; t++)
+    for (int t = 0; t < DK / 16; t++) {
+        if (TOTAL && at.map) {
 #pragma unroll
-        for (int nt = 0; nt < NT; nt++) {
-            const int col = col_of(nt);
-            if (TOTAL && map) {
+            for (int e = 0; e < 4; e++)
+                if (at.col_part + col < DK) w.maps[(long long)(row_of(t, e)) * DK + at.col_part + col + at.state0] = R[t][e];
+        } else if (TOTAL) {
+            *reinterpret_cast<f32x4 *>(total + t * 256) = R[t];
+        } else if (at.last && w.fin) {
 #pragma unroll
-                for (int e = 0; e < 4; e++)
-                    if (col_part + col < DK) w.maps[((slot * w.heads + h) * DK + row_of(t, e)) * (long long)DK + col_part + col] = R[t][nt][e];
-            } else if (TOTAL) {
-                *reinterpret_cast<f32x4 *>(total + (nt * (DK / 16) + t) * 256) = R[t][nt];
-            } else if (last && w.fin) {
-#pragma unroll
-                for (int e = 0; e < 4; e++)
-                    if (row_of(t, e) < w.dk && col < nc) w.fin[state0 + (long long)row_of(t, e) * w.dv + col] = R[t][nt][e];
-            }
+            for (int e = 0; e < 4; e++)
+                if (row_of(t, e) < w.dk && here) w.fin[at.state0 + (long long)row_of(t, e) * w.dv + col] = R[t][e];
         }
+    }
 }
 
 // grid: slots heads parts, in one order; the parts of a head and segment run on one XCD (of 8, dealt round robin), whose L2 has what they share
-template <typename S, int DK, int DV, int NW, int MODE>
-__global__ __launch_bounds__(NW * 64, (DeltaLds<S, DK, DV, NW, MODE>::per_simd)) void delta_walk_kernel(DeltaArgs w)
+template <typename S, int DK, int DV, int MODE>
+__global__ __launch_bounds__((DeltaLds<S, DK, DV, MODE>::WAVES * 64), (DeltaLds<S, DK, DV, MODE>::per_simd)) void delta_walk_kernel(const DeltaArgs w)
 {
+    typedef DeltaLds<S, DK, DV, MODE> Lds;
     extern __shared__ __align__(16) unsigned char lds[];
     const int parts = w.parts + (MODE == MAPS ? w.map_parts : 0);
     const long long block = block_of(), group = block / (8 * parts);
-    const int in = (int)(block % (8 * parts));
+    const int in = (int)(block % (8 * parts)), part = in / 8;
     const long long item = group * 8 + in % 8;
     if (item >= (long long)w.slots * w.heads) return;
-    const int h = (int)(item % w.heads);
     const long long slot = item / w.heads;
-    const Place at = find_place(w.seg, slot);
-    if (at.seg < 0 || at.seg >= at.nseg) return; // a slot that no sequence has
-    delta_walk<S, DK, DV, NW, MODE>(w, at, slot, h, in / 8, lds);
+    const Place place = find_place(w.seg, slot);
+    if (place.seg < 0 || place.seg >= place.nseg) return; // a slot that no sequence has
+    WalkPlace at;
+    at.h = (int)(item % w.heads);
+    at.kh = at.h / w.share;
+    at.last = Lds::REV ? place.seg == 0 : place.seg == place.nseg - 1; // in walking order
+    at.map = MODE == MAPS && part >= w.parts;                          // columns of A
+    if ((MODE == MAPS || MODE == BACK_MAPS) && at.last && !(at.map && w.back)) return; // (the way back goes through the last segment's A as well)
+    at.start = place.start;
+    at.len = place.len;
+    at.col_part = (at.map ? part - w.parts : part) * DV;
+    const int columns = at.map ? w.dk : w.dv;
+    at.nc = columns - at.col_part < DV ? columns - at.col_part : DV;
+    at.seg0 = place.seg * w.seg.seg_len;
+    at.seg1 = at.seg0 + w.seg.seg_len < at.len ? at.seg0 + w.seg.seg_len : at.len;
+    at.nchunks = (int)((at.seg1 - at.seg0 + Lds::CH - 1) / Lds::CH);
+    at.chunk0 = at.len ? first_slot(w.chunk, place.seq) + at.seg0 / Lds::CH : 0;
+    at.state0 = at.map ? item * (DK * DK) : (place.seq * w.heads + at.h) * (long long)w.dk * w.dv + at.col_part;
+    float *const total = w.totals && !at.map ? w.totals + (item * w.parts + part) * (long long)(DK * DV) : nullptr;
+    if (threadIdx.x >= LOADERS * 64) delta_walk<S, DK, DV, MODE>(w, at, total, lds);
+    else if (at.nchunks > 0) delta_load<S, DK, DV, MODE>(w, at, lds);
 }
 
 // Segments' maps -> incoming states, in walking order: S <- A S + B (REV: A^T D + B).  A workgroup has 16 NW columns of one head's state.
 // grid: seqs heads (dv / 16 NW)
-template <int DK, int DV, int NW, int NT, bool REV> __global__ __launch_bounds__(NW * 64) void delta_carry_kernel(DeltaArgs w)
+template <int DK, int DV, bool REV> __global__ __launch_bounds__(DV * 4) void delta_carry_kernel(DeltaArgs w)
 {
-    constexpr int CS = NT == 2 ? 8 : 4, KS = DK / 32;
+    constexpr int NT = 1, CS = 4, KS = DK / 32;
     const long long block = block_of();
     const int part = (int)(block % w.parts), h = (int)(block / w.parts % w.heads);
     const long long s = block / w.parts / w.heads;
@@ -722,26 +712,26 @@ template <int DK, int DV, int NW, int NT, bool REV> __global__ __launch_bounds__
 // ---- the gradients of q, k, the decays and beta, a chunk and head a workgroup
 
 template <typename S, int DK, int DV> struct GradLds {
-    static constexpr int CH = chunk_of<S>(), IP = Parts<S>::IN, PK = DK + PITCH_PAD, SLAB = DV < 64 ? DV : 64, PV = SLAB + PITCH_PAD;
-    static constexpr int NW = DK / 16 < 4 ? 4 : DK / 16;
-    static constexpr int K_TILE = CH * PK * IP, V_PLANE = CH * PV, ROWS = V_PLANE * (2 * COMPUTED + 2 * IP); // U, dV in parts, dO, V
-    static constexpr int JOBS = 4 * pair_blocks(CH);
-    static constexpr size_t frag_bytes = JOBS * COMPUTED * 64 * sizeof(Frag), row_bytes = ROWS * sizeof(bf16);
-    static constexpr size_t shared_bytes = frag_bytes > row_bytes ? frag_bytes : row_bytes;
+    static constexpr int CH = chunk_of<S>(), IP = Parts<S>::IN, PK = DK + PITCH_PAD, SLAB = DV < 64 ? DV : 64, PV = SLAB + PITCH_PAD, PP = CH + PITCH_PAD;
+    static constexpr int NW = DK == 128 ? 8 : 4; // (four waves of two column tiles, two workgroups a CU, had to spill: 818 us where this takes GRADUS)
+    static constexpr int K_TILE = CH * PK * IP, V_PLANE = CH * PV, ROWS = V_PLANE * (2 * COMPUTED + 2 * IP), PAIRS_PLANE = CH * PP; // rows: U, dV in parts, dO, V
+    // first the rows along dv, a slab at a time, then those of k and q and the pairs
+    static constexpr size_t row_bytes = ROWS * sizeof(bf16), pair_bytes = (COMPUTED * PAIRS_PLANE + 2 * K_TILE) * sizeof(bf16);
+    static constexpr size_t shared_bytes = row_bytes > pair_bytes ? row_bytes : pair_bytes;
     // + sums of q . dq by waves, betas' gradients, v . dv, and single sums
-    static constexpr size_t bytes = shared_bytes + 2 * K_TILE * sizeof(bf16) + CH * sizeof(double) + (3 * CH + NW * CH + 2 * CH + 2 * NW) * sizeof(float);
+    static constexpr size_t bytes = shared_bytes + CH * sizeof(double) + (3 * CH + NW * CH + 2 * CH + 2 * NW) * sizeof(float);
+    static constexpr int fit = (int)((160 << 10) / bytes), resident = fit > 8 / NW ? 8 / NW : fit, per_simd = resident * NW / 4;
 };
 
-template <typename S, int DK, int DV> __global__ __launch_bounds__((GradLds<S, DK, DV>::NW * 64)) void delta_grad_kernel(DeltaArgs w)
+template <typename S, int DK, int DV> __global__ __launch_bounds__((GradLds<S, DK, DV>::NW * 64), (GradLds<S, DK, DV>::per_simd)) void delta_grad_kernel(DeltaArgs w)
 {
     typedef GradLds<S, DK, DV> Lds;
-    constexpr int CH = Lds::CH, IP = Lds::IP, PK = Lds::PK, PV = Lds::PV, SLAB = Lds::SLAB, NW = Lds::NW, THREADS = NW * 64, KP = CH * PK, VP = CH * PV;
-    constexpr int TT = CH / 16, HALVES = CH / 32, BLOCKS = pair_blocks(CH), MINE = (Lds::JOBS + NW - 1) / NW, UNITS = CH * SLAB / 8;
+    constexpr int CH = Lds::CH, IP = Lds::IP, PK = Lds::PK, PV = Lds::PV, PP = Lds::PP, SLAB = Lds::SLAB, NW = Lds::NW, NT = 1, THREADS = NW * 64, KP = CH * PK, VP = CH * PV;
+    constexpr int TT = CH / 16, HALVES = CH / 32, BLOCKS = pair_blocks(CH), CS = 4, UNITS = CH * SLAB / 8, ACTIVE = DK / 16 / NT; // waves that have columns
     extern __shared__ __align__(16) unsigned char lds[];
-    Frag *const frags = reinterpret_cast<Frag *>(lds);
     bf16 *const u_lds = reinterpret_cast<bf16 *>(lds), *const dv_lds = u_lds + COMPUTED * VP, *const do_lds = dv_lds + COMPUTED * VP, *const v_lds = do_lds + IP * VP;
-    bf16 *const k_lds = reinterpret_cast<bf16 *>(lds + Lds::shared_bytes), *const q_lds = k_lds + Lds::K_TILE;
-    double *const b2 = reinterpret_cast<double *>(q_lds + Lds::K_TILE);
+    bf16 *const pairs = reinterpret_cast<bf16 *>(lds), *const k_lds = pairs + COMPUTED * Lds::PAIRS_PLANE, *const q_lds = k_lds + Lds::K_TILE;
+    double *const b2 = reinterpret_cast<double *>(lds + Lds::shared_bytes);
     float *const up = reinterpret_cast<float *>(b2 + CH), *const down = up + CH, *const beta = down + CH, *const qdq = beta + CH, *const gbeta = qdq + NW * CH,
                  *const vdv = gbeta + CH, *const sums = vdv + CH;
 
@@ -754,17 +744,12 @@ template <typename S, int DK, int DV> __global__ __launch_bounds__((GradLds<S, D
     const long long t0 = at.seg * CH, tok = at.start + t0, record = slot * w.heads + h;
     const int n = at.len - t0 < CH ? (int)(at.len - t0) : CH;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-    const bool columns = wave < DK / 16; // the wave's columns of q and k: 16 wave + 0 .. 15
+    const bool columns = wave < ACTIVE;
+    const int col0 = wave * NT * 16; // the wave's columns of q and k: col0 + (i / 4) CS + 4 nt + i % 4
+    auto col_of = [&](int nt) { return col0 + (i >> 2) * CS + 4 * nt + (i & 3); };
     const ChunkVec<CH> &vec = reinterpret_cast<const ChunkVec<CH> *>(w.vecs)[record];
     const S *const go = reinterpret_cast<const S *>(w.go) + tok * w.o_tok + h * (long long)w.dv;
     const S *const v = reinterpret_cast<const S *>(w.v) + tok * w.v_tok + h * w.v_head;
-    {
-        TileRows<S, DK, THREADS, CH> kx, qx;
-        kx.fetch(reinterpret_cast<const S *>(w.k) + tok * w.k_tok + kh * w.k_head, w.k_tok, n, w.dk);
-        qx.fetch(reinterpret_cast<const S *>(w.q) + tok * w.q_tok + kh * w.q_head, w.q_tok, n, w.dk);
-        kx.template put<PK>(k_lds, n, w.dk);
-        qx.template put<PK>(q_lds, n, w.dk);
-    }
     if (threadIdx.x < CH) {
         b2[threadIdx.x] = vec.b2[threadIdx.x];
         up[threadIdx.x] = vec.up[threadIdx.x];
@@ -773,152 +758,229 @@ template <typename S, int DK, int DV> __global__ __launch_bounds__((GradLds<S, D
         gbeta[threadIdx.x] = vdv[threadIdx.x] = 0.0f;
     }
 
-    f32x4 dq[TT], k_last[TT], k_row[TT];
+    f32x4 dq[TT][NT], k_last[TT][NT], k_row[TT][NT];
 #pragma unroll
-    for (int t = 0; t < TT; t++) dq[t] = k_last[t] = k_row[t] = f32x4{0, 0, 0, 0};
-    f32x4 job0[MINE], job1[MINE];
+    for (int t = 0; t < TT; t++)
 #pragma unroll
-    for (int u = 0; u < MINE; u++) job0[u] = job1[u] = f32x4{0, 0, 0, 0};
+        for (int nt = 0; nt < NT; nt++) dq[t][nt] = k_last[t][nt] = k_row[t][nt] = f32x4{0, 0, 0, 0};
+    // The pairs' sums, blocks of 16 rows by 32: dO_i . U_j, up to two blocks of those on and below the diagonal; dV_r . U_s and U_r . dV_s for a
+    // block on the diagonal, and one of the two off it
+    struct Dots { f32x4 a, b; };
+    const Dots zero = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    Dots p_dots[2] = {zero, zero}, low = zero, high = zero, off = zero;
+    int p_t[2], p_ks[2];
+    bool p_mine[2];
+#pragma unroll
+    for (int u = 0; u < 2; u++) {
+        const int b = (CH == 64 ? NW == 8 ? wave - 4 : wave : wave - 2) + 4 * u;
+        p_mine[u] = b >= 0 && b < BLOCKS && (CH == 64 || u == 0);
+        p_place<false>(p_mine[u] ? b : 0, CH, p_t[u], p_ks[u]);
+    }
+    const bool z_mine = wave < TT, o_mine = CH == 64 && (NW == 4 || wave >= 4); // dG + dG^T: the diagonal's block of rows 16 wave on, and the one beside it
+    const int o_t = wave & 3;
     float ds = 0;
-    // the pairs' jobs: dO . U and dV . U, each with the lane's row first (later token) and second
-    auto place = [&](int job, int &kind, int &t, int &ks) {
-        kind = job / BLOCKS;
-        if (kind & 1) p_place<true>(job % BLOCKS, CH, t, ks);
-        else p_place<false>(job % BLOCKS, CH, t, ks);
-    };
-    for (int slab = 0; slab < w.dv; slab += SLAB) {
+    // What comes from memory is on its way well before it is used: a slab's rows while the last one's pairs are summed, the states'
+    // entries of the next 32 columns while those of these are multiplied.  (Loaded where they are used, waits were two thirds of the kernel's time.)
+    constexpr int PER = (UNITS + THREADS - 1) / THREADS; // (whole waves have units or none)
+    TileRows<S, SLAB, THREADS, CH> gx, vx;
+    f32x8 e8[PER], w8[PER], s8[NT], d8[NT];
+    auto fetch_rows = [&](int slab) {
         const int nc = w.dv - slab < SLAB ? w.dv - slab : SLAB;
-        TileRows<S, SLAB, THREADS, CH> gx, vx;
         gx.fetch(go + slab, w.o_tok, n, nc);
         vx.fetch(v + slab, w.v_tok, n, nc);
-        __syncthreads();
-        gx.template put<PV>(do_lds, n, nc);
-        vx.template put<PV>(v_lds, n, nc);
-        __syncthreads();
-        for (int u = threadIdx.x; u < (UNITS + 63) / 64 * 64; u += THREADS) { // (whole waves, for the sums over rows' lanes)
-            const int row = u / (SLAB / 8), col = u % (SLAB / 8) * 8;
-            const bool there = u < UNITS;
-            const long long from = record * (CH * (long long)w.pitch) + (there ? row : 0) * (long long)w.pitch + slab + col;
-            const f32x8 e8 = *reinterpret_cast<const f32x8 *>(w.rows_e + from), w8 = *reinterpret_cast<const f32x8 *>(w.rows_w + from);
-            const float be = beta[there ? row : 0];
-            Frag parts[COMPUTED], vf[IP];
-            split(be * e8, parts);
 #pragma unroll
-            for (int p = 0; p < COMPUTED; p++)
-                if (there) *reinterpret_cast<Frag *>(u_lds + p * VP + row * PV + col) = parts[p];
-            const f32x8 dv8 = be * w8;
+        for (int x = 0; x < PER; x++) {
+            const int u = threadIdx.x + x * THREADS, row = u / (SLAB / 8), col = u % (SLAB / 8) * 8;
+            if (UNITS % THREADS && u >= UNITS) continue;
+            const long long from = record * (CH * (long long)w.pitch) + row * (long long)w.pitch + slab + col;
+            e8[x] = *reinterpret_cast<const f32x8 *>(w.rows_e + from);
+            w8[x] = *reinterpret_cast<const f32x8 *>(w.rows_w + from);
+        }
+    };
+    auto fetch_states = [&](int col) {
+        if (columns)
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++) {
+                const long long from = record * (DK * (long long)w.pitch) + col_of(nt) * (long long)w.pitch + col + g * 8;
+                d8[nt] = *reinterpret_cast<const f32x8 *>(w.kept_d + from);
+                s8[nt] = *reinterpret_cast<const f32x8 *>(w.kept_s + from);
+            }
+    };
+    fetch_rows(0);
+    for (int slab = 0; slab < w.dv; slab += SLAB) {
+        const int nc = w.dv - slab < SLAB ? w.dv - slab : SLAB;
+        const bool more = slab + SLAB < w.dv;
+        fetch_states(slab);
+        __syncthreads();
+        gx.template put_any<PV>(do_lds, n, nc);
+        vx.template put_any<PV>(v_lds, n, nc);
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < PER; x++) {
+            const int u = threadIdx.x + x * THREADS, row = u / (SLAB / 8), col = u % (SLAB / 8) * 8;
+            if (UNITS % THREADS && u >= UNITS) continue;
+            const float be = beta[row];
+            Frag parts[COMPUTED], vf[IP];
+            split(be * e8[x], parts);
+#pragma unroll
+            for (int p = 0; p < COMPUTED; p++) *reinterpret_cast<Frag *>(u_lds + p * VP + row * PV + col) = parts[p];
+            const f32x8 dv8 = be * w8[x];
             split(dv8, parts);
 #pragma unroll
-            for (int p = 0; p < COMPUTED; p++)
-                if (there) *reinterpret_cast<Frag *>(dv_lds + p * VP + row * PV + col) = parts[p];
-            row_frag(vf, v_lds + (there ? row : 0) * PV + col, VP);
+            for (int p = 0; p < COMPUTED; p++) *reinterpret_cast<Frag *>(dv_lds + p * VP + row * PV + col) = parts[p];
+            row_frag(vf, v_lds + row * PV + col, VP);
             const f32x8 v8 = widen(vf);
             float a = 0, b = 0;
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                a += e8[e] * w8[e];
+                a += e8[x][e] * w8[x][e];
                 b += v8[e] * dv8[e];
             }
 #pragma unroll
-            for (int x = 1; x < SLAB / 8; x *= 2) {
-                a += __shfl_xor(a, x);
-                b += __shfl_xor(b, x);
+            for (int y = 1; y < SLAB / 8; y *= 2) {
+                a += __shfl_xor(a, y);
+                b += __shfl_xor(b, y);
             }
-            if (there && col == 0) {
+            if (col == 0) {
                 gbeta[row] += a;
                 vdv[row] += b;
             }
         }
         __syncthreads();
         if (columns) {
-            const float *const s0 = w.kept_s + record * (DK * (long long)w.pitch) + (wave * 16 + i) * (long long)w.pitch + slab + g * 8;
-            const float *const d0 = w.kept_d + record * (DK * (long long)w.pitch) + (wave * 16 + i) * (long long)w.pitch + slab + g * 8;
 #pragma unroll
             for (int kk = 0; kk < SLAB / 32; kk++) {
-                const f32x8 s8 = *reinterpret_cast<const f32x8 *>(s0 + kk * 32), d8 = *reinterpret_cast<const f32x8 *>(d0 + kk * 32);
+                Frag f[NT][COMPUTED];
 #pragma unroll
-                for (int e = 0; e < 8; e++) ds += s8[e] * d8[e];
-                Frag sf[COMPUTED], df[COMPUTED];
-                split(s8, sf);
-                split(d8, df);
+                for (int nt = 0; nt < NT; nt++) {
+#pragma unroll
+                    for (int e = 0; e < 8; e++) ds += s8[nt][e] * d8[nt][e];
+                    split(d8[nt], f[nt]);
+                }
+                auto rows = [&](int t) { return (t * 16 + i) * PV + kk * 32 + g * 8; };
 #pragma unroll
                 for (int t = 0; t < TT; t++) {
-                    const int from = (t * 16 + i) * PV + kk * 32 + g * 8;
-                    Frag gf[IP], uf[COMPUTED], vf[COMPUTED];
-                    row_frag(gf, do_lds + from, VP);
-                    row_frag(uf, u_lds + from, VP);
-                    row_frag(vf, dv_lds + from, VP);
-                    dq[t] = product(sf, gf, dq[t]);
-                    k_last[t] = product(df, uf, k_last[t]);
-                    k_row[t] = product(sf, vf, k_row[t]);
+                    Frag uf[COMPUTED];
+                    row_frag(uf, u_lds + rows(t), VP);
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt++) k_last[t][nt] = product(f[nt], uf, k_last[t][nt]);
                 }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) split(s8[nt], f[nt]);
+                if (kk + 1 < SLAB / 32) fetch_states(slab + kk * 32 + 32);
+#pragma unroll
+                for (int t = 0; t < TT; t++) {
+                    Frag gf[IP], vf[COMPUTED];
+                    row_frag(gf, do_lds + rows(t), VP);
+                    row_frag(vf, dv_lds + rows(t), VP);
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt++) {
+                        dq[t][nt] = product(f[nt], gf, dq[t][nt]);
+                        k_row[t][nt] = product(f[nt], vf, k_row[t][nt]);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
+        if (more) fetch_rows(slab + SLAB);
+        auto dots = [&](auto lane_parts, const bf16 *lane_rows, auto other_parts, const bf16 *others, int t, int ks, Dots &to) {
 #pragma unroll
-        for (int u = 0; u < MINE; u++) {
-            const int job = wave + u * NW;
-            if (job >= Lds::JOBS) continue;
-            int kind, t, ks;
-            place(job, kind, t, ks);
-            const int mine = (t * 16 + i) * PV + g * 8, other = turned_row(2 * ks, i) * PV + g * 8;
-            auto dots = [&](auto lane_parts, const bf16 *lane_rows, auto other_parts, const bf16 *others) {
+            for (int kk = 0; kk < SLAB / 32; kk++) {
+                Frag a[decltype(lane_parts)::value], b0[decltype(other_parts)::value], b1[decltype(other_parts)::value];
+                const bf16 *const other = others + turned_row(2 * ks, i) * PV + g * 8 + kk * 32;
+                row_frag(a, lane_rows + (t * 16 + i) * PV + g * 8 + kk * 32, VP);
+                row_frag(b0, other, VP);
+                row_frag(b1, other + 4 * PV, VP);
+                to.a = product(b0, a, to.a);
+                to.b = product(b1, a, to.b);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        typedef std::integral_constant<int, IP> In;
+        typedef std::integral_constant<int, COMPUTED> Three;
 #pragma unroll
-                for (int kk = 0; kk < SLAB / 32; kk++) {
-                    Frag a[decltype(lane_parts)::value], b0[decltype(other_parts)::value], b1[decltype(other_parts)::value];
-                    row_frag(a, lane_rows + mine + kk * 32, VP);
-                    row_frag(b0, others + other + kk * 32, VP);
-                    row_frag(b1, others + other + 4 * PV + kk * 32, VP);
-                    job0[u] = product(b0, a, job0[u]);
-                    job1[u] = product(b1, a, job1[u]);
-                }
-            };
-            typedef std::integral_constant<int, IP> In;
-            typedef std::integral_constant<int, COMPUTED> Three;
-            if (kind == 0) dots(In(), do_lds, Three(), u_lds);
-            else if (kind == 1) dots(Three(), u_lds, In(), do_lds);
-            else if (kind == 2) dots(Three(), dv_lds, Three(), u_lds);
-            else dots(Three(), u_lds, Three(), dv_lds);
+        for (int u = 0; u < 2; u++)
+            if (p_mine[u]) dots(In(), do_lds, Three(), u_lds, p_t[u], p_ks[u], p_dots[u]);
+        if (z_mine) {
+            dots(Three(), dv_lds, Three(), u_lds, wave, wave / 2, low);
+            dots(Three(), u_lds, Three(), dv_lds, wave, wave / 2, high);
+        }
+        if (o_mine) {
+            if (o_t >= 2) dots(Three(), dv_lds, Three(), u_lds, o_t, 0, off);
+            else dots(Three(), u_lds, Three(), dv_lds, o_t, 1, off);
         }
     }
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < MINE; u++) {
-        const int job = wave + u * NW;
-        if (job >= Lds::JOBS) continue;
-        int kind, t, ks;
-        place(job, kind, t, ks);
-        const int row = t * 16 + i, col = ks * 32 + g * 8;
-        f32x8 x = __builtin_shufflevector(job0[u], job1[u], 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-            const int c = col + e, later = kind & 1 ? c : row, earlier = kind & 1 ? row : c;
-            const bool there = kind < 2 ? later >= earlier : later > earlier;
-            x[e] = there ? (kind < 2 ? w.scale : -1.0f) * x[e] * power2(b2[later] - b2[earlier]) : 0.0f;
-        }
+
+    // ---- the pairs, row by row
+    TileRows<S, DK, THREADS, CH> kx, qx;
+    kx.fetch(reinterpret_cast<const S *>(w.k) + tok * w.k_tok + kh * w.k_head, w.k_tok, n, w.dk);
+    qx.fetch(reinterpret_cast<const S *>(w.q) + tok * w.q_tok + kh * w.q_head, w.q_tok, n, w.dk);
+    auto eight = [&](const Dots &d) { return f32x8(__builtin_shufflevector(d.a, d.b, 0, 1, 2, 3, 4, 5, 6, 7)); };
+    auto write = [&](int t, int ks, const f32x8 &x) {
         Frag parts[COMPUTED];
         split(x, parts);
 #pragma unroll
-        for (int p = 0; p < COMPUTED; p++) frags[(job * COMPUTED + p) * 64 + lane] = parts[p];
-    }
-    const int col0 = wave * 16;
+        for (int p = 0; p < COMPUTED; p++) *reinterpret_cast<Frag *>(pairs + p * Lds::PAIRS_PLANE + (t * 16 + i) * PP + ks * 32 + g * 8) = parts[p];
+    };
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 2; u++)
+        if (p_mine[u]) {
+            const int row = p_t[u] * 16 + i, col = p_ks[u] * 32 + g * 8;
+            f32x8 x = eight(p_dots[u]);
+#pragma unroll
+            for (int e = 0; e < 8; e++) x[e] = row >= col + e ? w.scale * x[e] * power2(b2[row] - b2[col + e]) : 0.0f;
+            write(p_t[u], p_ks[u], x);
+        }
+    kx.template put_any<PK>(k_lds, n, w.dk);
+    qx.template put_any<PK>(q_lds, n, w.dk);
+    __syncthreads();
     float kdk = 0;
-    auto four = [&](const bf16 *tile, int t) { // the lane's four entries of a row
+    auto entries = [&](const bf16 *tile, int t, int nt) { // the lane's four entries of a row
         f32x4 x = {0, 0, 0, 0};
-        const bf16 *const p = tile + (t * 16 + i) * PK + col0 + g * 4;
+        const bf16 *const p = tile + (t * 16 + i) * PK + col0 + g * CS + 4 * nt;
 #pragma unroll
         for (int u = IP - 1; u >= 0; u--) x += __builtin_convertvector(*reinterpret_cast<const bf16x4 *>(p + u * KP), f32x4);
         return x;
     };
-    if (columns)
+    auto dot = [](const f32x4 &a, const f32x4 &b) { return a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3]; };
+    if (columns) {
 #pragma unroll
-        for (int t = 0; t < TT; t++) {
-            const int row = t * 16 + i;
-            dq[t] *= w.scale * up[row];
-            k_last[t] *= down[row];
-            const f32x4 k4 = four(k_lds, t);
-            kdk += k4[0] * k_last[t][0] + k4[1] * k_last[t][1] + k4[2] * k_last[t][2] + k4[3] * k_last[t][3];
-            k_row[t] = k_last[t] - up[row] * k_row[t];
+        for (int t = 0; t < TT; t++)
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++) {
+                const int row = t * 16 + i;
+                dq[t][nt] *= w.scale * up[row];
+                k_last[t][nt] *= down[row];
+                kdk += dot(entries(k_lds, t, nt), k_last[t][nt]);
+                k_row[t][nt] = k_last[t][nt] - up[row] * k_row[t][nt];
+            }
+#pragma unroll
+        for (int half = 0; half < HALVES; half++) {
+            Frag kf[NT][IP], qf[NT][IP];
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++) {
+                col_frag<PK>(kf[nt], k_lds, KP, half * 32, col0 + 4 * nt, CS, lane);
+                col_frag<PK>(qf[nt], q_lds, KP, half * 32, col0 + 4 * nt, CS, lane);
+            }
+#pragma unroll
+            for (int t = 0; t < TT; t++) {
+                Frag x[COMPUTED];
+                if (p_has<false>(t, half)) {
+                    row_frag(x, pairs + (t * 16 + i) * PP + half * 32 + g * 8, Lds::PAIRS_PLANE);
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt++) dq[t][nt] = product(kf[nt], x, dq[t][nt]);
+                }
+                if (p_has<true>(t, half)) {
+                    col_frag<PP>(x, pairs, Lds::PAIRS_PLANE, half * 32, t * 16, 4, lane);
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt++) k_row[t][nt] = product(qf[nt], x, k_row[t][nt]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
+    }
 #pragma unroll
     for (int x = 1; x < 64; x *= 2) {
         kdk += __shfl_xor(kdk, x);
@@ -929,51 +991,60 @@ template <typename S, int DK, int DV> __global__ __launch_bounds__((GradLds<S, D
         sums[NW + wave] = ds;
     }
     __syncthreads();
+    if (z_mine) { // - (dG + dG^T)
+        const int row = wave * 16 + i, col = wave / 2 * 32 + g * 8;
+        f32x8 x;
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const int c = col + e;
+            const float a = e < 4 ? low.a[e & 3] : low.b[e & 3], b = e < 4 ? high.a[e & 3] : high.b[e & 3];
+            x[e] = c < row ? -a * power2(b2[row] - b2[c]) : c > row ? -b * power2(b2[c] - b2[row]) : 0.0f;
+        }
+        write(wave, wave / 2, x);
+    }
+    if (o_mine) {
+        const int row = o_t * 16 + i, col = (1 - o_t / 2) * 32 + g * 8;
+        f32x8 x = eight(off);
+#pragma unroll
+        for (int e = 0; e < 8; e++) x[e] *= -power2(o_t >= 2 ? b2[row] - b2[col + e] : b2[col + e] - b2[row]);
+        write(o_t, 1 - o_t / 2, x);
+    }
+    __syncthreads();
     if (columns) {
 #pragma unroll
         for (int half = 0; half < HALVES; half++) {
-            Frag kf[IP], qf[IP];
-            col_frag<PK>(kf, k_lds, KP, half * 32, col0, 4, lane);
-            col_frag<PK>(qf, q_lds, KP, half * 32, col0, 4, lane);
+            Frag kf[NT][IP];
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++) col_frag<PK>(kf[nt], k_lds, KP, half * 32, col0 + 4 * nt, CS, lane);
 #pragma unroll
             for (int t = 0; t < TT; t++) {
-                auto frag = [&](int kind, int at, Frag (&x)[COMPUTED]) {
-#pragma unroll
-                    for (int p = 0; p < COMPUTED; p++) x[p] = frags[((kind * BLOCKS + at) * COMPUTED + p) * 64 + lane];
-                };
                 Frag x[COMPUTED];
-                if (p_has<false>(t, half)) {
-                    frag(0, p_block<false>(t, half, CH), x);
-                    dq[t] = product(kf, x, dq[t]);
-                    frag(2, p_block<false>(t, half, CH), x);
-                    k_row[t] = product(kf, x, k_row[t]);
-                }
-                if (p_has<true>(t, half)) {
-                    frag(1, p_block<true>(t, half, CH), x);
-                    k_row[t] = product(qf, x, k_row[t]);
-                    frag(3, p_block<true>(t, half, CH), x);
-                    k_row[t] = product(kf, x, k_row[t]);
-                }
+                row_frag(x, pairs + (t * 16 + i) * PP + half * 32 + g * 8, Lds::PAIRS_PLANE);
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) k_row[t][nt] = product(kf[nt], x, k_row[t][nt]);
             }
         }
 #pragma unroll
         for (int t = 0; t < TT; t++) {
-            const int row = t * 16 + i, col = col0 + g * 4;
-            const f32x4 q4 = four(q_lds, t);
-            float a = q4[0] * dq[t][0] + q4[1] * dq[t][1] + q4[2] * dq[t][2] + q4[3] * dq[t][3];
+            const int row = t * 16 + i, col = col0 + g * CS;
+            float a = 0;
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++) a += dot(entries(q_lds, t, nt), dq[t][nt]);
             a += __shfl_xor(a, 16);
             a += __shfl_xor(a, 32);
             if (g == 0) qdq[wave * CH + row] = a;
             if (row < n) {
                 const long long to = ((tok + row) * w.heads + h) * (long long)w.dk + col;
-                auto store = [&](void *out, const f32x4 &x) {
-                    float y[4] = {x[0], x[1], x[2], x[3]};
-                    if (col + 4 <= w.dk) {
-                        if (w.grad_float) store_floats_unaligned<float, 4>(reinterpret_cast<float *>(out) + to, y);
-                        else store_floats_unaligned<S, 4>(reinterpret_cast<S *>(out) + to, y);
+                auto store = [&](void *out, const f32x4 (&x)[NT]) {
+                    float y[NT * 4];
+#pragma unroll
+                    for (int e = 0; e < NT * 4; e++) y[e] = x[e / 4][e % 4];
+                    if (col + NT * 4 <= w.dk) {
+                        if (w.grad_float) store_floats_unaligned<float, NT * 4>(reinterpret_cast<float *>(out) + to, y);
+                        else store_floats_unaligned<S, NT * 4>(reinterpret_cast<S *>(out) + to, y);
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 4; e++)
+                        for (int e = 0; e < NT * 4; e++)
                             if (col + e < w.dk) {
                                 if (w.grad_float) reinterpret_cast<float *>(out)[to + e] = y[e];
                                 else reinterpret_cast<S *>(out)[to + e] = (S)y[e];
@@ -990,11 +1061,11 @@ template <typename S, int DK, int DV> __global__ __launch_bounds__((GradLds<S, D
         double s = 0;
         if (lane < CH) {
             s = -(double)vdv[lane];
-            for (int x = 0; x < DK / 16; x++) s += qdq[x * CH + lane];
+            for (int x = 0; x < ACTIVE; x++) s += qdq[x * CH + lane];
         }
         if (lane == n - 1) {
             double end = 0, d = 0;
-            for (int x = 0; x < DK / 16; x++) {
+            for (int x = 0; x < ACTIVE; x++) {
                 end += sums[x];
                 d += sums[NW + x];
             }
@@ -1016,30 +1087,31 @@ template <typename S, int DK, int DV> __global__ __launch_bounds__((GradLds<S, D
 
 // ---- launches
 
-template <typename S, int DK, int DV, int NW, int MODE> static int launch_delta_walk_sized(goom_ctx *ctx, DeltaArgs w, long long slots, const char *label)
+template <typename S, int DK, int DV, int MODE> static int launch_delta_walk_sized(goom_ctx *ctx, DeltaArgs w, long long slots, const char *label)
 {
     w.slots = (unsigned)slots;
     const int parts = w.parts + (MODE == MAPS ? w.map_parts : 0);
-    auto *kernel = delta_walk_kernel<S, DK, DV, NW, MODE>;
-    constexpr size_t bytes = DeltaLds<S, DK, DV, NW, MODE>::bytes;
+    typedef DeltaLds<S, DK, DV, MODE> Lds;
+    auto *kernel = delta_walk_kernel<S, DK, DV, MODE>;
+    constexpr size_t bytes = Lds::bytes;
     static_assert(bytes <= (160 << 10), "LDS of a CU");
     static std::atomic<unsigned long long> done{0};
     if (int st = allow_lds(ctx, reinterpret_cast<const void *>(kernel), bytes, done)) return st;
     goom::prof_begin(ctx, label);
-    kernel<<<grid_of((slots * w.heads + 7) / 8 * 8 * parts, NW * 64), NW * 64, bytes, ctx->stream>>>(w);
+    kernel<<<grid_of((slots * w.heads + 7) / 8 * 8 * parts, Lds::WAVES * 64), Lds::WAVES * 64, bytes, ctx->stream>>>(w);
     goom::prof_end(ctx);
     return goom::check_hip(ctx, hipGetLastError(), label);
 }
 
-// columns of a workgroup, and its waves
+// columns of a workgroup
 constexpr int delta_columns(int dv) { return dv <= 32 ? 32 : 64; }
 constexpr int delta_rows(int dk) { return dk <= 32 ? 32 : dk <= 64 ? 64 : 128; }
 
 template <typename F> static int with_delta(int dk, int dv, F f)
 {
     auto columns = [&](auto rows) {
-        if (dv <= 32) return f(rows, std::integral_constant<int, 32>(), std::integral_constant<int, 2>());
-        return f(rows, std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
+        if (dv <= 32) return f(rows, std::integral_constant<int, 32>());
+        return f(rows, std::integral_constant<int, 64>());
     };
     return dk <= 32 ? columns(std::integral_constant<int, 32>()) : dk <= 64 ? columns(std::integral_constant<int, 64>()) : columns(std::integral_constant<int, 128>());
 }
@@ -1053,7 +1125,7 @@ template <typename S> int launch_delta_gradients(goom_ctx *ctx, const DeltaArgs 
 template <typename S> int launch_delta_within_typed(goom_ctx *ctx, DeltaArgs w, long long slots)
 {
     w.slots = (unsigned)slots;
-    return with_delta(w.dk, 64, [&](auto rows, auto, auto) {
+    return with_delta(w.dk, 64, [&](auto rows, auto) {
         constexpr int DK = decltype(rows)::value;
         auto *kernel = within_kernel<S, DK>;
         static std::atomic<unsigned long long> done{0};
@@ -1067,11 +1139,11 @@ template <typename S> int launch_delta_within_typed(goom_ctx *ctx, DeltaArgs w, 
 
 template <typename S, int FIRST, int SECOND, int THIRD> int launch_delta_walk_typed(goom_ctx *ctx, const DeltaArgs &w, int mode, long long slots, const char *label)
 {
-    return with_delta(w.dk, w.dv, [&](auto rows, auto cols, auto waves) {
-        constexpr int DK = decltype(rows)::value, DV = decltype(cols)::value, NW = decltype(waves)::value;
-        if (mode == FIRST) return launch_delta_walk_sized<S, DK, DV, NW, FIRST>(ctx, w, slots, label);
-        if (mode == SECOND) return launch_delta_walk_sized<S, DK, DV, NW, SECOND>(ctx, w, slots, label);
-        return launch_delta_walk_sized<S, DK, DV, NW, THIRD>(ctx, w, slots, label);
+    return with_delta(w.dk, w.dv, [&](auto rows, auto cols) {
+        constexpr int DK = decltype(rows)::value, DV = decltype(cols)::value;
+        if (mode == FIRST) return launch_delta_walk_sized<S, DK, DV, FIRST>(ctx, w, slots, label);
+        if (mode == SECOND) return launch_delta_walk_sized<S, DK, DV, SECOND>(ctx, w, slots, label);
+        return launch_delta_walk_sized<S, DK, DV, THIRD>(ctx, w, slots, label);
     });
 }
 
@@ -1090,7 +1162,7 @@ template <typename S> int launch_delta_gradients_typed(goom_ctx *ctx, DeltaArgs 
         goom::prof_end(ctx);
         return goom::check_hip(ctx, hipGetLastError(), "gated delta rule: gradients");
     };
-    return with_delta(w.dk, w.dv, [&](auto rows, auto cols, auto) { return run(rows, cols); });
+    return with_delta(w.dk, w.dv, run);
 }
 
 } // namespace goom_layer
