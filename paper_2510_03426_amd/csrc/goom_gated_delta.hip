@@ -153,7 +153,6 @@ static DeltaPlan plan_of(const goom_delta_shape &sh, bool packed, bool backward)
     // Segments where the walks are fewer than the chip has CUs: as many as make two a CU.  A cut costs a walk without outputs over the columns of A and B:
     // with 256 walks of 64 chunks (8 x 4096 tokens, 16 heads of 128, bfloat16) both directions took 2120 us uncut, 2450 us in two segments each.
     const long long walks = sh.seqs * sh.heads * p.parts, mean = sh.seqs > 0 ? (sh.tokens + sh.seqs - 1) / sh.seqs : 0, least = 4 * p.ch;
-    
     long long want = walks > 0 && walks < 256 ? 512 / walks : 1;
     if (want > mean / least) want = mean / least;
     p.maps = want > 1;
@@ -204,10 +203,12 @@ template <typename S> static int launch_carry(goom_ctx *ctx, const goom_delta_sh
 {
     return with_delta(sh.dk, sh.dv, [&](auto rows, auto cols) {
         constexpr int DK = decltype(rows)::value, DV = decltype(cols)::value;
-        const dim3 grid = grid_of(sh.seqs * sh.heads * w.parts, DV * 4);
+        constexpr size_t bytes = carry_bytes<DK>();
+        static std::atomic<unsigned long long> done{0}, done_back{0};
+        auto *kernel = back ? delta_carry_kernel<DK, DV, true> : delta_carry_kernel<DK, DV, false>;
+        if (int st = allow_lds(ctx, reinterpret_cast<const void *>(kernel), bytes, back ? done_back : done)) return st;
         goom::prof_begin(ctx, "gated delta rule: carries");
-        if (back) delta_carry_kernel<DK, DV, true><<<grid, DV * 4, 0, ctx->stream>>>(w);
-        else delta_carry_kernel<DK, DV, false><<<grid, DV * 4, 0, ctx->stream>>>(w);
+        kernel<<<grid_of(sh.seqs * sh.heads * w.parts, DV * 4), DV * 4, bytes, ctx->stream>>>(w);
         goom::prof_end(ctx);
         return goom::check_hip(ctx, hipGetLastError(), "gated delta rule: carries");
     });

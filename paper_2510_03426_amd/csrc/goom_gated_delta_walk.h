@@ -75,6 +75,14 @@ __device__ inline double log2_of(float log_decay)
 }
 __device__ inline float power2(double x) { return __builtin_amdgcn_exp2f((float)x); }
 
+__device__ inline int wave_of() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); } // (in a scalar register)
+// a value the compiler knows nothing about: what is computed from it stays where it is, and out of registers everywhere else
+__device__ inline int opaque(int x)
+{
+    asm("" : "+v"(x));
+    return x;
+}
+
 // rows of a tile of 16 in the order in which a lane's accumulator entries of two tiles are eight consecutive ones
 __device__ inline int turned_row(int t, int i) { return t / 2 * 32 + (i >> 2) * 8 + t % 2 * 4 + (i & 3); }
 
@@ -82,46 +90,52 @@ __device__ inline int turned_row(int t, int i) { return t / 2 * 32 + (i >> 2) * 
 
 template <typename S, int DK> struct WithinLds {
     static constexpr int CH = chunk_of<S>(), PK = DK + PITCH_PAD, TILE = CH * PK * Parts<S>::IN, PM = CH + 4;
-    static constexpr size_t tiles = TILE * sizeof(bf16), squares = 2 * CH * PM * sizeof(float); // first the rows, then their products
-    static constexpr size_t bytes = (tiles > squares ? tiles : squares) + CH * (sizeof(double) + sizeof(float));
-    static constexpr int fit = (int)((160 << 10) / bytes), resident = fit > 4 ? 4 : fit;
+    static constexpr size_t tile = TILE * sizeof(bf16), square = CH * PM * sizeof(float); // first the rows of k, then the matrix
+    static constexpr size_t bytes = (tile > square ? tile : square) + CH * (sizeof(double) + sizeof(float));
+    static constexpr int fit = (int)((160 << 10) / bytes), resident = fit > 5 ? 5 : fit;
 };
 
-// M21 = (I - M22 beta2) G21 (I - beta1 M11) for the pairs of diagonal blocks of SIZE: every wave has tiles of 16 x 16
+// M21 = (I - M22 beta2) G21 (I - beta1 M11) for the pairs of diagonal blocks of SIZE, by tiles of 16 x 16, a wave each; what comes of the
+// first product waits at the pair's place above the diagonal
 template <int SIZE, int CH> __device__ inline void join_blocks(float *m, const float *beta)
 {
     constexpr int PM = CH + 4, TILES = (SIZE / 16) * (SIZE / 16), ALL = CH / (2 * SIZE) * TILES;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = wave_of(), i = lane & 15, g = lane >> 4;
     const bool mine = wave < ALL;
-    const int r0 = wave / TILES * 2 * SIZE, tr = r0 + SIZE + wave % TILES / (SIZE / 16) * 16, tc = r0 + wave % TILES % (SIZE / 16) * 16;
-#pragma unroll
-    for (int pass = 0; pass < 2; pass++) { // G21 - (G21 beta1) M11, then that less M22 (beta2 that)
+    const int r0 = wave / TILES * 2 * SIZE, tr = wave % TILES / (SIZE / 16) * 16, tc = wave % TILES % (SIZE / 16) * 16;
+    float *const below = m + (r0 + SIZE) * PM + r0, *const above = m + r0 * PM + r0 + SIZE;
+    const float *const m11 = m + r0 * PM + r0, *const m22 = m + (r0 + SIZE) * PM + r0 + SIZE, *const b1 = beta + r0, *const b2 = b1 + SIZE;
+    if (mine) { // G21 - (G21 beta1) M11
         f32x4 c = {0, 0, 0, 0};
-        if (mine) {
 #pragma unroll
-            for (int k = 0; k < SIZE; k += 4) {
-                const int x = pass == 0 ? r0 + k + g : r0 + SIZE + k + g;
-                c = __builtin_amdgcn_mfma_f32_16x16x4f32(m[(tr + i) * PM + x] * beta[x], m[x * PM + tc + i], c, 0, 0, 0);
-            }
+        for (int k = g; k < SIZE; k += 4) c = __builtin_amdgcn_mfma_f32_16x16x4f32(below[(tr + i) * PM + k] * b1[k], m11[k * PM + tc + i], c, 0, 0, 0);
 #pragma unroll
-            for (int e = 0; e < 4; e++) c[e] = m[(tr + g * 4 + e) * PM + tc + i] - c[e];
-        }
-        __syncthreads();
-        if (mine)
-#pragma unroll
-            for (int e = 0; e < 4; e++) m[(tr + g * 4 + e) * PM + tc + i] = c[e];
-        __syncthreads();
+        for (int e = 0; e < 4; e++) above[(tr + g * 4 + e) * PM + tc + i] = below[(tr + g * 4 + e) * PM + tc + i] - c[e];
     }
+    if (TILES > 1) __syncthreads(); // (one tile: the wave's own)
+    if (mine) { // and that less M22 (beta2 that)
+        f32x4 c = {0, 0, 0, 0};
+#pragma unroll
+        for (int k = g; k < SIZE; k += 4) c = __builtin_amdgcn_mfma_f32_16x16x4f32(m22[(tr + i) * PM + k] * b2[k], above[k * PM + tc + i], c, 0, 0, 0);
+#pragma unroll
+        for (int e = 0; e < 4; e++) below[(tr + g * 4 + e) * PM + tc + i] = above[(tr + g * 4 + e) * PM + tc + i] - c[e];
+    }
+    __syncthreads();
+    if (mine && SIZE == 16) // rows of 32 are written whole
+#pragma unroll
+        for (int e = 0; e < 4; e++) above[(g * 4 + e) * PM + i] = 0.0f;
 }
 
+// Bound by its waits (barriers, and the rows of a block of 16 one after another), of five workgroups a CU: 8 x 4096 tokens of 16 heads of
+// 128, bfloat16: WITHINUS us for 270 MB.
 template <typename S, int DK> __global__ __launch_bounds__(256, (WithinLds<S, DK>::resident)) void within_kernel(DeltaArgs w)
 {
     typedef WithinLds<S, DK> Lds;
     constexpr int CH = Lds::CH, PK = Lds::PK, PM = Lds::PM, IP = Parts<S>::IN, KP = CH * PK;
     extern __shared__ __align__(16) unsigned char lds[];
     bf16 *const k_lds = reinterpret_cast<bf16 *>(lds);
-    float *const kk = reinterpret_cast<float *>(lds), *const m = kk + CH * PM;
-    double *const b2 = reinterpret_cast<double *>(lds + (Lds::tiles > Lds::squares ? Lds::tiles : Lds::squares));
+    float *const m = reinterpret_cast<float *>(lds);
+    double *const b2 = reinterpret_cast<double *>(lds + (Lds::tile > Lds::square ? Lds::tile : Lds::square));
     float *const beta = reinterpret_cast<float *>(b2 + CH);
     const int qk_heads = w.heads / w.share;
     const long long block = block_of();
@@ -132,8 +146,16 @@ template <typename S, int DK> __global__ __launch_bounds__(256, (WithinLds<S, DK
     if (at.seg < 0 || at.seg >= at.nseg || at.len == 0) return;
     const long long t0 = at.seg * CH, tok = at.start + t0;
     const int n = at.len - t0 < CH ? (int)(at.len - t0) : CH;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-
+    const int lane = threadIdx.x & 63, wave = wave_of(), i = lane & 15, g = lane >> 4;
+    float ld = 0.0f, be = 0.0f; // of wave 0: the head's, a head ahead
+    auto fetch = [&](int h) {
+        if (wave == 0 && lane < n) {
+            const long long from = (tok + lane) * w.heads + h;
+            ld = w.log_decay[from];
+            be = w.beta[from];
+        }
+    };
+    fetch(kh * w.share);
     {
         TileRows<S, DK, 256, CH> kx;
         kx.fetch(reinterpret_cast<const S *>(w.k) + tok * w.k_tok + kh * w.k_head, w.k_tok, n, w.dk);
@@ -163,25 +185,12 @@ template <typename S, int DK> __global__ __launch_bounds__(256, (WithinLds<S, DK
             square[u] = product(a, b, square[u]);
         }
     }
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < TURNS; u++) {
-        if (wave + u * 4 >= TILES) continue;
-        int r, c;
-        tile_of(u, r, c);
-#pragma unroll
-        for (int e = 0; e < 4; e++) kk[(r * 16 + g * 4 + e) * PM + c * 16 + i] = square[u][e];
-    }
 
     for (int s = 0; s < w.share; s++) {
         const int h = kh * w.share + s;
         const long long record = slot * w.heads + h;
-        ChunkVec<CH> &vec = reinterpret_cast<ChunkVec<CH> *>(w.vecs)[record];
-        __syncthreads();
         if (wave == 0) {
-            const long long to = (tok + lane) * w.heads + h;
-            double sum = lane < n ? log2_of(w.log_decay[to]) : 0.0;
-            const float be = lane < n ? w.beta[to] : 0.0f;
+            double sum = lane < n ? log2_of(ld) : 0.0;
 #pragma unroll
             for (int step = 1; step < CH; step *= 2) {
                 const double x = __shfl_up(sum, step);
@@ -189,31 +198,42 @@ template <typename S, int DK> __global__ __launch_bounds__(256, (WithinLds<S, DK
             }
             const double end = __shfl(sum, CH - 1);
             if (lane < CH) {
+                const float mine = lane < n ? be : 0.0f;
+                ChunkVec<CH> &vec = reinterpret_cast<ChunkVec<CH> *>(w.vecs)[record];
                 b2[lane] = sum;
-                beta[lane] = be;
+                beta[lane] = mine;
                 vec.b2[lane] = sum;
-                vec.beta[lane] = be;
+                vec.beta[lane] = mine;
                 vec.up[lane] = lane < n ? power2(sum) : 0.0f;
                 vec.down[lane] = lane < n ? power2(end - sum) : 0.0f;
                 if (lane == 0) vec.whole = power2(end);
             }
+            if (s + 1 < w.share) fetch(h + 1);
         }
-        __syncthreads();
-        for (int u = threadIdx.x; u < CH * CH; u += 256) {
-            const int r = u / CH, c = u % CH;
-            m[r * PM + c] = c < r ? kk[r * PM + c] * power2(b2[r] - b2[c]) : 0.0f;
+        __syncthreads(); // (and the rows of k, or the last head's M, are read)
+#pragma unroll
+        for (int u = 0; u < TURNS; u++) {
+            if (wave + u * 4 >= TILES) continue;
+            int r, c;
+            tile_of(u, r, c);
+            const int col = c * 16 + i;
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const int row = r * 16 + g * 4 + e;
+                m[row * PM + col] = col < row ? square[u][e] * power2(b2[row] - b2[col]) : 0.0f;
+            }
         }
         __syncthreads();
         // rows of M one after another, in blocks of 16: M_i = G_i - sum_j G_ij beta_j M_j; a lane has a column of one block
         if (wave == 0 && lane < CH) {
             float x[16];
             float *const d = m + g * 16 * PM + g * 16;
-            const float *const be = beta + g * 16;
+            const float *const of = beta + g * 16;
 #pragma unroll
             for (int r = 0; r < 16; r++) {
                 float y = d[r * PM + i];
 #pragma unroll
-                for (int c = 0; c < r; c++) y -= d[r * PM + c] * be[c] * x[c];
+                for (int c = 0; c < r; c++) y -= d[r * PM + c] * (of[c] * x[c]);
                 x[r] = y;
             }
 #pragma unroll
@@ -222,7 +242,7 @@ template <typename S, int DK> __global__ __launch_bounds__(256, (WithinLds<S, DK
         __syncthreads();
         join_blocks<16, CH>(m, beta);
         if constexpr (CH == 64) join_blocks<32, CH>(m, beta);
-
+        else __syncthreads(); // (the places above the diagonal are zeros again)
         float *const to = w.m + record * m_floats(CH);
         for (int u = threadIdx.x; u < m_units(CH); u += 256) {
             const int row = u < 128 ? u / 4 : 32 + (u - 128) / 8, col = (u < 128 ? u % 4 : u % 8) * 8;
@@ -256,7 +276,7 @@ template <typename S, int DK, int DV, int MODE> struct DeltaLds {
     // next chunk's comes (forwards Q, V and M)
     static constexpr int Q_BUFFERS = OUT ? 1 : REV ? 2 : 0, OTHERS = OUT ? 1 : 2;
     static constexpr int FRAGS = P ? pair_frags(CH) : 0, VEC = 3 * CH + 4; // up, down, beta, whole
-    static constexpr size_t bytes = FRAGS * sizeof(Frag) + (K_TILE * (2 + Q_BUFFERS) + (V_TILE + M_TILE) * OTHERS) * sizeof(bf16) + CH * sizeof(double) + 2 * VEC * sizeof(float);
+    static constexpr size_t bytes = FRAGS * sizeof(Frag) + (K_TILE * (2 + Q_BUFFERS) + (V_TILE + M_TILE) * OTHERS) * sizeof(bf16) + (P ? CH * sizeof(double) : 0) + 2 * VEC * sizeof(float);
     static constexpr int fit = (int)((160 << 10) / bytes), resident = fit > 2 ? 2 : fit;
     static constexpr int per_simd = (resident * WAVES + 3) / 4;
 };
@@ -273,8 +293,8 @@ template <typename S, int DK, int DV, int MODE> __device__ inline void delta_loa
     bf16 *const k_lds = reinterpret_cast<bf16 *>(p_lds + Lds::FRAGS), *const q_lds = k_lds + 2 * Lds::K_TILE, *const v_lds = q_lds + Lds::Q_BUFFERS * Lds::K_TILE,
                *const m_lds = v_lds + Lds::OTHERS * Lds::V_TILE;
     double *const b2_lds = reinterpret_cast<double *>(m_lds + Lds::OTHERS * Lds::M_TILE);
-    float *const vec_lds = reinterpret_cast<float *>(b2_lds + CH);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+    float *const vec_lds = reinterpret_cast<float *>(b2_lds + (Lds::P ? CH : 0));
+    const int lane = threadIdx.x & 63, wave = wave_of(), i = lane & 15, g = lane >> 4;
 
     const S *const k = reinterpret_cast<const S *>(w.k) + at.start * w.k_tok + at.kh * w.k_head;
     const S *const q = reinterpret_cast<const S *>(w.q) + at.start * w.q_tok + at.kh * w.q_head;
@@ -305,7 +325,7 @@ template <typename S, int DK, int DV, int MODE> __device__ inline void delta_loa
         }
         const ChunkVec<CH> &cv = reinterpret_cast<const ChunkVec<CH> *>(w.vecs)[record];
         const int x = threadIdx.x & (CH - 1);
-        b2 = cv.b2[x];
+        if (Lds::P) b2 = cv.b2[x];
         vec[0] = cv.up[x];
         vec[1] = cv.down[x];
         vec[2] = cv.beta[x];
@@ -331,13 +351,13 @@ template <typename S, int DK, int DV, int MODE> __device__ inline void delta_loa
 #pragma unroll
             for (int x = 0; x < 3; x++) to[x * CH + threadIdx.x] = vec[x];
             if (threadIdx.x == 0) to[3 * CH] = whole;
-            b2_lds[threadIdx.x] = b2;
+            if (Lds::P) b2_lds[threadIdx.x] = b2;
         }
         if (Lds::Q_BUFFERS) qx.template put_any<Lds::PK>(q_lds + (Lds::Q_BUFFERS == 2 ? two : 0) * Lds::K_TILE, n, w.dk);
     };
     fetch(0);
     put(0);
-    if (at.nchunks > 1) fetch(1);
+    if (Lds::P && at.nchunks > 1) fetch(1);
     __syncthreads();
     for (int step = 0; step < at.nchunks; step++) {
         if (Lds::P) {
@@ -372,8 +392,11 @@ template <typename S, int DK, int DV, int MODE> __device__ inline void delta_loa
             }
             __syncthreads();
         }
-        if (step + 1 < at.nchunks) put(step + 1); // on its way since the last chunk
-        if (step + 2 < at.nchunks) fetch(step + 2);
+        // With P to form, a chunk's rows have been on their way since the chunk before; without, they are fetched and put within one (measured: the other
+        // way round the walks that keep states take 15 % longer, the adjoints' 16 %)
+        if (!Lds::P && step + 1 < at.nchunks) fetch(step + 1);
+        if (step + 1 < at.nchunks) put(step + 1);
+        if (Lds::P && step + 2 < at.nchunks) fetch(step + 2);
         __syncthreads();
     }
 }
@@ -387,10 +410,11 @@ template <typename S, int DK, int DV, int MODE> __device__ inline void delta_wal
     const Frag *const p_lds = reinterpret_cast<const Frag *>(lds);
     const bf16 *const k_lds = reinterpret_cast<const bf16 *>(p_lds + Lds::FRAGS), *const q_lds = k_lds + 2 * Lds::K_TILE, *const v_lds = q_lds + Lds::Q_BUFFERS * Lds::K_TILE,
                      *const m_lds = v_lds + Lds::OTHERS * Lds::V_TILE;
-    const float *const vec_lds = reinterpret_cast<const float *>(reinterpret_cast<const double *>(m_lds + Lds::OTHERS * Lds::M_TILE) + CH);
-    const int lane = threadIdx.x & 63, wave = (threadIdx.x >> 6) - LOADERS, i = lane & 15, g = lane >> 4, col0 = wave * 16, col = col0 + i;
+    const float *const vec_lds = reinterpret_cast<const float *>(reinterpret_cast<const double *>(m_lds + Lds::OTHERS * Lds::M_TILE) + (Lds::P ? CH : 0));
+    const int lane = threadIdx.x & 63, wave = wave_of() - LOADERS, i = lane & 15, g = lane >> 4, col0 = wave * 16, col = col0 + i;
     auto row_of = [&](int t, int e) { return t / 2 * 32 + g * 8 + t % 2 * 4 + e; };
     const bool here = col < at.nc;
+    const unsigned own = (unsigned)(g * 8 * w.pitch + col); // the lane's place in what is kept of a chunk
 
     // ---- the incoming state
     f32x4 R[DK / 16];
@@ -422,11 +446,11 @@ template <typename S, int DK, int DV, int MODE> __device__ inline void delta_wal
         auto eight = [&](int which, int half) { return *reinterpret_cast<const f32x8 *>(vec + which * CH + half * 32 + g * 8); };
 
         if (MODE == KEEP || MODE == BACK) {
-            float *const to = w.kept + record * (DK * (long long)w.pitch) + at.col_part + col;
+            float *const to = w.kept + record * (DK * (long long)w.pitch) + at.col_part;
 #pragma unroll
             for (int t = 0; t < DK / 16; t++)
 #pragma unroll
-                for (int e = 0; e < 4; e++) to[row_of(t, e) * w.pitch] = R[t][e];
+                for (int e = 0; e < 4; e++) (to + (t / 2 * 32 + t % 2 * 4 + e) * w.pitch)[own] = R[t][e];
         }
 
         // ---- K against the state, a lane with eight consecutive tokens of a column; Q with consecutive columns of a token
@@ -509,11 +533,11 @@ template <typename S, int DK, int DV, int MODE> __device__ inline void delta_wal
         }
         if (OUT) __syncthreads(); // P is there, and Q, V and M are read
         if (MODE == KEEP || MODE == BACK) {
-            float *const to = w.rows + record * (CH * (long long)w.pitch) + at.col_part + col;
+            float *const to = w.rows + record * (CH * (long long)w.pitch) + at.col_part;
 #pragma unroll
             for (int half = 0; half < HALVES; half++)
 #pragma unroll
-                for (int e = 0; e < 8; e++) to[(half * 32 + g * 8 + e) * w.pitch] = get(half)[e];
+                for (int e = 0; e < 8; e++) (to + (half * 32 + e) * w.pitch)[own] = get(half)[e];
         }
         // ---- U (or dV)
 #pragma unroll
@@ -639,11 +663,13 @@ __global__ __launch_bounds__((DeltaLds<S, DK, DV, MODE>::WAVES * 64), (DeltaLds<
     else if (at.nchunks > 0) delta_load<S, DK, DV, MODE>(w, at, lds);
 }
 
-// Segments' maps -> incoming states, in walking order: S <- A S + B (REV: A^T D + B).  A workgroup has 16 NW columns of one head's state.
-// grid: seqs heads (dv / 16 NW)
+// Segments' maps -> incoming states, in walking order: S <- A S + B (REV: A^T D + B).  A workgroup has DV columns of one head's state, 16 a
+// wave; the next A and B are on their way while these are multiplied, A in parts in LDS.  grid: seqs heads parts
 template <int DK, int DV, bool REV> __global__ __launch_bounds__(DV * 4) void delta_carry_kernel(DeltaArgs w)
 {
-    constexpr int NT = 1, CS = 4, KS = DK / 32;
+    constexpr int KS = DK / 32, THREADS = DV * 4, PA = DK + PITCH_PAD, PLANE = DK * PA, UNITS = DK * DK / 8, PER = (UNITS + THREADS - 1) / THREADS;
+    extern __shared__ __align__(16) unsigned char lds[];
+    bf16 *const a_lds = reinterpret_cast<bf16 *>(lds);
     const long long block = block_of();
     const int part = (int)(block % w.parts), h = (int)(block / w.parts % w.heads);
     const long long s = block / w.parts / w.heads;
@@ -651,251 +677,245 @@ template <int DK, int DV, bool REV> __global__ __launch_bounds__(DV * 4) void de
     long long start, len;
     span(w.seg, s, start, len);
     const long long nseg = len > 0 ? (len + w.seg.seg_len - 1) / w.seg.seg_len : 0, slot0 = first_slot(w.seg, s);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-    f32x4 R[DK / 16][NT];
-#pragma unroll
-    for (int t = 0; t < DK / 16; t++)
-#pragma unroll
-        for (int nt = 0; nt < NT; nt++) {
-            f32x4 x = {0, 0, 0, 0};
-            const int col = part * DV + wave * NT * 16 + (i >> 2) * CS + 4 * nt + (i & 3);
-            if (w.init)
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const int row = t / 2 * 32 + g * 8 + t % 2 * 4 + e;
-                    if (row < w.dk && col < w.dv) x[e] = w.init[((s * w.heads + h) * (long long)w.dk + row) * w.dv + col];
-                }
-            R[t][nt] = x;
-        }
-    for (long long c = 0; c < nseg; c++) {
+    const int lane = threadIdx.x & 63, wave = wave_of(), i = lane & 15, g = lane >> 4, col = part * DV + wave * 16 + i;
+    f32x4 R[DK / 16], B[DK / 16];
+    f32x8 A[PER];
+    auto total = [&](long long c) {
         const long long slot = slot0 + (REV ? nseg - 1 - c : c);
-        float *const total = w.totals + ((slot * w.heads + h) * w.parts + part) * (long long)(DK * DV) + (long long)wave * NT * (DK / 16) * 256 + lane * 4;
-        f32x4 B[DK / 16][NT];
-        const bool more = c + 1 < nseg;
+        return reinterpret_cast<f32x4 *>(w.totals + ((slot * w.heads + h) * w.parts + part) * (long long)(DK * DV) + (long long)wave * (DK / 16) * 256 + lane * 4);
+    };
+    auto fetch = [&](long long c) {
+        const long long slot = slot0 + (REV ? nseg - 1 - c : c);
+        const float *const from = w.maps + (slot * w.heads + h) * (long long)(DK * DK);
 #pragma unroll
-        for (int t = 0; t < DK / 16; t++)
+        for (int u = 0; u < PER; u++)
+            if (UNITS % THREADS == 0 || u * THREADS + threadIdx.x < UNITS) A[u] = *reinterpret_cast<const f32x8 *>(from + (u * THREADS + threadIdx.x) * 8);
+        const f32x4 *const b = total(c);
 #pragma unroll
-            for (int nt = 0; nt < NT; nt++) {
-                f32x4 *const at = reinterpret_cast<f32x4 *>(total + (nt * (DK / 16) + t) * 256);
-                if (more) B[t][nt] = *at;
-                *at = R[t][nt];
+        for (int t = 0; t < DK / 16; t++) B[t] = b[t * 64];
+    };
+#pragma unroll
+    for (int t = 0; t < DK / 16; t++) {
+        f32x4 x = {0, 0, 0, 0};
+        if (w.init)
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const int row = t / 2 * 32 + g * 8 + t % 2 * 4 + e;
+                if (row < w.dk && col < w.dv) x[e] = w.init[((s * w.heads + h) * (long long)w.dk + row) * w.dv + col];
             }
-        if (!more) break;
-        const float *const A = w.maps + (slot * w.heads + h) * (long long)(DK * DK);
+        R[t] = x;
+    }
+    if (nseg > 1) fetch(0);
+    for (long long c = 0; c < nseg; c++) {
+        f32x4 *const to = total(c);
+#pragma unroll
+        for (int t = 0; t < DK / 16; t++) to[t * 64] = R[t]; // (B is in registers)
+        if (c + 1 == nseg) break;
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < PER; u++) {
+            const int at = (u * THREADS + threadIdx.x) * 8, row = at / DK, x = at % DK;
+            if (UNITS % THREADS && at >= UNITS * 8) continue;
+            Frag parts[COMPUTED];
+            split(A[u], parts);
+#pragma unroll
+            for (int p = 0; p < COMPUTED; p++) *reinterpret_cast<Frag *>(a_lds + p * PLANE + row * PA + x) = parts[p];
+        }
+        f32x4 X[DK / 16];
+#pragma unroll
+        for (int t = 0; t < DK / 16; t++) X[t] = B[t];
+        __syncthreads();
+        if (c + 2 < nseg) fetch(c + 1);
 #pragma unroll
         for (int kk = 0; kk < KS; kk++) {
-            Frag rf[NT][COMPUTED];
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++) split(__builtin_shufflevector(R[2 * kk][nt], R[2 * kk + 1][nt], 0, 1, 2, 3, 4, 5, 6, 7), rf[nt]);
+            Frag rf[COMPUTED];
+            split(__builtin_shufflevector(R[2 * kk], R[2 * kk + 1], 0, 1, 2, 3, 4, 5, 6, 7), rf);
 #pragma unroll
             for (int t = 0; t < DK / 16; t++) {
-                f32x8 a;
-                if (REV) {
-#pragma unroll
-                    for (int e = 0; e < 8; e++) a[e] = A[(kk * 32 + g * 8 + e) * DK + turned_row(t, i)];
-                } else {
-                    a = *reinterpret_cast<const f32x8 *>(A + turned_row(t, i) * DK + kk * 32 + g * 8);
-                }
                 Frag af[COMPUTED];
-                split(a, af);
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++) B[t][nt] = product(af, rf[nt], B[t][nt]);
+                if (REV) col_frag<PA>(af, a_lds, PLANE, kk * 32, t / 2 * 32 + t % 2 * 4, 8, lane);
+                else row_frag(af, a_lds + turned_row(t, i) * PA + kk * 32 + g * 8, PLANE);
+                X[t] = product(af, rf, X[t]);
             }
         }
 #pragma unroll
-        for (int t = 0; t < DK / 16; t++)
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++) R[t][nt] = B[t][nt];
+        for (int t = 0; t < DK / 16; t++) R[t] = X[t];
     }
 }
+template <int DK> constexpr size_t carry_bytes() { return COMPUTED * DK * (DK + PITCH_PAD) * sizeof(bf16); }
 
-// ---- the gradients of q, k, the decays and beta, a chunk and head a workgroup
+// ---- the gradients of q, k, the decays and beta, a chunk and head a workgroup: four waves, each with 16 or 32 columns of q and k (of fewer than
+// 64, and some of the chunk's rows), 64 of the dv columns (a slab) at a time
 
 template <typename S, int DK, int DV> struct GradLds {
-    static constexpr int CH = chunk_of<S>(), IP = Parts<S>::IN, PK = DK + PITCH_PAD, SLAB = DV < 64 ? DV : 64, PV = SLAB + PITCH_PAD, PP = CH + PITCH_PAD;
-    static constexpr int NW = DK == 128 ? 8 : 4; // (four waves of two column tiles, two workgroups a CU, had to spill: 818 us where this takes GRADUS)
-    static constexpr int K_TILE = CH * PK * IP, V_PLANE = CH * PV, ROWS = V_PLANE * (2 * COMPUTED + 2 * IP), PAIRS_PLANE = CH * PP; // rows: U, dV in parts, dO, V
-    // first the rows along dv, a slab at a time, then those of k and q and the pairs
-    static constexpr size_t row_bytes = ROWS * sizeof(bf16), pair_bytes = (COMPUTED * PAIRS_PLANE + 2 * K_TILE) * sizeof(bf16);
+    static constexpr int CH = chunk_of<S>(), IP = Parts<S>::IN, PK = DK + PITCH_PAD, SLAB = DV, PV = SLAB + PITCH_PAD, PP = CH + PITCH_PAD;
+    static constexpr int NW = 4, THREADS = NW * 64, NT = DK == 128 ? 2 : 1, TILES = DK / 16 / NT;
+    static constexpr int TT = CH / 16, GROUPS = NW / TILES < TT ? NW / TILES : TT, EACH = TT / GROUPS; // waves of a tile share the chunk's rows, EACH 16
+    static constexpr int K_TILE = CH * PK * IP, V_PLANE = CH * PV, PAIRS = CH * PP;
+    // first the rows of U, dV (in parts) and dO, a slab at a time, then those of k and q and the pairs
+    static constexpr size_t row_bytes = V_PLANE * (2 * COMPUTED + IP) * sizeof(bf16), pair_bytes = (COMPUTED * PAIRS + 2 * K_TILE) * sizeof(bf16);
     static constexpr size_t shared_bytes = row_bytes > pair_bytes ? row_bytes : pair_bytes;
-    // + sums of q . dq by waves, betas' gradients, v . dv, and single sums
-    static constexpr size_t bytes = shared_bytes + CH * sizeof(double) + (3 * CH + NW * CH + 2 * CH + 2 * NW) * sizeof(float);
-    static constexpr int fit = (int)((160 << 10) / bytes), resident = fit > 8 / NW ? 8 / NW : fit, per_simd = resident * NW / 4;
+    // .. and b, e^b, e^(b_C - b), v . dv, q . dq by tiles, single sums
+    static constexpr size_t bytes = shared_bytes + CH * sizeof(double) + (3 * CH + TILES * CH + 2 * NW) * sizeof(float);
+    static constexpr int resident = 2 * bytes <= (160 << 10) ? 2 : 1;
 };
 
-template <typename S, int DK, int DV> __global__ __launch_bounds__((GradLds<S, DK, DV>::NW * 64), (GradLds<S, DK, DV>::per_simd)) void delta_grad_kernel(DeltaArgs w)
+template <typename S, int DK, int DV> __global__ __launch_bounds__(256, (GradLds<S, DK, DV>::resident)) void delta_grad_kernel(const DeltaArgs w)
 {
     typedef GradLds<S, DK, DV> Lds;
-    constexpr int CH = Lds::CH, IP = Lds::IP, PK = Lds::PK, PV = Lds::PV, PP = Lds::PP, SLAB = Lds::SLAB, NW = Lds::NW, NT = 1, THREADS = NW * 64, KP = CH * PK, VP = CH * PV;
-    constexpr int TT = CH / 16, HALVES = CH / 32, BLOCKS = pair_blocks(CH), CS = 4, UNITS = CH * SLAB / 8, ACTIVE = DK / 16 / NT; // waves that have columns
+    constexpr int CH = Lds::CH, IP = Lds::IP, PK = Lds::PK, PV = Lds::PV, PP = Lds::PP, SLAB = Lds::SLAB, NW = Lds::NW, THREADS = Lds::THREADS, KP = CH * PK, VP = Lds::V_PLANE;
+    constexpr int TT = Lds::TT, EACH = Lds::EACH, HALVES = CH / 32, BLOCKS = pair_blocks(CH), TILES = Lds::TILES, NT = Lds::NT, CS = NT == 2 ? 8 : 4;
     extern __shared__ __align__(16) unsigned char lds[];
-    bf16 *const u_lds = reinterpret_cast<bf16 *>(lds), *const dv_lds = u_lds + COMPUTED * VP, *const do_lds = dv_lds + COMPUTED * VP, *const v_lds = do_lds + IP * VP;
-    bf16 *const pairs = reinterpret_cast<bf16 *>(lds), *const k_lds = pairs + COMPUTED * Lds::PAIRS_PLANE, *const q_lds = k_lds + Lds::K_TILE;
+    bf16 *const u_lds = reinterpret_cast<bf16 *>(lds), *const dv_lds = u_lds + COMPUTED * VP, *const do_lds = dv_lds + COMPUTED * VP;
+    bf16 *const pairs = reinterpret_cast<bf16 *>(lds), *const k_lds = pairs + COMPUTED * Lds::PAIRS, *const q_lds = k_lds + Lds::K_TILE;
     double *const b2 = reinterpret_cast<double *>(lds + Lds::shared_bytes);
-    float *const up = reinterpret_cast<float *>(b2 + CH), *const down = up + CH, *const beta = down + CH, *const qdq = beta + CH, *const gbeta = qdq + NW * CH,
-                 *const vdv = gbeta + CH, *const sums = vdv + CH;
+    float *const up = reinterpret_cast<float *>(b2 + CH), *const down = up + CH, *const vdv_lds = down + CH, *const qdq = vdv_lds + CH, *const sums = qdq + TILES * CH;
 
-    const long long block = block_of();
-    const int h = (int)(block % w.heads), kh = h / w.share;
-    const long long slot = block / w.heads;
+    const long long block = block_of(), slot = block / w.heads;
     if (slot >= w.slots) return;
+    const int h = (int)(block - slot * w.heads), kh = h / w.share;
     const Place at = find_place(w.chunk, slot);
     if (at.seg < 0 || at.seg >= at.nseg || at.len == 0) return;
-    const long long t0 = at.seg * CH, tok = at.start + t0, record = slot * w.heads + h;
+    const long long t0 = at.seg * CH, tok = at.start + t0, record = block;
     const int n = at.len - t0 < CH ? (int)(at.len - t0) : CH;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-    const bool columns = wave < ACTIVE;
-    const int col0 = wave * NT * 16; // the wave's columns of q and k: col0 + (i / 4) CS + 4 nt + i % 4
-    auto col_of = [&](int nt) { return col0 + (i >> 2) * CS + 4 * nt + (i & 3); };
+    const int lane = threadIdx.x & 63, wave = wave_of(), i = lane & 15, g = lane >> 4;
+    const int tile = wave % TILES, first = wave / TILES * EACH, col0 = tile * NT * 16; // the wave's columns of q and k, col0 + (i / 4) CS + 4 nt + i % 4, and its rows: tiles of 16 from `first` on
+    const bool columns = wave / TILES < Lds::GROUPS;
     const ChunkVec<CH> &vec = reinterpret_cast<const ChunkVec<CH> *>(w.vecs)[record];
-    const S *const go = reinterpret_cast<const S *>(w.go) + tok * w.o_tok + h * (long long)w.dv;
-    const S *const v = reinterpret_cast<const S *>(w.v) + tok * w.v_tok + h * w.v_head;
-    if (threadIdx.x < CH) {
-        b2[threadIdx.x] = vec.b2[threadIdx.x];
-        up[threadIdx.x] = vec.up[threadIdx.x];
-        down[threadIdx.x] = vec.down[threadIdx.x];
-        beta[threadIdx.x] = vec.beta[threadIdx.x];
-        gbeta[threadIdx.x] = vdv[threadIdx.x] = 0.0f;
-    }
 
-    f32x4 dq[TT][NT], k_last[TT][NT], k_row[TT][NT];
-#pragma unroll
-    for (int t = 0; t < TT; t++)
-#pragma unroll
-        for (int nt = 0; nt < NT; nt++) dq[t][nt] = k_last[t][nt] = k_row[t][nt] = f32x4{0, 0, 0, 0};
-    // The pairs' sums, blocks of 16 rows by 32: dO_i . U_j, up to two blocks of those on and below the diagonal; dV_r . U_s and U_r . dV_s for a
-    // block on the diagonal, and one of the two off it
-    struct Dots { f32x4 a, b; };
-    const Dots zero = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-    Dots p_dots[2] = {zero, zero}, low = zero, high = zero, off = zero;
-    int p_t[2], p_ks[2];
-    bool p_mine[2];
-#pragma unroll
-    for (int u = 0; u < 2; u++) {
-        const int b = (CH == 64 ? NW == 8 ? wave - 4 : wave : wave - 2) + 4 * u;
-        p_mine[u] = b >= 0 && b < BLOCKS && (CH == 64 || u == 0);
-        p_place<false>(p_mine[u] ? b : 0, CH, p_t[u], p_ks[u]);
-    }
-    const bool z_mine = wave < TT, o_mine = CH == 64 && (NW == 4 || wave >= 4); // dG + dG^T: the diagonal's block of rows 16 wave on, and the one beside it
-    const int o_t = wave & 3;
-    float ds = 0;
-    // What comes from memory is on its way well before it is used: a slab's rows while the last one's pairs are summed, the states'
-    // entries of the next 32 columns while those of these are multiplied.  (Loaded where they are used, waits were two thirds of the kernel's time.)
-    constexpr int PER = (UNITS + THREADS - 1) / THREADS; // (whole waves have units or none)
-    TileRows<S, SLAB, THREADS, CH> gx, vx;
-    f32x8 e8[PER], w8[PER], s8[NT], d8[NT];
-    auto fetch_rows = [&](int slab) {
-        const int nc = w.dv - slab < SLAB ? w.dv - slab : SLAB;
-        gx.fetch(go + slab, w.o_tok, n, nc);
-        vx.fetch(v + slab, w.v_tok, n, nc);
-#pragma unroll
-        for (int x = 0; x < PER; x++) {
-            const int u = threadIdx.x + x * THREADS, row = u / (SLAB / 8), col = u % (SLAB / 8) * 8;
-            if (UNITS % THREADS && u >= UNITS) continue;
-            const long long from = record * (CH * (long long)w.pitch) + row * (long long)w.pitch + slab + col;
-            e8[x] = *reinterpret_cast<const f32x8 *>(w.rows_e + from);
-            w8[x] = *reinterpret_cast<const f32x8 *>(w.rows_w + from);
-        }
-    };
+    // a slab's rows: a thread has eight entries of each of PER
+    typedef TileRows<S, SLAB, THREADS, CH> Rows;
+    constexpr int PER = Rows::N;
+    Rows gx, vx;
+    const int my_row = threadIdx.x / (SLAB / 8), my_col = threadIdx.x % (SLAB / 8) * 8;
+    const bool mine = my_row < CH; // (of fewer rows than threads)
+    f32x8 s8[NT], d8[NT];
     auto fetch_states = [&](int col) {
         if (columns)
 #pragma unroll
             for (int nt = 0; nt < NT; nt++) {
-                const long long from = record * (DK * (long long)w.pitch) + col_of(nt) * (long long)w.pitch + col + g * 8;
+                const long long from = (record * DK + col0 + 4 * nt) * (long long)w.pitch + col + (unsigned)(((i >> 2) * CS + (i & 3)) * w.pitch + g * 8);
                 d8[nt] = *reinterpret_cast<const f32x8 *>(w.kept_d + from);
                 s8[nt] = *reinterpret_cast<const f32x8 *>(w.kept_s + from);
             }
     };
-    fetch_rows(0);
+    if (threadIdx.x < CH) {
+        b2[threadIdx.x] = vec.b2[threadIdx.x];
+        up[threadIdx.x] = vec.up[threadIdx.x];
+        down[threadIdx.x] = vec.down[threadIdx.x];
+    }
+
+    f32x4 dq[EACH][NT], k_last[EACH][NT], k_row[EACH][NT];
+#pragma unroll
+    for (int t = 0; t < EACH; t++)
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++) dq[t][nt] = k_last[t][nt] = k_row[t][nt] = f32x4{0, 0, 0, 0};
+    // The pairs' sums, blocks of 16 rows by 32: dO_i . U_j for those on and below the diagonal; dV_r . U_s and U_r . dV_s for a block on it, and one of the
+    // two for the block beside that
+    struct Dots { f32x4 a, b; };
+    const Dots zero = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    Dots p_dots[2] = {zero, zero}, low = zero, high = zero, off = zero;
+    const bool z_mine = wave < TT, o_mine = CH == 64;
+    int p_t[2], p_ks[2];
+    bool p_mine[2];
+#pragma unroll
+    for (int u = 0; u < 2; u++) {
+        const int b = CH == 64 ? wave + 4 * u : wave - 2;
+        p_mine[u] = b >= 0 && b < BLOCKS && (CH == 64 || u == 0);
+        p_place<false>(p_mine[u] ? b : 0, CH, p_t[u], p_ks[u]);
+    }
+    float ds = 0, gbeta[PER], vdv[PER];
+#pragma unroll
+    for (int x = 0; x < PER; x++) gbeta[x] = vdv[x] = 0.0f;
     for (int slab = 0; slab < w.dv; slab += SLAB) {
         const int nc = w.dv - slab < SLAB ? w.dv - slab : SLAB;
-        const bool more = slab + SLAB < w.dv;
-        fetch_states(slab);
-        __syncthreads();
-        gx.template put_any<PV>(do_lds, n, nc);
-        vx.template put_any<PV>(v_lds, n, nc);
-        __syncthreads();
+        gx.fetch(reinterpret_cast<const S *>(w.go) + tok * w.o_tok + h * (long long)w.dv + slab, w.o_tok, n, nc);
+        vx.fetch(reinterpret_cast<const S *>(w.v) + tok * w.v_tok + h * w.v_head + slab, w.v_tok, n, nc);
+        f32x8 e8[PER], w8[PER];
+        float be[PER];
 #pragma unroll
         for (int x = 0; x < PER; x++) {
-            const int u = threadIdx.x + x * THREADS, row = u / (SLAB / 8), col = u % (SLAB / 8) * 8;
-            if (UNITS % THREADS && u >= UNITS) continue;
-            const float be = beta[row];
-            Frag parts[COMPUTED], vf[IP];
-            split(be * e8[x], parts);
-#pragma unroll
-            for (int p = 0; p < COMPUTED; p++) *reinterpret_cast<Frag *>(u_lds + p * VP + row * PV + col) = parts[p];
-            const f32x8 dv8 = be * w8[x];
-            split(dv8, parts);
-#pragma unroll
-            for (int p = 0; p < COMPUTED; p++) *reinterpret_cast<Frag *>(dv_lds + p * VP + row * PV + col) = parts[p];
-            row_frag(vf, v_lds + row * PV + col, VP);
-            const f32x8 v8 = widen(vf);
-            float a = 0, b = 0;
-#pragma unroll
-            for (int e = 0; e < 8; e++) {
-                a += e8[x][e] * w8[x][e];
-                b += v8[e] * dv8[e];
-            }
-#pragma unroll
-            for (int y = 1; y < SLAB / 8; y *= 2) {
-                a += __shfl_xor(a, y);
-                b += __shfl_xor(b, y);
-            }
-            if (col == 0) {
-                gbeta[row] += a;
-                vdv[row] += b;
-            }
+            const int row = mine ? my_row + x * Rows::STEP : 0;
+            const long long from = record * (CH * (long long)w.pitch) + slab + (unsigned)(row * w.pitch + my_col);
+            e8[x] = *reinterpret_cast<const f32x8 *>(w.rows_e + from);
+            w8[x] = *reinterpret_cast<const f32x8 *>(w.rows_w + from);
+            be[x] = vec.beta[row];
         }
+        if (slab) __syncthreads();
+        gx.template put_any<PV>(do_lds, n, nc);
+        if (mine)
+#pragma unroll
+            for (int x = 0; x < PER; x++) {
+                bf16 *const to = u_lds + (my_row + x * Rows::STEP) * PV + my_col;
+                Frag parts[COMPUTED], vf[IP];
+                split(be[x] * e8[x], parts);
+#pragma unroll
+                for (int p = 0; p < COMPUTED; p++) *reinterpret_cast<Frag *>(to + p * VP) = parts[p];
+                const f32x8 dv8 = be[x] * w8[x];
+                split(dv8, parts);
+#pragma unroll
+                for (int p = 0; p < COMPUTED; p++) *reinterpret_cast<Frag *>(to + (COMPUTED + p) * VP) = parts[p];
+                split_in(vx.unit(x, n, nc), vf);
+                const f32x8 v8 = widen(vf);
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    gbeta[x] += e8[x][e] * w8[x][e];
+                    vdv[x] += v8[e] * dv8[e];
+                }
+            }
+        __builtin_amdgcn_sched_barrier(0);
+        fetch_states(slab); // (not earlier: registers)
         __syncthreads();
-        if (columns) {
+        const int own = opaque(i * PV + g * 8), turned = opaque(turned_row(0, i) * PV + g * 8);
+        if (columns)
 #pragma unroll
             for (int kk = 0; kk < SLAB / 32; kk++) {
                 Frag f[NT][COMPUTED];
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++) {
+                    if (first == 0)
 #pragma unroll
-                    for (int e = 0; e < 8; e++) ds += s8[nt][e] * d8[nt][e];
+                        for (int e = 0; e < 8; e++) ds += s8[nt][e] * d8[nt][e];
                     split(d8[nt], f[nt]);
                 }
-                auto rows = [&](int t) { return (t * 16 + i) * PV + kk * 32 + g * 8; };
 #pragma unroll
-                for (int t = 0; t < TT; t++) {
+                for (int t = 0; t < EACH; t++) {
                     Frag uf[COMPUTED];
-                    row_frag(uf, u_lds + rows(t), VP);
+                    row_frag(uf, u_lds + (first + t) * 16 * PV + kk * 32 + own, VP);
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++) k_last[t][nt] = product(f[nt], uf, k_last[t][nt]);
+                    if (t % 2) __builtin_amdgcn_sched_barrier(0); // (registers: no more rows read ahead)
                 }
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++) split(s8[nt], f[nt]);
                 if (kk + 1 < SLAB / 32) fetch_states(slab + kk * 32 + 32);
 #pragma unroll
-                for (int t = 0; t < TT; t++) {
+                for (int t = 0; t < EACH; t++) {
                     Frag gf[IP], vf[COMPUTED];
-                    row_frag(gf, do_lds + rows(t), VP);
-                    row_frag(vf, dv_lds + rows(t), VP);
+                    row_frag(gf, do_lds + (first + t) * 16 * PV + kk * 32 + own, VP);
+                    row_frag(vf, dv_lds + (first + t) * 16 * PV + kk * 32 + own, VP);
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++) {
                         dq[t][nt] = product(f[nt], gf, dq[t][nt]);
                         k_row[t][nt] = product(f[nt], vf, k_row[t][nt]);
                     }
+                    if (t % 2) __builtin_amdgcn_sched_barrier(0);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-        }
-        if (more) fetch_rows(slab + SLAB);
         auto dots = [&](auto lane_parts, const bf16 *lane_rows, auto other_parts, const bf16 *others, int t, int ks, Dots &to) {
 #pragma unroll
             for (int kk = 0; kk < SLAB / 32; kk++) {
                 Frag a[decltype(lane_parts)::value], b0[decltype(other_parts)::value], b1[decltype(other_parts)::value];
-                const bf16 *const other = others + turned_row(2 * ks, i) * PV + g * 8 + kk * 32;
-                row_frag(a, lane_rows + (t * 16 + i) * PV + g * 8 + kk * 32, VP);
+                const bf16 *const other = others + ks * 32 * PV + kk * 32 + turned;
+                row_frag(a, lane_rows + t * 16 * PV + kk * 32 + own, VP);
                 row_frag(b0, other, VP);
                 row_frag(b1, other + 4 * PV, VP);
                 to.a = product(b0, a, to.a);
                 to.b = product(b1, a, to.b);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            __builtin_amdgcn_sched_barrier(0);
         };
         typedef std::integral_constant<int, IP> In;
         typedef std::integral_constant<int, COMPUTED> Three;
@@ -907,152 +927,171 @@ template <typename S, int DK, int DV> __global__ __launch_bounds__((GradLds<S, D
             dots(Three(), u_lds, Three(), dv_lds, wave, wave / 2, high);
         }
         if (o_mine) {
-            if (o_t >= 2) dots(Three(), dv_lds, Three(), u_lds, o_t, 0, off);
-            else dots(Three(), u_lds, Three(), dv_lds, o_t, 1, off);
+            if (wave >= 2) dots(Three(), dv_lds, Three(), u_lds, wave, 0, off);
+            else dots(Three(), u_lds, Three(), dv_lds, wave, 1, off);
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < PER; x++) { // the rows' sums over all slabs
+#pragma unroll
+        for (int y = 1; y < SLAB / 8; y *= 2) {
+            gbeta[x] += __shfl_xor(gbeta[x], y);
+            vdv[x] += __shfl_xor(vdv[x], y);
+        }
+        const int row = my_row + x * Rows::STEP;
+        if (mine && my_col == 0) {
+            vdv_lds[row] = vdv[x];
+            if (row < n) w.g_beta[(tok + row) * w.heads + h] = gbeta[x];
         }
     }
 
-    // ---- the pairs, row by row
-    TileRows<S, DK, THREADS, CH> kx, qx;
-    kx.fetch(reinterpret_cast<const S *>(w.k) + tok * w.k_tok + kh * w.k_head, w.k_tok, n, w.dk);
-    qx.fetch(reinterpret_cast<const S *>(w.q) + tok * w.q_tok + kh * w.q_head, w.q_tok, n, w.dk);
-    auto eight = [&](const Dots &d) { return f32x8(__builtin_shufflevector(d.a, d.b, 0, 1, 2, 3, 4, 5, 6, 7)); };
-    auto write = [&](int t, int ks, const f32x8 &x) {
-        Frag parts[COMPUTED];
-        split(x, parts);
+    // ---- the pairs, row by row: dP, then - (dG + dG^T)
+    {
+        TileRows<S, DK, THREADS, CH> kx, qx;
+        kx.fetch(reinterpret_cast<const S *>(w.k) + tok * w.k_tok + kh * w.k_head, w.k_tok, n, w.dk);
+        qx.fetch(reinterpret_cast<const S *>(w.q) + tok * w.q_tok + kh * w.q_head, w.q_tok, n, w.dk);
+        __syncthreads();
+        kx.template put_any<PK>(k_lds, n, w.dk);
+        qx.template put_any<PK>(q_lds, n, w.dk);
+    }
+    {
+        const int lane = opaque(threadIdx.x & 63), i = lane & 15, g = lane >> 4, own = i * PP + g * 8, in = i * PK + g * CS; // own, in: places in a tile of pairs, and of k and q
+        auto eight = [&](const Dots &d) { return f32x8(__builtin_shufflevector(d.a, d.b, 0, 1, 2, 3, 4, 5, 6, 7)); };
+        auto write = [&](int t, int ks, const f32x8 &x) {
+            Frag parts[COMPUTED];
+            split(x, parts);
 #pragma unroll
-        for (int p = 0; p < COMPUTED; p++) *reinterpret_cast<Frag *>(pairs + p * Lds::PAIRS_PLANE + (t * 16 + i) * PP + ks * 32 + g * 8) = parts[p];
-    };
-    __syncthreads();
+            for (int p = 0; p < COMPUTED; p++) *reinterpret_cast<Frag *>(pairs + p * Lds::PAIRS + t * 16 * PP + ks * 32 + own) = parts[p];
+        };
 #pragma unroll
-    for (int u = 0; u < 2; u++)
-        if (p_mine[u]) {
-            const int row = p_t[u] * 16 + i, col = p_ks[u] * 32 + g * 8;
-            f32x8 x = eight(p_dots[u]);
+        for (int u = 0; u < 2; u++)
+            if (p_mine[u]) {
+                const int row = p_t[u] * 16 + i, col = p_ks[u] * 32 + g * 8;
+                f32x8 x = eight(p_dots[u]);
 #pragma unroll
-            for (int e = 0; e < 8; e++) x[e] = row >= col + e ? w.scale * x[e] * power2(b2[row] - b2[col + e]) : 0.0f;
-            write(p_t[u], p_ks[u], x);
-        }
-    kx.template put_any<PK>(k_lds, n, w.dk);
-    qx.template put_any<PK>(q_lds, n, w.dk);
-    __syncthreads();
-    float kdk = 0;
-    auto entries = [&](const bf16 *tile, int t, int nt) { // the lane's four entries of a row
-        f32x4 x = {0, 0, 0, 0};
-        const bf16 *const p = tile + (t * 16 + i) * PK + col0 + g * CS + 4 * nt;
-#pragma unroll
-        for (int u = IP - 1; u >= 0; u--) x += __builtin_convertvector(*reinterpret_cast<const bf16x4 *>(p + u * KP), f32x4);
-        return x;
-    };
-    auto dot = [](const f32x4 &a, const f32x4 &b) { return a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3]; };
-    if (columns) {
-#pragma unroll
-        for (int t = 0; t < TT; t++)
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++) {
-                const int row = t * 16 + i;
-                dq[t][nt] *= w.scale * up[row];
-                k_last[t][nt] *= down[row];
-                kdk += dot(entries(k_lds, t, nt), k_last[t][nt]);
-                k_row[t][nt] = k_last[t][nt] - up[row] * k_row[t][nt];
+                for (int e = 0; e < 8; e++) x[e] = row >= col + e ? w.scale * x[e] * power2(b2[row] - b2[col + e]) : 0.0f;
+                write(p_t[u], p_ks[u], x);
             }
+        __syncthreads();
+        float kdk = 0;
+        auto entries = [&](const bf16 *from, int t, int nt) { // the lane's four entries of a row
+            f32x4 x = {0, 0, 0, 0};
+            const bf16 *const p = from + (first + t) * 16 * PK + col0 + 4 * nt + in;
 #pragma unroll
-        for (int half = 0; half < HALVES; half++) {
-            Frag kf[NT][IP], qf[NT][IP];
+            for (int u = IP - 1; u >= 0; u--) x += __builtin_convertvector(*reinterpret_cast<const bf16x4 *>(p + u * KP), f32x4);
+            return x;
+        };
+        auto dot = [](const f32x4 &a, const f32x4 &b) { return a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3]; };
+        if (columns) {
 #pragma unroll
-            for (int nt = 0; nt < NT; nt++) {
-                col_frag<PK>(kf[nt], k_lds, KP, half * 32, col0 + 4 * nt, CS, lane);
-                col_frag<PK>(qf[nt], q_lds, KP, half * 32, col0 + 4 * nt, CS, lane);
-            }
+            for (int t = 0; t < EACH; t++)
 #pragma unroll
-            for (int t = 0; t < TT; t++) {
-                Frag x[COMPUTED];
-                if (p_has<false>(t, half)) {
-                    row_frag(x, pairs + (t * 16 + i) * PP + half * 32 + g * 8, Lds::PAIRS_PLANE);
-#pragma unroll
-                    for (int nt = 0; nt < NT; nt++) dq[t][nt] = product(kf[nt], x, dq[t][nt]);
+                for (int nt = 0; nt < NT; nt++) {
+                    const int row = (first + t) * 16 + i;
+                    dq[t][nt] *= w.scale * up[row];
+                    k_last[t][nt] *= down[row];
+                    kdk += dot(entries(k_lds, t, nt), k_last[t][nt]);
+                    k_row[t][nt] = k_last[t][nt] - up[row] * k_row[t][nt];
                 }
-                if (p_has<true>(t, half)) {
-                    col_frag<PP>(x, pairs, Lds::PAIRS_PLANE, half * 32, t * 16, 4, lane);
 #pragma unroll
-                    for (int nt = 0; nt < NT; nt++) k_row[t][nt] = product(qf[nt], x, k_row[t][nt]);
+            for (int half = 0; half < HALVES; half++) {
+                Frag kf[NT][IP], qf[NT][IP];
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) {
+                    col_frag<PK>(kf[nt], k_lds, KP, half * 32, col0 + 4 * nt, CS, lane);
+                    col_frag<PK>(qf[nt], q_lds, KP, half * 32, col0 + 4 * nt, CS, lane);
                 }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        }
-    }
 #pragma unroll
-    for (int x = 1; x < 64; x *= 2) {
-        kdk += __shfl_xor(kdk, x);
-        ds += __shfl_xor(ds, x);
-    }
-    if (lane == 0) {
-        sums[wave] = kdk;
-        sums[NW + wave] = ds;
-    }
-    __syncthreads();
-    if (z_mine) { // - (dG + dG^T)
-        const int row = wave * 16 + i, col = wave / 2 * 32 + g * 8;
-        f32x8 x;
+                for (int t = 0; t < EACH; t++) {
+                    Frag x[COMPUTED];
+                    if (half <= (first + t) / 2) {
+                        row_frag(x, pairs + (first + t) * 16 * PP + half * 32 + own, Lds::PAIRS);
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-            const int c = col + e;
-            const float a = e < 4 ? low.a[e & 3] : low.b[e & 3], b = e < 4 ? high.a[e & 3] : high.b[e & 3];
-            x[e] = c < row ? -a * power2(b2[row] - b2[c]) : c > row ? -b * power2(b2[c] - b2[row]) : 0.0f;
-        }
-        write(wave, wave / 2, x);
-    }
-    if (o_mine) {
-        const int row = o_t * 16 + i, col = (1 - o_t / 2) * 32 + g * 8;
-        f32x8 x = eight(off);
-#pragma unroll
-        for (int e = 0; e < 8; e++) x[e] *= -power2(o_t >= 2 ? b2[row] - b2[col + e] : b2[col + e] - b2[row]);
-        write(o_t, 1 - o_t / 2, x);
-    }
-    __syncthreads();
-    if (columns) {
-#pragma unroll
-        for (int half = 0; half < HALVES; half++) {
-            Frag kf[NT][IP];
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++) col_frag<PK>(kf[nt], k_lds, KP, half * 32, col0 + 4 * nt, CS, lane);
-#pragma unroll
-            for (int t = 0; t < TT; t++) {
-                Frag x[COMPUTED];
-                row_frag(x, pairs + (t * 16 + i) * PP + half * 32 + g * 8, Lds::PAIRS_PLANE);
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++) k_row[t][nt] = product(kf[nt], x, k_row[t][nt]);
-            }
-        }
-#pragma unroll
-        for (int t = 0; t < TT; t++) {
-            const int row = t * 16 + i, col = col0 + g * CS;
-            float a = 0;
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++) a += dot(entries(q_lds, t, nt), dq[t][nt]);
-            a += __shfl_xor(a, 16);
-            a += __shfl_xor(a, 32);
-            if (g == 0) qdq[wave * CH + row] = a;
-            if (row < n) {
-                const long long to = ((tok + row) * w.heads + h) * (long long)w.dk + col;
-                auto store = [&](void *out, const f32x4 (&x)[NT]) {
-                    float y[NT * 4];
-#pragma unroll
-                    for (int e = 0; e < NT * 4; e++) y[e] = x[e / 4][e % 4];
-                    if (col + NT * 4 <= w.dk) {
-                        if (w.grad_float) store_floats_unaligned<float, NT * 4>(reinterpret_cast<float *>(out) + to, y);
-                        else store_floats_unaligned<S, NT * 4>(reinterpret_cast<S *>(out) + to, y);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < NT * 4; e++)
-                            if (col + e < w.dk) {
-                                if (w.grad_float) reinterpret_cast<float *>(out)[to + e] = y[e];
-                                else reinterpret_cast<S *>(out)[to + e] = (S)y[e];
-                            }
+                        for (int nt = 0; nt < NT; nt++) dq[t][nt] = product(kf[nt], x, dq[t][nt]);
                     }
-                };
-                store(w.gq, dq[t]);
-                store(w.gk, k_row[t]);
+                    if (half >= (first + t) / 2) {
+                        col_frag<PP>(x, pairs, Lds::PAIRS, half * 32, (first + t) * 16, 4, lane);
+#pragma unroll
+                        for (int nt = 0; nt < NT; nt++) k_row[t][nt] = product(qf[nt], x, k_row[t][nt]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+#pragma unroll
+        for (int x = 1; x < 64; x *= 2) {
+            kdk += __shfl_xor(kdk, x);
+            ds += __shfl_xor(ds, x);
+        }
+        if (lane == 0) {
+            sums[wave] = kdk;
+            sums[NW + wave] = ds;
+        }
+        __syncthreads();
+        if (z_mine) {
+            const int row = wave * 16 + i, col = wave / 2 * 32 + g * 8;
+            const f32x8 a = eight(low), b = eight(high);
+            f32x8 x;
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                const int c = col + e;
+                x[e] = c < row ? -a[e] * power2(b2[row] - b2[c]) : c > row ? -b[e] * power2(b2[c] - b2[row]) : 0.0f;
+            }
+            write(wave, wave / 2, x);
+        }
+        if (o_mine) {
+            const int row = wave * 16 + i, col = (1 - wave / 2) * 32 + g * 8;
+            f32x8 x = eight(off);
+#pragma unroll
+            for (int e = 0; e < 8; e++) x[e] *= -power2(wave >= 2 ? b2[row] - b2[col + e] : b2[col + e] - b2[row]);
+            write(wave, 1 - wave / 2, x);
+        }
+        __syncthreads();
+        if (columns) {
+#pragma unroll
+            for (int half = 0; half < HALVES; half++) {
+                Frag kf[NT][IP];
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) col_frag<PK>(kf[nt], k_lds, KP, half * 32, col0 + 4 * nt, CS, lane);
+#pragma unroll
+                for (int t = 0; t < EACH; t++) {
+                    Frag x[COMPUTED];
+                    row_frag(x, pairs + (first + t) * 16 * PP + half * 32 + own, Lds::PAIRS);
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt++) k_row[t][nt] = product(kf[nt], x, k_row[t][nt]);
+                    if (t % 2) __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < EACH; t++) {
+                const int row = (first + t) * 16 + i, col = col0 + g * CS;
+                float a = 0;
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) a += dot(entries(q_lds, t, nt), dq[t][nt]);
+                a += __shfl_xor(a, 16);
+                a += __shfl_xor(a, 32);
+                if (g == 0) qdq[tile * CH + row] = a;
+                if (row < n) {
+                    const long long to = ((tok + row) * w.heads + h) * (long long)w.dk + col;
+                    auto store = [&](void *out, const f32x4 (&x)[NT]) {
+                        float y[NT * 4];
+#pragma unroll
+                        for (int e = 0; e < NT * 4; e++) y[e] = x[e / 4][e % 4];
+                        if (col + NT * 4 <= w.dk) {
+                            if (w.grad_float) store_floats_unaligned<float, NT * 4>(reinterpret_cast<float *>(out) + to, y);
+                            else store_floats_unaligned<S, NT * 4>(reinterpret_cast<S *>(out) + to, y);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < NT * 4; e++)
+                                if (col + e < w.dk) {
+                                    if (w.grad_float) reinterpret_cast<float *>(out)[to + e] = y[e];
+                                    else reinterpret_cast<S *>(out)[to + e] = (S)y[e];
+                                }
+                        }
+                    };
+                    store(w.gq, dq[t]);
+                    store(w.gk, k_row[t]);
+                }
             }
         }
     }
@@ -1060,12 +1099,12 @@ template <typename S, int DK, int DV> __global__ __launch_bounds__((GradLds<S, D
     if (wave == 0) { // sums towards the chunk's end; a token's decay has what all later ones and the next state make of it
         double s = 0;
         if (lane < CH) {
-            s = -(double)vdv[lane];
-            for (int x = 0; x < ACTIVE; x++) s += qdq[x * CH + lane];
+            s = -(double)vdv_lds[lane];
+            for (int x = 0; x < TILES; x++) s += qdq[x * CH + lane];
         }
         if (lane == n - 1) {
             double end = 0, d = 0;
-            for (int x = 0; x < ACTIVE; x++) {
+            for (int x = 0; x < NW; x++) {
                 end += sums[x];
                 d += sums[NW + x];
             }
@@ -1073,13 +1112,12 @@ template <typename S, int DK, int DV> __global__ __launch_bounds__((GradLds<S, D
         }
         if (lane >= n) s = 0;
 #pragma unroll
-        for (int step = 1; step < 64; step *= 2) {
-            const double x = __shfl_down(s, step);
-            if (lane + step < 64) s += x;
+        for (int x = 1; x < 64; x *= 2) {
+            const double y = __shfl_down(s, x);
+            if (lane + x < 64) s += y;
         }
         if (lane < n) {
             const long long to = (tok + lane) * w.heads + h;
-            w.g_beta[to] = gbeta[lane];
             w.g_log_decay[to] = power2(log2_of(w.log_decay[to])) == 0.0f ? 0.0f : (float)s; // what is forgotten whole has no slope
         }
     }
@@ -1150,7 +1188,7 @@ template <typename S, int FIRST, int SECOND, int THIRD> int launch_delta_walk_ty
 template <typename S> int launch_delta_gradients_typed(goom_ctx *ctx, DeltaArgs w, long long slots)
 {
     w.slots = (unsigned)slots;
-    auto run = [&](auto rows, auto cols) {
+    return with_delta(w.dk, w.dv, [&](auto rows, auto cols) {
         constexpr int DK = decltype(rows)::value, DV = decltype(cols)::value;
         typedef GradLds<S, DK, DV> Lds;
         static_assert(Lds::bytes <= (160 << 10), "LDS of a CU");
@@ -1158,11 +1196,10 @@ template <typename S> int launch_delta_gradients_typed(goom_ctx *ctx, DeltaArgs 
         static std::atomic<unsigned long long> done{0};
         if (int st = allow_lds(ctx, reinterpret_cast<const void *>(kernel), Lds::bytes, done)) return st;
         goom::prof_begin(ctx, "gated delta rule: gradients within chunks");
-        kernel<<<grid_of(slots * w.heads, Lds::NW * 64), Lds::NW * 64, Lds::bytes, ctx->stream>>>(w);
+        kernel<<<grid_of(slots * w.heads, Lds::THREADS), Lds::THREADS, Lds::bytes, ctx->stream>>>(w);
         goom::prof_end(ctx);
         return goom::check_hip(ctx, hipGetLastError(), "gated delta rule: gradients");
-    };
-    return with_delta(w.dk, w.dv, run);
+    });
 }
 
 } // namespace goom_layer

@@ -255,26 +255,30 @@ template <typename S, int D, int THREADS, int CH> struct TileRows {
     }
     // the same in one way for all sizes, where the choice would be all but free: in one kernel of the gated delta rule (floats, heads of 32) the compiler
     // (clang 22, ROCm 7.2) lost the address of parts behind the first on the way that cuts rows and moves nothing
+    // unit k as it belongs into the tile
+    __device__ inline SV unit(int k, int n, int d) const
+    {
+        const int col = col0(), move = d >= 8 && col + 8 > d ? shift(d) : 0;
+        SV v = x[k];
+        if (d & 7) { // some lanes move
+            const SV z = {};
+            if (move & 4) v = __builtin_shufflevector(v, z, 4, 5, 6, 7, 8, 9, 10, 11);
+            if (move & 2) v = __builtin_shufflevector(v, z, 2, 3, 4, 5, 6, 7, 8, 9);
+            if (move & 1) v = __builtin_shufflevector(v, z, 1, 2, 3, 4, 5, 6, 7, 8);
+        }
+        if (col >= d || row0() + k * STEP >= n) v = SV{};
+        return v;
+    }
     template <int PITCH> __device__ inline void put_any(bf16 *tile, int n, int d) const
     {
-        const int first = row0(), col = col0(), move = d >= 8 && col + 8 > d ? shift(d) : 0;
-        const bool there = col < d, any = d & 7; // any: some lanes move
 #pragma unroll
         for (int k = 0; k < N; k++) {
-            const int row = first + k * STEP;
-            SV v = x[k];
-            if (any) {
-                const SV z = {};
-                if (move & 4) v = __builtin_shufflevector(v, z, 4, 5, 6, 7, 8, 9, 10, 11);
-                if (move & 2) v = __builtin_shufflevector(v, z, 2, 3, 4, 5, 6, 7, 8, 9);
-                if (move & 1) v = __builtin_shufflevector(v, z, 1, 2, 3, 4, 5, 6, 7, 8);
-            }
-            if (!there || row >= n) v = SV{};
+            const int row = row0() + k * STEP;
             Frag p[Parts<S>::IN];
-            split_in(v, p);
+            split_in(unit(k, n, d), p);
             if (UNITS % THREADS == 0 || row < CH)
 #pragma unroll
-                for (int q = 0; q < Parts<S>::IN; q++) *reinterpret_cast<Frag *>(tile + (q * CH + row) * PITCH + col) = p[q];
+                for (int q = 0; q < Parts<S>::IN; q++) *reinterpret_cast<Frag *>(tile + (q * CH + row) * PITCH + col0()) = p[q];
         }
     }
     // CUT: rows or columns may be missing; MOVE: the rows' last units are to be moved
