@@ -559,8 +559,8 @@ typedef struct goom_delta_shape {
  * solved for all chunks at once, then every head's state walks along its sequence, which is cut into segments, chained as affine maps of
  * the state, where sequences and heads are few.  Operands are held as for goom_linear_attention (24 bits where they are computed); sums of
  * logarithms take 64 bits.  A NaN or an infinity in an input may show in all outputs of its head in its sequence.
- * workspace: goom_gated_delta_workspace_bytes(shape, offsets != NULL) bytes: some 0.6 KB a token and head in bfloat16, 0.4 KB in the
- * other types, and the segments' maps. */
+ * workspace: goom_gated_delta_workspace_bytes(shape, offsets != NULL) bytes: some 0.2 KB a token and head, and the segments'
+ * maps. */
 int goom_gated_delta(goom_ctx *ctx, const goom_delta_shape *shape, const void *q, const void *k, const void *v, const float *log_decay, const float *beta,
                      const int64_t *offsets, const float *state, void *o, float *final_state, void *workspace, size_t workspace_bytes);
 size_t goom_gated_delta_workspace_bytes(const goom_delta_shape *shape, int packed);
@@ -574,7 +574,7 @@ int goom_gated_delta_step(goom_ctx *ctx, const goom_delta_shape *shape, const vo
  * final state: grad_q, grad_k, grad_v (contiguous, of the shape's type; those of heads that share q and k are summed in float, in a fixed order),
  * grad_log_decay and grad_beta ([tokens, heads] floats; a decay of zero has no slope) and, unless NULL, grad_state (floats; not the array grad_final).
  * The forward pass's inputs are given again.  workspace: goom_gated_delta_backward_workspace_bytes(shape, offsets != NULL) bytes: two states and
- * two chunks of rows in floats for each chunk and head (in bfloat16 with heads of 128, 4 KB a token and head). */
+ * two chunks of rows in floats for each chunk and head (with heads of 128, 3.3 KB a token and head in bfloat16, 5.3 KB in the other types). */
 int goom_gated_delta_backward(goom_ctx *ctx, const goom_delta_shape *shape, const void *q, const void *k, const void *v, const float *log_decay, const float *beta,
                               const int64_t *offsets, const float *state, const void *grad_o, const float *grad_final, void *grad_q, void *grad_k, void *grad_v,
                               float *grad_log_decay, float *grad_beta, float *grad_state, void *workspace, size_t workspace_bytes);
@@ -633,7 +633,7 @@ typedef struct goom_rotary_shape {
 } goom_rotary_shape;
 
 /* q: [tokens, heads, dim], k: [tokens, kv_heads, dim]; positions: [tokens] int64 (device); frequencies: [pairs] floats (device), radians a position;
- * q_out, k_out: contiguous.  No workspace. */
+ * q_out, k_out: contiguous, apart from q and k.  No workspace. */
 int goom_rotary(goom_ctx *ctx, const goom_rotary_shape *shape, const void *q, const void *k, const int64_t *positions, const float *frequencies, void *q_out,
                 void *k_out);
 
@@ -655,7 +655,7 @@ typedef struct goom_block_norm_shape {
 } goom_block_norm_shape;
 
 /* gate, residual: NULL (a factor of 1, and 0) or [tokens, channels]; weight, bias, scale: NULL (1, 0, 1) or [channels]; mean (with GOOM_NORM_MEAN; otherwise
- * zeros), rstd: NULL or [tokens, groups] floats, what the backward passes take; h: NULL or [tokens, channels]. */
+ * zeros), rstd: NULL or [tokens, groups] floats, what the backward passes take; h: NULL or [tokens, channels].  Outputs are other arrays than the inputs. */
 int goom_norm_after(goom_ctx *ctx, const goom_block_norm_shape *shape, const void *x, const void *gate, const void *residual, const void *weight, const void *bias,
                     const void *scale, void *y, float *mean, float *rstd);
 int goom_norm_before(goom_ctx *ctx, const goom_block_norm_shape *shape, const void *x, const void *gate, const void *residual, const void *weight, const void *bias,

@@ -369,9 +369,12 @@ class Goom:
         return out
 
     def workspace(self, nbytes: int):
-        """A cached 256-byte aligned scratch tensor of at least nbytes (None for 0)."""
+        """A cached 256-byte aligned scratch tensor of at least nbytes (None for 0).  A call that is captured into a graph has one of its own, from the
+        graph's memory: the cached one is let go when a later call needs more, and replays may go side by side."""
         if nbytes == 0:
             return None, 0
+        if self.torch.cuda.is_current_stream_capturing():
+            return self.torch.empty(nbytes, dtype=self.torch.uint8, device=self.device), nbytes
         if self._ws is None or self._ws.numel() < nbytes:
             self._ws = self.torch.empty(nbytes, dtype=self.torch.uint8, device=self.device)
         return self._ws, self._ws.numel()

@@ -126,8 +126,8 @@ template <int SIZE, int CH> __device__ inline void join_blocks(float *m, const f
         for (int e = 0; e < 4; e++) above[(g * 4 + e) * PM + i] = 0.0f;
 }
 
-// Bound by its waits (barriers, and the rows of a block of 16 one after another), of five workgroups a CU: 8 x 4096 tokens of 16 heads of
-// 128, bfloat16: WITHINUS us for 270 MB.
+// Bound by its waits (barriers, and the rows of a block of 16 one after another), of five workgroups a CU (two: 96 us): 8 x 4096 tokens of 16
+// heads of 128, bfloat16: 68 us for 245 MB, 3.6 TB/s.  M goes to memory in floats, once: with M and P in parts, as operands, it was 150 us.
 template <typename S, int DK> __global__ __launch_bounds__(256, (WithinLds<S, DK>::resident)) void within_kernel(DeltaArgs w)
 {
     typedef WithinLds<S, DK> Lds;
@@ -628,6 +628,11 @@ template <typename S, int DK, int DV, int MODE> __device__ inline void delta_wal
     }
 }
 
+// Bound by a chunk's chain of products, K S, M (beta Y), P U and the state's, each of which waits for the one before and for a barrier or two: the
+// first four waves fetch the next chunk and form its P meanwhile, the others own 16 columns of the state each.  8 x 4096 tokens of 16 heads of
+// 128, bfloat16, us: forward 356 (1.8 TB/s; with P formed by the waves that multiply 497, with two loading waves 454), the states before
+// every chunk again 266, the adjoints 483.  65,536 tokens of 16 heads of 64 in 16 segments a head: maps 251, walk 259.  A kernel whose
+// registers spill is 1.6 to 2.5 times as slow: scratch loads wait behind the chunk that is on its way.
 // grid: slots heads parts, in one order; the parts of a head and segment run on one XCD (of 8, dealt round robin), whose L2 has what they share
 template <typename S, int DK, int DV, int MODE>
 __global__ __launch_bounds__((DeltaLds<S, DK, DV, MODE>::WAVES * 64), (DeltaLds<S, DK, DV, MODE>::per_simd)) void delta_walk_kernel(const DeltaArgs w)
@@ -745,7 +750,9 @@ template <int DK, int DV, bool REV> __global__ __launch_bounds__(DV * 4) void de
 template <int DK> constexpr size_t carry_bytes() { return COMPUTED * DK * (DK + PITCH_PAD) * sizeof(bf16); }
 
 // ---- the gradients of q, k, the decays and beta, a chunk and head a workgroup: four waves, each with 16 or 32 columns of q and k (of fewer than
-// 64, and some of the chunk's rows), 64 of the dv columns (a slab) at a time
+// 64, and some of the chunk's rows).  Bound by products that wait for their operands from LDS, one workgroup a CU where rows of 128 fill it: 8 x 4096
+// tokens of 16 heads of 128, bfloat16: 709 us for 2.5 GB, 3.6 TB/s, the states and adjoints 1.1 of them (eight waves of a tile each: 782; persistent, with
+// waves that load: 778; two workgroups of eight waves a CU, whose registers spill: 1360)
 
 template <typename S, int DK, int DV> struct GradLds {
     static constexpr int CH = chunk_of<S>(), IP = Parts<S>::IN, PK = DK + PITCH_PAD, SLAB = DV, PV = SLAB + PITCH_PAD, PP = CH + PITCH_PAD;
