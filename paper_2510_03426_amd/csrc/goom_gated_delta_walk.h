@@ -288,7 +288,7 @@ template <typename S, int DK, int DV, int MODE> __device__ inline void delta_loa
 {
     typedef DeltaLds<S, DK, DV, MODE> Lds;
     constexpr int THREADS = LOADERS * 64, KS = DK / 32, IP = Parts<S>::IN, CH = Lds::CH, KP = CH * Lds::PK;
-    constexpr bool REV = Lds::REV;
+    constexpr bool REV = Lds::REV, EARLY = Lds::OUT && IP > 1;
     Frag *const p_lds = reinterpret_cast<Frag *>(lds);
     bf16 *const k_lds = reinterpret_cast<bf16 *>(p_lds + Lds::FRAGS), *const q_lds = k_lds + 2 * Lds::K_TILE, *const v_lds = q_lds + Lds::Q_BUFFERS * Lds::K_TILE,
                *const m_lds = v_lds + Lds::OTHERS * Lds::V_TILE;
@@ -332,9 +332,12 @@ template <typename S, int DK, int DV, int MODE> __device__ inline void delta_loa
         whole = cv.whole;
         if (Lds::Q_BUFFERS) qx.fetch(q + t0 * w.q_tok, w.q_tok, n, w.dk);
     };
+    // Rows of two or three parts cost the loading waves most: those of k, which have two buffers, are put beside P, which two of the four
+    // waves form (30,011 packed tokens of 12 heads of 50 x 72, floats: 361 -> 345 us; in bfloat16, whose P takes all four, 362 -> 373 us)
+    auto put_k = [&](int step) { kx.template put_any<Lds::PK>(k_lds + (step & 1) * Lds::K_TILE, rows_at(chunk_at(step)), w.dk); };
     auto put = [&](int step) {
         const int n = rows_at(chunk_at(step)), two = step & 1, other = Lds::OTHERS == 2 ? two : 0;
-        kx.template put_any<Lds::PK>(k_lds + two * Lds::K_TILE, n, w.dk);
+        if (!EARLY) put_k(step);
         if (!at.map) vx.template put_any<Lds::PV>(v_lds + other * Lds::V_TILE, n, at.nc);
 #pragma unroll
         for (int u = 0; u < MU; u++) {
@@ -356,6 +359,7 @@ template <typename S, int DK, int DV, int MODE> __device__ inline void delta_loa
         if (Lds::Q_BUFFERS) qx.template put_any<Lds::PK>(q_lds + (Lds::Q_BUFFERS == 2 ? two : 0) * Lds::K_TILE, n, w.dk);
     };
     fetch(0);
+    if (EARLY) put_k(0);
     put(0);
     if (Lds::P && at.nchunks > 1) fetch(1);
     __syncthreads();
@@ -390,6 +394,7 @@ template <typename S, int DK, int DV, int MODE> __device__ inline void delta_loa
 #pragma unroll
                 for (int p = 0; p < COMPUTED; p++) p_lds[(block * COMPUTED + p) * 64 + lane] = parts[p];
             }
+            if (EARLY && step + 1 < at.nchunks) put_k(step + 1);
             __syncthreads();
         }
         // With P to form, a chunk's rows have been on their way since the chunk before; without, they are fetched and put within one (measured: the other
@@ -750,7 +755,7 @@ template <int DK, int DV, bool REV> __global__ __launch_bounds__(DV * 4) void de
 template <int DK> constexpr size_t carry_bytes() { return COMPUTED * DK * (DK + PITCH_PAD) * sizeof(bf16); }
 
 // ---- the gradients of q, k, the decays and beta, a chunk and head a workgroup: four waves, each with 16 or 32 columns of q and k (of fewer than
-// 64, and some of the chunk's rows).  Bound by products that wait for their operands from LDS, one workgroup a CU where rows of 128 fill it: 8 x 4096
+// 64, and some of the chunk's rows).  Bound by what is kept of the walks and by products that wait for their operands from LDS, two workgroups a CU: 8 x 4096
 // tokens of 16 heads of 128, bfloat16: 709 us for 2.5 GB, 3.6 TB/s, the states and adjoints 1.1 of them (eight waves of a tile each: 782; persistent, with
 // waves that load: 778; two workgroups of eight waves a CU, whose registers spill: 1360)
 
