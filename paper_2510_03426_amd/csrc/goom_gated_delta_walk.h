@@ -79,7 +79,7 @@ __device__ inline int wave_of() { return __builtin_amdgcn_readfirstlane((int)thr
 // a value the compiler knows nothing about: what is computed from it stays where it is, and out of registers everywhere else
 __device__ inline int opaque(int x)
 {
-    asm("" : "+v"(x));
+    asm volatile("" : "+v"(x));
     return x;
 }
 
@@ -755,9 +755,9 @@ template <int DK, int DV, bool REV> __global__ __launch_bounds__(DV * 4) void de
 template <int DK> constexpr size_t carry_bytes() { return COMPUTED * DK * (DK + PITCH_PAD) * sizeof(bf16); }
 
 // ---- the gradients of q, k, the decays and beta, a chunk and head a workgroup: four waves, each with 16 or 32 columns of q and k (of fewer than
-// 64, and some of the chunk's rows).  Bound by what is kept of the walks and by products that wait for their operands from LDS, two workgroups a CU: 8 x 4096
-// tokens of 16 heads of 128, bfloat16: 709 us for 2.5 GB, 3.6 TB/s, the states and adjoints 1.1 of them (eight waves of a tile each: 782; persistent, with
-// waves that load: 778; two workgroups of eight waves a CU, whose registers spill: 1360)
+// 64, and some of the chunk's rows), two workgroups a CU.  Bound by the bytes of what is kept of the walks: 8 x 4096 tokens of 16 heads of 128,
+// bfloat16: 612 us for 2.4 GB, 3.9 TB/s, the states and adjoints 1.1 of them.  (With row addresses kept from slab to slab, 27 registers spilled and 0.2 GB
+// more, 720; eight waves of a tile each 782; persistent, with waves that load, 778; two workgroups of eight waves a CU, whose registers spill, 1360.)
 
 template <typename S, int DK, int DV> struct GradLds {
     static constexpr int CH = chunk_of<S>(), IP = Parts<S>::IN, PK = DK + PITCH_PAD, SLAB = DV, PV = SLAB + PITCH_PAD, PP = CH + PITCH_PAD;
@@ -799,16 +799,16 @@ template <typename S, int DK, int DV> __global__ __launch_bounds__(256, (GradLds
     typedef TileRows<S, SLAB, THREADS, CH> Rows;
     constexpr int PER = Rows::N;
     Rows gx, vx;
-    const int my_row = threadIdx.x / (SLAB / 8), my_col = threadIdx.x % (SLAB / 8) * 8;
-    const bool mine = my_row < CH; // (of fewer rows than threads)
     f32x8 s8[NT], d8[NT];
     auto fetch_states = [&](int col) {
         if (columns)
 #pragma unroll
             for (int nt = 0; nt < NT; nt++) {
-                const long long from = (record * DK + col0 + 4 * nt) * (long long)w.pitch + col + (unsigned)(((i >> 2) * CS + (i & 3)) * w.pitch + g * 8);
-                d8[nt] = *reinterpret_cast<const f32x8 *>(w.kept_d + from);
-                s8[nt] = *reinterpret_cast<const f32x8 *>(w.kept_s + from);
+                const long long from = (record * DK + col0 + 4 * nt) * (long long)w.pitch + col;
+                const int l = opaque(threadIdx.x);
+                const unsigned mine = ((unsigned)(((l >> 2 & 3) * CS + (l & 3)) * w.pitch + (l >> 4 & 3) * 8)) * 4; // bytes
+                d8[nt] = *reinterpret_cast<const f32x8 *>(reinterpret_cast<const char *>(w.kept_d + from) + mine);
+                s8[nt] = *reinterpret_cast<const f32x8 *>(reinterpret_cast<const char *>(w.kept_s + from) + mine);
             }
     };
     if (threadIdx.x < CH) {
@@ -841,20 +841,26 @@ template <typename S, int DK, int DV> __global__ __launch_bounds__(256, (GradLds
     for (int x = 0; x < PER; x++) gbeta[x] = vdv[x] = 0.0f;
     for (int slab = 0; slab < w.dv; slab += SLAB) {
         const int nc = w.dv - slab < SLAB ? w.dv - slab : SLAB;
-        gx.fetch(reinterpret_cast<const S *>(w.go) + tok * w.o_tok + h * (long long)w.dv + slab, w.o_tok, n, nc);
-        vx.fetch(reinterpret_cast<const S *>(w.v) + tok * w.v_tok + h * w.v_head + slab, w.v_tok, n, nc);
+        long long go_tok = w.o_tok, v_tok = w.v_tok; // formed anew for each slab, with the rows' places: kept from slab to slab they were spilled
+        int rows = n;
+        asm volatile("" : "+s"(go_tok), "+s"(v_tok), "+s"(rows));
+        const int me = opaque(threadIdx.x), my_row = me / (SLAB / 8), my_col = me % (SLAB / 8) * 8;
+        const bool mine = my_row < CH; // (of fewer rows than threads)
+        gx.fetch(reinterpret_cast<const S *>(w.go) + tok * w.o_tok + h * (long long)w.dv + slab, go_tok, rows, nc);
+        vx.fetch(reinterpret_cast<const S *>(w.v) + tok * w.v_tok + h * w.v_head + slab, v_tok, rows, nc);
         f32x8 e8[PER], w8[PER];
         float be[PER];
 #pragma unroll
         for (int x = 0; x < PER; x++) {
             const int row = mine ? my_row + x * Rows::STEP : 0;
-            const long long from = record * (CH * (long long)w.pitch) + slab + (unsigned)(row * w.pitch + my_col);
-            e8[x] = *reinterpret_cast<const f32x8 *>(w.rows_e + from);
-            w8[x] = *reinterpret_cast<const f32x8 *>(w.rows_w + from);
+            const long long from = record * (CH * (long long)w.pitch) + slab;
+            const unsigned here = (unsigned)(row * w.pitch + my_col) * 4; // bytes
+            e8[x] = *reinterpret_cast<const f32x8 *>(reinterpret_cast<const char *>(w.rows_e + from) + here);
+            w8[x] = *reinterpret_cast<const f32x8 *>(reinterpret_cast<const char *>(w.rows_w + from) + here);
             be[x] = vec.beta[row];
         }
         if (slab) __syncthreads();
-        gx.template put_any<PV>(do_lds, n, nc);
+        gx.template put_any<PV>(do_lds, rows, nc);
         if (mine)
 #pragma unroll
             for (int x = 0; x < PER; x++) {
@@ -867,7 +873,7 @@ template <typename S, int DK, int DV> __global__ __launch_bounds__(256, (GradLds
                 split(dv8, parts);
 #pragma unroll
                 for (int p = 0; p < COMPUTED; p++) *reinterpret_cast<Frag *>(to + (COMPUTED + p) * VP) = parts[p];
-                split_in(vx.unit(x, n, nc), vf);
+                split_in(vx.unit(x, rows, nc), vf);
                 const f32x8 v8 = widen(vf);
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
@@ -878,7 +884,7 @@ template <typename S, int DK, int DV> __global__ __launch_bounds__(256, (GradLds
         __builtin_amdgcn_sched_barrier(0);
         fetch_states(slab); // (not earlier: registers)
         __syncthreads();
-        const int own = opaque(i * PV + g * 8), turned = opaque(turned_row(0, i) * PV + g * 8);
+        const int l = opaque(threadIdx.x & 63), own = (l & 15) * PV + (l >> 4) * 8, turned = turned_row(0, l & 15) * PV + (l >> 4) * 8;
         if (columns)
 #pragma unroll
             for (int kk = 0; kk < SLAB / 32; kk++) {
@@ -945,13 +951,14 @@ template <typename S, int DK, int DV> __global__ __launch_bounds__(256, (GradLds
     }
 #pragma unroll
     for (int x = 0; x < PER; x++) { // the rows' sums over all slabs
+        const int me = opaque(threadIdx.x), my_row = me / (SLAB / 8);
 #pragma unroll
         for (int y = 1; y < SLAB / 8; y *= 2) {
             gbeta[x] += __shfl_xor(gbeta[x], y);
             vdv[x] += __shfl_xor(vdv[x], y);
         }
         const int row = my_row + x * Rows::STEP;
-        if (mine && my_col == 0) {
+        if (my_row < CH && me % (SLAB / 8) == 0) {
             vdv_lds[row] = vdv[x];
             if (row < n) w.g_beta[(tok + row) * w.heads + h] = gbeta[x];
         }
