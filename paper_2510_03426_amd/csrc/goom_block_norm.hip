@@ -6,7 +6,7 @@
 // Bound by the bytes of their tensors, each read and written once: a team of lanes holds one token's group in registers, 8 entries a lane
 // (16 for the longest), and statistics are taken about the mean itself.  A team keeps its group from token to token, so parameters are
 // loaded once and their gradients are summed in registers: one partial sum for each workgroup and channel, added up in a fixed order by a
-// second launch.  32,768 tokens of 2048 channels, bfloat16, both ways: 302 us, 4.4 TB/s.
+// second launch.  32,768 tokens of 2048 channels, bfloat16, both ways: 280 us, 4.8 TB/s.
 #include <cmath>
 
 #include "goom_activation.h"
@@ -66,7 +66,24 @@ template <typename S, int V, int J, int MOST, bool BEFORE, bool BACK> __global__
     const float count = (float)a.cg;
     const bool gated = a.gate, scaled = a.scale;
     int chan[J], skip[J];
-    float w[J][V], b[J][V], sc[J][V], sw[J][V], sb[J][V], ss[J][V];
+    // What 128 registers (1024 lanes) do not hold spills: with 16 entries a lane the parameters, read from L2 again for each token instead, and the next
+    // token's entries, which are then not asked for ahead; with 8 floats the parameters on the way back.  4096 tokens of 16,384 channels, both held and
+    // not, us: backwards 617 and 391 (bfloat16), 1353 and 611 (float), forwards in float 341 and 221; forwards in halves they fit: 110 and 125; 8192
+    // tokens of 8192, backwards: float 578 and 439, bfloat16 181 and 201.
+    constexpr bool WIDE = J * V == 16, SMALL = sizeof(S) == 2, AHEAD = !WIDE || (SMALL && !BACK), HOLD = WIDE ? SMALL && !BACK : SMALL || !(BACK && MOST == 1024);
+    float w[HOLD ? J : 1][V], b[HOLD ? J : 1][V], sc[HOLD ? J : 1][V], sw[J][V], sb[J][V], ss[J][V];
+    auto read_params = [&](int j, int at) {
+        params<V>(a.weight, a.type_w, at, 1.0f, w[j]);
+        params<V>(a.bias, a.type_w, at, 0.0f, b[j]);
+        params<V>(a.scale, a.type_w, at, 1.0f, sc[j]);
+    };
+    auto again = [&](int j) { // the parameters' place
+        if (HOLD) return j;
+        int at = chan[j] >= 0 ? chan[j] : 0;
+        asm volatile("" : "+v"(at)); // (read here, and kept no longer than needed)
+        read_params(0, at);
+        return 0;
+    };
 #pragma unroll
     for (int j = 0; j < J; j++) {
         const int u = lane + j * a.team;
@@ -74,9 +91,7 @@ template <typename S, int V, int J, int MOST, bool BEFORE, bool BACK> __global__
         skip[j] = end ? units * V - a.cg : 0;
         chan[j] = live && u < units ? group * a.cg + (end ? a.cg - V : u * V) : -1;
         const int c = chan[j] >= 0 ? chan[j] : 0;
-        params<V>(a.weight, a.type_w, c, 1.0f, w[j]);
-        params<V>(a.bias, a.type_w, c, 0.0f, b[j]);
-        params<V>(a.scale, a.type_w, c, 1.0f, sc[j]);
+        if (HOLD) read_params(j, c);
 #pragma unroll
         for (int e = 0; e < V; e++) sw[j][e] = sb[j][e] = ss[j][e] = 0.0f;
     }
@@ -97,11 +112,12 @@ template <typename S, int V, int J, int MOST, bool BEFORE, bool BACK> __global__
             if (BACK) ng[j] = load_unaligned<S, V>(reinterpret_cast<const S *>(a.gy) + at);
         }
     };
-    fetch((long long)blockIdx.x * a.ipw + ti);
+    if (AHEAD) fetch((long long)blockIdx.x * a.ipw + ti);
     for (long long token0 = (long long)blockIdx.x * a.ipw; token0 < a.tokens; token0 += (long long)gridDim.x * a.ipw) {
         const long long token = token0 + ti;
         const bool here = live && token < a.tokens; // (the same for a whole team; other lanes go along for the sums)
         const long long base = token * a.channels, stat = token * a.groups + group;
+        if (!AHEAD) fetch(token);
         float x[J][V], z[J][V], r[J][V], t[J][V], g[J][V];
 #pragma unroll
         for (int j = 0; j < J; j++)
@@ -114,15 +130,16 @@ template <typename S, int V, int J, int MOST, bool BEFORE, bool BACK> __global__
                 t[j][e] = BACK && BEFORE && there ? (float)nh[j][e] : 0.0f;
                 g[j][e] = BACK && there ? (float)ng[j][e] : 0.0f;
             }
-        if (token0 + (long long)gridDim.x * a.ipw < a.tokens) fetch(token + (long long)gridDim.x * a.ipw);
+        if (AHEAD && token0 + (long long)gridDim.x * a.ipw < a.tokens) fetch(token + (long long)gridDim.x * a.ipw);
         if (!BACK) {
             // t: what is normalised.  The stream is normalised as it is stored, so that the way back finds the same
             float sum = 0.0f, none = 0.0f;
 #pragma unroll
             for (int j = 0; j < J; j++) {
                 if (BEFORE) {
+                    const int p = again(j);
 #pragma unroll
-                    for (int e = 0; e < V; e++) t[j][e] = (float)(S)(r[j][e] + sc[j][e] * x[j][e] * (gated ? activate(z[j][e], a.act) : 1.0f));
+                    for (int e = 0; e < V; e++) t[j][e] = (float)(S)(r[j][e] + sc[p][e] * x[j][e] * (gated ? activate(z[j][e], a.act) : 1.0f));
                     if (a.h_out && here && chan[j] >= 0) store_floats_unaligned<S, V>(reinterpret_cast<S *>(a.h_out) + base + chan[j], t[j]);
                 } else {
 #pragma unroll
@@ -153,10 +170,11 @@ template <typename S, int V, int J, int MOST, bool BEFORE, bool BACK> __global__
 #pragma unroll
             for (int j = 0; j < J; j++)
                 if (here && chan[j] >= 0) {
+                    const int p = again(j);
 #pragma unroll
                     for (int e = 0; e < V; e++) {
-                        const float n = t[j][e] * rstd * w[j][e] + b[j][e];
-                        t[j][e] = BEFORE ? n : r[j][e] + sc[j][e] * n * (gated ? activate(z[j][e], a.act) : 1.0f);
+                        const float n = t[j][e] * rstd * w[p][e] + b[p][e];
+                        t[j][e] = BEFORE ? n : r[j][e] + sc[p][e] * n * (gated ? activate(z[j][e], a.act) : 1.0f);
                     }
                     store_floats_unaligned<S, V>(reinterpret_cast<S *>(a.y) + base + chan[j], t[j]);
                 }
@@ -167,19 +185,20 @@ template <typename S, int V, int J, int MOST, bool BEFORE, bool BACK> __global__
             for (int j = 0; j < J; j++)
                 if (here && chan[j] >= 0) {
                     float slope[V];
+                    const int p = again(j);
 #pragma unroll
                     for (int e = 0; e < V; e++) {
                         const float xhat = ((BEFORE ? t[j][e] : x[j][e]) - mean) * rstd;
                         float dn = g[j][e]; // the gradient of xhat weight + bias
                         if (!BEFORE) {
-                            const float n = xhat * w[j][e] + b[j][e], act = gated ? activate(z[j][e], a.act) : 1.0f;
-                            if (gated) slope[e] = dn * sc[j][e] * n * activate_slope(z[j][e], a.act);
+                            const float n = xhat * w[p][e] + b[p][e], act = gated ? activate(z[j][e], a.act) : 1.0f;
+                            if (gated) slope[e] = dn * sc[p][e] * n * activate_slope(z[j][e], a.act);
                             ss[j][e] += dn * n * act;
-                            dn *= sc[j][e] * act;
+                            dn *= sc[p][e] * act;
                         }
                         sw[j][e] += dn * xhat;
                         sb[j][e] += dn;
-                        dn *= w[j][e];
+                        dn *= w[p][e];
                         m1 += e >= skip[j] ? dn : 0.0f;
                         m2 += e >= skip[j] ? dn * xhat : 0.0f;
                         t[j][e] = xhat;
@@ -196,13 +215,14 @@ template <typename S, int V, int J, int MOST, bool BEFORE, bool BACK> __global__
 #pragma unroll
                     for (int e = 0; e < V; e++) g[j][e] = rstd * (g[j][e] - m1 - t[j][e] * m2);
                     if (BEFORE) {
+                        const int p = again(j);
 #pragma unroll
                         for (int e = 0; e < V; e++) {
                             const float total = g[j][e] + r[j][e], act = gated ? activate(z[j][e], a.act) : 1.0f;
                             r[j][e] = total;
                             ss[j][e] += total * x[j][e] * act;
-                            g[j][e] = total * sc[j][e] * act;
-                            if (gated) z[j][e] = total * sc[j][e] * x[j][e] * activate_slope(z[j][e], a.act);
+                            g[j][e] = total * sc[p][e] * act;
+                            if (gated) z[j][e] = total * sc[p][e] * x[j][e] * activate_slope(z[j][e], a.act);
                         }
                         store_floats_unaligned<S, V>(reinterpret_cast<S *>(a.gres) + base + chan[j], r[j]);
                         if (gated) store_floats_unaligned<S, V>(reinterpret_cast<S *>(a.ggate) + base + chan[j], z[j]);
@@ -250,18 +270,17 @@ __global__ __launch_bounds__(256) void block_norm_sums_kernel(const float *parti
 {
     __shared__ float part[8][32];
     const int col = blockIdx.x * 32 + (threadIdx.x & 31), row0 = threadIdx.x >> 5, all = 3 * channels;
+    const int which = col / channels, c = col % channels;
+    void *const to = which == 0 ? gw : which == 1 ? gb : which == 2 ? gs : nullptr;
     float sum = 0.0f;
-    if (col < all) {
+    if (to) {
 #pragma unroll 8
         for (int row = row0; row < n; row += 8) sum += partial[(long long)row * all + col];
     }
     part[row0][threadIdx.x & 31] = sum;
     __syncthreads();
-    if (row0 == 0 && col < all) {
+    if (row0 == 0 && to) {
         for (int k = 1; k < 8; k++) sum += part[k][threadIdx.x];
-        const int which = col / channels, c = col % channels;
-        void *const to = which == 0 ? gw : which == 1 ? gb : gs;
-        if (!to) return;
         if (type == GOOM_REAL_F32) reinterpret_cast<float *>(to)[c] = sum;
         else if (type == GOOM_REAL_BF16) reinterpret_cast<bf16 *>(to)[c] = (bf16)sum;
         else reinterpret_cast<f16 *>(to)[c] = (f16)sum;
@@ -272,7 +291,7 @@ __global__ __launch_bounds__(256) void block_norm_sums_kernel(const float *parti
 
 constexpr int MOST_CHANNELS = 16384; // of a group: 1024 lanes of 16
 
-struct BlockNormPlan { int v, j, threads, team, gpw, ipw; long long blocks, parts; size_t bytes; };
+struct BlockNormPlan { int v, j, threads, team, gpw, ipw; bool many; long long blocks, parts; size_t bytes; };
 
 static BlockNormPlan plan_norm(const goom_block_norm_shape &sh, bool back)
 {
@@ -289,12 +308,18 @@ static BlockNormPlan plan_norm(const goom_block_norm_shape &sh, bool back)
     while (p.team < lanes && p.team < 64) p.team *= 2;
     if (lanes > 64) p.team = (lanes + 63) / 64 * 64;
     p.threads = p.team > 64 ? p.team : 256;
+    // the kernel of 128 registers also where two workgroups of that one share a CU and one of the other: 16,384 tokens of 4096 channels, bfloat16,
+    // before a block, backwards 202 and 163 us
+    p.many = p.threads > (back && sh.type != GOOM_REAL_F32 ? 384 : 512);
     const int teams = p.threads / p.team;
     p.gpw = sh.groups < teams ? sh.groups : teams;
     p.ipw = teams / p.gpw;
     p.parts = (sh.groups + p.gpw - 1) / p.gpw;
-    // workgroups: as many as the chip holds and some more; backwards each leaves a row of partial sums
-    const long long want = (sh.tokens + p.ipw - 1) / p.ipw, most_blocks = (back ? 2048 : 4096) * 256ll / p.threads / p.parts;
+    // Workgroups: forwards as many as the chip holds several times over.  Backwards each leaves a row of partial sums, and as many as it holds at
+    // once, by the waves that the kernel's registers leave room for on a CU: 32,768 tokens of 2048 channels, bfloat16 (8 entries a lane, 12 waves): 768
+    // of 256 lanes 181 us with the sums, 512 205, 1024 230, 2048 218; 6000 of 1712, float (4 entries, 16 waves): 1024 58 us, 768 65, 2048 65.
+    const int entries = p.v * p.j, waves = p.many ? 16 : entries >= 8 ? 12 : entries == 4 ? 16 : 32, a_cu = waves * 64 / p.threads;
+    const long long want = (sh.tokens + p.ipw - 1) / p.ipw, most_blocks = (back ? 256ll * (a_cu > 0 ? a_cu : 1) : 4096 * 256ll / p.threads) / p.parts;
     p.blocks = want < most_blocks ? want : most_blocks;
     if (p.blocks < 1) p.blocks = 1;
     p.bytes = back ? goom::align_up((size_t)p.blocks * 3 * sh.channels * 4, 256) : 0;
@@ -344,7 +369,7 @@ template <bool BEFORE, bool BACK> static int launch_norm(goom_ctx *ctx, const go
         typedef std::integral_constant<int, 1024> Many; // lanes: half the registers
         if (p.v == W) {
             if (p.j == 16 / W) return run(Wide(), std::integral_constant<int, 16 / W>(), Many());
-            if (p.threads > 512) return run(Wide(), std::integral_constant<int, 8 / W>(), Many());
+            if (p.many) return run(Wide(), std::integral_constant<int, 8 / W>(), Many());
             if (p.j == 1) return run(Wide(), One(), Few());
             return run(Wide(), std::integral_constant<int, 8 / W>(), Few());
         }
