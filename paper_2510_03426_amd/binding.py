@@ -836,7 +836,7 @@ class Goom:
         shape, pq, pk, pv = self._delta(q, k, v, log_decay, beta, None, scale, step=True)
         ps = self._state(state, shape, "state")
         pn = ps if out_state is None else self._state(out_state, shape, "out_state")
-        o = self.torch.empty(v.shape, dtype=v.dtype, device=v.device)
+        o = self.torch.empty_like(v, memory_format=self.torch.contiguous_format)
         self._check(self.lib.goom_gated_delta_step(self._ctx, C.byref(shape), pq, pk, pv, _at(log_decay), _at(beta), ps, o.data_ptr(), pn))
         return o
 
@@ -919,8 +919,8 @@ class Goom:
                 raise ValueError("k: [..., kv_heads, dim] of q's leading shape and type")
             kv_heads = k.shape[-2]
             pk, k_token, k_head = _rows(k, "k")
-            out_k = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-        out_q = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out_k = torch.empty_like(k, memory_format=torch.contiguous_format)
+        out_q = torch.empty_like(q, memory_format=torch.contiguous_format)
         shape = RotaryShape(math.prod(lead), heads, kv_heads, dim, frequencies.numel(), code, flags | (ROTARY_INTERLEAVED if interleaved else 0), scale, q_token, q_head, k_token, k_head)
         self._check(self.lib.goom_rotary(self._ctx, C.byref(shape), pq, pk, _at(positions), _at(frequencies), out_q.data_ptr(), _at(out_k)))
         return out_q, out_k
@@ -940,19 +940,20 @@ class Goom:
         act = ACTIVATIONS.get(activation)
         if x.dim() < 1 or act is None or kind not in NORM_KINDS:
             raise ValueError("x: [..., channels]; kind: one of " + ", ".join(NORM_KINDS) + "; activation: one of " + ", ".join(ACTIVATIONS))
-        channels, code, first = x.shape[-1], REAL_F32, None
-        for p in (weight, bias, scale):
-            if p is None:
-                continue
-            if tuple(p.shape) != (channels,):
-                raise ValueError("weight, bias and scale: [channels]")
-            if first is not None and p.dtype != first.dtype:
-                raise TypeError("weight, bias and scale have one type")
-            first, code = p, _real_code(p)
+        sh, dtype = x.shape, x.dtype
+        channels, code, first = sh[-1], REAL_F32, self.torch.float32
+        given = [p for p in (weight, bias, scale) if p is not None]
+        if given:
+            first, code = given[0].dtype, _real_code(given[0])
+            for p in given:
+                if p.dim() != 1 or p.shape[0] != channels:
+                    raise ValueError("weight, bias and scale: [channels]")
+                if p.dtype != first:
+                    raise TypeError("weight, bias and scale have one type")
         for t in (gate, residual):
-            if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
+            if t is not None and (t.shape != sh or t.dtype != dtype):
                 raise ValueError("gate and residual: of x's shape and type")
-        return BlockNormShape(math.prod(x.shape[:-1]), channels, groups, _real_code(x), code, act, NORM_KINDS[kind], eps), self.torch.float32 if first is None else first.dtype
+        return BlockNormShape(x.numel() // channels if channels else 0, channels, groups, _real_code(x), code, act, NORM_KINDS[kind], eps), first
 
     def _stats(self, x, groups, kind, want):
         if not want:
