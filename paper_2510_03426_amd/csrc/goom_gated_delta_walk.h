@@ -121,9 +121,12 @@ template <int SIZE, int CH> __device__ inline void join_blocks(float *m, const f
         for (int e = 0; e < 4; e++) below[(tr + g * 4 + e) * PM + tc + i] = above[(tr + g * 4 + e) * PM + tc + i] - c[e];
     }
     __syncthreads();
-    if (mine && SIZE == 16) // rows of 32 are written whole
+    if (SIZE == 16) { // rows of 32 are written whole, and read whole by the next join: what waited above the diagonal is zero again
+        if (mine)
 #pragma unroll
-        for (int e = 0; e < 4; e++) above[(g * 4 + e) * PM + i] = 0.0f;
+            for (int e = 0; e < 4; e++) above[(g * 4 + e) * PM + i] = 0.0f;
+        __syncthreads();
+    }
 }
 
 // Bound by its waits (barriers, and the rows of a block of 16 one after another), of five workgroups a CU (two: 96 us): 8 x 4096 tokens of 16
@@ -242,7 +245,6 @@ template <typename S, int DK> __global__ __launch_bounds__(256, (WithinLds<S, DK
         __syncthreads();
         join_blocks<16, CH>(m, beta);
         if constexpr (CH == 64) join_blocks<32, CH>(m, beta);
-        else __syncthreads(); // (the places above the diagonal are zeros again)
         float *const to = w.m + record * m_floats(CH);
         for (int u = threadIdx.x; u < m_units(CH); u += 256) {
             const int row = u < 128 ? u / 4 : 32 + (u - 128) / 8, col = (u < 128 ? u % 4 : u % 8) * 8;

@@ -127,3 +127,25 @@ def test_one_tensor_as_two_inputs(g):
     at, f = torch.arange(70, device="cuda").repeat(2, 1), torch.rand(16, device="cuda")
     s, t = g.rotary(q, q, at, f)
     assert torch.equal(s, t)
+
+
+@pytest.mark.parametrize("seqs", [600, 5000])
+def test_the_order_of_sequences_changes_nothing(g, seqs):
+    """Few long sequences among many short ones, then all of them the other way round: the same bits for each."""
+    import torch
+    lengths = torch.randint(0, 40, (seqs,), generator=torch.Generator().manual_seed(seqs))
+    lengths[7], lengths[seqs // 2], lengths[-1] = 70000, 5000, 66000
+    n = int(lengths.sum())
+    ends = torch.cat([lengths.new_zeros(1), lengths.cumsum(0)])
+    turned = torch.cat([torch.arange(int(ends[s]), int(ends[s + 1])) for s in range(seqs - 1, -1, -1)]).cuda()
+    off, off2 = ends.cuda(), torch.cat([lengths.new_zeros(1), lengths.flip(0).cumsum(0)]).cuda()
+    *x, go = _delta(n, 1, 1, 16, torch.bfloat16)
+    state = torch.randn(seqs, 1, 16, 16, device="cuda")
+    o, last = g.gated_delta(*x, state=state, offsets=off, want_state=True)
+    grads = g.gated_delta_backward(*x, go, state=state, offsets=off)
+    y, go2, state2 = [t[turned] for t in x], go[turned], state.flip(0).contiguous()
+    o2, last2 = g.gated_delta(*y, state=state2, offsets=off2, want_state=True)
+    grads2 = g.gated_delta_backward(*y, go2, state=state2, offsets=off2)
+    assert torch.equal(o[turned], o2) and torch.equal(last.flip(0), last2) and torch.equal(grads[5].flip(0), grads2[5])
+    assert all(torch.equal(a[turned], b) for a, b in zip(grads[:5], grads2[:5]))
+    assert all(bool(t.float().isfinite().all()) for t in (o, last) + grads)
