@@ -557,7 +557,7 @@ typedef struct goom_delta_shape {
  * o: [tokens, heads, dv], contiguous; offsets, state, final_state: as for goom_linear_attention (final_state may be the array `state`;
  * outputs of tokens that no sequence has are not written).  Chunks of 64 tokens (32 for halves and floats): what lies within them is
  * solved for all chunks at once, then every head's state walks along its sequence, which is cut into segments, chained as affine maps of
- * the state, where sequences and heads are few.  Operands are held as for goom_linear_attention (24 bits where they are computed); sums of
+ * the state, where sequences and heads are few.  (Where they are many, packed sequences start longest first.)  Operands are held as for goom_linear_attention (24 bits where they are computed); sums of
  * logarithms take 64 bits.  A NaN or an infinity in an input may show in all outputs of its head in its sequence.
  * workspace: goom_gated_delta_workspace_bytes(shape, offsets != NULL) bytes: some 0.2 KB a token and head, and the segments'
  * maps. */

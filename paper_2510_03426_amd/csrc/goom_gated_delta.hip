@@ -138,7 +138,7 @@ struct DeltaPlan {
     Pieces chunk, seg;
     bool maps;      // sequences are cut into segments
     int dk, cols, pitch, parts, map_parts, ch;
-    size_t m, vecs, totals, map, state, rows, sum, bytes; // state, rows, sum: two each
+    size_t m, vecs, totals, map, order, state, rows, sum, bytes; // state, rows, sum: two each
 };
 
 static DeltaPlan plan_of(const goom_delta_shape &sh, bool packed, bool backward)
@@ -165,10 +165,14 @@ static DeltaPlan plan_of(const goom_delta_shape &sh, bool packed, bool backward)
     p.vecs = goom::align_up(records * (p.ch == 64 ? sizeof(ChunkVec<64>) : sizeof(ChunkVec<32>)), 256);
     p.totals = p.maps ? goom::align_up(cuts * p.dk * p.pitch * 4, 256) : 0;
     p.map = p.maps ? goom::align_up(cuts * p.dk * p.dk * 4, 256) : 0;
+    // Packed sequences, whole, of more walks than CUs: the longest first (us, in any order and so: 37 sequences of up to 2198 tokens, 888 walks, floats
+    // 347 and 260, 444 walks 267 and 250; 30 of up to 3914, 960 walks, bfloat16 587 and 489; the ordering itself, beside the chunks' matrices, up to 6).  Of
+    // very many none is long beside all the others.
+    p.order = packed && !p.maps && sh.seqs > 1 && sh.seqs <= 4096 && walks > 256 ? goom::align_up((size_t)sh.seqs * sizeof(int), 256) : 0;
     p.state = backward ? goom::align_up(records * p.dk * p.pitch * 4, 256) : 0;
     p.rows = backward ? goom::align_up(records * p.ch * p.pitch * 4, 256) : 0;
     p.sum = backward && sh.heads != sh.qk_heads ? goom::align_up((size_t)sh.tokens * sh.heads * sh.dk * 4, 256) : 0;
-    p.bytes = p.m + p.vecs + p.totals + p.map + 2 * (p.state + p.rows + p.sum);
+    p.bytes = p.m + p.vecs + p.totals + p.map + p.order + 2 * (p.state + p.rows + p.sum);
     return p;
 }
 
@@ -304,6 +308,7 @@ int goom_gated_delta(goom_ctx *ctx, const goom_delta_shape *shape, const void *q
     w.vecs = ws + p.m;
     w.totals = p.maps ? reinterpret_cast<float *>(ws + p.m + p.vecs) : nullptr;
     w.maps = reinterpret_cast<float *>(ws + p.m + p.vecs + p.totals);
+    w.order = p.order ? reinterpret_cast<int *>(ws + p.m + p.vecs + p.totals + p.map) : nullptr;
     w.init = state;
     w.fin = final_state;
     w.o = o;
@@ -371,6 +376,7 @@ int goom_gated_delta_backward(goom_ctx *ctx, const goom_delta_shape *shape, cons
     w.vecs = take(p.vecs);
     w.totals = take(p.totals);
     w.maps = take(p.map);
+    w.order = reinterpret_cast<int *>(take(p.order));
     float *const kept_s = take(p.state), *const kept_d = take(p.state), *const rows_e = take(p.rows), *const rows_w = take(p.rows);
     float *const sum_q = take(p.sum), *const sum_k = take(p.sum);
     w.back = 1;

@@ -65,6 +65,7 @@ struct DeltaArgs {
     unsigned slots;
     int back, grad_float;    // back: of a backward pass
     float scale;
+    int *order;              // NULL, or the sequences in the order in which their walks start
 };
 
 // log2 of a decay; below 2^-160, which is zero as a float whatever it is divided by, finite (a NaN stays one)
@@ -129,6 +130,43 @@ template <int SIZE, int CH> __device__ inline void join_blocks(float *m, const f
     }
 }
 
+// The sequences, longest first: walks take as long as their sequences, and a long one that starts last is waited for.  One workgroup, by counting
+// chunks (1023 and more are one number); among equals the order is any, which changes nothing but when a walk starts.
+__device__ inline void order_sequences(const DeltaArgs &w, unsigned *count)
+{
+    constexpr int MOST = 1024;
+    __shared__ unsigned wave_sum[4];
+    auto place = [&](long long s) {
+        long long start, len;
+        span(w.seg, s, start, len);
+        const long long chunks = (len + w.chunk.seg_len - 1) / w.chunk.seg_len;
+        return MOST - 1 - (int)(chunks < MOST - 1 ? chunks : MOST - 1);
+    };
+    for (int x = threadIdx.x; x < MOST; x += 256) count[x] = 0;
+    __syncthreads();
+    for (long long s = threadIdx.x; s < w.seg.seqs; s += 256) atomicAdd(&count[place(s)], 1u);
+    __syncthreads();
+    unsigned own[4], sum = 0; // four neighbouring counts, then sums of all before
+#pragma unroll
+    for (int x = 0; x < 4; x++) {
+        own[x] = sum;
+        sum += count[threadIdx.x * 4 + x];
+    }
+    unsigned before = sum;
+    for (int x = 1; x < 64; x *= 2) {
+        const unsigned y = __shfl_up(before, x);
+        if ((int)(threadIdx.x & 63) >= x) before += y;
+    }
+    if ((threadIdx.x & 63) == 63) wave_sum[threadIdx.x >> 6] = before;
+    __syncthreads();
+    before -= sum;
+    for (int x = 0; x < (int)(threadIdx.x >> 6); x++) before += wave_sum[x];
+#pragma unroll
+    for (int x = 0; x < 4; x++) count[threadIdx.x * 4 + x] = before + own[x];
+    __syncthreads();
+    for (long long s = threadIdx.x; s < w.seg.seqs; s += 256) w.order[atomicAdd(&count[place(s)], 1u)] = (int)s;
+}
+
 // Bound by its waits (barriers, and the rows of a block of 16 one after another), of five workgroups a CU (two: 96 us): 8 x 4096 tokens of 16
 // heads of 128, bfloat16: 68 us for 245 MB, 3.6 TB/s.  M goes to memory in floats, once: with M and P in parts, as operands, it was 150 us.
 template <typename S, int DK> __global__ __launch_bounds__(256, (WithinLds<S, DK>::resident)) void within_kernel(DeltaArgs w)
@@ -144,7 +182,10 @@ template <typename S, int DK> __global__ __launch_bounds__(256, (WithinLds<S, DK
     const long long block = block_of();
     const int kh = block % qk_heads;
     const long long slot = block / qk_heads;
-    if (slot >= w.slots) return;
+    if (slot >= w.slots) { // the last workgroup's
+        if (w.order && block == (long long)w.slots * qk_heads) order_sequences(w, reinterpret_cast<unsigned *>(lds));
+        return;
+    }
     const Place at = find_place(w.chunk, slot);
     if (at.seg < 0 || at.seg >= at.nseg || at.len == 0) return;
     const long long t0 = at.seg * CH, tok = at.start + t0;
@@ -651,7 +692,8 @@ __global__ __launch_bounds__((DeltaLds<S, DK, DV, MODE>::WAVES * 64), (DeltaLds<
     const int in = (int)(block % (8 * parts)), part = in / 8;
     const long long item = group * 8 + in % 8;
     if (item >= (long long)w.slots * w.heads) return;
-    const long long slot = item / w.heads;
+    long long slot = item / w.heads;
+    if (w.order) slot = w.order[slot];
     const Place place = find_place(w.seg, slot);
     if (place.seg < 0 || place.seg >= place.nseg) return; // a slot that no sequence has
     WalkPlace at;
@@ -1190,7 +1232,7 @@ template <typename S> int launch_delta_within_typed(goom_ctx *ctx, DeltaArgs w, 
         static std::atomic<unsigned long long> done{0};
         if (int st = allow_lds(ctx, reinterpret_cast<const void *>(kernel), WithinLds<S, DK>::bytes, done)) return st;
         goom::prof_begin(ctx, "gated delta rule: within chunks");
-        kernel<<<grid_of(slots * (w.heads / w.share), 256), 256, WithinLds<S, DK>::bytes, ctx->stream>>>(w);
+        kernel<<<grid_of(slots * (w.heads / w.share) + (w.order ? 1 : 0), 256), 256, WithinLds<S, DK>::bytes, ctx->stream>>>(w);
         goom::prof_end(ctx);
         return goom::check_hip(ctx, hipGetLastError(), "gated delta rule: within chunks");
     });
