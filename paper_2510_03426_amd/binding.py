@@ -941,7 +941,7 @@ class Goom:
         if x.dim() < 1 or act is None or kind not in NORM_KINDS:
             raise ValueError("x: [..., channels]; kind: one of " + ", ".join(NORM_KINDS) + "; activation: one of " + ", ".join(ACTIVATIONS))
         sh, dtype = x.shape, x.dtype
-        channels, code, first = sh[-1], REAL_F32, self.torch.float32
+        channels, code = sh[-1], REAL_F32
         given = [p for p in (weight, bias, scale) if p is not None]
         if given:
             first, code = given[0].dtype, _real_code(given[0])
@@ -953,12 +953,12 @@ class Goom:
         for t in (gate, residual):
             if t is not None and (t.shape != sh or t.dtype != dtype):
                 raise ValueError("gate and residual: of x's shape and type")
-        return BlockNormShape(x.numel() // channels if channels else 0, channels, groups, _real_code(x), code, act, NORM_KINDS[kind], eps), first
+        return BlockNormShape(x.numel() // channels if channels else 0, channels, groups, _real_code(x), code, act, NORM_KINDS[kind], eps)
 
     def _stats(self, x, groups, kind, want):
         if not want:
             return None, None
-        rstd = self.torch.empty(x.shape[:-1] + (groups,), dtype=self.torch.float32, device=x.device)
+        rstd = x.new_empty(x.shape[:-1] + (groups,), dtype=self.torch.float32)
         return self.torch.empty_like(rstd) if kind == "layer" else None, rstd
 
     def norm_after(self, x, groups: int = 1, weight=None, bias=None, scale=None, gate=None, residual=None, kind: str = "rms", activation: str = "silu", eps: float = 1e-5,
@@ -966,7 +966,7 @@ class Goom:
         """residual + scale * (norm(x) * weight + bias) * act(gate): what closes a block whose output is x, [..., channels].  Every group of channels /
         groups neighbouring channels is normalised by itself, by its root mean square ("rms") or, less its mean, by its deviation ("layer").
         weight, bias, scale: [channels]; gate, residual: of x's shape.  want_stats: also mean (None for "rms") and rstd, float32 [..., groups]."""
-        shape, _ = self._block_norm(x, groups, weight, bias, scale, gate, residual, kind, activation, eps)
+        shape = self._block_norm(x, groups, weight, bias, scale, gate, residual, kind, activation, eps)
         px = _at(x)
         y = self.torch.empty_like(x)
         mean, rstd = self._stats(x, groups, kind, want_stats)
@@ -977,7 +977,7 @@ class Goom:
                     want_stats: bool = False):
         """h = residual + scale * x * act(gate), y = norm(h) * weight + bias: what opens the next block, x being the last one's output.  Returns y and
         h (x itself where there is nothing to add), with want_stats also mean (None for "rms") and rstd.  Arguments as for norm_after."""
-        shape, _ = self._block_norm(x, groups, weight, bias, scale, gate, residual, kind, activation, eps)
+        shape = self._block_norm(x, groups, weight, bias, scale, gate, residual, kind, activation, eps)
         px = _at(x)
         y = self.torch.empty_like(x)
         h = x if scale is None and gate is None and residual is None else self.torch.empty_like(x)
@@ -986,20 +986,20 @@ class Goom:
                                               y.data_ptr(), _at(mean), _at(rstd)))
         return (y, h, mean, rstd) if want_stats else (y, h)
 
-    def _norm_grads(self, x, grads, mean, rstd, groups, kind, params, dtype, gate):
+    def _norm_grads(self, x, grads, mean, rstd, groups, kind, params, gate):
         for t in grads:
             if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
                 raise ValueError("gradients and h: of x's shape and type")
         for t in (mean, rstd) if kind == "layer" else (rstd,):
             if t is None or tuple(t.shape) != tuple(x.shape[:-1]) + (groups,) or t.dtype != self.torch.float32:
                 raise ValueError("mean (for layer), rstd: float32 [..., groups]")
-        new = [None if p is None else self.torch.empty(x.shape[-1], dtype=dtype, device=x.device) for p in params]
+        new = [None if p is None else self.torch.empty_like(p) for p in params]
         return self.torch.empty_like(x), None if gate is None else self.torch.empty_like(x), new
 
     def norm_after_backward(self, x, grad_y, mean, rstd, groups: int = 1, weight=None, bias=None, scale=None, gate=None, kind: str = "rms", activation: str = "silu"):
         """Gradients with respect to x, gate, weight, bias and scale (None for those that there are not); the residual's is grad_y."""
-        shape, dtype = self._block_norm(x, groups, weight, bias, scale, gate, None, kind, activation, 0.0)
-        gx, ggate, (gw, gb, gs) = self._norm_grads(x, (grad_y,), mean, rstd, groups, kind, (weight, bias, scale), dtype, gate)
+        shape = self._block_norm(x, groups, weight, bias, scale, gate, None, kind, activation, 0.0)
+        gx, ggate, (gw, gb, gs) = self._norm_grads(x, (grad_y,), mean, rstd, groups, kind, (weight, bias, scale), gate)
         ws, wsn = self.workspace(self.lib.goom_block_norm_backward_workspace_bytes(C.byref(shape)))
         self._check(self.lib.goom_norm_after_backward(self._ctx, C.byref(shape), _at(x), _at(gate), _at(grad_y), _at(mean), _at(rstd), _at(weight), _at(bias), _at(scale),
                                                       gx.data_ptr(), _at(ggate), _at(gw), _at(gb), _at(gs), _at(ws), wsn))
@@ -1009,8 +1009,8 @@ class Goom:
                              activation: str = "silu"):
         """Gradients with respect to residual, x, gate, weight, bias and scale (None for those that there are not; without gate and scale residual's and
         x's are one tensor), given those with respect to y and (None: none) to h."""
-        shape, dtype = self._block_norm(x, groups, weight, bias, scale, gate, None, kind, activation, 0.0)
-        gres, ggate, (gw, gb, gs) = self._norm_grads(x, (h, grad_y, grad_h), mean, rstd, groups, kind, (weight, bias, scale), dtype, gate)
+        shape = self._block_norm(x, groups, weight, bias, scale, gate, None, kind, activation, 0.0)
+        gres, ggate, (gw, gb, gs) = self._norm_grads(x, (h, grad_y, grad_h), mean, rstd, groups, kind, (weight, bias, scale), gate)
         gx = gres if gate is None and scale is None else self.torch.empty_like(x)
         ws, wsn = self.workspace(self.lib.goom_block_norm_backward_workspace_bytes(C.byref(shape)))
         self._check(self.lib.goom_norm_before_backward(self._ctx, C.byref(shape), _at(x), _at(gate), _at(h), _at(grad_y), _at(grad_h), _at(mean), _at(rstd), _at(weight), _at(scale),
