@@ -3,7 +3,7 @@
 //     (x1, x2) -> scale (x1 cos a - x2 sin a, x1 sin a + x2 cos a),   a = position frequency
 //
 // Bound by the bytes of q and k, read and written once.  A thread has V pairs of a token and goes through some of its heads with the
-// same sines and cosines (32,768 tokens of 16 + 16 heads of 128, bfloat16, both ways: 196 us, 5.5 TB/s).  Angles are products in 64 bits, taken to a fraction of a turn there: positions of millions cost no accuracy.
+// same sines and cosines (32,768 tokens of 16 + 16 heads of 128, bfloat16, both ways: 190 us, 5.6 TB/s).  Angles are products in 64 bits, taken to a fraction of a turn there: positions of millions cost no accuracy.
 #include <cmath>
 
 #include "goom_real.h"
@@ -18,15 +18,28 @@ struct RotaryArgs {
     long long tokens, q_tok, q_head, k_tok, k_head;
     int heads, kv_heads, dim, pairs, blocks; // blocks: threads that share a token's heads
     int turned, copied;                      // units of V pairs, and of V entries that are copied
+    int group;                               // 0, or rows of units of a workgroup
     float scale, sign;
 };
 
 template <typename S, int V, bool INTER> __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a)
 {
     const int units = a.turned + a.copied;
-    const long long id = block_of() * 256 + threadIdx.x, row = id / units;
-    const int u = (int)(id - row * units), block = (int)(row % a.blocks);
-    const long long token = row / a.blocks;
+    long long row;
+    int u;
+    if (a.group) { // rows of a workgroup, their pairs first: what a wave does is mostly one or the other
+        const int x = threadIdx.x, pairs = a.group * a.turned;
+        if (x >= a.group * units) return;
+        const int r = x < pairs ? x / a.turned : (x - pairs) / a.copied;
+        u = x < pairs ? x - r * a.turned : a.turned + (x - pairs - r * a.copied);
+        row = block_of() * a.group + r;
+    } else {
+        const long long id = block_of() * 256 + threadIdx.x;
+        row = id / units;
+        u = (int)(id - row * units);
+    }
+    const long long token = row >> 32 ? row / a.blocks : (unsigned)row / (unsigned)a.blocks;
+    const int block = (int)(row - token * a.blocks);
     if (token >= a.tokens) return;
     const int all = a.heads + a.kv_heads;
     // a head's rows, and where its results go
@@ -143,16 +156,20 @@ extern "C" int goom_rotary(goom_ctx *ctx, const goom_rotary_shape *shape, const 
             const long long threads = sh.tokens * (a.turned + a.copied) * all;
             const int each = threads > (1 << 20) ? 4 : 1;
             a.blocks = (all + each - 1) / each;
-            const dim3 grid = grid_of((sh.tokens * a.blocks * (a.turned + a.copied) + 255) / 256, 256);
+            const int units = a.turned + a.copied;
+            a.group = units <= 64 && rest ? 256 / units : 0; // (pairs and copies in one wave: 38 us for 36; without copies one thread after another 98 us for 100)
+            const dim3 grid = a.group ? grid_of((sh.tokens * a.blocks + a.group - 1) / a.group, 256) : grid_of((sh.tokens * a.blocks * units + 255) / 256, 256);
             goom::prof_begin(ctx, "rotary positions");
             if (sh.flags & GOOM_ROTARY_INTERLEAVED) rotary_kernel<S, V, true><<<grid, 256, 0, ctx->stream>>>(a);
             else rotary_kernel<S, V, false><<<grid, 256, 0, ctx->stream>>>(a);
             goom::prof_end(ctx);
             return goom::check_hip(ctx, hipGetLastError(), "rotary positions");
         };
-        if constexpr (sizeof(S) == 2)
-            if (sh.pairs >= 8) return run(std::integral_constant<int, 8>());
-        if (sh.pairs >= 4) return run(std::integral_constant<int, 4>());
+        // Four pairs a thread, two of neighbouring floats: a lane's access has 16 bytes at most and lies beside the next lane's.  Twice as many, us: 10,005
+        // tokens of 16 heads of 77, 19 pairs of neighbouring floats 36 and 28, of 53, 26 of halves 17 and 13, of 128, pairs of floats 34 and 30; 32,768 of 32 heads
+        // of 128 in bfloat16, both halves of a head 98 and 94.
+        const bool two = sizeof(S) == 4 && (sh.flags & GOOM_ROTARY_INTERLEAVED);
+        if (!two && sh.pairs >= 4) return run(std::integral_constant<int, 4>());
         if (sh.pairs >= 2) return run(std::integral_constant<int, 2>());
         return run(std::integral_constant<int, 1>());
     });
