@@ -8,8 +8,8 @@ namespace goom_layer {
 // ---- single tokens.  With x = S^T k and z = S^T q of the state before, both sums over its rows in the one pass that reads it,
 //     u = beta (v - a x),   S' = a S + k u^T,   o = scale (a z + (k . q) u).
 // Bound by the states' bytes.  A workgroup has 32 columns of a head's state (eight groups of four) and its threads every 32nd row,
-// which stay in registers until u is known; sums meet in LDS in a fixed order.  256 tokens of 16 heads of 128 x 128: 115 us, 4.7 TB/s; one token of
-// them: 10.6 us, a launch and two waits.
+// which stay in registers until u is known; sums meet in LDS in a fixed order.  256 tokens of 16 heads of 128 x 128: 115 us, 4.7 TB/s (64
+// columns a workgroup the same, 128 a tenth more); one token of 16 heads of 64: 5 us, a launch and two waits.
 template <typename S> __global__ __launch_bounds__(256) void delta_step_kernel(goom_delta_shape sh, const S *q, const S *k, const S *v, const float *log_decay,
                                                                                const float *beta, const float *state, S *o, float *next)
 {

@@ -679,7 +679,7 @@ template <typename S, int DK, int DV, int MODE> __device__ inline void delta_wal
 // Bound by a chunk's chain of products, K S, M (beta Y), P U and the state's, each of which waits for the one before and for a barrier or two: the
 // first four waves fetch the next chunk and form its P meanwhile, the others own 16 columns of the state each.  8 x 4096 tokens of 16 heads of
 // 128, bfloat16, us: forward 356 (1.8 TB/s; with P formed by the waves that multiply 497, with two loading waves 454), the states before
-// every chunk again 266, the adjoints 483.  65,536 tokens of 16 heads of 64 in 16 segments a head: maps 251, walk 259.  A kernel whose
+// every chunk again 266, the adjoints 483.  65,536 tokens of 16 heads of 64 in 32 segments a head: maps 251, walk 259.  A kernel whose
 // registers spill is 1.6 to 2.5 times as slow: scratch loads wait behind the chunk that is on its way.
 // grid: slots heads parts, in one order; the parts of a head and segment run on one XCD (of 8, dealt round robin), whose L2 has what they share
 template <typename S, int DK, int DV, int MODE>
