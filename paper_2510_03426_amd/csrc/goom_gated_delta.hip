@@ -160,6 +160,8 @@ static DeltaPlan plan_of(const goom_delta_shape &sh, bool packed, bool backward)
     const long long len = p.maps ? ((mean + want - 1) / want + p.ch - 1) / p.ch * p.ch : (sh.tokens / p.ch + 1) * p.ch; // (no sequence is longer)
     p.seg = pieces_of(sh, packed, len);
     if (!p.maps) p.seg = {len, sh.seqs, 1};
+    // Without tokens one walk passes the states on, and nothing is kept: what is in the workspace then is written by kernels that are not launched
+    if (sh.tokens == 0) return p;
     const size_t records = (size_t)p.chunk.slots * sh.heads, cuts = (size_t)p.seg.slots * sh.heads;
     p.m = goom::align_up(records * m_floats(p.ch) * sizeof(float), 256);
     p.vecs = goom::align_up(records * (p.ch == 64 ? sizeof(ChunkVec<64>) : sizeof(ChunkVec<32>)), 256);
