@@ -146,7 +146,7 @@ template <typename S, int V, int J, int MOST, bool BEFORE, bool BACK> __global__
                     for (int e = 0; e < V; e++) t[j][e] = x[j][e];
                 }
 #pragma unroll
-                for (int e = 0; e < V; e++) sum += e >= skip[j] ? t[j][e] : 0.0f;
+                for (int e = 0; e < V; e++) sum += chan[j] >= 0 && e >= skip[j] ? t[j][e] : 0.0f; // (a lane without channels has another one's scale, times zero)
             }
             float mean = 0.0f, square = 0.0f;
             if (a.layer) {
