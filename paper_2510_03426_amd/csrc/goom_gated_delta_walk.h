@@ -113,7 +113,13 @@ template <int SIZE, int CH> __device__ inline void join_blocks(float *m, const f
 #pragma unroll
         for (int e = 0; e < 4; e++) above[(tr + g * 4 + e) * PM + tc + i] = below[(tr + g * 4 + e) * PM + tc + i] - c[e];
     }
-    if (TILES > 1) __syncthreads(); // (one tile: the wave's own)
+    if (TILES > 1) {
+        __syncthreads();
+    } else { // one tile, of the wave's own: its lanes read what others of them wrote, in that order
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
     if (mine) { // and that less M22 (beta2 that)
         f32x4 c = {0, 0, 0, 0};
 #pragma unroll
