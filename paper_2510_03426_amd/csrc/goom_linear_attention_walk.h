@@ -228,8 +228,10 @@ template <typename S, int D, int THREADS, int CH> struct TileRows {
             if (n == CH) {
                 const unsigned at = row0() * bytes + col, step = STEP * bytes;
 #pragma unroll
-                for (int k = 0; k < N; k++)
+                for (int k = 0; k < N; k++) {
+                    x[k] = SV{}; // (of threads without a row: what is split must be some number)
                     if (UNITS % THREADS == 0 || row0() + k * STEP < CH) x[k] = load_unaligned<S, 8>(reinterpret_cast<const S *>(p + (at + k * step)));
+                }
             } else {
 #pragma unroll
                 for (int k = 0; k < N; k++) {
@@ -253,9 +255,7 @@ template <typename S, int D, int THREADS, int CH> struct TileRows {
         else if (d < 8 || !shift(d)) put_units<PITCH, true, false>(tile, n, d);
         else put_units<PITCH, true, true>(tile, n, d);
     }
-    // the same in one way for all sizes, where the choice would be all but free: in one kernel of the gated delta rule (floats, heads of 32) the compiler
-    // (clang 22, ROCm 7.2) lost the address of parts behind the first on the way that cuts rows and moves nothing
-    // unit k as it belongs into the tile
+    // unit k as it belongs into the tile, in one way for all sizes
     __device__ inline SV unit(int k, int n, int d) const
     {
         const int col = col0(), move = d >= 8 && col + 8 > d ? shift(d) : 0;
@@ -269,6 +269,7 @@ template <typename S, int D, int THREADS, int CH> struct TileRows {
         if (col >= d || row0() + k * STEP >= n) v = SV{};
         return v;
     }
+    // put() without its three ways, where the choice would be all but free: a kernel of the gated delta rule has up to nine of these
     template <int PITCH> __device__ inline void put_any(bf16 *tile, int n, int d) const
     {
 #pragma unroll
