@@ -617,8 +617,8 @@ size_t goom_group_norm_backward_workspace_bytes(const goom_norm_shape *shape);
 /* Rotary positions: of every head's dim entries the first 2 pairs are turned, pair i by the angle position frequency_i,
  *     (x1, x2) -> scale (x1 cos a - x2 sin a, x1 sin a + x2 cos a);
  * the entries behind them are copied as they are (without the scale).  A pair is (x[i], x[pairs + i]), or with GOOM_ROTARY_INTERLEAVED
- * (x[2 i], x[2 i + 1]).  Longer contexts are a matter of the frequencies and the scale.  Angles are formed in 64 bits, so positions may be as large as they like
- * below 2^53.  With GOOM_ROTARY_BACK the turn is the other way: the gradient's way back, with the same scale. */
+ * (x[2 i], x[2 i + 1]).  Longer contexts are a matter of the frequencies and the scale.  Angles are formed in two doubles, so positions up to 2^53 either way
+ * cost no accuracy (with frequencies up to 2^20).  With GOOM_ROTARY_BACK the turn is the other way: the gradient's way back, with the same scale. */
 #define GOOM_ROTARY_INTERLEAVED 1
 #define GOOM_ROTARY_BACK 2
 typedef struct goom_rotary_shape {

@@ -3,7 +3,8 @@
 //     (x1, x2) -> scale (x1 cos a - x2 sin a, x1 sin a + x2 cos a),   a = position frequency
 //
 // Bound by the bytes of q and k, read and written once.  A thread has V pairs of a token and goes through some of its heads with the
-// same sines and cosines (32,768 tokens of 16 + 16 heads of 128, bfloat16, both ways: 190 us, 5.6 TB/s).  Angles are products in 64 bits, taken to a fraction of a turn there: positions of millions cost no accuracy.
+// same sines and cosines (32,768 tokens of 16 + 16 heads of 128, bfloat16, both ways: 190 us, 5.6 TB/s).  Angles are products in two
+// doubles, taken to a fraction of a turn there: positions up to 2^53 cost no accuracy (a single double's product is off by 2^-10 of a turn from 2^40 on).
 #include <cmath>
 
 #include "goom_real.h"
@@ -21,6 +22,8 @@ struct RotaryArgs {
     int group;                               // 0, or rows of units of a workgroup
     float scale, sign;
 };
+
+constexpr double ONE_BY_2PI = 0.15915494309189535, ONE_BY_2PI_REST = -9.839338337591243e-18; // 1 / 2 pi to 107 bits
 
 template <typename S, int V, bool INTER> __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a)
 {
@@ -73,7 +76,9 @@ template <typename S, int V, bool INTER> __global__ __launch_bounds__(256) void 
     const double position = (double)a.positions[token];
 #pragma unroll
     for (int e = 0; e < V; e++) {
-        const double turns = position * ((double)a.frequencies[first + e] * 0.15915494309189535);
+        // turns a position in two doubles; of the product the whole turns go before anything is rounded
+        const double f = a.frequencies[first + e], each = f * ONE_BY_2PI, rest = __builtin_fma(f, ONE_BY_2PI_REST, __builtin_fma(f, ONE_BY_2PI, -each));
+        const double turns = __builtin_fma(position, rest, __builtin_fma(position, each, -rint(position * each)));
         sincospif(2.0f * (float)(turns - rint(turns)), &s[e], &c[e]);
         s[e] *= a.scale * a.sign;
         c[e] *= a.scale;
