@@ -369,14 +369,19 @@ class Goom:
         return out
 
     def workspace(self, nbytes: int):
-        """A cached 256-byte aligned scratch tensor of at least nbytes (None for 0).  A call that is captured into a graph has one of its own, from the
-        graph's memory: the cached one is let go when a later call needs more, and replays may go side by side."""
+        """A cached 256-byte aligned scratch tensor of at least nbytes (None for 0), of the context's stream: what comes after it in memory that was let go
+        waits for that stream's work, whatever torch's current one is.  A call that is captured (torch.cuda.graph, torch.cuda.CUDAGraph) has one of its own, from
+        the graph's memory: the cached one is let go when a later call needs more, and replays may go side by side.  Captures that torch does not know of have no
+        such memory: they take the C entry points, with a workspace that their program keeps."""
         if nbytes == 0:
             return None, 0
-        if self.torch.cuda.is_current_stream_capturing():
-            return self.torch.empty(nbytes, dtype=self.torch.uint8, device=self.device), nbytes
-        if self._ws is None or self._ws.numel() < nbytes:
-            self._ws = self.torch.empty(nbytes, dtype=self.torch.uint8, device=self.device)
+        captured = self.torch.cuda.is_current_stream_capturing()
+        if captured or self._ws is None or self._ws.numel() < nbytes:
+            with self.torch.cuda.stream(self._stream):
+                ws = self.torch.empty(nbytes, dtype=self.torch.uint8, device=self.device)
+            if captured:
+                return ws, nbytes
+            self._ws = ws
         return self._ws, self._ws.numel()
 
     # ---- codecs
