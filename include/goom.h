@@ -559,8 +559,8 @@ typedef struct goom_delta_shape {
  * solved for all chunks at once, then every head's state walks along its sequence, which is cut into segments, chained as affine maps of
  * the state, where sequences and heads are few.  (Where they are many, packed sequences start longest first.)  Operands are held as for goom_linear_attention (24 bits where they are computed); sums of
  * logarithms take 64 bits.  A NaN or an infinity in an input may show in all outputs of its head in its sequence.
- * workspace: goom_gated_delta_workspace_bytes(shape, offsets != NULL) bytes: some 0.2 KB a token and head, and the segments'
- * maps. */
+ * workspace: goom_gated_delta_workspace_bytes(shape, offsets != NULL) bytes: for each head a record of 13.6 KB (4.8 KB for halves and floats) for each chunk, and
+ * the segments' maps.  Packed, tokens / 64 (or 32) chunks are counted and one more for every sequence, however short it is; without tokens nothing is needed. */
 int goom_gated_delta(goom_ctx *ctx, const goom_delta_shape *shape, const void *q, const void *k, const void *v, const float *log_decay, const float *beta,
                      const int64_t *offsets, const float *state, void *o, float *final_state, void *workspace, size_t workspace_bytes);
 size_t goom_gated_delta_workspace_bytes(const goom_delta_shape *shape, int packed);
@@ -573,8 +573,10 @@ int goom_gated_delta_step(goom_ctx *ctx, const goom_delta_shape *shape, const vo
 /* Gradients of a loss, given grad_o ([tokens, heads, dv], contiguous, of the shape's type) and, unless NULL, grad_final, that with respect to the
  * final state: grad_q, grad_k, grad_v (contiguous, of the shape's type; those of heads that share q and k are summed in float, in a fixed order),
  * grad_log_decay and grad_beta ([tokens, heads] floats; a decay of zero has no slope) and, unless NULL, grad_state (floats; not the array grad_final).
- * The forward pass's inputs are given again.  workspace: goom_gated_delta_backward_workspace_bytes(shape, offsets != NULL) bytes: two states and
- * two chunks of rows in floats for each chunk and head (with heads of 128, 3.3 KB a token and head in bfloat16, 5.3 KB in the other types). */
+ * The forward pass's inputs are given again.  workspace: goom_gated_delta_backward_workspace_bytes(shape, offsets != NULL) bytes: besides those records
+ * two states and two chunks of rows in floats for each chunk, counted likewise, and head (of 128: 197 KB, 164 KB for halves and floats, so 3.3 KB a token and head
+ * in bfloat16, 5.3 KB in the other types, where sequences are long; with 4096 packed sequences of one token and 16 heads 14 GB), and where heads share q and k
+ * 8 dk bytes for each token and head.  dk counts as the next of 32, 64 and 128, dv as 32 or the next multiple of 64. */
 int goom_gated_delta_backward(goom_ctx *ctx, const goom_delta_shape *shape, const void *q, const void *k, const void *v, const float *log_decay, const float *beta,
                               const int64_t *offsets, const float *state, const void *grad_o, const float *grad_final, void *grad_q, void *grad_k, void *grad_v,
                               float *grad_log_decay, float *grad_beta, float *grad_state, void *workspace, size_t workspace_bytes);
