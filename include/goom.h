@@ -538,7 +538,8 @@ size_t goom_linear_attention_backward_workspace_bytes(const goom_attention_shape
  * and, before it adds its value, takes off beta times what the state already holds for its key:
  *     S_t = a_t (S_{t-1} - beta_t k_t (k_t^T S_{t-1})) + beta_t k_t v_t^T,      o_t = scale q_t^T S_t,      a_t = exp(log_decay_t).
  * -inf, a decay of zero, forgets everything before the token; logarithms below -110 count as that.  Keys are usually of length one and beta
- * between 0 and 1, or 2: with beta |k|^2 above 2 the recurrence itself grows, and its rounding errors with it. */
+ * between 0 and 1, or 2: with beta |k|^2 above 2 the recurrence itself grows, and its rounding errors with it.  Decays
+ * above one are taken as long as their product over a chunk (below) is a float's. */
 typedef struct goom_delta_shape {
     int64_t seqs;      /* sequences */
     int64_t tokens;    /* tokens of all sequences; without offsets every sequence has tokens / seqs of them */

@@ -6,7 +6,7 @@
 // Bound by the bytes of their tensors, each read and written once: a team of lanes holds one token's group in registers, 8 entries a lane
 // (16 for the longest), and statistics are taken about the mean itself.  A team keeps its group from token to token, so parameters are
 // loaded once and their gradients are summed in registers: one partial sum for each workgroup and channel, added up in a fixed order by a
-// second launch.  32,768 tokens of 2048 channels, bfloat16, both ways: 280 us, 4.8 TB/s.
+// second launch.  32,768 tokens of 2048 channels, bfloat16, before a block, both ways: 269 us, 5.0 TB/s.
 #include <cmath>
 
 #include "goom_activation.h"
@@ -68,8 +68,9 @@ template <typename S, int V, int J, int MOST, bool BEFORE, bool BACK> __global__
     int chan[J], skip[J];
     // What 128 registers (1024 lanes) do not hold spills: with 16 entries a lane the parameters, read from L2 again for each token instead, and the next
     // token's entries, which are then not asked for ahead; with 8 floats the parameters on the way back.  4096 tokens of 16,384 channels, both held and
-    // not, us: backwards 617 and 391 (bfloat16), 1353 and 611 (float), forwards in float 341 and 221; forwards in halves they fit: 110 and 125; 8192
-    // tokens of 8192, backwards: float 578 and 439, bfloat16 181 and 201.
+    // not, us: backwards 617 and 391 (bfloat16), 1353 and 611 (float), forwards in float 341 and 221; forwards in halves holding is faster, 110 and 125, though
+    // some spills; 8192 tokens of 8192, backwards: float 578 and 439, bfloat16 181 and 201.  Scratch that is left, bytes a lane after and before a block: 16 entries
+    // backwards 136 and 156 in 16 bits, 132 and 224 in floats, forwards 68 and 12 in bfloat16, 52 and 12 in halves; 8 entries of 1024 lanes, backwards, 60 and 20 in 16 bits, 0 and 72.
     constexpr bool WIDE = J * V == 16, SMALL = sizeof(S) == 2, AHEAD = !WIDE || (SMALL && !BACK), HOLD = WIDE ? SMALL && !BACK : SMALL || !(BACK && MOST == 1024);
     float w[HOLD ? J : 1][V], b[HOLD ? J : 1][V], sc[HOLD ? J : 1][V], sw[J][V], sb[J][V], ss[J][V];
     auto read_params = [&](int j, int at) {

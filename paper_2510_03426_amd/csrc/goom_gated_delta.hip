@@ -206,7 +206,7 @@ static DeltaArgs delta_args(const goom_delta_shape &sh, const DeltaPlan &p, cons
     return w;
 }
 
-template <typename S> static int launch_carry(goom_ctx *ctx, const goom_delta_shape &sh, const DeltaArgs &w, bool back)
+static int launch_carry(goom_ctx *ctx, const goom_delta_shape &sh, const DeltaArgs &w, bool back)
 {
     return with_delta(sh.dk, sh.dv, [&](auto rows, auto cols) {
         constexpr int DK = decltype(rows)::value, DV = decltype(cols)::value;
@@ -227,7 +227,7 @@ template <typename S> static int run_forward(goom_ctx *ctx, const goom_delta_sha
         if (int s = launch_delta_within<S>(ctx, w, p.chunk.slots)) return s;
         if (p.maps) {
             if (int s = launch_delta_walk<S>(ctx, w, MAPS, p.seg.slots, "gated delta rule: segments' maps")) return s;
-            if (int s = launch_carry<S>(ctx, sh, w, false)) return s;
+            if (int s = launch_carry(ctx, sh, w, false)) return s;
         }
     }
     return launch_delta_walk<S>(ctx, w, FORWARD, p.seg.slots, "gated delta rule");
@@ -243,7 +243,7 @@ template <typename S> static int run_backward(goom_ctx *ctx, const goom_delta_sh
         w.init = b.state;
         if (p.maps) {
             if (int s = launch_delta_walk<S>(ctx, w, MAPS, p.seg.slots, "gated delta rule: segments' maps")) return s;
-            if (int s = launch_carry<S>(ctx, sh, w, false)) return s;
+            if (int s = launch_carry(ctx, sh, w, false)) return s;
         }
         w.kept = kept_s;
         w.rows = rows_e;
@@ -257,7 +257,7 @@ template <typename S> static int run_backward(goom_ctx *ctx, const goom_delta_sh
     w.rows = rows_w;
     if (p.maps && sh.tokens > 0) {
         if (int s = launch_delta_back<S>(ctx, w, BACK_MAPS, p.seg.slots, "gated delta rule: segments' adjoints")) return s;
-        if (int s = launch_carry<S>(ctx, sh, w, true)) return s;
+        if (int s = launch_carry(ctx, sh, w, true)) return s;
     }
     if (int s = launch_delta_back<S>(ctx, w, BACK, p.seg.slots, "gated delta rule: adjoints")) return s;
     if (sh.tokens == 0) return GOOM_OK;

@@ -696,7 +696,8 @@ template <typename S, int DK, int DV, int MODE> __device__ inline void delta_wal
 // first four waves fetch the next chunk and form its P meanwhile, the others own 16 columns of the state each.  8 x 4096 tokens of 16 heads of
 // 128, bfloat16, us: forward 356 (1.8 TB/s; with P formed by the waves that multiply 497, with two loading waves 454), the states before
 // every chunk again 266, the adjoints 483.  65,536 tokens of 16 heads of 64 in 32 segments a head: maps 251, walk 259.  A kernel whose
-// registers spill is 1.6 to 2.5 times as slow: scratch loads wait behind the chunk that is on its way.
+// registers spill is 1.6 to 2.5 times as slow: scratch loads wait behind the chunk that is on its way.  (One still does: segments' adjoints of floats with
+// heads of up to 32 and values of more, 7 registers at its bound of 128.)
 // grid: slots heads parts, in one order; the parts of a head and segment run on one XCD (of 8, dealt round robin), whose L2 has what they share
 template <typename S, int DK, int DV, int MODE>
 __global__ __launch_bounds__((DeltaLds<S, DK, DV, MODE>::WAVES * 64), (DeltaLds<S, DK, DV, MODE>::per_simd)) void delta_walk_kernel(const DeltaArgs w)
@@ -850,8 +851,8 @@ template <typename S, int DK, int DV> __global__ __launch_bounds__(256, (GradLds
     if (at.seg < 0 || at.seg >= at.nseg || at.len == 0) return;
     const long long t0 = at.seg * CH, tok = at.start + t0, record = block;
     const int n = at.len - t0 < CH ? (int)(at.len - t0) : CH;
-    const int lane = threadIdx.x & 63, wave = wave_of(), i = lane & 15, g = lane >> 4;
-    const int tile = wave % TILES, first = wave / TILES * EACH, col0 = tile * NT * 16; // the wave's columns of q and k, col0 + (i / 4) CS + 4 nt + i % 4, and its rows: tiles of 16 from `first` on
+    const int lane = threadIdx.x & 63, wave = wave_of();
+    const int tile = wave % TILES, first = wave / TILES * EACH, col0 = tile * NT * 16; // the wave's columns of q and k, col0 + (i / 4) CS + 4 nt + i % 4 of lane i of 16, and its rows: tiles of 16 from `first` on
     const bool columns = wave / TILES < Lds::GROUPS;
     const ChunkVec<CH> &vec = reinterpret_cast<const ChunkVec<CH> *>(w.vecs)[record];
 

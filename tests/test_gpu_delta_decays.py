@@ -85,3 +85,38 @@ def test_what_is_forgotten_and_what_is_not(g):
     g.gated_delta_step(q.cuda(), k.cuda(), v.cuda(), ld.cuda(), torch.zeros(n, 1).cuda(), state.cuda(), out_state=out)
     out = out.cpu()
     assert (out[:4] == 0).all() and torch.equal(out[4], state[4]) and not out[5:].isfinite().any()
+
+
+@pytest.mark.parametrize("dtype,n,rate,dk,dv", [("bfloat16", 64, 1.2, 64, 64), ("float32", 32, 2.4, 32, 40), ("float16", 20, 0.3, 50, 20), ("float32", 200, 0.4, 128, 128), ("bfloat16", 700, 0.11, 32, 32), ("bfloat16", 3, 25.0, 16, 16)])
+def test_growing_decays(g, dtype, n, rate, dk, dv):
+    """Decays above one, up to e^80 in all.  An error grows as the decays' product from where it is made, by matrices a (I - beta k k^T) of norms of at most a:
+    E_t = max(a_t E_{t-1}, S_t + |v_t|) stands for the largest state in test_gpu_gated_delta.py's bound, twelve random roundings of sums of dk + 136 terms a token.
+    Pairs' weights round their exponents: half a unit of b - b' <= 116 bits, 116 u log 2 = 80 u of a weight, less than the 12 sqrt(dk + 136) >= 147 u that are allowed for a single token.
+    Gradients: finite, and within four such bounds, over all entries of a state, of the largest of their kind."""
+    import torch
+    from oracle import layer_oracle as lo
+    t = getattr(torch, dtype)
+    gen = torch.Generator().manual_seed(n)
+    H = 2
+    q, k, v, go = (torch.randn(1, n, H, d, generator=gen) for d in (dk, dk, dv, dv))
+    q, k = (torch.nn.functional.normalize(x, dim=-1) for x in (q, k))
+    q, k, v, go = (x.to(t) for x in (q, k, v, go))
+    ld, beta = rate * (1 - 0.1 * torch.rand(1, n, H, generator=gen)), torch.rand(1, n, H, generator=gen)
+    scale = 1e-3 if dtype == "float16" else 1.0  # (halves end at 65504)
+    f = lambda x: x.double().numpy()[0]  # noqa: E731
+    o, last = g.gated_delta(*(x.cuda() for x in (q, k, v, ld, beta)), scale=scale, want_state=True)
+    E, S, share = np.zeros((n, H)), np.zeros((H, dk, dv)), np.arange(H)
+    for i in range(n):
+        S = lo._delta_step(S, f(k)[i], f(v)[i], f(ld)[i], f(beta)[i])[0]
+        E[i] = np.maximum(np.exp(f(ld)[i]) * E[i - 1] if i else 0, np.sqrt((S * S).sum((1, 2))) + np.linalg.norm(f(v)[i], axis=-1))
+    want, wl, _ = lo.gated_delta(*(f(x) for x in (q, k, v, ld, beta)), None, None, scale)
+    err = 12 * U * math.sqrt(n * (dk + 136.0))
+    qn = np.linalg.norm(f(q), axis=-1)
+    assert (np.abs(f(o.cpu()) - want) <= torch.finfo(t).eps / 2 * np.abs(want) + err * scale * (qn * E)[..., None] + 2.0 ** -25).all()
+    assert (np.abs(last.double().cpu().numpy()[0] - wl[0]) <= err * E[-1][:, None, None]).all()
+    grads = g.gated_delta_backward(*(x.cuda() for x in (q, k, v, ld, beta, go)), scale=scale)[:5]
+    wants = lo.gated_delta_backward(*(f(x) for x in (q, k, v, ld, beta, go)), scale=scale)[:5]
+    for name, y, w in zip(("q", "k", "v", "log_decay", "beta"), grads, wants):
+        y, most = f(y.cpu()), np.abs(w).max()
+        assert np.isfinite(y).all(), name
+        assert np.abs(y - w).max() <= (torch.finfo(t).eps / 2 if name in "qkv" else 0) * most + 4 * err * math.sqrt(dk * dv) * most, name
